@@ -248,8 +248,9 @@ def _plain_qlinear(s):
     top = _QMAX[s["prec"]]
     x = s["x"].float()
     amax = x.abs().amax(1)
-    scale = amax / top
-    inverse = torch.where(amax > 0, top / amax, torch.zeros_like(amax))
+    most = torch.full_like(amax, top)  # (a tensor: division by a Python number is a product with its inverse)
+    scale = amax / most
+    inverse = torch.where(amax > 0, most / amax, torch.zeros_like(amax))
     q = torch.round(x * inverse[:, None]).clamp(-top, top)
     w = (_unpack_s4(s["w"]) if s["prec"] == "s4" else s["w"]).float()
     y = (q @ w.t()) * scale[:, None] * s["col_scale"][None, :]
@@ -280,7 +281,7 @@ def _plain_append(s, name):
     x = x.transpose(2, 3)  # [batch, pages, heads, page, dim]
     old = torch.where(is_old[:, :, None, :, None], cache[slot].float(), torch.zeros((), device="cuda"))
     was = torch.where(is_old[:, :, :1], scale[slot], torch.zeros((), device="cuda"))  # [batch, pages, heads]
-    now = torch.maximum(was, x.abs().amax((3, 4)) / 127.0)
+    now = torch.maximum(was, x.abs().amax((3, 4)) / torch.full_like(was, 127.0))
     inverse = torch.where(now > 0, 1.0 / now, torch.zeros((), device="cuda"))
     codes = torch.round(x * inverse[..., None, None]) + torch.round(old * (was * inverse)[..., None, None])
     codes = codes.clamp(-127, 127).to(torch.int8)
