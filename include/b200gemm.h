@@ -184,6 +184,65 @@ int gemm_s4_dequant(int M, int N, int K, const uint8_t* A, const uint8_t* B,
                     gemm_stream_t stream);
 
 /*
+ * Linear layers: the product with what follows it in a model fused into its
+ * epilogue,
+ *
+ *     C[i][j] = act(x[i][j] + bias[j]) + residual[i][j],
+ *     x = sum_k a(i,k) b(j,k)                                  (gemm_fp16_linear)
+ *     x = float(sum_k a(i,k) b(j,k)) * row_scale[i] * col_scale[j]   (s8, s4)
+ *
+ * computed in FP32 and rounded once where C is binary16.  A, B, K rules, scales
+ * and (INT4) the internal workspace are those of gemm_fp16, gemm_s8_dequant and
+ * gemm_s4_dequant.  C and residual have the same element type and may have row
+ * pitches of their own (a column block of a larger matrix); they need only the
+ * alignment of their elements, and rows that start on 16 bytes are faster.
+ * residual == C (with the same pitch) adds in place; any other overlap of C with
+ * an input gives undefined results.  K is never split over CTAs that add into C.
+ */
+enum {
+  GEMM_ACT_NONE = 0,
+  GEMM_ACT_RELU = 1,
+  GEMM_ACT_GELU = 2,      /* x/2 (1 + erf(x / sqrt 2)) */
+  GEMM_ACT_GELU_TANH = 3, /* x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
+  GEMM_ACT_SILU = 4       /* x / (1 + exp(-x)) */
+};
+
+typedef struct gemm_epilogue {
+  const float* bias;    /* N floats, or NULL */
+  int activation;       /* GEMM_ACT_* */
+  int c_is_fp16;        /* element type of C and residual: 1 = binary16, 0 = FP32 */
+  const void* residual; /* M x N, or NULL */
+  long long ldr;        /* row pitch of residual in elements; 0 = N */
+  long long ldc;        /* row pitch of C in elements; 0 = N */
+} gemm_epilogue_t;
+
+int gemm_fp16_linear(int M, int N, int K, const void* A, const void* B, void* C,
+                     const gemm_epilogue_t* epilogue, gemm_stream_t stream);
+int gemm_s8_linear(int M, int N, int K, const int8_t* A, const int8_t* B, const float* row_scale,
+                   const float* col_scale, void* C, const gemm_epilogue_t* epilogue,
+                   gemm_stream_t stream);
+int gemm_s4_linear(int M, int N, int K, const uint8_t* A, const uint8_t* B, const float* row_scale,
+                   const float* col_scale, void* C, const gemm_epilogue_t* epilogue,
+                   gemm_stream_t stream);
+
+/*
+ * Quantises rows for the integer products (the activations in front of a
+ * linear layer): with amax = max_k |x[k]| of a row and T = 127 (GEMM_PREC_S8) or
+ * 7 (GEMM_PREC_S4),
+ *
+ *     row_scale = amax / T,   q[k] = rint(x[k] * (T / amax))
+ *
+ * in FP32 (IEEE divisions, ties to even).  X: `rows` rows of K binary16
+ * (x_is_fp16 = 1) or FP32 values, row pitch ldx elements (0 = K).  Q: K int8 or
+ * K / 2 bytes of packed INT4 per row, as gemm_s8 / gemm_s4 take them; 16-byte
+ * aligned.  A row of zeros gets scale 0 and codes 0; a row that holds an infinity
+ * or a NaN gets that as its scale, so that products with it are NaN.
+ * K % 16 == 0 (S8) or K % 32 == 0 (S4), K <= 131071.
+ */
+int gemm_quantize_rows(int precision, int rows, int K, const void* X, long long ldx, int x_is_fp16,
+                       void* Q, float* row_scale, gemm_stream_t stream);
+
+/*
  * The same GEMM for operands and result in HOST memory (the end-to-end path:
  * the study times kernels only, Sec. III-B; a caller whose data lives on the
  * host also pays the PCIe transfers).  A, B, C are HOST pointers with the

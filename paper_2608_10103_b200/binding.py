@@ -22,11 +22,28 @@ PRECISION_ID = {"fp16": PREC_FP16, "s8": PREC_S8, "s4": PREC_S4}
 EXPORTS = (
     "gemm_fp16", "gemm_s8", "gemm_s4", "gemm_s4_workspace_bytes", "gemm_s4_ws",
     "gemm_fp16_f16out", "gemm_s8_dequant", "gemm_s4_dequant", "gemm_host", "gemm_host_release",
+    "gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows",
     "gemm_s4_static", "gemm_s4_static_capacity", "gemm_release_workspaces", "gemm_unpack_s4", "gemm_mma_peak_probe", "gemm_query_config",
     "gemm_set_config_override", "gemm_set_kernel_family", "gemm_set_s4_scheme", "gemm_set_swap_ab", "gemm_set_l2_policy", "gemm_trace_enable", "gemm_trace_read", "gemm_set_stages_override", "gemm_debug_counters", "gemm_debug_host_cost", "gemm_debug_read_probe", "gemm_debug_reset_l2",
     "gemm_last_device_status", "gemm_read_device_status", "gemm_last_cuda_error",
     "gemm_status_string", "gemm_version",
 )
+
+KV_EXPORTS = ("kv_append_s8", "kv_read_s8", "kv_attention_s8")   # include/b200kv.h
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+class _Epilogue(ctypes.Structure):        # gemm_epilogue_t
+    _fields_ = [("bias", ctypes.c_void_p), ("activation", ctypes.c_int), ("c_is_fp16", ctypes.c_int),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_longlong), ("ldc", ctypes.c_longlong)]
+
+
+class _KvCache(ctypes.Structure):         # kv_cache_s8_t
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("num_pages", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int)]
+
 
 _lib = None
 
@@ -63,6 +80,14 @@ def lib() -> ctypes.CDLL:
         L.gemm_host.argtypes = [i, i, i, i, vp, vp, vp, vp]
         L.gemm_s8_dequant.argtypes = [i, i, i, vp, vp, vp, vp, vp, i, vp]
         L.gemm_s4_dequant.argtypes = [i, i, i, vp, vp, vp, vp, vp, i, vp]
+        ep, kc, ll = ctypes.POINTER(_Epilogue), ctypes.POINTER(_KvCache), ctypes.c_longlong
+        L.gemm_fp16_linear.argtypes = [i, i, i, vp, vp, vp, ep, vp]
+        L.gemm_s8_linear.argtypes = [i, i, i, vp, vp, vp, vp, vp, ep, vp]
+        L.gemm_s4_linear.argtypes = [i, i, i, vp, vp, vp, vp, vp, ep, vp]
+        L.gemm_quantize_rows.argtypes = [i, i, i, vp, ll, i, vp, vp, vp]
+        L.kv_append_s8.argtypes = [kc, i, vp, vp, vp, i, i, vp, vp, ll, ll, vp]
+        L.kv_read_s8.argtypes = [kc, i, vp, vp, vp, i, i, vp, vp, vp]
+        L.kv_attention_s8.argtypes = [kc, i, vp, vp, vp, i, i, i, vp, ll, ll, ctypes.c_float, i, vp, ll, vp]
         L.gemm_s4_workspace_bytes.argtypes = [i, i, i]
         L.gemm_s4_workspace_bytes.restype = sz
         L.gemm_s4_static.argtypes = [i, i, i, vp, vp, vp, vp]
@@ -85,7 +110,7 @@ def lib() -> ctypes.CDLL:
         L.gemm_trace_read.argtypes = [ctypes.POINTER(ctypes.c_ulonglong), i]
         L.gemm_status_string.argtypes = [i]
         L.gemm_status_string.restype = ctypes.c_char_p
-        for name in EXPORTS:
+        for name in EXPORTS + KV_EXPORTS:
             fn = getattr(L, name)
             if name not in ("gemm_s4_workspace_bytes", "gemm_s4_static_capacity",
                             "gemm_status_string"):
@@ -231,6 +256,202 @@ def gemm_s4_dequant(A, B, row_scale, col_scale, C=None, out_dtype=torch.float32,
         raise ValueError("A and B disagree on K")
     return _dequant("gemm_s4_dequant", A, B, 2 * A.shape[1], row_scale, col_scale, C, out_dtype,
                     torch.uint8, stream)
+
+
+def _new_out(shape, dtype, device, stream):
+    """An output of our own: if the work runs on another stream than the current one, the
+    allocator must not hand its memory on before that stream is done with it."""
+    out = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None and stream != torch.cuda.current_stream():
+        out.record_stream(stream)
+    return out
+
+
+def _rows_2d(t, dtype, shape, what):
+    """Pointer and row pitch of a matrix whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.dtype != dtype:
+        raise TypeError("%s must have dtype %s, got %s" % (what, dtype, t.dtype))
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, got %s" % (what, shape, tuple(t.shape)))
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+
+
+def _linear(fn_name, A, B, in_dtype, K, scales, bias, activation, residual, C, out_dtype, stream):
+    if A.dim() != 2 or B.dim() != 2 or A.shape[1] != B.shape[1]:
+        raise ValueError("A and B disagree on K")
+    M, N = A.shape[0], B.shape[0]
+    if C is not None:
+        out_dtype = C.dtype
+    if out_dtype not in (torch.float32, torch.float16):
+        raise TypeError("the result is float32 or float16")
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation is one of %s" % ", ".join(ACTIVATIONS))
+    if bias is not None and bias.numel() != N:
+        raise ValueError("bias needs N entries")
+    if C is None:
+        C = _new_out((M, N), out_dtype, A.device, stream)
+    e = _Epilogue(activation=ACTIVATIONS[activation], c_is_fp16=1 if out_dtype == torch.float16 else 0)
+    if bias is not None:
+        e.bias = _dev_ptr(bias, torch.float32, "bias")
+    if residual is not None:
+        e.residual, e.ldr = _rows_2d(residual, out_dtype, (M, N), "residual")
+    c_ptr, e.ldc = _rows_2d(C, out_dtype, (M, N), "C")
+    args = [_dev_ptr(A, in_dtype, "A"), _dev_ptr(B, in_dtype, "B")]
+    if scales is not None:
+        if scales[0].numel() != M or scales[1].numel() != N:
+            raise ValueError("row_scale needs M entries, col_scale N")
+        args += [_dev_ptr(scales[0], torch.float32, "row_scale"),
+                 _dev_ptr(scales[1], torch.float32, "col_scale")]
+    _check(getattr(lib(), fn_name)(M, N, K, *args, c_ptr, ctypes.byref(e), _stream_handle(stream)), fn_name)
+    return C
+
+
+def gemm_fp16_linear(A, B, bias=None, activation="none", residual=None, C=None,
+                     out_dtype=torch.float16, stream=None):
+    """act(A @ B^T + bias) + residual for float16 A (M, K), B (N, K); bias float32 (N,), residual
+    and result (M, N) in out_dtype (float16 or float32), with contiguous rows of any pitch.
+    activation: a key of ACTIVATIONS.  residual may be C itself."""
+    return _linear("gemm_fp16_linear", A, B, torch.float16, A.shape[-1], None, bias, activation,
+                   residual, C, out_dtype, stream)
+
+
+def gemm_s8_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
+                   out_dtype=torch.float16, stream=None):
+    """act(float(A @ B^T) * row_scale[:, None] * col_scale + bias) + residual for int8 operands."""
+    return _linear("gemm_s8_linear", A, B, torch.int8, A.shape[-1], (row_scale, col_scale), bias,
+                   activation, residual, C, out_dtype, stream)
+
+
+def gemm_s4_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
+                   out_dtype=torch.float16, stream=None):
+    """gemm_s8_linear for packed signed 4-bit operands ((rows, K/2) uint8)."""
+    return _linear("gemm_s4_linear", A, B, torch.uint8, 2 * A.shape[-1], (row_scale, col_scale), bias,
+                   activation, residual, C, out_dtype, stream)
+
+
+def gemm_quantize_rows(X, precision="s8", Q=None, row_scale=None, stream=None):
+    """Rows of X (float16 or float32, contiguous rows of any pitch) as int8 codes (rows, K) or packed
+    4-bit ones (rows, K/2) uint8, and float32 scales (rows,): amax / 127 resp. amax / 7."""
+    if precision not in ("s8", "s4"):
+        raise ValueError("precision is s8 or s4")
+    if X.dim() != 2 or X.dtype not in (torch.float16, torch.float32):
+        raise TypeError("X must be a float16 or float32 matrix")
+    rows, K = X.shape
+    x_ptr, ldx = _rows_2d(X, X.dtype, (rows, K), "X")
+    width, dtype = (K, torch.int8) if precision == "s8" else (K // 2, torch.uint8)
+    if Q is None:
+        Q = _new_out((rows, width), dtype, X.device, stream)
+    elif tuple(Q.shape) != (rows, width):
+        raise ValueError("Q must have shape (%d, %d)" % (rows, width))
+    if row_scale is None:
+        row_scale = _new_out((rows,), torch.float32, X.device, stream)
+    elif row_scale.numel() != rows:
+        raise ValueError("row_scale needs one entry per row")
+    _check(lib().gemm_quantize_rows(PRECISION_ID[precision], rows, K, x_ptr, ldx,
+                                    1 if X.dtype == torch.float16 else 0, _dev_ptr(Q, dtype, "Q"),
+                                    _dev_ptr(row_scale, torch.float32, "row_scale"),
+                                    _stream_handle(stream)), "gemm_quantize_rows")
+    return Q, row_scale
+
+
+# ----------------------------------------------------------------- INT8 key/value cache
+def kv_cache_s8(num_pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda"):
+    """(k, v, k_scale, v_scale) of an empty cache: int8 (num_pages, kv_heads, page_size, head_dim) and
+    float32 (num_pages, kv_heads), as the kv_* functions take it."""
+    shape = (num_pages, kv_heads, page_size, head_dim)
+    return (torch.zeros(shape, dtype=torch.int8, device=device),
+            torch.zeros(shape, dtype=torch.int8, device=device),
+            torch.zeros(shape[:2], dtype=torch.float32, device=device),
+            torch.zeros(shape[:2], dtype=torch.float32, device=device))
+
+
+def _kv_cache(cache):
+    k, v, k_scale, v_scale = cache
+    if k.dim() != 4 or v.shape != k.shape or k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+        raise ValueError("cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim), two (pages, heads)")
+    return _KvCache(_dev_ptr(k, torch.int8, "k"), _dev_ptr(v, torch.int8, "v"),
+                    _dev_ptr(k_scale, torch.float32, "k_scale"),
+                    _dev_ptr(v_scale, torch.float32, "v_scale"), *k.shape)
+
+
+def _kv_batch(cu, start, table, what):
+    if cu.numel() != start.numel() + 1:
+        raise ValueError("cu needs one entry more than %s" % what)
+    if table.dim() != 2 or table.shape[0] != start.numel():
+        raise ValueError("block_table needs one row per sequence")
+    return (start.numel(), _dev_ptr(cu, torch.int32, "cu"), _dev_ptr(start, torch.int32, what),
+            _dev_ptr(table, torch.int32, "block_table"), table.shape[1])
+
+
+def _kv_rows(t, heads, dim, what):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor" % what)
+    if t.dtype != torch.float16:
+        raise TypeError("%s must have dtype torch.float16, got %s" % (what, t.dtype))
+    if t.dim() != 3 or t.shape[2] != dim or (heads and t.shape[1] != heads) or t.stride(2) != 1:
+        raise ValueError("%s must be (tokens, heads, %d) with contiguous heads" % (what, dim))
+    token = t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
+    return t.data_ptr(), token, (t.stride(1) if t.shape[1] > 1 else dim)
+
+
+def kv_append_s8(cache, k, v, cu, past, block_table, max_new: int, stream=None):
+    """Quantises the rows of k and v (float16 (tokens, kv_heads, head_dim) views with one common pair of
+    strides) into the cache: rows cu[b] .. cu[b+1] become tokens past[b], past[b] + 1, ... of sequence b."""
+    c = _kv_cache(cache)
+    kp, ts, hs = _kv_rows(k, c.kv_heads, c.head_dim, "k")
+    vp, ts2, hs2 = _kv_rows(v, c.kv_heads, c.head_dim, "v")
+    if k.shape != v.shape or (ts, hs) != (ts2, hs2):
+        raise ValueError("k and v must have the same shape and strides")
+    if k.shape[0] == 0:
+        return
+    _check(lib().kv_append_s8(ctypes.byref(c), *_kv_batch(cu, past, block_table, "past"), int(max_new),
+                              kp, vp, ts, hs, _stream_handle(stream)), "kv_append_s8")
+
+
+def kv_read_s8(cache, cu, first, block_table, max_read: int, tokens: int | None = None, out=None,
+               stream=None):
+    """Tokens first[b] .. first[b] + cu[b+1] - cu[b] - 1 of every sequence as float16 (k, v), each (tokens,
+    kv_heads, head_dim).  tokens = cu[-1], which is read from the device when not given."""
+    c = _kv_cache(cache)
+    if out is None:
+        tokens = int(cu[-1]) if tokens is None else tokens
+        shape = (tokens, c.kv_heads, c.head_dim)
+        out = tuple(_new_out(shape, torch.float16, cache[0].device, stream) for _ in range(2))
+    for t in out:
+        if tuple(t.shape[1:]) != (c.kv_heads, c.head_dim):
+            raise ValueError("outputs are (tokens, kv_heads, head_dim)")
+    if out[0].shape[0] == 0:
+        return out
+    _check(lib().kv_read_s8(ctypes.byref(c), *_kv_batch(cu, first, block_table, "first"), int(max_read),
+                            _dev_ptr(out[0], torch.float16, "k"), _dev_ptr(out[1], torch.float16, "v"),
+                            _stream_handle(stream)), "kv_read_s8")
+    return out
+
+
+def kv_attention_s8(q, cache, cu, kv_len, block_table, max_q: int, softmax_scale: float | None = None,
+                    window: int = 0, out=None, stream=None):
+    """Attention of q (float16 (tokens, q_heads, head_dim), rows cu[b] .. cu[b+1] the last tokens of sequence
+    b) over the kv_len[b] tokens each sequence has in the cache; softmax_scale defaults to head_dim ** -0.5."""
+    c = _kv_cache(cache)
+    qp, ts, hs = _kv_rows(q, 0, c.head_dim, "q")
+    if out is None:
+        out = _new_out(tuple(q.shape), torch.float16, q.device, stream)
+    elif tuple(out.shape) != tuple(q.shape):
+        raise ValueError("out must have the shape of q")
+    op, out_ts, out_hs = _kv_rows(out, 0, c.head_dim, "out")
+    if out_hs != c.head_dim:
+        raise ValueError("the heads of a row of out must be contiguous")
+    if q.shape[0] == 0:
+        return out
+    scale = c.head_dim ** -0.5 if softmax_scale is None else float(softmax_scale)
+    _check(lib().kv_attention_s8(ctypes.byref(c), *_kv_batch(cu, kv_len, block_table, "kv_len"), int(max_q),
+                                 q.shape[1], qp, ts, hs, scale, int(window), op, out_ts,
+                                 _stream_handle(stream)), "kv_attention_s8")
+    return out
 
 
 def gemm_s4_workspace_bytes(M: int, N: int, K: int) -> int:

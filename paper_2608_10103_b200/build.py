@@ -1,6 +1,8 @@
 """Builds libb200gemm.so in-tree with nvcc for sm_100a (cross-compiles without a GPU).
 
     python -m paper_2608_10103_b200.build [--force] [--verbose]
+
+One object per .cu file, compiled side by side, linked into one shared library.
 """
 from __future__ import annotations
 
@@ -8,6 +10,7 @@ import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
@@ -17,9 +20,9 @@ INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 NVCC_FLAGS = [
     "-std=c++17", "-O3", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-shared",
-    "-cudart", "shared",
+    "-Xcompiler", "-fPIC",
 ]
+LINK_FLAGS = ["-shared", "-cudart", "shared"]
 
 
 def sources():
@@ -38,10 +41,21 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + sources()
-    subprocess.check_call(cmd)
-    os.replace(tmp, LIB)
+    extra = ["-Xptxas", "-v"] if verbose else []
+    with tempfile.TemporaryDirectory(prefix="b200gemm_build_") as tmp:
+        objects, running = [], []
+        for src in sources():
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            cmd = [nvcc] + NVCC_FLAGS + extra + ["-c", "-o", obj, src]
+            running.append((cmd, subprocess.Popen(cmd)))
+            objects.append(obj)
+        codes = [(cmd, p.wait()) for cmd, p in running]
+        for cmd, rc in codes:
+            if rc != 0:
+                raise subprocess.CalledProcessError(rc, cmd)
+        out = LIB + ".tmp.%d" % os.getpid()
+        subprocess.check_call([nvcc] + NVCC_FLAGS + LINK_FLAGS + ["-o", out] + objects)
+    os.replace(out, LIB)
     return LIB
 
 

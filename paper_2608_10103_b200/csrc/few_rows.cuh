@@ -46,6 +46,7 @@
 
 #include "gemm_kernel.cuh"
 #include "ptx.cuh"
+#include "warp_pieces.cuh"
 
 namespace b200gemm {
 
@@ -62,11 +63,14 @@ struct FewRowsParams {
   const float* scale_l;
   int scale_s_first;    // 1: float(sum) * scale_s * scale_l, 0: float(sum) * scale_l * scale_s
                         // (the caller's row factor is applied first either way)
+  // linear layers (EPI_LIN16 / EPI_LIN32): act(x + bias[l or s]) + residual, residual element
+  // (s, l) at s * r_stride_s + l * r_stride_l
+  LinearEpilogue lin;   // row_bias: per long row, col_bias: per short row
+  long long r_stride_s, r_stride_l;
   int wait_prior_grid;  // launched to start early: wait for the grid in front before any access
   int depth;            // ring slots per thread = steps in flight per warp, 2 .. FEW_ROWS_MAX_DEPTH
 };
 
-constexpr int FEW_ROWS_MAX_DEPTH = 8;
 // Operand kinds of few_rows_kernel: int8, packed signed 4-bit, binary16.
 constexpr int FEW_ROWS_S8 = 0, FEW_ROWS_S4 = 1, FEW_ROWS_F16 = 2;
 
@@ -82,72 +86,7 @@ __host__ __device__ constexpr int few_rows_red_bytes(int mt, int nt, int warps) 
 
 namespace few_rows_detail {
 
-// 16 bytes global -> shared, asynchronously; bytes = 0 writes zeros and reads nothing.
-// cg: through L2 only (the long operand, read once); ca: kept in L1 too (the short operand,
-// which every CTA of the SM reads again: a third of the kernel's requests).
-__device__ __forceinline__ void cp_async_16_cg(uint32_t dst, const uint8_t* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
-               : "memory");
-}
-__device__ __forceinline__ void cp_async_16_ca(uint32_t dst, const uint8_t* src, int bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
-               : "memory");
-}
-// (The kernel may have been launched while the grid in front of it was still writing its
-// operands -- programmatic dependent launch -- and reads nothing before griddepcontrol.wait.  The
-// non-coherent path, ld.global.nc / __ldg, carries no order against that wait and promises
-// nothing for data written during the kernel's lifetime: a version that fetched a step into
-// registers with it returned a few hundred wrong sums per call for INT4 through gemm_host, whose
-// int8 scratch is rewritten by the unpack kernel right in front.  Nothing here uses it.)
-__device__ __forceinline__ void prefetch_l2(const uint8_t* p) {
-  asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
-}
-// Scale factors: an ordinary load, for the same reason.
-__device__ __forceinline__ float ld_f32(const float* p) {
-  float v;
-  asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
-  return v;
-}
-__device__ __forceinline__ void cp_async_commit() {
-  asm volatile("cp.async.commit_group;" ::: "memory");
-}
-template <int PENDING>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory");
-}
-// The instruction takes its count as an immediate; pending is 0 .. FEW_ROWS_MAX_DEPTH - 1 (0, a
-// ring of one slot, is never launched but must not fall through to a wait that waits for less).
-__device__ __forceinline__ void cp_async_wait_all_but(int pending) {
-  switch (pending) {
-    case 0: cp_async_wait<0>(); break;
-    case 1: cp_async_wait<1>(); break;
-    case 2: cp_async_wait<2>(); break;
-    case 3: cp_async_wait<3>(); break;
-    case 4: cp_async_wait<4>(); break;
-    case 5: cp_async_wait<5>(); break;
-    case 6: cp_async_wait<6>(); break;
-    default: cp_async_wait<7>(); break;
-  }
-}
-
-__device__ __forceinline__ void mma_s8_m16n8k32(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                                uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-      "{%8, %9}, {%0, %1, %2, %3};"
-      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// FP16 operands: 16 rows x 16 values against 8 rows per instruction, FP32 accumulators; a 32-bit
-// word holds two values, and words w, w + 1 of a thread's piece fill its K positions 2t, 2t + 1
-// and 2t + 8, 2t + 9 on both sides.
-__device__ __forceinline__ void mma_f16_m16n8k16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                                 uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-      "{%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
+using namespace warp_pieces;
 
 template <bool F16>
 struct AccOf {
@@ -157,10 +96,6 @@ template <>
 struct AccOf<true> {
   using type = float;
 };
-
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) {
-  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-}
 
 __device__ __forceinline__ uint32_t low_nibbles_x16(uint32_t w) { return (w << 4) & 0xF0F0F0F0u; }
 __device__ __forceinline__ uint32_t high_nibbles_x16(uint32_t w) { return w & 0xF0F0F0F0u; }
@@ -362,7 +297,27 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
       Acc sum = 0;
       for (int w = 0; w < warps; ++w) sum += red[w * (8 * NT * RED_PITCH) + s * RED_PITCH + l];
       const long long at = s * p.c_stride_s + static_cast<long long>(l0 + l) * p.c_stride_l;
-      if constexpr (EPI == EPI_RAW32) {
+      if constexpr (epi_linear(EPI)) {
+        float x = static_cast<float>(sum);
+        if constexpr (!F16) {
+          const float fs = ld_f32(p.scale_s + s), fl = ld_f32(p.scale_l + l0 + l);
+          x = p.scale_s_first ? x * fs * fl : x * fl * fs;
+        }
+        if (p.lin.row_bias) x += ld_f32(p.lin.row_bias + l0 + l);
+        if (p.lin.col_bias) x += ld_f32(p.lin.col_bias + s);
+        x = lin_activate(x, p.lin);
+        if (p.lin.residual) {
+          const long long rat = s * p.r_stride_s + static_cast<long long>(l0 + l) * p.r_stride_l;
+          if constexpr (EPI == EPI_LIN16)
+            x += __half2float(*(static_cast<const volatile __half*>(p.lin.residual) + rat));
+          else
+            x += ld_f32(static_cast<const float*>(p.lin.residual) + rat);
+        }
+        if constexpr (EPI == EPI_LIN16)
+          static_cast<__half*>(p.C)[at] = __float2half_rn(x);
+        else
+          static_cast<float*>(p.C)[at] = x;
+      } else if constexpr (EPI == EPI_RAW32) {
         static_cast<Acc*>(p.C)[at] = sum;
       } else if constexpr (F16) {
         static_cast<__half*>(p.C)[at] = __float2half_rn(sum);  // EPI_OUT16: rounded once

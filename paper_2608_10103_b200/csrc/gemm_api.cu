@@ -16,9 +16,52 @@
 #include "peak_probe.cuh"
 #include "runtime.cuh"
 #include "selector.cuh"
+#include "shared_state.h"
 #include "unpack_s4.cuh"
 
 using namespace b200gemm;
+
+// What the other translation unit sees of this one's state (shared_state.h).
+namespace b200gemm {
+namespace {
+ScratchPool g_kv_pool[MAX_DEVICES];  // apart from g_pool: its heads hold other bookkeeping
+}
+
+int shared_device(SharedDevice* out) {
+  DeviceState* s = nullptr;
+  const int rc = device_state(&s, &out->device);
+  if (rc != GEMM_OK) return rc;
+  out->num_sms = s->num_sms;
+  out->status = s->status_ptr;
+  out->plain_order = (g_l2_policy & 32) != 0;
+  return GEMM_OK;
+}
+
+int shared_cuda_fail(cudaError_t e) { return cuda_fail(e); }
+
+int shared_scratch(int device, cudaStream_t stream, size_t need, size_t head, SharedLease* out) {
+  ScratchPool::Lease l;
+  const int rc = g_kv_pool[device].acquire(stream, need, head, &l);
+  if (rc != 0) return pool_fail(rc);
+  out->ptr = l.ptr;
+  out->head = l.ptr;
+  out->data = static_cast<uint8_t*>(l.ptr) + l.head_bytes;
+  out->bytes = l.bytes;
+  out->head_bytes = l.head_bytes;
+  out->slot = l.slot;
+  return GEMM_OK;
+}
+
+int shared_scratch_done(int device, cudaStream_t stream, const SharedLease& lease) {
+  ScratchPool::Lease l;
+  l.ptr = lease.ptr;
+  l.bytes = lease.bytes;
+  l.head_bytes = lease.head_bytes;
+  l.slot = lease.slot;
+  const int rc = g_kv_pool[device].release(l, stream);
+  return rc == 0 ? GEMM_OK : pool_fail(rc);
+}
+}  // namespace b200gemm
 
 extern "C" {
 
@@ -97,20 +140,80 @@ int gemm_s4_dequant(int M, int N, int K, const uint8_t* A, const uint8_t* B,
   return s4_auto(M, N, K, A, B, C, out, reinterpret_cast<cudaStream_t>(stream));
 }
 
+// A, B of the linear layers: as for the plain products; C and the residual only need the
+// alignment of their elements.
+static int check_linear_operands(int M, int N, int K, const void* A, const void* B) {
+  return check_common(M, N, K, A, B, A);
+}
+
+int gemm_fp16_linear(int M, int N, int K, const void* A, const void* B, void* C,
+                     const gemm_epilogue_t* epilogue, gemm_stream_t stream) {
+  int rc = check_linear_operands(M, N, K, A, B);
+  if (rc != GEMM_OK) return rc;
+  if (K % 8) return GEMM_ERR_MISALIGNED;
+  OutputSpec out;
+  rc = check_linear(M, N, C, epilogue, nullptr, nullptr, false, &out);
+  if (rc != GEMM_OK) return rc;
+  return launch_gemm<ptx::KIND_F16>(M, N, K, A, static_cast<size_t>(K) * 2, B,
+                                    static_cast<size_t>(K) * 2, C,
+                                    reinterpret_cast<cudaStream_t>(stream), out);
+}
+
+int gemm_s8_linear(int M, int N, int K, const int8_t* A, const int8_t* B, const float* row_scale,
+                   const float* col_scale, void* C, const gemm_epilogue_t* epilogue,
+                   gemm_stream_t stream) {
+  int rc = check_linear_operands(M, N, K, A, B);
+  if (rc != GEMM_OK) return rc;
+  if (K % 16) return GEMM_ERR_MISALIGNED;
+  if (K > K_LIMIT_INT) return GEMM_ERR_K_TOO_LARGE;
+  OutputSpec out;
+  rc = check_linear(M, N, C, epilogue, row_scale, col_scale, true, &out);
+  if (rc != GEMM_OK) return rc;
+  return launch_gemm<ptx::KIND_I8>(M, N, K, A, static_cast<size_t>(K), B, static_cast<size_t>(K), C,
+                                   reinterpret_cast<cudaStream_t>(stream), out);
+}
+
+int gemm_s4_linear(int M, int N, int K, const uint8_t* A, const uint8_t* B, const float* row_scale,
+                   const float* col_scale, void* C, const gemm_epilogue_t* epilogue,
+                   gemm_stream_t stream) {
+  int rc = check_s4(M, N, K, A, B, A);
+  if (rc != GEMM_OK) return rc;
+  OutputSpec out;
+  rc = check_linear(M, N, C, epilogue, row_scale, col_scale, true, &out);
+  if (rc != GEMM_OK) return rc;
+  return s4_auto(M, N, K, A, B, C, out, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int gemm_quantize_rows(int precision, int rows, int K, const void* X, long long ldx, int x_is_fp16,
+                       void* Q, float* row_scale, gemm_stream_t stream) {
+  if ((precision != GEMM_PREC_S8 && precision != GEMM_PREC_S4) || rows <= 0 || K <= 0 || !X || !Q ||
+      !row_scale || (x_is_fp16 != 0 && x_is_fp16 != 1) || (ldx && ldx < K))
+    return GEMM_ERR_INVALID_ARG;
+  if (K % (precision == GEMM_PREC_S4 ? 32 : 16) || (reinterpret_cast<uintptr_t>(Q) & 15) ||
+      (reinterpret_cast<uintptr_t>(row_scale) & 3) ||
+      (reinterpret_cast<uintptr_t>(X) & (x_is_fp16 ? 1 : 3)))
+    return GEMM_ERR_MISALIGNED;
+  if (K > K_LIMIT_INT) return GEMM_ERR_K_TOO_LARGE;
+  return launch_quantize_rows(rows, K, X, ldx ? ldx : K, x_is_fp16 != 0, precision == GEMM_PREC_S4, Q,
+                              row_scale, reinterpret_cast<cudaStream_t>(stream));
+}
+
 int gemm_release_workspaces(void) {
   int cur = 0;
   if (cudaGetDevice(&cur) != cudaSuccess) cur = -1;
   int rc = GEMM_OK;
   for (int d = 0; d < MAX_DEVICES; ++d) {
-    if (g_pool[d].buffers() == 0) continue;
+    if (g_pool[d].buffers() == 0 && g_kv_pool[d].buffers() == 0) continue;
     cudaError_t e = cudaSetDevice(d);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e != cudaSuccess) {
       rc = cuda_fail(e);
       continue;
     }
-    const int r = g_pool[d].release_all();
-    if (r != 0) rc = cuda_fail(static_cast<cudaError_t>(r));
+    for (ScratchPool* pool : {&g_pool[d], &g_kv_pool[d]}) {
+      const int r = pool->release_all();
+      if (r != 0) rc = cuda_fail(static_cast<cudaError_t>(r));
+    }
   }
   if (cur >= 0) cudaSetDevice(cur);
   return rc;

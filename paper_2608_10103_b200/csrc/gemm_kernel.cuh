@@ -56,6 +56,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "linear_epilogue.cuh"
 #include "ptx.cuh"
 #include "s4_ahead.cuh"
 
@@ -89,7 +90,12 @@ enum EpiMode {
   EPI_OUT16 = 1,       // binary16: FP32 accumulators rounded once (RNE); INT32 accumulators
                        // converted to float and multiplied by row_scale[i] * col_scale[j] first
   EPI_F32_SCALED = 2,  // float(INT32 accumulator) * row_scale[i] * col_scale[j]
+  // linear layers (see linear_epilogue.cuh): act(sum [* scales] + bias) + residual,
+  EPI_LIN16 = 3,       // ... rounded once to binary16
+  EPI_LIN32 = 4,       // ... as FP32
 };
+__host__ __device__ constexpr bool epi_linear(int epi) { return epi >= EPI_LIN16; }
+__host__ __device__ constexpr bool epi_out16(int epi) { return epi == EPI_OUT16 || epi == EPI_LIN16; }
 
 struct GemmParams {
   int M, N, K;
@@ -128,6 +134,7 @@ struct GemmParams {
   int wait_prior_grid;
   const float* row_scale;  // EPI_OUT16 (integer kinds) / EPI_F32_SCALED: M per-row factors
   const float* col_scale;  // and N per-column factors; both null = no scaling (FP16 kind)
+  LinearEpilogue lin;      // EPI_LIN16 / EPI_LIN32: bias, activation, residual
   int* status;           // device status word (0 = ok)
   // Optional per-CTA cycle accounting (TRACE_SLOTS 64-bit words per CTA), or null.
   unsigned long long* trace;
@@ -958,7 +965,15 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       const int row0 = tm * TILE_M + static_cast<int>(cta_rank) * BM + quarter * 32;
       const int row = row0 + lane;
       const int col0 = tn * BN;
-      float rs = 1.0f;
+      float rs = 1.0f, rb = 0.0f;
+      if constexpr (epi_linear(EPI)) {
+        // (the grid in front has finished: see the wait above)
+        if (!xpeer) {
+          if (p.lin.row_bias && row < p.M) rb = ptx::ld_global_f32(p.lin.row_bias + row);
+          if (p.lin.residual && !p.transpose_c && row < p.M)
+            lin_prefetch_row<epi_out16(EPI) ? 2 : 4, BN>(p.lin, row, col0, p.N);
+        }
+      }
       if constexpr (EPI != EPI_RAW32) {
         // The scale factors are fetched while the mainloop still runs: this thread's row
         // factor into a register, the tile's column factors into L1 (one line per lane).
@@ -1036,7 +1051,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       // spreads the warp's 16-byte stores over all banks.
       // (The 32-wide tile with 16-bit output has no staging form -- a block would be 64 bytes
       // wide -- and only ever runs with plain stores: c_vec_ok = 0, set by the host.)
-      constexpr int BLOCK_COLS = (EPI == EPI_OUT16 && BN >= 64) ? 64 : 32;
+      constexpr int BLOCK_COLS = (epi_out16(EPI) && BN >= 64) ? 64 : 32;
       static_assert(BN % BLOCK_COLS == 0, "tile width must be a multiple of the store block");
 #pragma unroll 1
       for (int c = 0; c < BN / BLOCK_COLS && !xpeer; ++c) {
@@ -1091,6 +1106,37 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           for (int v = 0; v < 32; ++v) {
             const float cs = __shfl_sync(0xffffffffu, cs_mine, v);
             w[v] = __float_as_uint(acc_to_float<KIND>(fix(w[v])) * rs * cs);
+          }
+        } else if constexpr (epi_linear(EPI)) {
+#pragma unroll
+          for (int h = 0; h < BLOCK_COLS / 32; ++h) {
+            const int c32 = col + h * 32, cc = c32 + lane;
+            constexpr int RBYTES = epi_out16(EPI) ? 2 : 4;
+            uint32_t res[RBYTES * 8];  // requested first: they arrive while the sums are fetched
+            if (p.lin.residual)
+              lin_load_residual<RBYTES>(p.lin, row, c32, p.M, p.N, p.transpose_c, res);
+            const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
+            const float cb_mine =
+                (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
+            uint32_t r[32];
+            ptx::tmem_ld_32x32b_x32(
+                tmem_base + lane_base + static_cast<uint32_t>(acc * BN + c * BLOCK_COLS + h * 32), r);
+            ptx::tmem_wait_ld();
+            add_partial(r, c * (BLOCK_COLS / 32) + h);
+            float x[32];
+#pragma unroll
+            for (int v = 0; v < 32; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
+            lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
+            lin_activate32(x, p.lin);
+            if (p.lin.residual) lin_add_residual<RBYTES>(x, res);
+#pragma unroll
+            for (int v = 0; v < 32; ++v) {
+              if constexpr (epi_out16(EPI)) {
+                if (v % 2 == 0) w[h * 16 + v / 2] = pack_half2(x[v], x[v + 1]);
+              } else {
+                w[v] = __float_as_uint(x[v]);
+              }
+            }
           }
         } else {
 #pragma unroll
@@ -1161,7 +1207,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           // element (row, col + v) sits at row * rstep + (col + v) * cstep
           const size_t rstep = p.transpose_c ? 1 : static_cast<size_t>(p.ldc);
           const size_t cstep = p.transpose_c ? static_cast<size_t>(p.ldc) : 1;
-          if constexpr (EPI == EPI_OUT16) {
+          if constexpr (epi_out16(EPI)) {
             uint16_t* crow = reinterpret_cast<uint16_t*>(p.C) + static_cast<size_t>(row) * rstep;
 #pragma unroll
             for (int v = 0; v < BLOCK_COLS; ++v)

@@ -328,7 +328,7 @@ gemm_wide_kernel(const __grid_constant__ CUtensorMap tmap_a,
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t buf = base + L::EPI_OFFSET + static_cast<uint32_t>(ew * L::EPI_BUF_BYTES);
     const uint64_t pol_c = p.c_evict_first ? ptx::policy_evict_first() : ptx::policy_evict_normal();
-    constexpr int C_ELEM = (EPI == EPI_OUT16) ? 2 : 4;
+    constexpr int C_ELEM = epi_out16(EPI) ? 2 : 4;
     constexpr int BLOCK_COLS = 128 / C_ELEM;  // columns of C in one staged block (128-byte rows)
     constexpr int BLOCKS = 128 / BLOCK_COLS;  // blocks per accumulator for this warp
     const size_t pitch = static_cast<size_t>(p.ldc) * C_ELEM;
@@ -345,6 +345,13 @@ gemm_wide_kernel(const __grid_constant__ CUtensorMap tmap_a,
       const int cta_row0 = tm * WIDE_TILE_M + static_cast<int>(cta_rank) * WIDE_CTA_ROWS;
       const int col_base = tn * WIDE_BN + half * 128;
       float rs[2] = {1.0f, 1.0f};
+      if constexpr (epi_linear(EPI)) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          const int row = cta_row0 + a * BM + quarter * 32 + lane;
+          if (p.lin.residual && row < p.M) lin_prefetch_row<C_ELEM, 128>(p.lin, row, col_base, p.N);
+        }
+      }
       if constexpr (EPI != EPI_RAW32) {
         // scale factors are fetched while the mainloop still runs (they may come from the grid
         // in front, whose end the producer awaits as well before its first load)
@@ -410,6 +417,30 @@ gemm_wide_kernel(const __grid_constant__ CUtensorMap tmap_a,
               const float cs = __shfl_sync(0xffffffffu, cs_mine, i);
               w[i] = __float_as_uint(acc_to_float<KIND>(v[c][i]) * rs_a * cs);
             }
+          } else if constexpr (epi_linear(EPI)) {
+#pragma unroll
+            for (int h = 0; h < BLOCK_COLS / 32; ++h) {
+              const int c32 = col + h * 32, cc = c32 + lane;
+              uint32_t res[C_ELEM * 8];
+              if (p.lin.residual) lin_load_residual<C_ELEM>(p.lin, row, c32, p.M, p.N, 0, res);
+              const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
+              const float cb_mine =
+                  (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
+              float x[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) x[i] = acc_to_float<KIND>(v[c * (BLOCK_COLS / 32) + h][i]);
+              lin_scale_bias(x, KIND == ptx::KIND_I8, rs_a, cs_mine, 0.0f, cb_mine, true);
+              lin_activate32(x, p.lin);
+              if (p.lin.residual) lin_add_residual<C_ELEM>(x, res);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                if constexpr (C_ELEM == 2) {
+                  if (i % 2 == 0) w[h * 16 + i / 2] = pack_half2(x[i], x[i + 1]);
+                } else {
+                  w[i] = __float_as_uint(x[i]);
+                }
+              }
+            }
           } else {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -444,7 +475,7 @@ gemm_wide_kernel(const __grid_constant__ CUtensorMap tmap_a,
             __syncwarp();  // the buffer is rewritten by the next block
           } else if (row < p.M) {
             // rows of C are not 16-byte multiples: plain predicated stores, one row per thread
-            if constexpr (EPI == EPI_OUT16) {
+            if constexpr (epi_out16(EPI)) {
               uint16_t* crow = reinterpret_cast<uint16_t*>(p.C) + static_cast<size_t>(row) * p.ldc;
 #pragma unroll
               for (int i = 0; i < BLOCK_COLS; ++i)

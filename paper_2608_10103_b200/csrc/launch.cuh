@@ -6,6 +6,7 @@
 
 #include "few_rows.cuh"
 #include "gemm_wide.cuh"
+#include "quantize_rows.cuh"
 #include "runtime.cuh"
 #include "selector.cuh"
 #include "unpack_s4.cuh"
@@ -43,6 +44,11 @@ constexpr int dbg_twin_bit() {
   if (KIND == ptx::KIND_I8 && EPI == EPI_OUT16 && CSPLIT == 4 && PSTAGES == 0) return 214;
   return -1;
 }
+
+// attr_set bits: every family below numbers its variants with four output modes in mind; the
+// fifth one has a bank of bits of its own.
+constexpr int epi_slot(int epi) { return epi & 3; }
+constexpr int epi_bank(int epi) { return (epi >> 2) * 320; }
 
 template <class Kernel>
 int launch_kernel(DeviceState* s, Kernel kernel, int variant, int dyn_bytes, int threads,
@@ -105,7 +111,7 @@ int launch_wide(DeviceState* s, const CUtensorMap& ta, const CUtensorMap& tb, co
                 cudaStream_t stream) {
   const bool dbg = p.ablate != 0;
   if (dbg && EPI != EPI_RAW32) return GEMM_ERR_INVALID_ARG;  // switches exist for the raw outputs
-  const int variant = 160 + ((KIND == ptx::KIND_F16) ? 0 : 8) + EPI * 2 + (dbg ? 1 : 0);
+  const int variant = 160 + ((KIND == ptx::KIND_F16) ? 0 : 8) + epi_slot(EPI) * 2 + epi_bank(EPI) + (dbg ? 1 : 0);
   void (*kernel)(CUtensorMap, CUtensorMap, GemmParams) = gemm_wide_kernel<KIND, EPI, false>;
   if constexpr (EPI == EPI_RAW32) {
     if (dbg) kernel = gemm_wide_kernel<KIND, EPI, true>;
@@ -180,6 +186,7 @@ struct OutputSpec {
   const float* row_scale = nullptr;
   const float* col_scale = nullptr;
   long long ldc = 0;        // row pitch of C in elements; 0 = dense (N)
+  LinearEpilogue lin = {};  // EPI_LIN16 / EPI_LIN32, in the caller's orientation (bias in col_bias)
   bool no_split = false;    // C is a block of a larger matrix: never zero / add into it
   bool tiles_only = false;  // the GEMM of the INT4 pre-pass route: always a tile kernel
 };
@@ -212,7 +219,7 @@ constexpr int GEMM_WANT_A8 = 3;
 // Index in attr_set of the unfused cluster split-K variants: 96.., by kind, output mode, width.
 template <int KIND, int EPI>
 constexpr int csplit_variant_base() {
-  return 96 + ((KIND == ptx::KIND_F16) ? 0 : 16) + EPI * 2;
+  return 96 + ((KIND == ptx::KIND_F16) ? 0 : 16) + epi_slot(EPI) * 2 + epi_bank(EPI);
 }
 
 // How many clusters of four CTAs of the 4-way cluster split-K kernel the device holds at once.
@@ -391,11 +398,13 @@ bool s4_hybrid_wanted(int M, int N, int K) {
 // (INT8, M = 48-64: 3-8 %; FP16 -> FP16, M = 40-64: 1-13 %; FP16 -> FP32 even; from M = 80 on,
 // where the narrow side needs the 128-wide tile, 4-20 % slower).
 bool swap_ab_wanted(int M, int N, bool integer_kind, const OutputSpec& out) {
-  if (out.no_split || out.ldc) return false;  // C is a block of a larger matrix
+  // C is a block of a larger matrix (a linear layer's pitch is no obstacle: it has plain stores
+  // for both orders and never adds into C)
+  if (out.no_split || (out.ldc && !epi_linear(out.epi))) return false;
   if (g_swap_ab == 1) return false;
   if (g_swap_ab == 2) return true;
   // (FP16 -> FP32 at M = 33..64: 3-4 % faster from N = 16384 on, 2-4 % slower at N = 8192)
-  return N >= 1024 && M <= ((integer_kind || out.epi == EPI_OUT16 || N >= 16384) ? 64 : 32);
+  return N >= 1024 && M <= ((integer_kind || epi_out16(out.epi) || N >= 16384) ? 64 : 32);
 }
 
 // Returned (never to the caller of the library) when the fused INT4 kernel does not cover the
@@ -415,7 +424,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   int rc = device_state(&s);
   if (rc != GEMM_OK) return rc;
   constexpr int ELEM = (KIND == ptx::KIND_F16) ? 2 : 1;
-  constexpr int C_ELEM = (EPI == EPI_OUT16) ? 2 : 4;
+  constexpr int C_ELEM = epi_out16(EPI) ? 2 : 4;
   const long long ldc = out.ldc ? out.ldc : N;
   const int user_m = M, user_n = N;
   const bool swap = swap_ab_wanted(M, N, KIND == ptx::KIND_I8, out);
@@ -430,7 +439,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   int k_blocks = ceil_div(static_cast<long long>(K) * ELEM, BK_BYTES);
   // 16-bit outputs are staged 64 columns at a time; with exchanged operands C goes out by
   // plain stores and the 32-wide tile serves them too
-  const int min_bn = (EPI == EPI_OUT16 && !swap) ? 64 : 32;
+  const int min_bn = (epi_out16(EPI) && !swap) ? 64 : 32;
   const bool split_through_c = EPI == EPI_RAW32 && !out.no_split;
   TileConfig cfg = select_config(M, N, s->num_sms, k_blocks, min_bn, split_through_c);
   bool fused_cfg = false;
@@ -450,7 +459,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
       const TileConfig c2 =
           select_config(M, N, s->num_sms, k_blocks, min_bn, true, packed_s4 ? 2 : 0, cap);
       if (c2.bn == 0 || !cluster_split_ok(c2, M, N)) continue;
-      if (c2.splits == 4 && (EPI != EPI_OUT16 || swap)) {
+      if (c2.splits == 4 && (!epi_out16(EPI) || swap)) {
         if (!g_override_splits &&
             c2.split_tiles > quad_clusters_resident<KIND, EPI>(s, csplit_variant_base<KIND, EPI>() + 8))
           continue;
@@ -506,7 +515,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
     // against 495 k + a 36 us (~50 k cycle) pre-pass.  The same role inside the 512 x 256 kernel,
     // whose L2 port has a quarter to spare, measured no better (596 k against ~520 k).
     const long long tiles = static_cast<long long>(ceil_div(M, 2 * BM)) * ceil_div(N, 256);
-    ahead = KIND == ptx::KIND_I8 && !wide && !swap && !csplit && !packed_s4 && cfg.bn == 256 &&
+    ahead = KIND == ptx::KIND_I8 && !epi_linear(EPI) && !wide && !swap && !csplit && !packed_s4 && cfg.bn == 256 &&
             cfg.cta_group == 2 && cfg.stages == 6 && g_s4_scheme == 4 && (g_trace_on >> 1) == 0 &&
             tiles >= 2 * (s->num_sms / 2);
     if (!ahead) return GEMM_NOT_AHEAD;
@@ -541,7 +550,9 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   // otherwise include the time spent waiting for the predecessor's tail
   p.wait_prior_grid = ((g_l2_policy & 32) || (g_trace_on & 1)) ? 0 : 1;
   p.c_vec_ok = !swap && (ldc % (16 / C_ELEM) == 0) && (reinterpret_cast<uintptr_t>(C) % 16 == 0);
-  if (wide && N % (16 / C_ELEM)) p.c_vec_ok = 0;  // its 16-byte stores must end on a row's end
+  // 16-byte stores must end on a row's end (the copy engine clips a box at N, but writes whole
+  // 16-byte pieces: with a pitch beyond N, N = 1100 binary16 columns had zeros put behind them)
+  if (N % (16 / C_ELEM)) p.c_vec_ok = 0;
   CUtensorMap tc;
   if (wide) {
     tc = ta;  // the wide kernel writes C with plain stores
@@ -558,6 +569,8 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   p.C = static_cast<uint32_t*>(C);
   p.row_scale = swap ? out.col_scale : out.row_scale;  // indexed by the kernel's rows
   p.col_scale = swap ? out.row_scale : out.col_scale;
+  p.lin = out.lin;
+  if (swap) std::swap(p.lin.row_bias, p.lin.col_bias);
   p.status = s->status_ptr;
   p.trace = (g_trace_on & 1) ? s->trace_ptr : nullptr;
   p.ablate = (g_trace_on >> 1) & 63;
@@ -650,12 +663,12 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   }
   if (csplit && packed_s4) {  // attr_set bits 128..
     if constexpr (KIND == ptx::KIND_I8) {
-      const int cb = 128 + EPI * 2;
+      const int cb = 128 + epi_slot(EPI) * 2 + epi_bank(EPI);
       if (cfg.bn == 64)
         return launch_variant<KIND, 64, 4, 1, 1, EPI, 2, 2>(s, cb + 1, ta, tb, tc, p, stream);
-      if (EPI != EPI_OUT16 || swap) {
+      if (!epi_out16(EPI) || swap) {
         if (cfg.splits == 4)
-          return launch_variant<KIND, 32, 4, 1, 1, EPI, 3, 4>(s, 136 + EPI, ta, tb, tc, p, stream);
+          return launch_variant<KIND, 32, 4, 1, 1, EPI, 3, 4>(s, 136 + epi_slot(EPI) + epi_bank(EPI), ta, tb, tc, p, stream);
         return launch_variant<KIND, 32, 4, 1, 1, EPI, 4, 2>(s, cb, ta, tb, tc, p, stream);
       }
     }
@@ -665,19 +678,19 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
     const int cb = csplit_variant_base<KIND, EPI>();
     if (cfg.bn == 64)
       return launch_variant<KIND, 64, 3, 1, 2, EPI, 0, 2>(s, cb + 1, ta, tb, tc, p, stream);
-    if (EPI != EPI_OUT16 || swap) {
+    if (!epi_out16(EPI) || swap) {
       if (cfg.splits == 4)
         return launch_variant<KIND, 32, 3, 1, 2, EPI, 0, 4>(s, cb + 8, ta, tb, tc, p, stream);
       return launch_variant<KIND, 32, 4, 1, 2, EPI, 0, 2>(s, cb, ta, tb, tc, p, stream);
     }
     return GEMM_ERR_INVALID_ARG;
   }
-  const int vbase = ((KIND == ptx::KIND_F16) ? 0 : 32) + EPI * 8;  // bit index in attr_set
+  const int vbase = ((KIND == ptx::KIND_F16) ? 0 : 32) + epi_slot(EPI) * 8 + epi_bank(EPI);  // bit index in attr_set
   if (packed_s4) {
     // fused INT4 variants: (int8 slots, packed slots) sized to fill shared memory; attr_set
     // bits 64.. (one per tile shape and output mode)
     if constexpr (KIND == ptx::KIND_I8) {
-      const int fb = 64 + EPI * 8;
+      const int fb = 64 + epi_slot(EPI) * 8 + epi_bank(EPI);
       if (hybrid) {  // (int8 slots, packed B slots) = (4, 4): two groups of expansion warps
         if (cfg.bn == 128) {
           using L = SmemLayout<128, 4, 2, 1, 4, 1, true>;
@@ -698,7 +711,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
         case 128: return launch_variant<KIND, 128, 4, 1, 1, EPI, 2>(s, fb + 2, ta, tb, tc, p, stream);
         case 64: return launch_variant<KIND, 64, 4, 1, 1, EPI, 4>(s, fb + 3, ta, tb, tc, p, stream);
         case 32:
-          if (EPI != EPI_OUT16 || swap)
+          if (!epi_out16(EPI) || swap)
             return launch_variant<KIND, 32, 4, 1, 1, EPI, 5>(s, fb + 4, ta, tb, tc, p, stream);
           return GEMM_ERR_INVALID_ARG;
         default: return GEMM_ERR_INVALID_ARG;
@@ -709,7 +722,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   if (cfg.cta_group == 2) {
     switch (cfg.bn) {
       case 256:
-        if constexpr (KIND == ptx::KIND_I8) {
+        if constexpr (KIND == ptx::KIND_I8 && !epi_linear(EPI)) {
           if (ahead) {  // attr_set bits 224..
             t_last_s4_overlapped = 1;
             using L = SmemLayout<256, 6, 2, 1, 0, 1>;
@@ -735,7 +748,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
     case 128: return launch_variant<KIND, 128, 3, 1, 2, EPI>(s, vbase + 1, ta, tb, tc, p, stream);
     case 64: return launch_variant<KIND, 64, 4, 1, 2, EPI>(s, vbase + 2, ta, tb, tc, p, stream);
     case 32:
-      if (EPI != EPI_OUT16 || swap)
+      if (!epi_out16(EPI) || swap)
         return launch_variant<KIND, 32, 4, 1, 2, EPI>(s, vbase + 3, ta, tb, tc, p, stream);
       return GEMM_ERR_INVALID_ARG;
     default: return GEMM_ERR_INVALID_ARG;
@@ -839,8 +852,9 @@ FewRowsShape few_rows_shape(int rows_l, int rows_s, int row_bytes, int num_sms) 
 template <int FKIND, int NT, int EPI>
 int launch_few_rows_nt(DeviceState* s, FewRowsParams& p, const FewRowsShape& f,
                        cudaStream_t stream) {
-  // attr_set bits 256..282: by operand kind, short-row groups, output mode
-  constexpr int variant = 256 + (FKIND * 3 + (NT == 1 ? 0 : NT == 2 ? 1 : 2)) * 3 + EPI;
+  // attr_set bits 256..291: by operand kind, short-row groups, output mode
+  constexpr int variant =
+      256 + (FKIND * 3 + (NT == 1 ? 0 : NT == 2 ? 1 : 2)) * 4 + epi_slot(EPI) + epi_bank(EPI);
   auto kernel = few_rows_kernel<FKIND, FEW_ROWS_MT, NT, EPI>;
   if (!(s->attr_set[variant >> 6].load(std::memory_order_relaxed) & (1ull << (variant & 63)))) {
     const cudaError_t e = cudaFuncSetAttribute(
@@ -886,6 +900,11 @@ int launch_few_rows(int M, int N, int K, const void* A, size_t a_pitch, const vo
   p.scale_s = a_short ? out.row_scale : out.col_scale;
   p.scale_l = a_short ? out.col_scale : out.row_scale;
   p.scale_s_first = a_short ? 1 : 0;
+  p.lin = out.lin;  // the bias goes by the caller's columns
+  p.lin.row_bias = a_short ? out.lin.col_bias : nullptr;
+  p.lin.col_bias = a_short ? nullptr : out.lin.col_bias;
+  p.r_stride_s = a_short ? out.lin.ldr : 1;
+  p.r_stride_l = a_short ? 1 : out.lin.ldr;
   p.wait_prior_grid = (g_l2_policy & 32) ? 0 : 1;
   const FewRowsShape f = few_rows_shape(p.rows_l, p.rows_s, p.row_bytes, s->num_sms);
   switch (ceil_div(p.rows_s, 8)) {
@@ -914,6 +933,12 @@ int launch_gemm(int M, int N, int K, const void* A, size_t a_pitch, const void* 
         case EPI_F32_SCALED:
           return packed_s4 ? launch_few_rows<FEW_ROWS_S4, EPI_F32_SCALED>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream)
                            : launch_few_rows<FEW_ROWS_S8, EPI_F32_SCALED>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
+        case EPI_LIN16:
+          return packed_s4 ? launch_few_rows<FEW_ROWS_S4, EPI_LIN16>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream)
+                           : launch_few_rows<FEW_ROWS_S8, EPI_LIN16>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
+        case EPI_LIN32:
+          return packed_s4 ? launch_few_rows<FEW_ROWS_S4, EPI_LIN32>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream)
+                           : launch_few_rows<FEW_ROWS_S8, EPI_LIN32>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
         default: return GEMM_ERR_INVALID_ARG;
       }
     }
@@ -923,6 +948,10 @@ int launch_gemm(int M, int N, int K, const void* A, size_t a_pitch, const void* 
         return launch_few_rows<FEW_ROWS_F16, EPI_RAW32>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
       if (out.epi == EPI_OUT16)
         return launch_few_rows<FEW_ROWS_F16, EPI_OUT16>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
+      if (out.epi == EPI_LIN16)
+        return launch_few_rows<FEW_ROWS_F16, EPI_LIN16>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
+      if (out.epi == EPI_LIN32)
+        return launch_few_rows<FEW_ROWS_F16, EPI_LIN32>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream);
     }
   }
   switch (out.epi) {
@@ -937,6 +966,12 @@ int launch_gemm(int M, int N, int K, const void* A, size_t a_pitch, const void* 
         return launch_gemm_epi<KIND, EPI_F32_SCALED>(M, N, K, A, a_pitch, B, b_pitch, C, out,
                                                      stream, packed_s4, req, hyb);
       return GEMM_ERR_INVALID_ARG;
+    case EPI_LIN16:
+      return launch_gemm_epi<KIND, EPI_LIN16>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream,
+                                              packed_s4, req, hyb);
+    case EPI_LIN32:
+      return launch_gemm_epi<KIND, EPI_LIN32>(M, N, K, A, a_pitch, B, b_pitch, C, out, stream,
+                                              packed_s4, req, hyb);
     default: return GEMM_ERR_INVALID_ARG;
   }
 }
@@ -1110,6 +1145,91 @@ int check_scales(const float* row_scale, const float* col_scale, const void* C, 
   out->row_scale = row_scale;
   out->col_scale = col_scale;
   return GEMM_OK;
+}
+
+// The epilogue of a linear layer (see gemm_epilogue_t).  Fills `out` for launch_gemm.
+int check_linear(int M, int N, const void* C, const gemm_epilogue_t* e, const float* row_scale,
+                 const float* col_scale, bool scaled, OutputSpec* out) {
+  if (!C || !e || (scaled && (!row_scale || !col_scale))) return GEMM_ERR_INVALID_ARG;
+  if (e->c_is_fp16 != 0 && e->c_is_fp16 != 1) return GEMM_ERR_INVALID_ARG;
+  const long long ldc = e->ldc ? e->ldc : N, ldr = e->ldr ? e->ldr : N;
+  const int size = e->c_is_fp16 ? 2 : 4;
+  if (ldc < N || (M > 1 && ldc > (1ll << 37))) return GEMM_ERR_INVALID_ARG;
+  if (e->residual && (ldr < N || (e->residual == C && ldr != ldc))) return GEMM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(C) | reinterpret_cast<uintptr_t>(e->residual)) & (size - 1))
+    return GEMM_ERR_MISALIGNED;
+  if ((reinterpret_cast<uintptr_t>(row_scale) | reinterpret_cast<uintptr_t>(col_scale) |
+       reinterpret_cast<uintptr_t>(e->bias)) & 3)
+    return GEMM_ERR_MISALIGNED;
+  LinearEpilogue l = {};
+  l.col_bias = e->bias;
+  l.residual = e->residual;
+  l.ldr = ldr;
+  l.r_vec_ok = ldr % (16 / size) == 0 && reinterpret_cast<uintptr_t>(e->residual) % 16 == 0;
+  switch (e->activation) {
+    case GEMM_ACT_NONE: l.act = LIN_ACT_NONE; break;
+    case GEMM_ACT_RELU: l.act = LIN_ACT_RELU; break;
+    case GEMM_ACT_GELU: l.act = LIN_ACT_ERF; break;
+    case GEMM_ACT_GELU_TANH:  // 2 sqrt(2/pi) (x + 0.044715 x^3)
+      l.act = LIN_ACT_GATE;
+      l.gate_a = 1.5957691216057308f;
+      l.gate_b = 0.07135481282635852f;
+      break;
+    case GEMM_ACT_SILU:
+      l.act = LIN_ACT_GATE;
+      l.gate_a = 1.0f;
+      break;
+    default: return GEMM_ERR_INVALID_ARG;
+  }
+  out->epi = e->c_is_fp16 ? EPI_LIN16 : EPI_LIN32;
+  out->row_scale = scaled ? row_scale : nullptr;
+  out->col_scale = scaled ? col_scale : nullptr;
+  out->ldc = ldc == N ? 0 : ldc;
+  out->lin = l;
+  return GEMM_OK;
+}
+
+// Attribute of every small kernel here: may start while the grid in front still runs.
+cudaLaunchConfig_t chained_config(dim3 grid, dim3 block, size_t smem, cudaStream_t stream,
+                                  cudaLaunchAttribute* attr) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr->val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = (g_l2_policy & 32) ? 0 : 1;
+  return cfg;
+}
+
+int launch_quantize_rows(int rows, int K, const void* x, long long ldx, bool f16, bool s4, void* q,
+                         float* scale, cudaStream_t stream) {
+  DeviceState* s = nullptr;
+  const int rc = device_state(&s);
+  if (rc != GEMM_OK) return rc;
+  QuantRowsParams p;
+  p.x = x;
+  p.ldx = ldx;
+  p.q = static_cast<uint8_t*>(q);
+  p.scale = scale;
+  p.rows = rows;
+  p.K = K;
+  const int size = f16 ? 2 : 4;
+  p.vec_ok = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || ldx * size % 16 == 0);
+  // two pieces per thread: enough loads in flight, and a row of up to 16 K values stays in registers
+  p.row_threads = 32;
+  while (p.row_threads < QR_THREADS && p.row_threads * 16 < K) p.row_threads *= 2;
+  const int rows_per_cta = QR_THREADS / p.row_threads;
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = chained_config(dim3(ceil_div(rows, rows_per_cta)), dim3(QR_THREADS), 0, stream, &attr);
+  const cudaError_t e =
+      f16 ? (s4 ? cudaLaunchKernelEx(&cfg, quantize_rows_kernel<true, true>, p)
+                : cudaLaunchKernelEx(&cfg, quantize_rows_kernel<true, false>, p))
+          : (s4 ? cudaLaunchKernelEx(&cfg, quantize_rows_kernel<false, true>, p)
+                : cudaLaunchKernelEx(&cfg, quantize_rows_kernel<false, false>, p));
+  return e == cudaSuccess ? GEMM_OK : cuda_fail(e);
 }
 }  // namespace
 }  // namespace b200gemm

@@ -38,10 +38,10 @@ struct DeviceState {
   int* status_ptr = nullptr;
   unsigned long long* trace_ptr = nullptr;
   // bit i: dynamic-smem attribute set for kernel variant i (setting it twice is harmless)
-  std::atomic<uint64_t> attr_set[5] = {};
+  std::atomic<uint64_t> attr_set[10] = {};
   // clusters of four CTAs (cluster split-K) the device runs at once, per kind and output
   // mode; 0 = not asked yet
-  std::atomic<int> quad_clusters[2][4] = {};
+  std::atomic<int> quad_clusters[2][5] = {};
 };
 
 std::mutex g_mutex;  // first-use initialisation only
