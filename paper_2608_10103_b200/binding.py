@@ -119,8 +119,14 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+# The current stream's handle without a Stream object around it (3 us a call), where torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_handle(stream) -> int:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
@@ -258,55 +264,69 @@ def gemm_s4_dequant(A, B, row_scale, col_scale, C=None, out_dtype=torch.float32,
                     torch.uint8, stream)
 
 
-def _new_out(shape, dtype, device, stream):
+def _new_out(like, shape, dtype, stream):
     """An output of our own: if the work runs on another stream than the current one, the
     allocator must not hand its memory on before that stream is done with it."""
-    out = torch.empty(shape, dtype=dtype, device=device)
+    out = like.new_empty(shape, dtype=dtype)
     if stream is not None and stream != torch.cuda.current_stream():
         out.record_stream(stream)
     return out
 
 
-def _rows_2d(t, dtype, shape, what):
+def _rows_2d(t, dtype, rows, cols, what):
     """Pointer and row pitch of a matrix whose rows are contiguous."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % what)
     if t.dtype != dtype:
         raise TypeError("%s must have dtype %s, got %s" % (what, dtype, t.dtype))
-    if tuple(t.shape) != shape:
-        raise ValueError("%s must have shape %s, got %s" % (what, shape, tuple(t.shape)))
-    if shape[1] > 1 and t.stride(1) != 1:
+    if t.shape != (rows, cols):
+        raise ValueError("%s must have shape %s, got %s" % (what, (rows, cols), tuple(t.shape)))
+    pitch, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % what)
-    return t.data_ptr(), (t.stride(0) if shape[0] > 1 else shape[1])
+    return t.data_ptr(), (pitch if rows > 1 else cols)
 
 
-def _linear(fn_name, A, B, in_dtype, K, scales, bias, activation, residual, C, out_dtype, stream):
-    if A.dim() != 2 or B.dim() != 2 or A.shape[1] != B.shape[1]:
+def _linear(fn_name, A, B, in_dtype, per_byte, scales, bias, activation, residual, C, out_dtype, stream):
+    M, K = A.shape
+    N, Kb = B.shape
+    if K != Kb:
         raise ValueError("A and B disagree on K")
-    M, N = A.shape[0], B.shape[0]
-    if C is not None:
-        out_dtype = C.dtype
-    if out_dtype not in (torch.float32, torch.float16):
-        raise TypeError("the result is float32 or float16")
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError("activation is one of %s" % ", ".join(ACTIVATIONS))
-    if bias is not None and bias.numel() != N:
-        raise ValueError("bias needs N entries")
+    a, b = _dev_ptr(A, in_dtype, "A"), _dev_ptr(B, in_dtype, "B")
     if C is None:
-        C = _new_out((M, N), out_dtype, A.device, stream)
-    e = _Epilogue(activation=ACTIVATIONS[activation], c_is_fp16=1 if out_dtype == torch.float16 else 0)
+        C = _new_out(A, (M, N), out_dtype, stream)
+        c, ldc = C.data_ptr(), N
+    else:
+        out_dtype = C.dtype
+        c, ldc = _rows_2d(C, out_dtype, M, N, "C")
+    if out_dtype is torch.float16:
+        half = 1
+    elif out_dtype is torch.float32:
+        half = 0
+    else:
+        raise TypeError("the result is float32 or float16")
+    bias_ptr = res_ptr = None
+    ldr = 0
     if bias is not None:
-        e.bias = _dev_ptr(bias, torch.float32, "bias")
+        if bias.numel() != N:
+            raise ValueError("bias needs N entries")
+        bias_ptr = _dev_ptr(bias, torch.float32, "bias")
     if residual is not None:
-        e.residual, e.ldr = _rows_2d(residual, out_dtype, (M, N), "residual")
-    c_ptr, e.ldc = _rows_2d(C, out_dtype, (M, N), "C")
-    args = [_dev_ptr(A, in_dtype, "A"), _dev_ptr(B, in_dtype, "B")]
-    if scales is not None:
-        if scales[0].numel() != M or scales[1].numel() != N:
+        res_ptr, ldr = _rows_2d(residual, out_dtype, M, N, "residual")
+    e = ctypes.byref(_Epilogue(bias_ptr, act, half, res_ptr, ldr, ldc))
+    fn = getattr(lib(), fn_name)
+    if scales is None:
+        rc = fn(M, N, K, a, b, c, e, _stream_handle(stream))
+    else:
+        rs, cs = scales
+        if rs.numel() != M or cs.numel() != N:
             raise ValueError("row_scale needs M entries, col_scale N")
-        args += [_dev_ptr(scales[0], torch.float32, "row_scale"),
-                 _dev_ptr(scales[1], torch.float32, "col_scale")]
-    _check(getattr(lib(), fn_name)(M, N, K, *args, c_ptr, ctypes.byref(e), _stream_handle(stream)), fn_name)
+        rc = fn(M, N, K * per_byte, a, b, _dev_ptr(rs, torch.float32, "row_scale"),
+                _dev_ptr(cs, torch.float32, "col_scale"), c, e, _stream_handle(stream))
+    _check(rc, fn_name)
     return C
 
 
@@ -315,21 +335,21 @@ def gemm_fp16_linear(A, B, bias=None, activation="none", residual=None, C=None,
     """act(A @ B^T + bias) + residual for float16 A (M, K), B (N, K); bias float32 (N,), residual
     and result (M, N) in out_dtype (float16 or float32), with contiguous rows of any pitch.
     activation: a key of ACTIVATIONS.  residual may be C itself."""
-    return _linear("gemm_fp16_linear", A, B, torch.float16, A.shape[-1], None, bias, activation,
+    return _linear("gemm_fp16_linear", A, B, torch.float16, 1, None, bias, activation,
                    residual, C, out_dtype, stream)
 
 
 def gemm_s8_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
                    out_dtype=torch.float16, stream=None):
     """act(float(A @ B^T) * row_scale[:, None] * col_scale + bias) + residual for int8 operands."""
-    return _linear("gemm_s8_linear", A, B, torch.int8, A.shape[-1], (row_scale, col_scale), bias,
+    return _linear("gemm_s8_linear", A, B, torch.int8, 1, (row_scale, col_scale), bias,
                    activation, residual, C, out_dtype, stream)
 
 
 def gemm_s4_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
                    out_dtype=torch.float16, stream=None):
     """gemm_s8_linear for packed signed 4-bit operands ((rows, K/2) uint8)."""
-    return _linear("gemm_s4_linear", A, B, torch.uint8, 2 * A.shape[-1], (row_scale, col_scale), bias,
+    return _linear("gemm_s4_linear", A, B, torch.uint8, 2, (row_scale, col_scale), bias,
                    activation, residual, C, out_dtype, stream)
 
 
@@ -338,21 +358,22 @@ def gemm_quantize_rows(X, precision="s8", Q=None, row_scale=None, stream=None):
     4-bit ones (rows, K/2) uint8, and float32 scales (rows,): amax / 127 resp. amax / 7."""
     if precision not in ("s8", "s4"):
         raise ValueError("precision is s8 or s4")
-    if X.dim() != 2 or X.dtype not in (torch.float16, torch.float32):
+    x_dtype = X.dtype
+    if X.dim() != 2 or (x_dtype is not torch.float16 and x_dtype is not torch.float32):
         raise TypeError("X must be a float16 or float32 matrix")
     rows, K = X.shape
-    x_ptr, ldx = _rows_2d(X, X.dtype, (rows, K), "X")
+    x_ptr, ldx = _rows_2d(X, x_dtype, rows, K, "X")
     width, dtype = (K, torch.int8) if precision == "s8" else (K // 2, torch.uint8)
     if Q is None:
-        Q = _new_out((rows, width), dtype, X.device, stream)
-    elif tuple(Q.shape) != (rows, width):
+        Q = _new_out(X, (rows, width), dtype, stream)
+    elif Q.shape != (rows, width):
         raise ValueError("Q must have shape (%d, %d)" % (rows, width))
     if row_scale is None:
-        row_scale = _new_out((rows,), torch.float32, X.device, stream)
+        row_scale = _new_out(X, (rows,), torch.float32, stream)
     elif row_scale.numel() != rows:
         raise ValueError("row_scale needs one entry per row")
     _check(lib().gemm_quantize_rows(PRECISION_ID[precision], rows, K, x_ptr, ldx,
-                                    1 if X.dtype == torch.float16 else 0, _dev_ptr(Q, dtype, "Q"),
+                                    1 if x_dtype is torch.float16 else 0, _dev_ptr(Q, dtype, "Q"),
                                     _dev_ptr(row_scale, torch.float32, "row_scale"),
                                     _stream_handle(stream)), "gemm_quantize_rows")
     return Q, row_scale
@@ -371,42 +392,47 @@ def kv_cache_s8(num_pages: int, kv_heads: int, page_size: int, head_dim: int, de
 
 def _kv_cache(cache):
     k, v, k_scale, v_scale = cache
-    if k.dim() != 4 or v.shape != k.shape or k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
         raise ValueError("cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim), two (pages, heads)")
     return _KvCache(_dev_ptr(k, torch.int8, "k"), _dev_ptr(v, torch.int8, "v"),
                     _dev_ptr(k_scale, torch.float32, "k_scale"),
-                    _dev_ptr(v_scale, torch.float32, "v_scale"), *k.shape)
+                    _dev_ptr(v_scale, torch.float32, "v_scale"), *shape)
 
 
 def _kv_batch(cu, start, table, what):
-    if cu.numel() != start.numel() + 1:
+    batch = start.numel()
+    if cu.numel() != batch + 1:
         raise ValueError("cu needs one entry more than %s" % what)
-    if table.dim() != 2 or table.shape[0] != start.numel():
+    rows, width = table.shape
+    if rows != batch:
         raise ValueError("block_table needs one row per sequence")
-    return (start.numel(), _dev_ptr(cu, torch.int32, "cu"), _dev_ptr(start, torch.int32, what),
-            _dev_ptr(table, torch.int32, "block_table"), table.shape[1])
+    return (batch, _dev_ptr(cu, torch.int32, "cu"), _dev_ptr(start, torch.int32, what),
+            _dev_ptr(table, torch.int32, "block_table"), width)
 
 
 def _kv_rows(t, heads, dim, what):
+    """Pointer, tokens, heads and the strides of both of a (tokens, heads, dim) view."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a CUDA tensor" % what)
     if t.dtype != torch.float16:
         raise TypeError("%s must have dtype torch.float16, got %s" % (what, t.dtype))
-    if t.dim() != 3 or t.shape[2] != dim or (heads and t.shape[1] != heads) or t.stride(2) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != dim or (heads and shape[1] != heads) or stride[2] != 1:
         raise ValueError("%s must be (tokens, heads, %d) with contiguous heads" % (what, dim))
-    token = t.stride(0) if t.shape[0] > 1 else t.shape[1] * dim
-    return t.data_ptr(), token, (t.stride(1) if t.shape[1] > 1 else dim)
+    head = stride[1] if shape[1] > 1 else dim
+    return t.data_ptr(), shape[0], shape[1], (stride[0] if shape[0] > 1 else shape[1] * dim), head
 
 
 def kv_append_s8(cache, k, v, cu, past, block_table, max_new: int, stream=None):
     """Quantises the rows of k and v (float16 (tokens, kv_heads, head_dim) views with one common pair of
     strides) into the cache: rows cu[b] .. cu[b+1] become tokens past[b], past[b] + 1, ... of sequence b."""
     c = _kv_cache(cache)
-    kp, ts, hs = _kv_rows(k, c.kv_heads, c.head_dim, "k")
-    vp, ts2, hs2 = _kv_rows(v, c.kv_heads, c.head_dim, "v")
-    if k.shape != v.shape or (ts, hs) != (ts2, hs2):
+    kp, tokens, _, ts, hs = _kv_rows(k, c.kv_heads, c.head_dim, "k")
+    vp, *rest = _kv_rows(v, c.kv_heads, c.head_dim, "v")
+    if rest != [tokens, c.kv_heads, ts, hs]:
         raise ValueError("k and v must have the same shape and strides")
-    if k.shape[0] == 0:
+    if tokens == 0:
         return
     _check(lib().kv_append_s8(ctypes.byref(c), *_kv_batch(cu, past, block_table, "past"), int(max_new),
                               kp, vp, ts, hs, _stream_handle(stream)), "kv_append_s8")
@@ -420,10 +446,9 @@ def kv_read_s8(cache, cu, first, block_table, max_read: int, tokens: int | None 
     if out is None:
         tokens = int(cu[-1]) if tokens is None else tokens
         shape = (tokens, c.kv_heads, c.head_dim)
-        out = tuple(_new_out(shape, torch.float16, cache[0].device, stream) for _ in range(2))
-    for t in out:
-        if tuple(t.shape[1:]) != (c.kv_heads, c.head_dim):
-            raise ValueError("outputs are (tokens, kv_heads, head_dim)")
+        out = (_new_out(cache[0], shape, torch.float16, stream), _new_out(cache[0], shape, torch.float16, stream))
+    elif out[0].shape[1:] != (c.kv_heads, c.head_dim) or out[1].shape != out[0].shape:
+        raise ValueError("outputs are two (tokens, kv_heads, head_dim)")
     if out[0].shape[0] == 0:
         return out
     _check(lib().kv_read_s8(ctypes.byref(c), *_kv_batch(cu, first, block_table, "first"), int(max_read),
@@ -437,19 +462,21 @@ def kv_attention_s8(q, cache, cu, kv_len, block_table, max_q: int, softmax_scale
     """Attention of q (float16 (tokens, q_heads, head_dim), rows cu[b] .. cu[b+1] the last tokens of sequence
     b) over the kv_len[b] tokens each sequence has in the cache; softmax_scale defaults to head_dim ** -0.5."""
     c = _kv_cache(cache)
-    qp, ts, hs = _kv_rows(q, 0, c.head_dim, "q")
+    qp, tokens, q_heads, ts, hs = _kv_rows(q, 0, c.head_dim, "q")
     if out is None:
-        out = _new_out(tuple(q.shape), torch.float16, q.device, stream)
-    elif tuple(out.shape) != tuple(q.shape):
-        raise ValueError("out must have the shape of q")
-    op, out_ts, out_hs = _kv_rows(out, 0, c.head_dim, "out")
-    if out_hs != c.head_dim:
-        raise ValueError("the heads of a row of out must be contiguous")
-    if q.shape[0] == 0:
+        out = _new_out(q, (tokens, q_heads, c.head_dim), torch.float16, stream)
+        op, out_ts = out.data_ptr(), q_heads * c.head_dim
+    else:
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+        op, _, _, out_ts, out_hs = _kv_rows(out, 0, c.head_dim, "out")
+        if out_hs != c.head_dim:
+            raise ValueError("the heads of a row of out must be contiguous")
+    if tokens == 0:
         return out
-    scale = c.head_dim ** -0.5 if softmax_scale is None else float(softmax_scale)
-    _check(lib().kv_attention_s8(ctypes.byref(c), *_kv_batch(cu, kv_len, block_table, "kv_len"), int(max_q),
-                                 q.shape[1], qp, ts, hs, scale, int(window), op, out_ts,
+    scale = c.head_dim ** -0.5 if softmax_scale is None else softmax_scale
+    _check(lib().kv_attention_s8(ctypes.byref(c), *_kv_batch(cu, kv_len, block_table, "kv_len"), max_q,
+                                 q_heads, qp, ts, hs, scale, window, op, out_ts,
                                  _stream_handle(stream)), "kv_attention_s8")
     return out
 

@@ -68,15 +68,16 @@ int launch(const SharedDevice& dev, Kernel kernel, dim3 grid, int threads, size_
 
 constexpr int MAX_DEV = 64;
 
-// Shared memory a CTA of the few-rows attention kernel takes, and how many fit an SM.
-template <int D, int MT>
+// D: head size, NR: groups of eight rows per tile.
+template <int D, int NR>
 int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stream) {
   static std::atomic<int> resident[MAX_DEV];
-  constexpr int slots = (227 * 1024 / kva_ctas(D, MT) - 2048 - kva_q_bytes(D, MT)) / (KVA_WARPS * kva_slot_bytes(D));
+  constexpr int room = 227 * 1024 / kva_ctas(D, NR) - 2048 - kva_q_bytes(D, NR);
+  constexpr int slots = room / (KVA_WARPS * kva_slot_bytes(D));
   constexpr int depth = slots < 8 ? slots : 8;
   static_assert(depth >= 2, "the ring holds two steps at least");
-  constexpr int smem = kva_smem(D, MT, depth);
-  auto kernel = kv_attention_kernel<D, MT>;
+  constexpr int smem = kva_smem(D, NR, depth);
+  auto kernel = kv_attention_kernel<D, NR, depth>;
   int per_sm = resident[dev.device].load();
   if (per_sm == 0) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -85,11 +86,14 @@ int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stre
     if (per_sm < 1) return shared_cuda_fail(cudaErrorLaunchOutOfResources);
     resident[dev.device].store(per_sm);
   }
-  p.depth = depth;
-  p.min_share = 16;
+  p.min_share = 8;
   const int grid = per_sm * dev.num_sms;
-  const int rows = 16 * MT;
+  const int rows = 8 * NR;
   const long long tiles = (static_cast<long long>(p.max_q) * p.group + rows - 1) / rows;
+  // the kernel counts steps of 16 tokens in 32 bits
+  const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1;
+  if (tiles * p.c.heads >= (1ll << 30) / steps / p.batch || static_cast<long long>(p.max_q + 1ll) * p.group + rows >= (1ll << 31))
+    return GEMM_ERR_TOO_LARGE;
   const size_t counters = static_cast<size_t>(p.batch) * tiles * p.c.heads * 4;
   const size_t bytes = 2ull * grid * kva_rows_floats(rows, D) * 4;
   SharedLease lease;
@@ -196,11 +200,18 @@ int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const 
   p.window = window;
   p.status = dev.status;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  const bool few = static_cast<long long>(max_q) * p.group <= 16;
+  const long long max_len = static_cast<long long>(table_stride) * p.c.page;
+  p.max_len = max_len < 0x7fffffff - 256 ? static_cast<int>(max_len) : 0x7fffffff - 256;
+  const long long rows = static_cast<long long>(max_q) * p.group;
+  const int groups = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   switch (p.c.dim) {
-    case 64: return few ? launch_attention<64, 1>(dev, p, st) : launch_attention<64, 2>(dev, p, st);
-    case 128: return few ? launch_attention<128, 1>(dev, p, st) : launch_attention<128, 2>(dev, p, st);
-    default: return launch_attention<256, 1>(dev, p, st);
+    case 64:
+      return groups == 1 ? launch_attention<64, 1>(dev, p, st)
+                         : groups == 2 ? launch_attention<64, 2>(dev, p, st) : launch_attention<64, 4>(dev, p, st);
+    case 128:
+      return groups == 1 ? launch_attention<128, 1>(dev, p, st)
+                         : groups == 2 ? launch_attention<128, 2>(dev, p, st) : launch_attention<128, 4>(dev, p, st);
+    default: return groups == 1 ? launch_attention<256, 1>(dev, p, st) : launch_attention<256, 2>(dev, p, st);
   }
 }
 
