@@ -56,6 +56,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "bounded_wait.cuh"
 #include "linear_epilogue.cuh"
 #include "ptx.cuh"
 #include "s4_ahead.cuh"
@@ -72,17 +73,6 @@ constexpr int NUM_THREADS_FUSED = NUM_THREADS + 32 * UNPACK_WARPS;
 constexpr int NUM_THREADS_FUSED_A8 = NUM_THREADS_FUSED + 32;  // hybrid: warp 14 fetches the A image
 constexpr int AHEAD_WARPS = 4;    // overlapped INT4 pre-pass only: warps 6..9
 constexpr int NUM_THREADS_AHEAD = NUM_THREADS + 32 * AHEAD_WARPS;
-constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;  // every barrier wait gives up after 2 s
-
-// Device status codes written to the status word when a wait gives up.
-enum DeviceStatus {
-  DEV_OK = 0,
-  DEV_TIMEOUT_PRODUCER = 1,
-  DEV_TIMEOUT_MMA = 2,
-  DEV_TIMEOUT_EPILOGUE = 3,
-  DEV_TIMEOUT_DRAIN = 4,
-  DEV_TIMEOUT_UNPACK = 5,
-};
 
 // What the epilogue writes.
 enum EpiMode {
@@ -220,33 +210,6 @@ struct SmemLayout {
   static_assert(B_BYTES % 1024 == 0, "B tile must keep the next slot 1024-byte aligned");
   static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");
 };
-
-// Bounded wait: polls the barrier; after the limit (or once another role has
-// given up) records `code` and returns false.  The caller then leaves its loop.
-template <bool BACKOFF = false>
-__device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity,
-                                             volatile uint32_t* abort_flag, int* status, int code,
-                                             uint32_t backoff_ns = 0) {
-  auto done = [&]() { return ptx::mbar_try_wait(bar, parity); };
-  if (done()) return true;
-  uint64_t t0 = 0;
-  uint32_t spins = 0;
-  while (true) {
-    if (done()) return true;
-    if (BACKOFF && backoff_ns) __nanosleep(backoff_ns);
-    if ((++spins & 255u) == 0) {
-      if (*abort_flag) return false;
-      uint64_t now = ptx::globaltimer_ns();
-      if (t0 == 0) {
-        t0 = now;
-      } else if (now - t0 > WAIT_LIMIT_NS) {
-        *abort_flag = 1;
-        atomicCAS(status, 0, code);
-        return false;
-      }
-    }
-  }
-}
 
 // Tile index -> (tile row, tile column).  Tiles are numbered down bands of
 // `group_m` tile rows so that the CTAs running at the same time share A rows

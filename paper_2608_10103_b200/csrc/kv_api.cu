@@ -6,6 +6,7 @@
 
 #include "../../include/b200kv.h"
 #include "kv_attention.cuh"
+#include "kv_attention_tiles.cuh"
 #include "kv_cache.cuh"
 #include "shared_state.h"
 
@@ -89,11 +90,9 @@ int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stre
   p.min_share = 8;
   const int grid = per_sm * dev.num_sms;
   const int rows = 8 * NR;
-  const long long tiles = (static_cast<long long>(p.max_q) * p.group + rows - 1) / rows;
-  // the kernel counts steps of 16 tokens in 32 bits
-  const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1;
-  if (tiles * p.c.heads >= (1ll << 30) / steps / p.batch || static_cast<long long>(p.max_q + 1ll) * p.group + rows >= (1ll << 31))
-    return GEMM_ERR_TOO_LARGE;
+  const long long most = static_cast<long long>(p.max_q) * p.group;
+  const long long tiles = ((most < p.split_rows ? most : p.split_rows) + rows - 1) / rows;
+  p.max_tiles = static_cast<int>(tiles);
   const size_t counters = static_cast<size_t>(p.batch) * tiles * p.c.heads * 4;
   const size_t bytes = 2ull * grid * kva_rows_floats(rows, D) * 4;
   SharedLease lease;
@@ -104,6 +103,43 @@ int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stre
   rc = launch(dev, kernel, dim3(grid), KVA_THREADS, smem, stream, p);
   const int done = shared_scratch_done(dev.device, stream, lease);
   return rc != GEMM_OK ? rc : done;
+}
+
+// Sequences with more than p.split_rows rows, on the tensor cores.
+template <int D>
+int launch_attention_tiles(const SharedDevice& dev, const KvAttnParams& p, cudaStream_t stream) {
+  static std::atomic<bool> ready[MAX_DEV];
+  using T = KvTileShape<D>;
+  auto kernel = kv_attention_tiles_kernel<D>;
+  if (!ready[dev.device].load()) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::DYN_BYTES);
+    if (e != cudaSuccess) return shared_cuda_fail(e);
+    ready[dev.device].store(true);
+  }
+  const long long tiles = (static_cast<long long>(p.max_q) * p.group + T::ROWS - 1) / T::ROWS;
+  const long long blocks = tiles * p.c.heads * p.batch;
+  if (blocks > 0x7fffffffll) return GEMM_ERR_TOO_LARGE;
+  return launch(dev, kernel, dim3(static_cast<unsigned>(blocks)), T::THREADS, T::DYN_BYTES, stream, p);
+}
+
+template <int D, int MAX_NR>
+int attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stream) {
+  const long long rows = static_cast<long long>(p.max_q) * p.group;
+  p.split_rows = 8 * MAX_NR;
+  // the few-rows kernel counts a sequence's tiles by the bound it is given
+  KvAttnParams few = p;
+  const long long bound = rows < p.split_rows ? rows : p.split_rows;
+  // ... and counts its steps of 16 tokens in 32 bits
+  const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1;
+  if (rows + p.group + 512 >= (1ll << 31) || (bound + 7) / 8 * p.c.heads >= (1ll << 30) / steps / p.batch)
+    return GEMM_ERR_TOO_LARGE;
+  if (rows > p.split_rows) {
+    const int rc = launch_attention_tiles<D>(dev, p, stream);
+    if (rc != GEMM_OK) return rc;
+  }
+  if (bound <= 8) return launch_attention<D, 1>(dev, few, stream);
+  if (bound <= 16 || MAX_NR == 2) return launch_attention<D, 2>(dev, few, stream);
+  return launch_attention<D, MAX_NR>(dev, few, stream);
 }
 
 }  // namespace
@@ -202,16 +238,10 @@ int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const 
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const long long max_len = static_cast<long long>(table_stride) * p.c.page;
   p.max_len = max_len < 0x7fffffff - 256 ? static_cast<int>(max_len) : 0x7fffffff - 256;
-  const long long rows = static_cast<long long>(max_q) * p.group;
-  const int groups = rows <= 8 ? 1 : rows <= 16 ? 2 : 4;
   switch (p.c.dim) {
-    case 64:
-      return groups == 1 ? launch_attention<64, 1>(dev, p, st)
-                         : groups == 2 ? launch_attention<64, 2>(dev, p, st) : launch_attention<64, 4>(dev, p, st);
-    case 128:
-      return groups == 1 ? launch_attention<128, 1>(dev, p, st)
-                         : groups == 2 ? launch_attention<128, 2>(dev, p, st) : launch_attention<128, 4>(dev, p, st);
-    default: return groups == 1 ? launch_attention<256, 1>(dev, p, st) : launch_attention<256, 2>(dev, p, st);
+    case 64: return attention<64, 4>(dev, p, st);
+    case 128: return attention<128, 4>(dev, p, st);
+    default: return attention<256, 2>(dev, p, st);
   }
 }
 

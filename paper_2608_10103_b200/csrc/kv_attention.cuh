@@ -66,8 +66,10 @@ struct KvAttnParams {
   long long out_token_stride;
   float scale_log2;  // softmax_scale * log2(e)
   int window;        // 0 = all
+  int split_rows;    // sequences of more than this many rows (queries x group) go to the tile kernel
   int* status;
   int min_share;     // steps per CTA at least
+  int max_tiles;     // row tiles of a sequence at most
   float* partial;    // [2 * grid][rows * D + rows * 2]
   unsigned* arrived; // per unit, zero before and after
 };
@@ -216,7 +218,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
 
   // ---- this CTA's share.  Thread i looks at the sequences [i * chunk, (i + 1) * chunk).
   const int heads = p.c.heads;
-  auto tiles_of = [&](const KvSeq& s) { return (s.n * p.group + ROWS - 1) / ROWS; };
+  auto tiles_of = [&](const KvSeq& s) { return s.n * p.group > p.split_rows ? 0 : (s.n * p.group + ROWS - 1) / ROWS; };
   auto tile_steps = [&](const KvSeq& s, int qt, int& lo, int& hi) {
     const int i0 = qt * ROWS / p.group, i1 = min(s.n, ((qt + 1) * ROWS + p.group - 1) / p.group);
     kv_visible(p, s, i0, i1, lo, hi);
@@ -680,8 +682,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
             c_last = (u_begin + unit_steps - 1) / share;
             second = u_begin > share * c_first;
           }
-          const int tiles_max = (p.max_q * p.group + ROWS - 1) / ROWS;
-          unsigned* const counter = p.arrived + (static_cast<long long>(b) * tiles_max + qt) * heads + head;
+          unsigned* const counter = p.arrived + (static_cast<long long>(b) * p.max_tiles + qt) * heads + head;
           __threadfence();
           __syncthreads();
           if (tid == 0) s_last = atomicAdd(counter, 1u);

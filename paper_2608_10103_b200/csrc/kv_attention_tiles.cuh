@@ -1,0 +1,460 @@
+// Attention over the INT8 cache for many query rows per KV head (a chunk of a prompt): the two products
+// on the 5th-generation tensor cores.  Same mathematics as kv_attention.cuh, except that q stays binary16.
+//
+// A CTA owns QT tiles of 128 rows (queries x heads of a group) of one KV head and walks its tokens in tiles of
+// TN.  Per tile of rows and tokens: S = Q K^T (tcgen05.mma, operands in shared memory) into tensor memory; four warps,
+// one thread per row, turn S into weights, rounded to binary16, in the same place; O += P V (A operand in tensor
+// memory).  With two tiles of rows one is in its softmax while the tensor cores work on the other.
+// K and V arrive as int8: four warps read the codes (16 bytes a thread, a tile ahead, in registers), convert them
+// exactly to binary16 and write them as rows of 64 d in the 128-byte swizzle.  Such a tile is K-major for the
+// first product and, read the other way round, MN-major for the second: no transpose anywhere.
+// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own.
+//
+// What bounds it: at 128 d, 1024 cycles of tensor pipe a tile pair of 128 x 128 against as many of exponentials
+// (16 a cycle and SM); the conversion takes a tenth of the issue slots.  O is rescaled in tensor memory only
+// when a row's maximum has grown by 2^8 (see kv_attention.cuh), so that it need not pass through registers.
+// Tiles of rows are launched with the longest of every sequence first.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "bounded_wait.cuh"
+#include "kv_attention.cuh"
+#include "ptx.cuh"
+
+namespace b200gemm {
+
+template <int D>
+struct KvTileShape {
+  static constexpr int QT = D <= 128 ? 2 : 1;      // row tiles of 128 per CTA (O fills tensor memory beyond that)
+  static constexpr int TN = D <= 128 ? 128 : 64;   // tokens per tile
+  static constexpr int ROWS = 128 * QT;
+  static constexpr int SOFTMAX_WARPS = 4 * QT;
+  static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 5);
+  static constexpr int STAGES = 2;
+  static constexpr int GROUPS = TN / 16;
+  static constexpr int CHUNK = TN * 128;           // bytes of 64 d of a K or V tile
+  static constexpr int Q_BYTES = QT * (D / 64) * 128 * 128;
+  static constexpr int KV_BYTES = (D / 64) * CHUNK;
+  static constexpr int K_OFFSET = Q_BYTES;
+  static constexpr int V_OFFSET = K_OFFSET + STAGES * KV_BYTES;
+  static constexpr int SCALES = 4;                 // ring of scale tables
+  static constexpr int SCALE_OFFSET = V_OFFSET + STAGES * KV_BYTES;
+  static constexpr int BAR_OFFSET = SCALE_OFFSET + SCALES * GROUPS * 16;
+  // q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2], scale_full[4], drain
+  static constexpr int BARS = 1 + 4 * STAGES + 6 + SCALES + 1;
+  static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
+  static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
+  static constexpr uint32_t O_COLUMN = 256;        // S (and P) of tile q at 128 q, O behind both
+  static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");
+  static_assert(O_COLUMN + QT * D <= 512, "tensor memory");
+};
+
+template <int D>
+__global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles_kernel(const KvAttnParams p) {
+  using namespace kva;
+  using T = KvTileShape<D>;
+  constexpr int QT = T::QT, TN = T::TN, GROUPS = T::GROUPS, STAGES = T::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = ptx::smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* const base_ptr = smem_raw + (base - raw);
+  const uint32_t bar0 = base + T::BAR_OFFSET;
+  const uint32_t q_full = bar0;
+  auto k_full = [&](int s) { return bar0 + 8u * (1 + s); };
+  auto k_empty = [&](int s) { return bar0 + 8u * (3 + s); };
+  auto v_full = [&](int s) { return bar0 + 8u * (5 + s); };
+  auto v_empty = [&](int s) { return bar0 + 8u * (7 + s); };
+  auto s_full = [&](int q) { return bar0 + 8u * (9 + q); };
+  auto p_full = [&](int q) { return bar0 + 8u * (11 + q); };
+  auto o_done = [&](int q) { return bar0 + 8u * (13 + q); };
+  auto scale_full = [&](int s) { return bar0 + 8u * (15 + s); };
+  const uint32_t drain = bar0 + 8u * 19;
+  static_assert(T::BARS == 20, "barrier numbering");
+  volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
+  volatile uint32_t* const abort_flag = tmem_holder + 1;
+
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) ptx::grid_dep_launch_dependents();
+
+  // ---- what this CTA works on: the longest row tile of every (sequence, head) first
+  ptx::grid_dep_wait();
+  const int heads = p.c.heads;
+  const int per_tile = heads * p.batch;
+  const int nth = static_cast<int>(blockIdx.x) / per_tile, rest = static_cast<int>(blockIdx.x) - nth * per_tile;
+  const int b = rest / heads, head = rest - b * heads;
+  const KvSeq s = kv_seq(p, b, tid == 0 && nth == 0 && head == 0);
+  const int all_rows = s.n * p.group;
+  const int qt = (all_rows + T::ROWS - 1) / T::ROWS - 1 - nth;
+  if (all_rows <= p.split_rows || qt < 0) return;
+  const int row_first = qt * T::ROWS, rows = min(T::ROWS, all_rows - row_first);
+  const int active = QT == 2 && rows > 128 ? 2 : 1;  // row tiles with a row in them
+  int lo, hi;
+  kv_visible(p, s, row_first / p.group, (row_first + rows + p.group - 1) / p.group, lo, hi);
+  lo = lo / TN * TN;
+  const int tiles = (hi - lo + TN - 1) / TN;  // 0: nothing is visible
+
+  if (tid == 0) {
+    ptx::mbar_init(q_full, T::SOFTMAX_WARPS);
+    for (int i = 0; i < STAGES; ++i) {
+      ptx::mbar_init(k_full(i), 4);
+      ptx::mbar_init(k_empty(i), 1);
+      ptx::mbar_init(v_full(i), 4);
+      ptx::mbar_init(v_empty(i), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(s_full(i), 1);
+      ptx::mbar_init(p_full(i), 4);
+      ptx::mbar_init(o_done(i), 1);
+    }
+    for (int i = 0; i < T::SCALES; ++i) ptx::mbar_init(scale_full(i), 1);
+    ptx::mbar_init(drain, 1);
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == T::SOFTMAX_WARPS + 4) {
+    ptx::tmem_alloc<1>(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), 512);
+    ptx::tmem_relinquish<1>();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = *tmem_holder;
+
+  if (warp < T::SOFTMAX_WARPS) {
+    // ------------------------------------------------------------------ softmax, one thread per row
+    const int q = warp >> 2;
+    const int r = q * 128 + (warp & 3) * 32 + lane;  // row of the CTA
+    const int row = row_first + r, qi = row / p.group, hq = head * p.group + (row - qi * p.group);
+    const bool live = r < rows;
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(q * 128);
+    const uint32_t o_at = tmem + lane_base + T::O_COLUMN + static_cast<uint32_t>(q * D);
+    if (q < active) {  // this row of Q, in the 128-byte swizzle
+      const __half* const src = p.q + (static_cast<long long>(s.row0) + (live ? qi : 0)) * p.q_token_stride +
+                                static_cast<long long>(live ? hq : 0) * p.q_head_stride;
+      const uint32_t dst = base + static_cast<uint32_t>(q * (D / 64) * 16384 + (r & 127) * 128);
+#pragma unroll 8
+      for (int u = 0; u < D / 8; ++u) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (live) x = ptx::ld_global_stream_v4(src + u * 8);
+        ptx::st_shared_v4(dst + static_cast<uint32_t>((u >> 3) * 16384 + (((u & 7) ^ (r & 7)) << 4)), x.x, x.y, x.z, x.w);
+      }
+      ptx::fence_proxy_async_smem();
+    }
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(q_full);
+
+    const int pos = s.len - s.n + qi;  // sees tokens from .. pos
+    const int from = p.window > 0 ? pos - p.window + 1 : 0;
+    const int all_hi = s.len - s.n + (row_first + q * 128) / p.group;
+    const int all_lo = p.window > 0 ? s.len - s.n + (row_first + min(rows, q * 128 + 128) - 1) / p.group - p.window + 1 : 0;
+    float m = -INFINITY, l = 0.0f;
+    bool ok = true;
+    const int my_tiles = q < active ? tiles : 0;
+#pragma unroll 1
+    for (int j = 0; j < my_tiles; ++j) {
+      ok = wait_bounded(scale_full(j & 3), (j >> 2) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE) &&
+           wait_bounded(s_full(q), j & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      ptx::tc_fence_after_sync();
+      const float4* const scale = reinterpret_cast<const float4*>(base_ptr + T::SCALE_OFFSET) + (j & 3) * GROUPS;
+      const int tok0 = lo + j * TN;
+      const bool masked = tok0 + TN - 1 > all_hi || tok0 < all_lo;
+      // the largest score of the row
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < TN / 32; ++h) {
+        uint32_t x[32];
+        ptx::tmem_ld_32x32b_x32(s_at + h * 32, x);
+        ptx::tmem_wait_ld();
+        if (masked) {
+#pragma unroll
+          for (int v = 0; v < 32; ++v) {
+            const int tok = tok0 + h * 32 + v;
+            if (tok > pos || tok < from) x[v] = 0xff800000u;  // -inf
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          float mx = __uint_as_float(x[16 * g]);
+#pragma unroll
+          for (int v = 1; v < 16; ++v) mx = fmaxf(mx, __uint_as_float(x[16 * g + v]));
+          const float4 c = scale[2 * h + g];
+          top = fmaxf(top, fmaf(mx, c.x, c.y));
+        }
+      }
+      const bool grow = top > m + 8.0f;
+      if (__any_sync(0xffffffffu, grow)) {
+        const float now = grow ? top : m;
+        const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
+        m = now;
+        l *= f;
+        if (j > 0) {  // O of the tiles before, once their products are done
+          ok = wait_bounded(o_done(q), (j - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t x[32];
+            ptx::tmem_ld_32x32b_x32(o_at + c, x);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int v = 0; v < 32; ++v) x[v] = __float_as_uint(__uint_as_float(x[v]) * f);
+            ptx::tmem_st_32x32b_x32(o_at + c, x);
+          }
+          ptx::tmem_wait_st();
+        }
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      // weights, two per column, over the scores that have been read: 64 tokens take 32 columns
+#pragma unroll
+      for (int h = 0; h < TN / 64; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          uint32_t x[32];
+          ptx::tmem_ld_32x32b_x32(s_at + h * 64 + u * 32, x);
+          ptx::tmem_wait_ld();
+          if (masked) {
+#pragma unroll
+            for (int v = 0; v < 32; ++v) {
+              const int tok = tok0 + h * 64 + u * 32 + v;
+              if (tok > pos || tok < from) x[v] = 0xff800000u;
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const float4 c = scale[4 * h + 2 * u + g];
+            const float at_ref = c.y - ref;
+            float sum0 = 0.0f, sum1 = 0.0f;
+#pragma unroll
+            for (int v = 0; v < 16; v += 2) {
+              const float e0 = exp2_approx(fmaf(__uint_as_float(x[16 * g + v]), c.x, at_ref));
+              const float e1 = exp2_approx(fmaf(__uint_as_float(x[16 * g + v + 1]), c.x, at_ref));
+              sum0 += e0;
+              sum1 += e1;
+              w[16 * u + 8 * g + v / 2] = pack_halves(e0, e1);
+            }
+            l = fmaf(sum0 + sum1, c.z, l);
+          }
+        }
+        ptx::tmem_st_32x32b_x32(s_at + h * 32, w);
+      }
+      ptx::tmem_wait_st();
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(p_full(q));
+    }
+    // ---- the rows' results
+    if (q < active && ok) {
+      if (tiles > 0) {
+        ok = wait_bounded(o_done(q), (tiles - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+        ok = __all_sync(0xffffffffu, ok);
+        ptx::tc_fence_after_sync();
+      }
+      const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
+      __half* const dst = p.out + (static_cast<long long>(s.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
+#pragma unroll 1
+      for (int c = 0; c < D && ok; c += 32) {
+        uint32_t x[32];
+        if (tiles > 0) {
+          ptx::tmem_ld_32x32b_x32(o_at + c, x);
+          ptx::tmem_wait_ld();
+        }
+        if (!live) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          uint32_t y[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            y[u] = tiles > 0 ? pack_halves(__uint_as_float(x[8 * v + 2 * u]) * inv, __uint_as_float(x[8 * v + 2 * u + 1]) * inv) : 0u;
+          *reinterpret_cast<uint4*>(dst + c + 8 * v) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      }
+    }
+  } else if (warp < T::SOFTMAX_WARPS + 4) {
+    // ------------------------------------------------------------------ K and V: int8 codes to binary16 tiles
+    const int ct = tid - 32 * T::SOFTMAX_WARPS;       // 0 .. 127
+    constexpr int PER_TOKEN = D / 16;                 // 16-byte pieces of a token
+    constexpr int N = TN * PER_TOKEN / 128;           // pieces per thread and tile
+    constexpr int TOKENS_AT_ONCE = 128 / PER_TOKEN;   // tokens the 128 threads cover together
+    const int c = ct % PER_TOKEN, t0 = ct / PER_TOKEN;
+    const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
+    const uint64_t page_bytes = static_cast<uint64_t>(heads) * p.c.page * D;
+    // the two 16-byte pieces of the 128-byte row; odd chunks of 64 d store them in the other order, which
+    // keeps eight neighbouring lanes on different banks
+    const uint32_t chunk_at = static_cast<uint32_t>((c >> 2) * T::CHUNK);
+    const uint32_t unit = static_cast<uint32_t>((c & 3) * 2), flip = static_cast<uint32_t>((c >> 2) & 1);
+    auto load_ids = [&](int j) {  // page of the tile's lane-th group of 16 tokens, or -1
+      const int tok = lo + j * TN + 16 * (lane % GROUPS);
+      int id = -1;
+      if (j < tiles && tok < hi) {
+        id = kv_ld(table + (tok >> p.c.page_shift));
+        if (id < 0 || id >= p.c.num_pages) {
+          kv_report(p.status);
+          id = -1;
+        }
+      }
+      return id;
+    };
+    auto load = [&](const int8_t* codes, int ids, int j, uint4 (&x)[N]) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int tok = i * TOKENS_AT_ONCE + t0;
+        const int id = __shfl_sync(0xffffffffu, ids, tok >> 4);
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (id >= 0)
+          x[i] = ptx::ld_global_stream_v4(codes + static_cast<uint64_t>(id) * page_bytes +
+                                          static_cast<uint32_t>((head * p.c.page + ((lo + j * TN + tok) & (p.c.page - 1))) * D + c * 16));
+      }
+    };
+    auto store = [&](uint32_t tile, const uint4 (&x)[N]) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int tok = i * TOKENS_AT_ONCE + t0;
+        const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
+        const uint32_t at = tile + chunk_at + static_cast<uint32_t>(tok * 128);
+        const uint32_t sw = static_cast<uint32_t>(tok & 7);
+        const uint32_t a0 = flip ? w[2] : w[0], a1 = flip ? w[3] : w[1];
+        const uint32_t b0 = flip ? w[0] : w[2], b1 = flip ? w[1] : w[3];
+        ptx::st_shared_v4(at + (((unit + flip) ^ sw) << 4), lo_halves(a0), hi_halves(a0), lo_halves(a1), hi_halves(a1));
+        ptx::st_shared_v4(at + (((unit + (flip ^ 1u)) ^ sw) << 4), lo_halves(b0), hi_halves(b0), lo_halves(b1), hi_halves(b1));
+      }
+    };
+    bool ok = true;
+    int ids = load_ids(0), ids_next = load_ids(1);
+    uint4 kx[N], vx[N];
+    float sk = 0.0f, sv = 1.0f;
+    auto load_scales = [&](int id) {
+      sk = 0.0f;
+      sv = 1.0f;
+      if (id >= 0 && ct < GROUPS) {
+        const long long ph = static_cast<long long>(id) * heads + head;
+        sk = ptx::ld_global_f32(p.c.scales[0] + ph);
+        sv = ptx::ld_global_f32(p.c.scales[1] + ph);
+      }
+    };
+    if (tiles > 0) {
+      load(p.c.codes[0], ids, 0, kx);
+      load_scales(ids);
+      load(p.c.codes[1], ids, 0, vx);
+    }
+#pragma unroll 1
+    for (int j = 0; j < tiles; ++j) {
+      const int st = j & 1;
+      const uint32_t ph = ((j >> 1) & 1) ^ 1u;
+      ok = wait_bounded(k_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      store(base + T::K_OFFSET + st * T::KV_BYTES, kx);
+      if (ct < GROUPS) {
+        // (a page of zeros: its codes are 0, its tokens still count in l; a hidden token's -inf must stay one)
+        const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
+        reinterpret_cast<float4*>(base_ptr + T::SCALE_OFFSET)[(j & 3) * GROUPS + ct] =
+            make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
+      }
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        ptx::mbar_arrive(k_full(st));
+        if (ct == 0) ptx::mbar_arrive(scale_full(j & 3));
+      }
+      const int ids_now = ids_next;
+      ids_next = load_ids(j + 2);
+      if (j + 1 < tiles) {
+        load(p.c.codes[0], ids_now, j + 1, kx);
+        load_scales(ids_now);
+      }
+      ok = wait_bounded(v_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      store(base + T::V_OFFSET + st * T::KV_BYTES, vx);
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(v_full(st));
+      if (j + 1 < tiles) load(p.c.codes[1], ids_now, j + 1, vx);
+    }
+  } else {
+    // ------------------------------------------------------------------ MMA issuer
+    const bool elected = ptx::elect_one();
+    constexpr uint32_t idesc_qk = ptx::make_idesc<ptx::KIND_F16>(128, TN);
+    constexpr uint32_t idesc_pv = ptx::make_idesc<ptx::KIND_F16>(128, D) | ptx::IDESC_B_MN_MAJOR;
+    auto qk = [&](int q, int j) {
+      if (elected) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = static_cast<uint32_t>((kk & 3) * 32);
+          const uint64_t a = ptx::smem_desc_sw128(base + (q * (D / 64) + (kk >> 2)) * 16384 + off);
+          const uint64_t k = ptx::smem_desc_sw128(base + T::K_OFFSET + (j & 1) * T::KV_BYTES + (kk >> 2) * T::CHUNK + off);
+          ptx::mma_ss<ptx::KIND_F16, 1>(tmem + q * 128, a, k, idesc_qk, kk > 0);
+        }
+        ptx::mma_commit<1>(s_full(q));
+      }
+    };
+    auto pv = [&](int q, int j) {
+      if (elected) {
+#pragma unroll
+        for (int kk = 0; kk < TN / 16; ++kk) {
+          const uint64_t v = ptx::smem_desc_sw128_mn(base + T::V_OFFSET + (j & 1) * T::KV_BYTES + kk * 2048, T::CHUNK);
+          ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + q * 128 + kk * 8, v, idesc_pv, j > 0 || kk > 0);
+        }
+        ptx::mma_commit<1>(o_done(q));
+      }
+    };
+    bool ok = true;
+    if (tiles > 0) {
+      ok = wait_bounded(q_full, 0, abort_flag, p.status, DEV_TIMEOUT_MMA) &&
+           wait_bounded(k_full(0), 0, abort_flag, p.status, DEV_TIMEOUT_MMA);
+      if (ok) {
+        ptx::tc_fence_after_sync();
+        for (int q = 0; q < active; ++q) qk(q, 0);
+        if (elected) ptx::mma_commit<1>(k_empty(0));
+      }
+    }
+#pragma unroll 1
+    for (int j = 0; j < tiles && ok; ++j) {
+      ok = wait_bounded(v_full(j & 1), (j >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+#pragma unroll 1
+      for (int q = 0; q < active && ok; ++q) {
+        ok = wait_bounded(p_full(q), j & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        pv(q, j);
+        if (j + 1 < tiles) {  // (the scores go where the weights are: the MMAs of this thread run in order)
+          if (q == 0) {
+            ok = wait_bounded(k_full((j + 1) & 1), ((j + 1) >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+          }
+          qk(q, j + 1);
+        }
+      }
+      if (ok && elected) {
+        ptx::mma_commit<1>(v_empty(j & 1));
+        if (j + 1 < tiles) ptx::mma_commit<1>(k_empty((j + 1) & 1));
+      }
+    }
+    if (!ok && elected) {
+      // Gave up: wait for the MMAs already issued before tensor memory is released.
+      ptx::mma_commit<1>(drain);
+      const uint64_t start = ptx::globaltimer_ns();
+      while (!ptx::mbar_try_wait(drain, 0) && ptx::globaltimer_ns() - start < WAIT_LIMIT_NS) {
+      }
+    }
+    __syncwarp();
+  }
+
+  // Every role gets here: all waits are bounded, and the last products have been waited for above.
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == T::SOFTMAX_WARPS + 4) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc<1>(tmem, 512);
+  }
+}
+
+}  // namespace b200gemm
