@@ -5,7 +5,7 @@
 // TN.  Per tile of rows and tokens: S = Q K^T (tcgen05.mma, operands in shared memory) into tensor memory; four warps,
 // one thread per row, turn S into weights, rounded to binary16, in the same place; O += P V (A operand in tensor
 // memory).  With two tiles of rows one is in its softmax while the tensor cores work on the other.
-// K and V arrive as int8: four warps read the codes (16 bytes a thread, a tile ahead, in registers), convert them
+// K and V arrive as int8, by bulk copies of whole pages of a head; four warps convert them
 // exactly to binary16 and write them as rows of 64 d in the 128-byte swizzle.  Such a tile is K-major for the
 // first product and, read the other way round, MN-major for the second: no transpose anywhere.
 // Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own.
@@ -31,7 +31,7 @@ struct KvTileShape {
   static constexpr int TN = D <= 128 ? 128 : 64;   // tokens per tile
   static constexpr int ROWS = 128 * QT;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
-  static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 5);
+  static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 8);  // + 4 converting, MMA issuer, loader, two idle
   static constexpr int STAGES = 2;
   static constexpr int GROUPS = TN / 16;
   static constexpr int CHUNK = TN * 128;           // bytes of 64 d of a K or V tile
@@ -40,10 +40,13 @@ struct KvTileShape {
   static constexpr int K_OFFSET = Q_BYTES;
   static constexpr int V_OFFSET = K_OFFSET + STAGES * KV_BYTES;
   static constexpr int SCALES = 4;                 // ring of scale tables
-  static constexpr int SCALE_OFFSET = V_OFFSET + STAGES * KV_BYTES;
+  static constexpr int RAW_BYTES = TN * D;         // int8 codes of a K or V tile
+  static constexpr int RAW_OFFSET = V_OFFSET + STAGES * KV_BYTES;  // K, V of one tile; then of the next
+  static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_BYTES;
   static constexpr int BAR_OFFSET = SCALE_OFFSET + SCALES * GROUPS * 16;
-  // q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2], scale_full[4], drain
-  static constexpr int BARS = 1 + 4 * STAGES + 6 + SCALES + 1;
+  // q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_done[2], scale_full[4], drain,
+  // raw_full[2], raw_empty[2] (K, V)
+  static constexpr int BARS = 1 + 4 * STAGES + 6 + SCALES + 1 + 4;
   static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
   static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
   static constexpr uint32_t O_COLUMN = 256;        // S (and P) of tile q at 128 q, O behind both
@@ -71,7 +74,9 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
   auto o_done = [&](int q) { return bar0 + 8u * (13 + q); };
   auto scale_full = [&](int s) { return bar0 + 8u * (15 + s); };
   const uint32_t drain = bar0 + 8u * 19;
-  static_assert(T::BARS == 20, "barrier numbering");
+  auto raw_full = [&](int w) { return bar0 + 8u * (20 + w); };
+  auto raw_empty = [&](int w) { return bar0 + 8u * (22 + w); };
+  static_assert(T::BARS == 24, "barrier numbering");
   volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
   volatile uint32_t* const abort_flag = tmem_holder + 1;
 
@@ -110,6 +115,10 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
     }
     for (int i = 0; i < T::SCALES; ++i) ptx::mbar_init(scale_full(i), 1);
     ptx::mbar_init(drain, 1);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(raw_full(i), 1);
+      ptx::mbar_init(raw_empty(i), 4);
+    }
     *abort_flag = 0;
     ptx::fence_mbar_init();
   }
@@ -122,6 +131,17 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
   ptx::tc_fence_after_sync();
   const uint32_t tmem = *tmem_holder;
 
+  if constexpr (QT == 2) {
+    // Register shares of the four groups of four warps, which sum up to the 4 x 128 they were launched with:
+    // the scores of a row stay in registers between the maximum and the weights.
+    if (warp < T::SOFTMAX_WARPS) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    } else if (warp < T::SOFTMAX_WARPS + 4) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    }
+  }
   if (warp < T::SOFTMAX_WARPS) {
     // ------------------------------------------------------------------ softmax, one thread per row
     const int q = warp >> 2;
@@ -163,28 +183,28 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
       const float4* const scale = reinterpret_cast<const float4*>(base_ptr + T::SCALE_OFFSET) + (j & 3) * GROUPS;
       const int tok0 = lo + j * TN;
       const bool masked = tok0 + TN - 1 > all_hi || tok0 < all_lo;
-      // the largest score of the row
-      float top = -INFINITY;
+      uint32_t x[TN / 32][32];
 #pragma unroll
-      for (int h = 0; h < TN / 32; ++h) {
-        uint32_t x[32];
-        ptx::tmem_ld_32x32b_x32(s_at + h * 32, x);
-        ptx::tmem_wait_ld();
-        if (masked) {
+      for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
+      ptx::tmem_wait_ld();
+      if (masked) {
+#pragma unroll
+        for (int h = 0; h < TN / 32; ++h)
 #pragma unroll
           for (int v = 0; v < 32; ++v) {
             const int tok = tok0 + h * 32 + v;
-            if (tok > pos || tok < from) x[v] = 0xff800000u;  // -inf
+            if (tok > pos || tok < from) x[h][v] = 0xff800000u;  // -inf
           }
-        }
+      }
+      // the largest score of the row
+      float top = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float mx = __uint_as_float(x[16 * g]);
+      for (int g = 0; g < GROUPS; ++g) {
+        float mx = __uint_as_float(x[g / 2][16 * (g & 1)]);
 #pragma unroll
-          for (int v = 1; v < 16; ++v) mx = fmaxf(mx, __uint_as_float(x[16 * g + v]));
-          const float4 c = scale[2 * h + g];
-          top = fmaxf(top, fmaf(mx, c.x, c.y));
-        }
+        for (int v = 1; v < 16; ++v) mx = fmaxf(mx, __uint_as_float(x[g / 2][16 * (g & 1) + v]));
+        const float4 c = scale[g];
+        top = fmaxf(top, fmaf(mx, c.x, c.y));
       }
       const bool grow = top > m + 8.0f;
       if (__any_sync(0xffffffffu, grow)) {
@@ -198,51 +218,38 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
           if (!ok) break;
           ptx::tc_fence_after_sync();
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t x[32];
-            ptx::tmem_ld_32x32b_x32(o_at + c, x);
+          for (int c = 0; c < D; c += 16) {
+            uint32_t y[16];  // (few registers: the scores are in the others)
+            ptx::tmem_ld_32x32b_x16(o_at + c, y);
             ptx::tmem_wait_ld();
 #pragma unroll
-            for (int v = 0; v < 32; ++v) x[v] = __float_as_uint(__uint_as_float(x[v]) * f);
-            ptx::tmem_st_32x32b_x32(o_at + c, x);
+            for (int v = 0; v < 16; ++v) y[v] = __float_as_uint(__uint_as_float(y[v]) * f);
+            ptx::tmem_st_32x32b_x16(o_at + c, y);
           }
           ptx::tmem_wait_st();
         }
       }
       const float ref = m == -INFINITY ? 0.0f : m;
-      // weights, two per column, over the scores that have been read: 64 tokens take 32 columns
+      // weights, two per column, over the scores: 32 tokens take 16 columns
 #pragma unroll
-      for (int h = 0; h < TN / 64; ++h) {
-        uint32_t w[32];
+      for (int h = 0; h < TN / 32; ++h) {
+        uint32_t w[16];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          uint32_t x[32];
-          ptx::tmem_ld_32x32b_x32(s_at + h * 64 + u * 32, x);
-          ptx::tmem_wait_ld();
-          if (masked) {
+        for (int g = 0; g < 2; ++g) {
+          const float4 c = scale[2 * h + g];
+          const float at_ref = c.y - ref;
+          float sum0 = 0.0f, sum1 = 0.0f;
 #pragma unroll
-            for (int v = 0; v < 32; ++v) {
-              const int tok = tok0 + h * 64 + u * 32 + v;
-              if (tok > pos || tok < from) x[v] = 0xff800000u;
-            }
+          for (int v = 0; v < 16; v += 2) {
+            const float e0 = exp2_approx(fmaf(__uint_as_float(x[h][16 * g + v]), c.x, at_ref));
+            const float e1 = exp2_approx(fmaf(__uint_as_float(x[h][16 * g + v + 1]), c.x, at_ref));
+            sum0 += e0;
+            sum1 += e1;
+            w[8 * g + v / 2] = pack_halves(e0, e1);
           }
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float4 c = scale[4 * h + 2 * u + g];
-            const float at_ref = c.y - ref;
-            float sum0 = 0.0f, sum1 = 0.0f;
-#pragma unroll
-            for (int v = 0; v < 16; v += 2) {
-              const float e0 = exp2_approx(fmaf(__uint_as_float(x[16 * g + v]), c.x, at_ref));
-              const float e1 = exp2_approx(fmaf(__uint_as_float(x[16 * g + v + 1]), c.x, at_ref));
-              sum0 += e0;
-              sum1 += e1;
-              w[16 * u + 8 * g + v / 2] = pack_halves(e0, e1);
-            }
-            l = fmaf(sum0 + sum1, c.z, l);
-          }
+          l = fmaf(sum0 + sum1, c.z, l);
         }
-        ptx::tmem_st_32x32b_x32(s_at + h * 32, w);
+        ptx::tmem_st_32x32b_x16(s_at + h * 16, w);
       }
       ptx::tmem_wait_st();
       ptx::tc_fence_before_sync();
@@ -283,40 +290,19 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
     constexpr int N = TN * PER_TOKEN / 128;           // pieces per thread and tile
     constexpr int TOKENS_AT_ONCE = 128 / PER_TOKEN;   // tokens the 128 threads cover together
     const int c = ct % PER_TOKEN, t0 = ct / PER_TOKEN;
-    const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
-    const uint64_t page_bytes = static_cast<uint64_t>(heads) * p.c.page * D;
     // the two 16-byte pieces of the 128-byte row; odd chunks of 64 d store them in the other order, which
     // keeps eight neighbouring lanes on different banks
     const uint32_t chunk_at = static_cast<uint32_t>((c >> 2) * T::CHUNK);
     const uint32_t unit = static_cast<uint32_t>((c & 3) * 2), flip = static_cast<uint32_t>((c >> 2) & 1);
-    auto load_ids = [&](int j) {  // page of the tile's lane-th group of 16 tokens, or -1
-      const int tok = lo + j * TN + 16 * (lane % GROUPS);
-      int id = -1;
-      if (j < tiles && tok < hi) {
-        id = kv_ld(table + (tok >> p.c.page_shift));
-        if (id < 0 || id >= p.c.num_pages) {
-          kv_report(p.status);
-          id = -1;
-        }
-      }
-      return id;
-    };
-    auto load = [&](const int8_t* codes, int ids, int j, uint4 (&x)[N]) {
+    auto convert = [&](int which, uint32_t tile) {
+      const uint32_t src = base + T::RAW_OFFSET + which * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int tok = i * TOKENS_AT_ONCE + t0;
-        const int id = __shfl_sync(0xffffffffu, ids, tok >> 4);
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (id >= 0)
-          x[i] = ptx::ld_global_stream_v4(codes + static_cast<uint64_t>(id) * page_bytes +
-                                          static_cast<uint32_t>((head * p.c.page + ((lo + j * TN + tok) & (p.c.page - 1))) * D + c * 16));
-      }
-    };
-    auto store = [&](uint32_t tile, const uint4 (&x)[N]) {
+        uint32_t w[4];
+        ptx::ld_shared_v4(src + i * 2048, w[0], w[1], w[2], w[3]);
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int tok = i * TOKENS_AT_ONCE + t0;
-        const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
+        for (int v = 0; v < 4; ++v) w[v] ^= 0x80808080u;
         const uint32_t at = tile + chunk_at + static_cast<uint32_t>(tok * 128);
         const uint32_t sw = static_cast<uint32_t>(tok & 7);
         const uint32_t a0 = flip ? w[2] : w[0], a1 = flip ? w[3] : w[1];
@@ -324,61 +310,95 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
         ptx::st_shared_v4(at + (((unit + flip) ^ sw) << 4), lo_halves(a0), hi_halves(a0), lo_halves(a1), hi_halves(a1));
         ptx::st_shared_v4(at + (((unit + (flip ^ 1u)) ^ sw) << 4), lo_halves(b0), hi_halves(b0), lo_halves(b1), hi_halves(b1));
       }
+      ptx::fence_proxy_async_smem();
+      __syncwarp();
     };
     bool ok = true;
-    int ids = load_ids(0), ids_next = load_ids(1);
-    uint4 kx[N], vx[N];
-    float sk = 0.0f, sv = 1.0f;
-    auto load_scales = [&](int id) {
-      sk = 0.0f;
-      sv = 1.0f;
-      if (id >= 0 && ct < GROUPS) {
-        const long long ph = static_cast<long long>(id) * heads + head;
-        sk = ptx::ld_global_f32(p.c.scales[0] + ph);
-        sv = ptx::ld_global_f32(p.c.scales[1] + ph);
-      }
-    };
-    if (tiles > 0) {
-      load(p.c.codes[0], ids, 0, kx);
-      load_scales(ids);
-      load(p.c.codes[1], ids, 0, vx);
-    }
 #pragma unroll 1
     for (int j = 0; j < tiles; ++j) {
       const int st = j & 1;
       const uint32_t ph = ((j >> 1) & 1) ^ 1u;
-      ok = wait_bounded(k_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = wait_bounded(raw_full(0), j & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
+           wait_bounded(k_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      store(base + T::K_OFFSET + st * T::KV_BYTES, kx);
-      if (ct < GROUPS) {
-        // (a page of zeros: its codes are 0, its tokens still count in l; a hidden token's -inf must stay one)
-        const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
-        reinterpret_cast<float4*>(base_ptr + T::SCALE_OFFSET)[(j & 3) * GROUPS + ct] =
-            make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
-      }
-      ptx::fence_proxy_async_smem();
-      __syncwarp();
+      convert(0, base + T::K_OFFSET + st * T::KV_BYTES);
       if (lane == 0) {
         ptx::mbar_arrive(k_full(st));
-        if (ct == 0) ptx::mbar_arrive(scale_full(j & 3));
+        ptx::mbar_arrive(raw_empty(0));
       }
-      const int ids_now = ids_next;
-      ids_next = load_ids(j + 2);
-      if (j + 1 < tiles) {
-        load(p.c.codes[0], ids_now, j + 1, kx);
-        load_scales(ids_now);
-      }
-      ok = wait_bounded(v_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = wait_bounded(raw_full(1), j & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
+           wait_bounded(v_empty(st), ph, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      store(base + T::V_OFFSET + st * T::KV_BYTES, vx);
-      ptx::fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(v_full(st));
-      if (j + 1 < tiles) load(p.c.codes[1], ids_now, j + 1, vx);
+      convert(1, base + T::V_OFFSET + st * T::KV_BYTES);
+      if (lane == 0) {
+        ptx::mbar_arrive(v_full(st));
+        ptx::mbar_arrive(raw_empty(1));
+      }
     }
-  } else {
+  } else if (warp == T::SOFTMAX_WARPS + 5) {
+    // ------------------------------------------------------------------ loader: int8 pages and their scales
+    // Lane g looks after the tile's g-th run of `run` tokens: one page, or half a tile's worth of a longer one.
+    const int run = min(p.c.page, TN), runs = TN / run;
+    const uint32_t run_bytes = static_cast<uint32_t>(run * D);
+    const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
+    const uint64_t page_bytes = static_cast<uint64_t>(heads) * p.c.page * D;
+    auto load_id = [&](int j) {  // page of the lane's run of tile j, or -1
+      const int tok = lo + j * TN + run * lane;
+      return lane < runs && j < tiles && tok < hi ? kv_ld(table + (tok >> p.c.page_shift)) : -1;
+    };
+    bool ok = true;
+    int id = load_id(0);
+#pragma unroll 1
+    for (int j = 0; j < tiles && ok; ++j) {
+      const int id_next = load_id(j + 1);
+      const bool in = lane < runs && lo + j * TN + run * lane < hi;
+      const bool good = in && id >= 0 && id < p.c.num_pages;
+      if (in && !good) kv_report(p.status);
+      const int tok = lo + j * TN + run * lane;
+      const uint64_t off = good ? static_cast<uint64_t>(id) * page_bytes +
+                                      static_cast<uint32_t>((head * p.c.page + (tok & (p.c.page - 1))) * D)
+                                : 0;
+      const uint32_t bytes = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, good))) * run_bytes;
+      float sk = 0.0f, sv = 1.0f;
+      if (good) {
+        const long long ph = static_cast<long long>(id) * heads + head;
+        sk = ptx::ld_global_f32(p.c.scales[0] + ph);
+        sv = ptx::ld_global_f32(p.c.scales[1] + ph);
+      }
+#pragma unroll 1
+      for (int which = 0; which < 2; ++which) {
+        ok = wait_bounded(raw_empty(which), (j & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(raw_full(which), bytes);
+        __syncwarp();
+        // (runs that are left out keep what the buffer held: codes are finite, and their weights are 0)
+        if (good)
+          ptx::bulk_load(base + T::RAW_OFFSET + which * T::RAW_BYTES + lane * run_bytes,
+                         (which ? p.c.codes[1] : p.c.codes[0]) + off, run_bytes, raw_full(which));
+        if (which == 0) {
+          // scales by groups of 16 tokens.  (A page of zeros: its codes are 0, its tokens still count in l; a
+          // hidden token's -inf must stay one.)
+          const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
+          const float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
+          if (lane < runs)
+            for (int g = 0; g < run / 16; ++g)
+              reinterpret_cast<float4*>(base_ptr + T::SCALE_OFFSET)[(j & 3) * GROUPS + lane * (run / 16) + g] = c;
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(scale_full(j & 3));
+        }
+      }
+      id = id_next;
+    }
+    if (!ok) {
+      // Gave up: let the copies in flight land before the CTA exits.
+      const uint64_t start = ptx::globaltimer_ns();
+      while (ptx::globaltimer_ns() - start < 1000000ull) {
+      }
+    }
+  } else if (warp == T::SOFTMAX_WARPS + 4) {
     // ------------------------------------------------------------------ MMA issuer
     const bool elected = ptx::elect_one();
     constexpr uint32_t idesc_qk = ptx::make_idesc<ptx::KIND_F16>(128, TN);
