@@ -119,14 +119,8 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-# The current stream's handle without a Stream object around it (3 us a call), where torch has that.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-
-
 def _stream_handle(stream) -> int:
     if stream is None:
-        if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
@@ -264,93 +258,62 @@ def gemm_s4_dequant(A, B, row_scale, col_scale, C=None, out_dtype=torch.float32,
                     torch.uint8, stream)
 
 
-def _new_out(like, shape, dtype, stream):
-    """An output of our own: if the work runs on another stream than the current one, the
-    allocator must not hand its memory on before that stream is done with it."""
-    out = like.new_empty(shape, dtype=dtype)
-    if stream is not None and stream != torch.cuda.current_stream():
-        out.record_stream(stream)
-    return out
+_marshal = None
 
 
-def _rows_2d(t, dtype, rows, cols, what):
-    """Pointer and row pitch of a matrix whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % what)
-    if t.dtype != dtype:
-        raise TypeError("%s must have dtype %s, got %s" % (what, dtype, t.dtype))
-    if t.shape != (rows, cols):
-        raise ValueError("%s must have shape %s, got %s" % (what, (rows, cols), tuple(t.shape)))
-    pitch, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError("%s must have contiguous rows" % what)
-    return t.data_ptr(), (pitch if rows > 1 else cols)
+def _native():
+    """The compiled marshalling of the functions below (csrc/marshal.cpp), bound to the library."""
+    global _marshal
+    if _marshal is None:
+        L = lib()
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise ImportError("%s: build it with `python -m paper_2608_10103_b200.build`" % e) from e
+        names = ("gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows") + KV_EXPORTS
+        m.entries(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
+        _marshal = m
+    return _marshal
 
 
-def _linear(fn_name, A, B, in_dtype, per_byte, scales, bias, activation, residual, C, out_dtype, stream):
-    M, K = A.shape
-    N, Kb = B.shape
-    if K != Kb:
-        raise ValueError("A and B disagree on K")
+def _checked(result, where: str):
+    if type(result) is int:
+        raise GemmError(result, where)
+    return result
+
+
+def _linear(precision, where, A, B, row_scale, col_scale, bias, activation, residual, C, out_dtype, stream):
     act = ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError("activation is one of %s" % ", ".join(ACTIVATIONS))
-    a, b = _dev_ptr(A, in_dtype, "A"), _dev_ptr(B, in_dtype, "B")
-    if C is None:
-        C = _new_out(A, (M, N), out_dtype, stream)
-        c, ldc = C.data_ptr(), N
-    else:
-        out_dtype = C.dtype
-        c, ldc = _rows_2d(C, out_dtype, M, N, "C")
-    if out_dtype is torch.float16:
-        half = 1
-    elif out_dtype is torch.float32:
-        half = 0
-    else:
+    if out_dtype is not torch.float16 and out_dtype is not torch.float32:
         raise TypeError("the result is float32 or float16")
-    bias_ptr = res_ptr = None
-    ldr = 0
-    if bias is not None:
-        if bias.numel() != N:
-            raise ValueError("bias needs N entries")
-        bias_ptr = _dev_ptr(bias, torch.float32, "bias")
-    if residual is not None:
-        res_ptr, ldr = _rows_2d(residual, out_dtype, M, N, "residual")
-    e = ctypes.byref(_Epilogue(bias_ptr, act, half, res_ptr, ldr, ldc))
-    fn = getattr(lib(), fn_name)
-    if scales is None:
-        rc = fn(M, N, K, a, b, c, e, _stream_handle(stream))
-    else:
-        rs, cs = scales
-        if rs.numel() != M or cs.numel() != N:
-            raise ValueError("row_scale needs M entries, col_scale N")
-        rc = fn(M, N, K * per_byte, a, b, _dev_ptr(rs, torch.float32, "row_scale"),
-                _dev_ptr(cs, torch.float32, "col_scale"), c, e, _stream_handle(stream))
-    _check(rc, fn_name)
-    return C
+    return _checked((_marshal or _native()).linear(
+        precision, A, B, row_scale, col_scale, bias, act, residual, C, out_dtype is torch.float16,
+        None if stream is None else stream.cuda_stream), where)
 
 
 def gemm_fp16_linear(A, B, bias=None, activation="none", residual=None, C=None,
                      out_dtype=torch.float16, stream=None):
     """act(A @ B^T + bias) + residual for float16 A (M, K), B (N, K); bias float32 (N,), residual
-    and result (M, N) in out_dtype (float16 or float32), with contiguous rows of any pitch.
-    activation: a key of ACTIVATIONS.  residual may be C itself."""
-    return _linear("gemm_fp16_linear", A, B, torch.float16, 1, None, bias, activation,
-                   residual, C, out_dtype, stream)
+    and result (M, N) in out_dtype (float16 or float32; that of C if given), with contiguous rows of
+    any pitch.  activation: a key of ACTIVATIONS.  residual may be C itself."""
+    return _linear(PREC_FP16, "gemm_fp16_linear", A, B, None, None, bias, activation, residual, C,
+                   out_dtype, stream)
 
 
 def gemm_s8_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
                    out_dtype=torch.float16, stream=None):
     """act(float(A @ B^T) * row_scale[:, None] * col_scale + bias) + residual for int8 operands."""
-    return _linear("gemm_s8_linear", A, B, torch.int8, 1, (row_scale, col_scale), bias,
-                   activation, residual, C, out_dtype, stream)
+    return _linear(PREC_S8, "gemm_s8_linear", A, B, row_scale, col_scale, bias, activation, residual, C,
+                   out_dtype, stream)
 
 
 def gemm_s4_linear(A, B, row_scale, col_scale, bias=None, activation="none", residual=None, C=None,
                    out_dtype=torch.float16, stream=None):
     """gemm_s8_linear for packed signed 4-bit operands ((rows, K/2) uint8)."""
-    return _linear("gemm_s4_linear", A, B, torch.uint8, 2, (row_scale, col_scale), bias,
-                   activation, residual, C, out_dtype, stream)
+    return _linear(PREC_S4, "gemm_s4_linear", A, B, row_scale, col_scale, bias, activation, residual, C,
+                   out_dtype, stream)
 
 
 def gemm_quantize_rows(X, precision="s8", Q=None, row_scale=None, stream=None):
@@ -358,25 +321,9 @@ def gemm_quantize_rows(X, precision="s8", Q=None, row_scale=None, stream=None):
     4-bit ones (rows, K/2) uint8, and float32 scales (rows,): amax / 127 resp. amax / 7."""
     if precision not in ("s8", "s4"):
         raise ValueError("precision is s8 or s4")
-    x_dtype = X.dtype
-    if X.dim() != 2 or (x_dtype is not torch.float16 and x_dtype is not torch.float32):
-        raise TypeError("X must be a float16 or float32 matrix")
-    rows, K = X.shape
-    x_ptr, ldx = _rows_2d(X, x_dtype, rows, K, "X")
-    width, dtype = (K, torch.int8) if precision == "s8" else (K // 2, torch.uint8)
-    if Q is None:
-        Q = _new_out(X, (rows, width), dtype, stream)
-    elif Q.shape != (rows, width):
-        raise ValueError("Q must have shape (%d, %d)" % (rows, width))
-    if row_scale is None:
-        row_scale = _new_out(X, (rows,), torch.float32, stream)
-    elif row_scale.numel() != rows:
-        raise ValueError("row_scale needs one entry per row")
-    _check(lib().gemm_quantize_rows(PRECISION_ID[precision], rows, K, x_ptr, ldx,
-                                    1 if x_dtype is torch.float16 else 0, _dev_ptr(Q, dtype, "Q"),
-                                    _dev_ptr(row_scale, torch.float32, "row_scale"),
-                                    _stream_handle(stream)), "gemm_quantize_rows")
-    return Q, row_scale
+    return _checked((_marshal or _native()).quantize_rows(
+        PRECISION_ID[precision], X, Q, row_scale, None if stream is None else stream.cuda_stream),
+        "gemm_quantize_rows")
 
 
 # ----------------------------------------------------------------- INT8 key/value cache
@@ -390,95 +337,29 @@ def kv_cache_s8(num_pages: int, kv_heads: int, page_size: int, head_dim: int, de
             torch.zeros(shape[:2], dtype=torch.float32, device=device))
 
 
-def _kv_cache(cache):
-    k, v, k_scale, v_scale = cache
-    shape = k.shape
-    if len(shape) != 4 or v.shape != shape or k_scale.shape != shape[:2] or v_scale.shape != shape[:2]:
-        raise ValueError("cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim), two (pages, heads)")
-    return _KvCache(_dev_ptr(k, torch.int8, "k"), _dev_ptr(v, torch.int8, "v"),
-                    _dev_ptr(k_scale, torch.float32, "k_scale"),
-                    _dev_ptr(v_scale, torch.float32, "v_scale"), *shape)
-
-
-def _kv_batch(cu, start, table, what):
-    batch = start.numel()
-    if cu.numel() != batch + 1:
-        raise ValueError("cu needs one entry more than %s" % what)
-    rows, width = table.shape
-    if rows != batch:
-        raise ValueError("block_table needs one row per sequence")
-    return (batch, _dev_ptr(cu, torch.int32, "cu"), _dev_ptr(start, torch.int32, what),
-            _dev_ptr(table, torch.int32, "block_table"), width)
-
-
-def _kv_rows(t, heads, dim, what):
-    """Pointer, tokens, heads and the strides of both of a (tokens, heads, dim) view."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError("%s must be a CUDA tensor" % what)
-    if t.dtype != torch.float16:
-        raise TypeError("%s must have dtype torch.float16, got %s" % (what, t.dtype))
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[2] != dim or (heads and shape[1] != heads) or stride[2] != 1:
-        raise ValueError("%s must be (tokens, heads, %d) with contiguous heads" % (what, dim))
-    head = stride[1] if shape[1] > 1 else dim
-    return t.data_ptr(), shape[0], shape[1], (stride[0] if shape[0] > 1 else shape[1] * dim), head
-
-
 def kv_append_s8(cache, k, v, cu, past, block_table, max_new: int, stream=None):
     """Quantises the rows of k and v (float16 (tokens, kv_heads, head_dim) views with one common pair of
     strides) into the cache: rows cu[b] .. cu[b+1] become tokens past[b], past[b] + 1, ... of sequence b."""
-    c = _kv_cache(cache)
-    kp, tokens, _, ts, hs = _kv_rows(k, c.kv_heads, c.head_dim, "k")
-    vp, *rest = _kv_rows(v, c.kv_heads, c.head_dim, "v")
-    if rest != [tokens, c.kv_heads, ts, hs]:
-        raise ValueError("k and v must have the same shape and strides")
-    if tokens == 0:
-        return
-    _check(lib().kv_append_s8(ctypes.byref(c), *_kv_batch(cu, past, block_table, "past"), int(max_new),
-                              kp, vp, ts, hs, _stream_handle(stream)), "kv_append_s8")
+    _checked((_marshal or _native()).kv_append(cache, k, v, cu, past, block_table, max_new,
+                                               None if stream is None else stream.cuda_stream), "kv_append_s8")
 
 
 def kv_read_s8(cache, cu, first, block_table, max_read: int, tokens: int | None = None, out=None,
                stream=None):
     """Tokens first[b] .. first[b] + cu[b+1] - cu[b] - 1 of every sequence as float16 (k, v), each (tokens,
     kv_heads, head_dim).  tokens = cu[-1], which is read from the device when not given."""
-    c = _kv_cache(cache)
-    if out is None:
-        tokens = int(cu[-1]) if tokens is None else tokens
-        shape = (tokens, c.kv_heads, c.head_dim)
-        out = (_new_out(cache[0], shape, torch.float16, stream), _new_out(cache[0], shape, torch.float16, stream))
-    elif out[0].shape[1:] != (c.kv_heads, c.head_dim) or out[1].shape != out[0].shape:
-        raise ValueError("outputs are two (tokens, kv_heads, head_dim)")
-    if out[0].shape[0] == 0:
-        return out
-    _check(lib().kv_read_s8(ctypes.byref(c), *_kv_batch(cu, first, block_table, "first"), int(max_read),
-                            _dev_ptr(out[0], torch.float16, "k"), _dev_ptr(out[1], torch.float16, "v"),
-                            _stream_handle(stream)), "kv_read_s8")
-    return out
+    return _checked((_marshal or _native()).kv_read(cache, cu, first, block_table, max_read, tokens, out,
+                                                    None if stream is None else stream.cuda_stream), "kv_read_s8")
 
 
 def kv_attention_s8(q, cache, cu, kv_len, block_table, max_q: int, softmax_scale: float | None = None,
                     window: int = 0, out=None, stream=None):
     """Attention of q (float16 (tokens, q_heads, head_dim), rows cu[b] .. cu[b+1] the last tokens of sequence
     b) over the kv_len[b] tokens each sequence has in the cache; softmax_scale defaults to head_dim ** -0.5."""
-    c = _kv_cache(cache)
-    qp, tokens, q_heads, ts, hs = _kv_rows(q, 0, c.head_dim, "q")
-    if out is None:
-        out = _new_out(q, (tokens, q_heads, c.head_dim), torch.float16, stream)
-        op, out_ts = out.data_ptr(), q_heads * c.head_dim
-    else:
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
-        op, _, _, out_ts, out_hs = _kv_rows(out, 0, c.head_dim, "out")
-        if out_hs != c.head_dim:
-            raise ValueError("the heads of a row of out must be contiguous")
-    if tokens == 0:
-        return out
-    scale = c.head_dim ** -0.5 if softmax_scale is None else softmax_scale
-    _check(lib().kv_attention_s8(ctypes.byref(c), *_kv_batch(cu, kv_len, block_table, "kv_len"), max_q,
-                                 q_heads, qp, ts, hs, scale, window, op, out_ts,
-                                 _stream_handle(stream)), "kv_attention_s8")
-    return out
+    scale = q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale
+    return _checked((_marshal or _native()).kv_attention(q, cache, cu, kv_len, block_table, max_q, scale, window, out,
+                                                         None if stream is None else stream.cuda_stream),
+                    "kv_attention_s8")
 
 
 def gemm_s4_workspace_bytes(M: int, N: int, K: int) -> int:

@@ -92,39 +92,42 @@ __global__ void __launch_bounds__(512) kv_append_kernel(const KvAppendParams p) 
   const int index = (r.begin >> p.c.page_shift) + nth;
   const int pos0 = index << p.c.page_shift;
   if (pos0 >= r.end) return;
+  // the page's id is on its way while the new values are asked for, which do not need it
   const int slot = kv_ld(p.b.table + static_cast<long long>(seq) * p.b.table_stride + index);
+  const int per_row = p.c.dim / 8, pieces = p.c.page * per_row;
+  const __half* const src = (which ? p.x[1] : p.x[0]) +
+                            (static_cast<long long>(r.row0) + (pos0 - r.begin)) * p.token_stride + head * p.head_stride;
+  uint4 x[KV_APPEND_PIECES];  // eight new binary16 values, or in .x, .y eight old codes
+  int pos[KV_APPEND_PIECES];  // token of the piece; -1 = none
+#pragma unroll
+  for (int i = 0; i < KV_APPEND_PIECES; ++i) {
+    const int piece = static_cast<int>(threadIdx.x) + i * static_cast<int>(blockDim.x);
+    const int row = piece / per_row;
+    pos[i] = piece < pieces && pos0 + row < r.end ? pos0 + row : -1;
+    x[i] = make_uint4(0, 0, 0, 0);
+    if (pos[i] >= r.begin) x[i] = ptx::ld_global_stream_v4(src + row * p.token_stride + (piece - row * per_row) * 8);
+  }
   if (slot < 0 || slot >= p.c.num_pages) {
     if (lead) kv_report(p.b.status);
     return;
   }
   const long long page_head = static_cast<long long>(slot) * p.c.heads + head;
-  int8_t* const codes = p.c.codes[which] + page_head * p.c.page * p.c.dim;
-  float* const scale_at = p.c.scales[which] + page_head;
+  int8_t* const codes = (which ? p.c.codes[1] : p.c.codes[0]) + page_head * p.c.page * p.c.dim;
+  float* const scale_at = (which ? p.c.scales[1] : p.c.scales[0]) + page_head;
   const bool has_old = pos0 < r.begin;
   const float was = has_old ? ptx::ld_global_f32(scale_at) : 0.0f;
-
-  const int per_row = p.c.dim / 8, pieces = p.c.page * per_row;
-  uint4 x[KV_APPEND_PIECES];  // eight new binary16 values, or in .x, .y eight old codes
-  uint32_t m2 = 0;            // two maxima of magnitude bits
+  uint32_t m2 = 0;  // two maxima of magnitude bits: infinities and NaN compare above every finite value
 #pragma unroll
   for (int i = 0; i < KV_APPEND_PIECES; ++i) {
     const int piece = static_cast<int>(threadIdx.x) + i * static_cast<int>(blockDim.x);
-    x[i] = make_uint4(0, 0, 0, 0);
-    if (piece >= pieces) continue;
-    const int pos = pos0 + piece / per_row, d = piece % per_row * 8;
-    if (pos >= r.begin && pos < r.end) {
-      x[i] = ptx::ld_global_stream_v4(p.x[which] + (static_cast<long long>(r.row0) + (pos - r.begin)) * p.token_stride +
-                                      head * p.head_stride + d);
-      // infinities and NaN compare above every finite value
+    if (has_old && pos[i] >= 0 && pos[i] < r.begin)
+      asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(x[i].x), "=r"(x[i].y) : "l"(codes + piece * 8) : "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < KV_APPEND_PIECES; ++i)
+    if (pos[i] >= r.begin)
       m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu),
                                  __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
-    } else if (pos < r.begin) {
-      asm volatile("ld.global.v2.u32 {%0, %1}, [%2];"
-                   : "=r"(x[i].x), "=r"(x[i].y)
-                   : "l"(codes + piece * 8)
-                   : "memory");
-    }
-  }
   uint32_t m = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
   if (blockDim.x > 32) {
     if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = m;
@@ -143,11 +146,9 @@ __global__ void __launch_bounds__(512) kv_append_kernel(const KvAppendParams p) 
 #pragma unroll
   for (int i = 0; i < KV_APPEND_PIECES; ++i) {
     const int piece = static_cast<int>(threadIdx.x) + i * static_cast<int>(blockDim.x);
-    if (piece >= pieces) continue;
-    const int pos = pos0 + piece / per_row;
-    if (pos >= r.end || (pos < r.begin && !grew)) continue;
+    if (pos[i] < 0 || (pos[i] < r.begin && !grew)) continue;
     float v[8];
-    if (pos >= r.begin) {
+    if (pos[i] >= r.begin) {
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -179,6 +180,7 @@ struct KvReadParams {
 
 constexpr int KV_READ_TOKENS = 16;  // tokens per CTA
 constexpr int KV_READ_THREADS = 256;
+constexpr int KV_READ_UNITS = 4;    // 16-byte pieces a thread has in flight
 
 // grid: (batch * blocks_per_seq, 2)
 __global__ void __launch_bounds__(KV_READ_THREADS) kv_read_kernel(const KvReadParams p) {
@@ -195,36 +197,56 @@ __global__ void __launch_bounds__(KV_READ_THREADS) kv_read_kernel(const KvReadPa
   if (tokens <= 0) return;
   const int per_head = p.c.dim / 16, per_token = p.c.heads * per_head;
   const int* const table = p.b.table + static_cast<long long>(seq) * p.b.table_stride;
-#pragma unroll 4
-  for (int u = static_cast<int>(threadIdx.x); u < tokens * per_token; u += KV_READ_THREADS) {
-    const int t = u / per_token, rest = u - t * per_token;
-    const int head = rest / per_head, d = (rest - head * per_head) * 16;
-    const int pos = r.begin + t0 + t;
-    const int slot = kv_ld(table + (pos >> p.c.page_shift));
-    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-    if (slot < 0 || slot >= p.c.num_pages) {
-      kv_report(p.b.status);
-    } else {
-      const long long page_head = static_cast<long long>(slot) * p.c.heads + head;
-      const uint4 q = ptx::ld_global_stream_v4(
-          (which ? p.c.codes[1] : p.c.codes[0]) + (page_head * p.c.page + (pos & (p.c.page - 1))) * p.c.dim + d);
-      const float s = ptx::ld_global_f32((which ? p.c.scales[1] : p.c.scales[0]) + page_head);
-      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  const int8_t* const codes = which ? p.c.codes[1] : p.c.codes[0];
+  const float* const scales = which ? p.c.scales[1] : p.c.scales[0];
+  const int units = tokens * per_token;
+#pragma unroll 1
+  for (int first = static_cast<int>(threadIdx.x); first < units; first += KV_READ_UNITS * KV_READ_THREADS) {
+    // the ids of all pieces, then their codes and scales, then the results: three latencies for all
+    int slot[KV_READ_UNITS], pos[KV_READ_UNITS], head[KV_READ_UNITS], rest[KV_READ_UNITS];
+    uint4 q[KV_READ_UNITS];
+    float s[KV_READ_UNITS];
+#pragma unroll
+    for (int i = 0; i < KV_READ_UNITS; ++i) {
+      const int u = first + i * KV_READ_THREADS;
+      const int t = u / per_token;
+      rest[i] = u - t * per_token;
+      head[i] = rest[i] / per_head;
+      pos[i] = u < units ? t : -1;
+      slot[i] = -1;
+      if (u < units) slot[i] = kv_ld(table + ((r.begin + t0 + t) >> p.c.page_shift));
+    }
+#pragma unroll
+    for (int i = 0; i < KV_READ_UNITS; ++i) {
+      q[i] = make_uint4(0, 0, 0, 0);
+      s[i] = 0.0f;
+      if (slot[i] < 0 || slot[i] >= p.c.num_pages) {
+        if (pos[i] >= 0) kv_report(p.b.status);
+        continue;
+      }
+      const long long page_head = static_cast<long long>(slot[i]) * p.c.heads + head[i];
+      q[i] = ptx::ld_global_stream_v4(codes + (page_head * p.c.page + ((r.begin + t0 + pos[i]) & (p.c.page - 1))) * p.c.dim +
+                                      (rest[i] - head[i] * per_head) * 16);
+      s[i] = ptx::ld_global_f32(scales + page_head);
+    }
+#pragma unroll
+    for (int i = 0; i < KV_READ_UNITS; ++i) {
+      if (pos[i] < 0) continue;
+      const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
       uint32_t h[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float a = static_cast<float>(static_cast<int8_t>(w[j / 2] >> (16 * (j & 1)))) * s;
-        const float b = static_cast<float>(static_cast<int8_t>(w[j / 2] >> (16 * (j & 1) + 8))) * s;
+        const float a = static_cast<float>(static_cast<int8_t>(w[j / 2] >> (16 * (j & 1)))) * s[i];
+        const float b = static_cast<float>(static_cast<int8_t>(w[j / 2] >> (16 * (j & 1) + 8))) * s[i];
         const __half2 x = __floats2half2_rn(a, b);
         h[j] = *reinterpret_cast<const uint32_t*>(&x);
       }
-      lo = make_uint4(h[0], h[1], h[2], h[3]);
-      hi = make_uint4(h[4], h[5], h[6], h[7]);
+      // rows of a token are dense: heads x dim
+      uint4* const dst = reinterpret_cast<uint4*>(
+          out + ((static_cast<long long>(r.row0) + t0 + pos[i]) * per_token + rest[i]) * 16);
+      dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
+      dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
     }
-    uint4* const dst = reinterpret_cast<uint4*>(
-        out + ((static_cast<long long>(r.row0) + t0 + t) * p.c.heads + head) * p.c.dim + d);
-    dst[0] = lo;
-    dst[1] = hi;
   }
 }
 
