@@ -920,6 +920,29 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         }
       }
     };
+    // The same for 16 columns from 16 * b16.
+    auto add_partial16 = [&](uint32_t (&r)[16], int b16) {
+      if constexpr (CSPLIT > 1) {
+#pragma unroll
+        for (int peer = 0; peer < CSPLIT - 1; ++peer) {
+          const uint32_t xsrc = base + L::X_OFFSET +
+                                static_cast<uint32_t>(peer * L::X_PEER_BYTES + quarter * (32 * BN * 4) +
+                                                      (b16 >> 1) * 4096 + lane * 128);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t u[4];
+            ptx::ld_shared_v4(xsrc + static_cast<uint32_t>(((((b16 & 1) * 4 + j) ^ (lane & 7)) * 16)), u[0], u[1], u[2], u[3]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              if constexpr (KIND == ptx::KIND_F16)
+                r[4 * j + v] = __float_as_uint(__uint_as_float(r[4 * j + v]) + __uint_as_float(u[v]));
+              else
+                r[4 * j + v] += u[v];
+            }
+          }
+        }
+      }
+    };
     for (int t = first_tile; t < num_tiles && ok; t += tile_stride) {
       int tm, tn, tile, k_begin, k_end;
       bool add;
@@ -1016,8 +1039,81 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       // wide -- and only ever runs with plain stores: c_vec_ok = 0, set by the host.)
       constexpr int BLOCK_COLS = (epi_out16(EPI) && BN >= 64) ? 64 : 32;
       static_assert(BN % BLOCK_COLS == 0, "tile width must be a multiple of the store block");
+      if constexpr (epi_linear(EPI)) {
+        // 16 columns at a time, the next ones on their way out of tensor memory meanwhile
+        constexpr int RBYTES = epi_out16(EPI) ? 2 : 4;
+        constexpr int PER_BLOCK = BLOCK_COLS / 16;
+        const uint32_t t_acc = tmem_base + lane_base + static_cast<uint32_t>(acc * BN);
+        uint32_t next[16];
+        if (!xpeer) ptx::tmem_ld_32x32b_x16(t_acc, next);
+        uint32_t row_addr = 0;
 #pragma unroll 1
-      for (int c = 0; c < BN / BLOCK_COLS && !xpeer; ++c) {
+        for (int c = 0; c < BN / 16 && !xpeer; ++c) {
+          const int col = col0 + c * 16, cc = col + (lane & 15);
+          uint32_t res[RBYTES * 4];
+          if (p.lin.residual)
+            lin_load_residual<RBYTES, 16>(p.lin, row, col, p.M, p.N, p.transpose_c, res);
+          const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
+          const float cb_mine = (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
+          const bool first = c % PER_BLOCK == 0, last = c % PER_BLOCK == PER_BLOCK - 1;
+          if (p.c_vec_ok && first) {  // a staging buffer, as below
+            row_addr = epi_base + static_cast<uint32_t>((staged_blocks & 1) * L::EPI_BUF_BYTES + lane * 128);
+            if (lane == 0) ptx::bulk_wait_group_read<1>();
+            __syncwarp();
+          }
+          ptx::tmem_wait_ld();
+          uint32_t r[16];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) r[v] = next[v];
+          if (c + 1 < BN / 16) ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>((c + 1) * 16), next);
+          add_partial16(r, c);
+          float x[16];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
+          lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
+          lin_activate_all(x, p.lin);
+          if (p.lin.residual) lin_add_residual<RBYTES, 16>(x, res);
+          uint32_t w[RBYTES * 4];
+#pragma unroll
+          for (int v = 0; v < RBYTES * 4; ++v) {
+            if constexpr (RBYTES == 2)
+              w[v] = pack_half2(x[2 * v], x[2 * v + 1]);
+            else
+              w[v] = __float_as_uint(x[v]);
+          }
+          if (p.c_vec_ok) {
+#pragma unroll
+            for (int j = 0; j < RBYTES; ++j)
+              ptx::st_shared_v4(row_addr + static_cast<uint32_t>((((c % PER_BLOCK) * RBYTES + j) ^ (lane & 7)) * 16),
+                                w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+            if (last) {
+              ptx::fence_proxy_async_smem();
+              __syncwarp();
+              const int bcol = col0 + c / PER_BLOCK * BLOCK_COLS;
+              if (lane == 0) {
+                if (row0 < p.M && bcol < p.N)
+                  ptx::tma_store_2d(&tmap_c, bcol, row0, row_addr, pol_c);  // (lane 0: the buffer's start)
+                ptx::bulk_commit_group();
+              }
+              ++staged_blocks;
+            }
+          } else if (row < p.M) {
+            const size_t rstep = p.transpose_c ? 1 : static_cast<size_t>(p.ldc);
+            const size_t cstep = p.transpose_c ? static_cast<size_t>(p.ldc) : 1;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              if (col + v >= p.N) continue;
+              const size_t at = static_cast<size_t>(row) * rstep + static_cast<size_t>(col + v) * cstep;
+              if constexpr (RBYTES == 2)
+                reinterpret_cast<uint16_t*>(p.C)[at] = static_cast<uint16_t>(w[v / 2] >> (16 * (v & 1)));
+              else
+                p.C[at] = w[v];
+            }
+          }
+        }
+      }
+#pragma unroll 1
+      for (int c = 0; c < BN / BLOCK_COLS && !xpeer && !epi_linear(EPI); ++c) {
         const int col = col0 + c * BLOCK_COLS;
         uint32_t w[32];  // the thread's 128 bytes of output
         if constexpr (EPI == EPI_RAW32 && CSPLIT == 1) {
@@ -1069,37 +1165,6 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           for (int v = 0; v < 32; ++v) {
             const float cs = __shfl_sync(0xffffffffu, cs_mine, v);
             w[v] = __float_as_uint(acc_to_float<KIND>(fix(w[v])) * rs * cs);
-          }
-        } else if constexpr (epi_linear(EPI)) {
-#pragma unroll
-          for (int h = 0; h < BLOCK_COLS / 32; ++h) {
-            const int c32 = col + h * 32, cc = c32 + lane;
-            constexpr int RBYTES = epi_out16(EPI) ? 2 : 4;
-            uint32_t res[RBYTES * 8];  // requested first: they arrive while the sums are fetched
-            if (p.lin.residual)
-              lin_load_residual<RBYTES>(p.lin, row, c32, p.M, p.N, p.transpose_c, res);
-            const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
-            const float cb_mine =
-                (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
-            uint32_t r[32];
-            ptx::tmem_ld_32x32b_x32(
-                tmem_base + lane_base + static_cast<uint32_t>(acc * BN + c * BLOCK_COLS + h * 32), r);
-            ptx::tmem_wait_ld();
-            add_partial(r, c * (BLOCK_COLS / 32) + h);
-            float x[32];
-#pragma unroll
-            for (int v = 0; v < 32; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
-            lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
-            lin_activate32(x, p.lin);
-            if (p.lin.residual) lin_add_residual<RBYTES>(x, res);
-#pragma unroll
-            for (int v = 0; v < 32; ++v) {
-              if constexpr (epi_out16(EPI)) {
-                if (v % 2 == 0) w[h * 16 + v / 2] = pack_half2(x[v], x[v + 1]);
-              } else {
-                w[v] = __float_as_uint(x[v]);
-              }
-            }
           }
         } else {
 #pragma unroll

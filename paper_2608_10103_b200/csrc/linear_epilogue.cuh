@@ -48,36 +48,40 @@ __device__ __forceinline__ float lin_activate(float x, const LinearEpilogue& e) 
   }
 }
 
-// The same for a thread's 32 values; the choice is the same for the whole grid.
-__device__ __forceinline__ void lin_activate32(float (&x)[32], const LinearEpilogue& e) {
+// The same for N values of a thread; the choice is the same for the whole grid.  (N = 16 in the tile
+// kernels, in a rolled loop: an epilogue unrolled over 64 columns is some 2000 instructions that a CTA with
+// one tile fetches cold, at about ten cycles each.)
+template <int N>
+__device__ __forceinline__ void lin_activate_all(float (&x)[N], const LinearEpilogue& e) {
   if (e.act == LIN_ACT_NONE) return;
   if (e.act == LIN_ACT_GATE) {
     const float a = e.gate_a, b = e.gate_b;
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] = lin_gate(x[v], a, b);
+    for (int v = 0; v < N; ++v) x[v] = lin_gate(x[v], a, b);
   } else if (e.act == LIN_ACT_ERF) {
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] = lin_erf(x[v]);
+    for (int v = 0; v < N; ++v) x[v] = lin_erf(x[v]);
   } else {
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] = x[v] < 0.0f ? 0.0f : x[v];
+    for (int v = 0; v < N; ++v) x[v] = x[v] < 0.0f ? 0.0f : x[v];
   }
 }
 
 // Scales (integer sums) and bias.  Lane v holds the factors of column v of the block.
-__device__ __forceinline__ void lin_scale_bias(float (&x)[32], bool scaled, float row_scale,
+template <int N>
+__device__ __forceinline__ void lin_scale_bias(float (&x)[N], bool scaled, float row_scale,
                                                float col_scale_mine, float row_bias,
                                                float col_bias_mine, bool by_column) {
   if (scaled) {
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] = x[v] * row_scale * __shfl_sync(0xffffffffu, col_scale_mine, v);
+    for (int v = 0; v < N; ++v) x[v] = x[v] * row_scale * __shfl_sync(0xffffffffu, col_scale_mine, v);
   }
   if (by_column) {
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] += __shfl_sync(0xffffffffu, col_bias_mine, v);
+    for (int v = 0; v < N; ++v) x[v] += __shfl_sync(0xffffffffu, col_bias_mine, v);
   } else {
 #pragma unroll
-    for (int v = 0; v < 32; ++v) x[v] += row_bias;  // 0 without a bias
+    for (int v = 0; v < N; ++v) x[v] += row_bias;  // 0 without a bias
   }
 }
 
@@ -90,20 +94,20 @@ __device__ __forceinline__ void lin_prefetch_row(const LinearEpilogue& e, int ro
   for (int b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + b));
 }
 
-// Residual values of one row, columns col .. col + 31, as raw words (two halves or one float each).
+// Residual values of one row, columns col .. col + N - 1, as raw words (two halves or one float each).
 // Rows and columns outside C read nothing and give zeros.  Ordinary loads: the values may come
 // from the grid in front, whose end the caller has awaited.
-template <int BYTES>
+template <int BYTES, int N>
 __device__ __forceinline__ void lin_load_residual(const LinearEpilogue& e, int row, int col, int m,
-                                                  int n, int transposed, uint32_t (&r)[BYTES * 8]) {
+                                                  int n, int transposed, uint32_t (&r)[BYTES * N / 4]) {
 #pragma unroll
-  for (int v = 0; v < BYTES * 8; ++v) r[v] = 0;
+  for (int v = 0; v < BYTES * N / 4; ++v) r[v] = 0;
   if (row >= m) return;
-  if (!transposed && e.r_vec_ok && col + 32 <= n) {
+  if (!transposed && e.r_vec_ok && col + N <= n) {
     const char* at = static_cast<const char*>(e.residual) +
                      (static_cast<long long>(row) * e.ldr + col) * BYTES;
 #pragma unroll
-    for (int v = 0; v < BYTES * 2; ++v)
+    for (int v = 0; v < BYTES * N / 16; ++v)
       asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(r[4 * v]), "=r"(r[4 * v + 1]), "=r"(r[4 * v + 2]), "=r"(r[4 * v + 3])
                    : "l"(at + 16 * v)
@@ -113,7 +117,7 @@ __device__ __forceinline__ void lin_load_residual(const LinearEpilogue& e, int r
   const long long base = transposed ? row : static_cast<long long>(row) * e.ldr;
   const long long step = transposed ? e.ldr : 1;
 #pragma unroll
-  for (int v = 0; v < 32; ++v) {
+  for (int v = 0; v < N; ++v) {
     if (col + v >= n) continue;
     const long long at = base + (col + v) * step;
     if constexpr (BYTES == 4) {
@@ -132,10 +136,10 @@ __device__ __forceinline__ void lin_load_residual(const LinearEpilogue& e, int r
   }
 }
 
-template <int BYTES>
-__device__ __forceinline__ void lin_add_residual(float (&x)[32], const uint32_t (&r)[BYTES * 8]) {
+template <int BYTES, int N>
+__device__ __forceinline__ void lin_add_residual(float (&x)[N], const uint32_t (&r)[BYTES * N / 4]) {
 #pragma unroll
-  for (int v = 0; v < 32; ++v) {
+  for (int v = 0; v < N; ++v) {
     if constexpr (BYTES == 4) {
       x[v] += __uint_as_float(r[v]);
     } else {
