@@ -73,6 +73,12 @@ constexpr int NUM_THREADS_FUSED = NUM_THREADS + 32 * UNPACK_WARPS;
 constexpr int NUM_THREADS_FUSED_A8 = NUM_THREADS_FUSED + 32;  // hybrid: warp 14 fetches the A image
 constexpr int AHEAD_WARPS = 4;    // overlapped INT4 pre-pass only: warps 6..9
 constexpr int NUM_THREADS_AHEAD = NUM_THREADS + 32 * AHEAD_WARPS;
+// Linear layers on tiles of 128 or 256 columns: two epilogue warps per lane quarter, taking the staging
+// blocks in turn (one warp per scheduler could not keep pace with K = 4096 int8: 16 k cycles of MMAs
+// per 256 x 256 tile against 1.5-2 k per 16 columns).  Their buffers cost a ring slot.
+constexpr int epi_warps(int epi, int bn, int pstages, int csplit) {
+  return epi >= 3 && bn >= 128 && pstages == 0 && csplit == 1 ? 8 : EPI_WARPS;
+}
 
 // What the epilogue writes.
 enum EpiMode {
@@ -174,8 +180,9 @@ enum TraceSlot {
 // bytes of K in the 128-byte-swizzle layout (the widest a swizzled TMA box can
 // be).  KB = 2 halves the per-slot barrier work (one wait, one commit per 8 MMAs)
 // of the single issuing thread, whose instruction time is the scarce resource.
-template <int BN, int STAGES, int CTA_GROUP, int KB, int PSTAGES = 0, int CSPLIT = 1, bool A8 = false>
+template <int BN, int STAGES, int CTA_GROUP, int KB, int PSTAGES = 0, int CSPLIT = 1, bool A8 = false, int EPI = 0>
 struct SmemLayout {
+  static constexpr int EPI_W = epi_warps(EPI, BN, PSTAGES, CSPLIT);
   static constexpr int B_ROWS = BN / CTA_GROUP;  // B rows each CTA loads
   static constexpr int A_BYTES = BM * BK_BYTES;       // one A atom
   static constexpr int B_BYTES = B_ROWS * BK_BYTES;   // one B atom
@@ -192,7 +199,7 @@ struct SmemLayout {
   // Epilogue staging: per epilogue warp two buffers of 32 rows x 128 bytes (32 x 32 C values).
   static constexpr int EPI_BUF_BYTES = 32 * 128;
   static constexpr int EPI_OFFSET = RING_BYTES;
-  static constexpr int EPI_BYTES = EPI_WARPS * 2 * EPI_BUF_BYTES;
+  static constexpr int EPI_BYTES = EPI_W * 2 * EPI_BUF_BYTES;
   // Cluster split-K: the CTA of cluster rank 0 receives the other CTAs' 128 x BN partial
   // accumulators (32-bit) here, one buffer per sender.
   static constexpr int X_OFFSET = EPI_OFFSET + EPI_BYTES;
@@ -202,8 +209,9 @@ struct SmemLayout {
   // full[STAGES], empty[STAGES], acc_full[2], acc_empty[2], drain, p_full[PSTAGES], p_empty[PSTAGES]
   // fused INT4 adds ready[STAGES], its hybrid form a_full[A8_STAGES], a_empty[A8_STAGES];
   // cluster split-K adds part_full, part_free (last two)
-  static constexpr int NUM_BARS = 2 * STAGES + 5 + 2 * PSTAGES + (PSTAGES > 0 ? STAGES : 0) +
-                                  2 * A8_STAGES + (CSPLIT > 1 ? 2 : 0);
+  // linear layers add two per epilogue warp (residual block landed), in front of those
+  static constexpr int RES_BAR = 2 * STAGES + 5 + 2 * PSTAGES + (PSTAGES > 0 ? STAGES : 0) + 2 * A8_STAGES;
+  static constexpr int NUM_BARS = RES_BAR + (epi_linear(EPI) ? 2 * EPI_W : 0) + (CSPLIT > 1 ? 2 : 0);
   static constexpr int MISC_OFFSET = BAR_OFFSET + NUM_BARS * 8;
   static constexpr int TOTAL = MISC_OFFSET + 16;
   static constexpr int DYN_BYTES = TOTAL + 1024;  // slack to align the ring to 1024 bytes
@@ -241,10 +249,13 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 template <int KIND, int BN, int STAGES, int CTA_GROUP, int KB, int EPI = EPI_RAW32, int PSTAGES = 0,
           int CSPLIT = 1, bool DBG = false, bool AHEAD = false, bool A8 = false>
 __global__ void __launch_bounds__(A8 ? NUM_THREADS_FUSED_A8
-                                     : PSTAGES > 0 ? NUM_THREADS_FUSED : (AHEAD ? NUM_THREADS_AHEAD : NUM_THREADS), 1)
+                                     : PSTAGES > 0 ? NUM_THREADS_FUSED
+                                     : AHEAD ? NUM_THREADS_AHEAD : 64 + 32 * epi_warps(EPI, BN, PSTAGES, CSPLIT), 1)
 gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
-            const __grid_constant__ CUtensorMap tmap_c, const GemmParams p) {
-  using L = SmemLayout<BN, STAGES, CTA_GROUP, KB, PSTAGES, CSPLIT, A8>;
+            const __grid_constant__ CUtensorMap tmap_c, const __grid_constant__ CUtensorMap tmap_r,
+            const GemmParams p) {
+  using L = SmemLayout<BN, STAGES, CTA_GROUP, KB, PSTAGES, CSPLIT, A8, EPI>;
+  constexpr int EPI_W = L::EPI_W;
   constexpr bool FUSED = PSTAGES > 0;  // packed INT4 operands, expanded on the way to the MMAs
   static_assert(!A8 || (PSTAGES > 0 && CSPLIT == 1 && !DBG), "hybrid: a fused INT4 variant");
   const int ablate = DBG ? p.ablate : 0;
@@ -382,9 +393,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(acc_full_bar(a), 1);
-      ptx::mbar_init(acc_empty_bar(a), EPI_WARPS * CTA_GROUP);
+      ptx::mbar_init(acc_empty_bar(a), EPI_W * CTA_GROUP);
     }
     ptx::mbar_init(drain_bar, 1);
+    if constexpr (epi_linear(EPI))
+      for (int i = 0; i < 2 * EPI_W; ++i) ptx::mbar_init(bar0 + 8u * (L::RES_BAR + i), 1);
     if constexpr (CSPLIT > 1) {
       ptx::mbar_init(part_full_bar, 1);  // rank 0's own announcement; the rest is a byte count
       ptx::mbar_init(part_free_bar, EPI_WARPS);
@@ -943,6 +956,46 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         }
       }
     };
+    // ---- linear layers: state of the steps ahead
+    // One staging block = 32 rows x 128 bytes = 32 columns of 32-bit or 64 columns of 16-bit results.
+    constexpr int LIN_COLS = (epi_out16(EPI) && BN >= 64) ? 64 : 32;
+    constexpr int LIN_BYTES = epi_out16(EPI) ? 2 : 4;
+    constexpr int LIN_STEPS = LIN_COLS / 16, LIN_SIDES = EPI_W / 4;
+    [[maybe_unused]] const int lin_side = (warp - 2) / 4;  // which of the quarter's warps
+    [[maybe_unused]] const uint32_t res_bar = bar0 + 8u * static_cast<uint32_t>(L::RES_BAR + 2 * (warp - 2));
+    [[maybe_unused]] uint32_t res_phase = 0;   // parity of the two buffers' barriers
+    [[maybe_unused]] bool res_pending = false; // a residual block is on its way
+    [[maybe_unused]] float cs_next = 0.0f, cb_next = 0.0f;  // column factors of the next step
+    [[maybe_unused]] uint32_t res_next[4 * LIN_BYTES];      // ... and, with exchanged operands, its residual
+    // The residual's block of 32 rows from (row0, col) into the staging buffer of block number `block`.
+    [[maybe_unused]] auto lin_fetch_block = [&](uint32_t block, int row0, int col) {
+      if (row0 >= p.M || col >= p.N) return;
+      res_pending = true;
+      if (lane == 0) {
+        const uint32_t bar = res_bar + 8u * (block & 1);
+        ptx::mbar_arrive_expect_tx(bar, L::EPI_BUF_BYTES);
+        ptx::tma_load_2d(epi_base + static_cast<uint32_t>((block & 1) * L::EPI_BUF_BYTES), &tmap_r, col, row0, bar,
+                         ptx::policy_evict_first());
+      }
+    };
+    [[maybe_unused]] auto lin_factors = [&](int col) {
+      const int cc = col + (lane & 15);
+      cs_next = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
+      cb_next = (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
+    };
+    [[maybe_unused]] auto lin_first = [&](int row0, int row, int col0, float& rb) {
+      const int col = col0 + lin_side * LIN_COLS;
+      if (p.lin.row_bias && row < p.M) rb = ptx::ld_global_f32(p.lin.row_bias + row);
+      lin_factors(col);
+      if (!p.lin.residual) return;
+      if (p.transpose_c) {
+        lin_prefetch_transposed<LIN_BYTES, BN>(p.lin, row0, col0, p.M, p.N, lane);
+        lin_load_residual<LIN_BYTES, 16>(p.lin, row, col, p.M, p.N, 1, res_next);
+      } else if (p.lin.r_tma) {
+        if (lane == 0) ptx::bulk_wait_group_read<1>();  // the store two blocks ago has read the buffer
+        lin_fetch_block(staged_blocks, row0, col);
+      }
+    };
     for (int t = first_tile; t < num_tiles && ok; t += tile_stride) {
       int tm, tn, tile, k_begin, k_end;
       bool add;
@@ -953,11 +1006,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       const int col0 = tn * BN;
       float rs = 1.0f, rb = 0.0f;
       if constexpr (epi_linear(EPI)) {
-        // (the grid in front has finished: see the wait above)
+        // what the first step reads is on its way while the products are still being summed (the grid
+        // in front has finished: see the wait above)
         if (!xpeer) {
-          if (p.lin.row_bias && row < p.M) rb = ptx::ld_global_f32(p.lin.row_bias + row);
-          if (p.lin.residual && !p.transpose_c && row < p.M)
-            lin_prefetch_row<epi_out16(EPI) ? 2 : 4, BN>(p.lin, row, col0, p.N);
+          lin_first(row0, row, col0, rb);
         }
       }
       if constexpr (EPI != EPI_RAW32) {
@@ -1040,77 +1092,111 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       constexpr int BLOCK_COLS = (epi_out16(EPI) && BN >= 64) ? 64 : 32;
       static_assert(BN % BLOCK_COLS == 0, "tile width must be a multiple of the store block");
       if constexpr (epi_linear(EPI)) {
-        // 16 columns at a time, the next ones on their way out of tensor memory meanwhile
-        constexpr int RBYTES = epi_out16(EPI) ? 2 : 4;
-        constexpr int PER_BLOCK = BLOCK_COLS / 16;
         const uint32_t t_acc = tmem_base + lane_base + static_cast<uint32_t>(acc * BN);
         uint32_t next[16];
-        if (!xpeer) ptx::tmem_ld_32x32b_x16(t_acc, next);
-        uint32_t row_addr = 0;
+        if (!xpeer) ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>(lin_side * LIN_COLS), next);
 #pragma unroll 1
-        for (int c = 0; c < BN / 16 && !xpeer; ++c) {
-          const int col = col0 + c * 16, cc = col + (lane & 15);
-          uint32_t res[RBYTES * 4];
-          if (p.lin.residual)
-            lin_load_residual<RBYTES, 16>(p.lin, row, col, p.M, p.N, p.transpose_c, res);
-          const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
-          const float cb_mine = (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
-          const bool first = c % PER_BLOCK == 0, last = c % PER_BLOCK == PER_BLOCK - 1;
-          if (p.c_vec_ok && first) {  // a staging buffer, as below
-            row_addr = epi_base + static_cast<uint32_t>((staged_blocks & 1) * L::EPI_BUF_BYTES + lane * 128);
-            if (lane == 0) ptx::bulk_wait_group_read<1>();
-            __syncwarp();
+        for (int blk = lin_side; blk < BN / LIN_COLS && !xpeer; blk += LIN_SIDES) {
+          const int bcol = col0 + blk * LIN_COLS;
+          const uint32_t buf = epi_base + static_cast<uint32_t>((staged_blocks & 1) * L::EPI_BUF_BYTES);
+          const uint32_t row_addr = buf + static_cast<uint32_t>(lane * 128);
+          const bool from_buf = p.lin.residual && !p.transpose_c;
+          if (!p.transpose_c) {
+            if (from_buf && p.lin.r_tma) {
+              if (row0 < p.M && bcol < p.N) {
+                ok = wait_bounded(res_bar + 8u * (staged_blocks & 1), (res_phase >> (staged_blocks & 1)) & 1u, abort_flag,
+                                  p.status, DEV_TIMEOUT_EPILOGUE);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                res_phase ^= 1u << (staged_blocks & 1);
+                res_pending = false;
+              }
+            } else {
+              if (lane == 0) ptx::bulk_wait_group_read<1>();
+              __syncwarp();
+              if (from_buf) {
+                lin_block_copy<LIN_BYTES, LIN_COLS, false>(buf, const_cast<void*>(p.lin.residual), p.lin.ldr, row0, bcol,
+                                                           p.M, p.N, lane);
+                __syncwarp();
+              }
+            }
           }
-          ptx::tmem_wait_ld();
-          uint32_t r[16];
+#pragma unroll 1
+          for (int g = 0; g < LIN_STEPS; ++g) {
+            const int col = bcol + g * 16;
+            const int ahead = g + 1 < LIN_STEPS ? blk * LIN_COLS + (g + 1) * 16 : (blk + LIN_SIDES) * LIN_COLS;
+            const float cs_mine = cs_next, cb_mine = cb_next;
+            uint32_t res[4 * LIN_BYTES], r[16];
+            if (from_buf) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) r[v] = next[v];
-          if (c + 1 < BN / 16) ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>((c + 1) * 16), next);
-          add_partial16(r, c);
-          float x[16];
+              for (int j = 0; j < LIN_BYTES; ++j)
+                ptx::ld_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_BYTES + j) ^ (lane & 7)) * 16), res[4 * j],
+                                  res[4 * j + 1], res[4 * j + 2], res[4 * j + 3]);
+            } else {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
-          lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
-          lin_activate_all(x, p.lin);
-          if (p.lin.residual) lin_add_residual<RBYTES, 16>(x, res);
-          uint32_t w[RBYTES * 4];
+              for (int v = 0; v < 4 * LIN_BYTES; ++v) res[v] = res_next[v];
+            }
+            ptx::tmem_wait_ld();
 #pragma unroll
-          for (int v = 0; v < RBYTES * 4; ++v) {
-            if constexpr (RBYTES == 2)
-              w[v] = pack_half2(x[2 * v], x[2 * v + 1]);
-            else
-              w[v] = __float_as_uint(x[v]);
+            for (int v = 0; v < 16; ++v) r[v] = next[v];
+            if (ahead < BN) {
+              ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>(ahead), next);
+              lin_factors(col0 + ahead);
+              if (p.lin.residual && p.transpose_c)
+                lin_load_residual<LIN_BYTES, 16>(p.lin, row, col0 + ahead, p.M, p.N, 1, res_next);
+              if (from_buf && p.lin.r_tma && g == LIN_STEPS / 2 && blk + LIN_SIDES < BN / LIN_COLS) {
+                if (lane == 0) ptx::bulk_wait_group_read<0>();  // the other buffer's store was issued half a block ago
+                lin_fetch_block(staged_blocks + 1, row0, bcol + LIN_SIDES * LIN_COLS);
+              }
+            }
+            add_partial16(r, blk * LIN_STEPS + g);
+            float x[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
+            lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
+            lin_activate_all(x, p.lin);
+            if (p.lin.residual) lin_add_residual<LIN_BYTES, 16>(x, res);
+            uint32_t w[4 * LIN_BYTES];
+#pragma unroll
+            for (int v = 0; v < 4 * LIN_BYTES; ++v) {
+              if constexpr (LIN_BYTES == 2)
+                w[v] = pack_half2(x[2 * v], x[2 * v + 1]);
+              else
+                w[v] = __float_as_uint(x[v]);
+            }
+            if (!p.transpose_c) {
+#pragma unroll
+              for (int j = 0; j < LIN_BYTES; ++j)
+                ptx::st_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_BYTES + j) ^ (lane & 7)) * 16), w[4 * j],
+                                  w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+            } else if (row < p.M) {
+#pragma unroll
+              for (int v = 0; v < 16; ++v) {
+                if (col + v >= p.N) continue;
+                const size_t at = static_cast<size_t>(row) + static_cast<size_t>(col + v) * static_cast<size_t>(p.ldc);
+                if constexpr (LIN_BYTES == 2)
+                  reinterpret_cast<uint16_t*>(p.C)[at] = static_cast<uint16_t>(w[v / 2] >> (16 * (v & 1)));
+                else
+                  p.C[at] = w[v];
+              }
+            }
           }
-          if (p.c_vec_ok) {
-#pragma unroll
-            for (int j = 0; j < RBYTES; ++j)
-              ptx::st_shared_v4(row_addr + static_cast<uint32_t>((((c % PER_BLOCK) * RBYTES + j) ^ (lane & 7)) * 16),
-                                w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-            if (last) {
+          if (!p.transpose_c) {
+            if (p.c_vec_ok) {
               ptx::fence_proxy_async_smem();
               __syncwarp();
-              const int bcol = col0 + c / PER_BLOCK * BLOCK_COLS;
               if (lane == 0) {
-                if (row0 < p.M && bcol < p.N)
-                  ptx::tma_store_2d(&tmap_c, bcol, row0, row_addr, pol_c);  // (lane 0: the buffer's start)
+                if (row0 < p.M && bcol < p.N) ptx::tma_store_2d(&tmap_c, bcol, row0, buf, pol_c);
                 ptx::bulk_commit_group();
               }
-              ++staged_blocks;
+            } else {
+              __syncwarp();
+              lin_block_copy<LIN_BYTES, LIN_COLS, true>(buf, p.C, p.ldc, row0, bcol, p.M, p.N, lane);
             }
-          } else if (row < p.M) {
-            const size_t rstep = p.transpose_c ? 1 : static_cast<size_t>(p.ldc);
-            const size_t cstep = p.transpose_c ? static_cast<size_t>(p.ldc) : 1;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              if (col + v >= p.N) continue;
-              const size_t at = static_cast<size_t>(row) * rstep + static_cast<size_t>(col + v) * cstep;
-              if constexpr (RBYTES == 2)
-                reinterpret_cast<uint16_t*>(p.C)[at] = static_cast<uint16_t>(w[v / 2] >> (16 * (v & 1)));
-              else
-                p.C[at] = w[v];
-            }
+            ++staged_blocks;
           }
         }
+        if (!ok) break;
       }
 #pragma unroll 1
       for (int c = 0; c < BN / BLOCK_COLS && !xpeer && !epi_linear(EPI); ++c) {
@@ -1290,6 +1376,14 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       ++tiles_done;
       acc ^= 1;
       if (acc == 0) acc_phase ^= 1u;
+    }
+    if constexpr (epi_linear(EPI)) {
+      if (res_pending) {  // gave up: the residual block on its way must land before the CTA exits
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (!ptx::mbar_try_wait(res_bar + 8u * (staged_blocks & 1), (res_phase >> (staged_blocks & 1)) & 1u) &&
+               ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS) {
+        }
+      }
     }
     // C stores still in flight read this CTA's shared memory: wait until they have read it
     // (their global writes complete on their own before the grid counts as finished).  A

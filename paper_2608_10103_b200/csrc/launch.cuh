@@ -53,7 +53,7 @@ constexpr int epi_bank(int epi) { return (epi >> 2) * 320; }
 template <class Kernel>
 int launch_kernel(DeviceState* s, Kernel kernel, int variant, int dyn_bytes, int threads,
                   int cluster, const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& tc,
-                  const GemmParams& p, cudaStream_t stream) {
+                  const CUtensorMap& tr, const GemmParams& p, cudaStream_t stream) {
   if (!(s->attr_set[variant >> 6].load(std::memory_order_relaxed) & (1ull << (variant & 63)))) {
     cudaError_t e =
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dyn_bytes);
@@ -80,7 +80,7 @@ int launch_kernel(DeviceState* s, Kernel kernel, int variant, int dyn_bytes, int
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.wait_prior_grid ? 2 : 1;  // may start while the grid in front still runs
-  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, tc, p);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, ta, tb, tc, tr, p);
   if (e != cudaSuccess) return cuda_fail(e);
   return GEMM_OK;
 }
@@ -88,21 +88,21 @@ int launch_kernel(DeviceState* s, Kernel kernel, int variant, int dyn_bytes, int
 template <int KIND, int BN, int STAGES, int CTA_GROUP, int KB, int EPI, int PSTAGES = 0,
           int CSPLIT = 1>
 int launch_variant(DeviceState* s, int variant, const CUtensorMap& ta, const CUtensorMap& tb,
-                   const CUtensorMap& tc, const GemmParams& p, cudaStream_t stream) {
-  using L = SmemLayout<BN, STAGES, CTA_GROUP, KB, PSTAGES, CSPLIT>;
-  constexpr int THREADS = PSTAGES > 0 ? NUM_THREADS_FUSED : NUM_THREADS;
+                   const CUtensorMap& tc, const CUtensorMap& tr, const GemmParams& p, cudaStream_t stream) {
+  using L = SmemLayout<BN, STAGES, CTA_GROUP, KB, PSTAGES, CSPLIT, false, EPI>;
+  constexpr int THREADS = PSTAGES > 0 ? NUM_THREADS_FUSED : 64 + 32 * L::EPI_W;
   constexpr int CLUSTER = CTA_GROUP * CSPLIT;  // CTAs that work on one unit together
   if (p.ablate) {
     constexpr int twin = dbg_twin_bit<KIND, BN, STAGES, CTA_GROUP, KB, EPI, PSTAGES, CSPLIT>();
     if constexpr (twin >= 0) {
       return launch_kernel(s, gemm_kernel<KIND, BN, STAGES, CTA_GROUP, KB, EPI, PSTAGES, CSPLIT, true>,
-                           twin, L::DYN_BYTES, THREADS, CLUSTER, ta, tb, tc, p, stream);
+                           twin, L::DYN_BYTES, THREADS, CLUSTER, ta, tb, tc, tr, p, stream);
     } else {
       return GEMM_ERR_INVALID_ARG;  // this variant is not built with the switches
     }
   }
   return launch_kernel(s, gemm_kernel<KIND, BN, STAGES, CTA_GROUP, KB, EPI, PSTAGES, CSPLIT>,
-                       variant, L::DYN_BYTES, THREADS, CLUSTER, ta, tb, tc, p, stream);
+                       variant, L::DYN_BYTES, THREADS, CLUSTER, ta, tb, tc, tr, p, stream);
 }
 
 // The 512 x 256 CTA-pair kernel for large problems (gemm_wide.cuh).  attr_set bits 160..
@@ -229,7 +229,7 @@ template <int KIND, int EPI>
 int quad_clusters_resident(DeviceState* s, int variant) {
   std::atomic<int>& cached = s->quad_clusters[KIND == ptx::KIND_F16 ? 0 : 1][EPI];
   if (cached.load()) return cached.load();
-  using L = SmemLayout<32, 3, 1, 2, 0, 4>;
+  using L = SmemLayout<32, 3, 1, 2, 0, 4, false, EPI>;
   auto kernel = gemm_kernel<KIND, 32, 3, 1, 2, EPI, 0, 4>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::DYN_BYTES) !=
       cudaSuccess)
@@ -566,10 +566,16 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   } else {
     tc = ta;  // unused by the kernel on the plain-store path
   }
+  CUtensorMap tr = ta;  // residual of a linear layer, in the same blocks as C
+  p.lin = out.lin;
+  p.lin.r_tma = epi_linear(EPI) && !wide && p.c_vec_ok && p.lin.residual && p.lin.r_vec_ok;
+  if (p.lin.r_tma) {
+    rc = encode_c_map(&tr, p.lin.residual, M, N, p.lin.ldr, C_ELEM);
+    if (rc != GEMM_OK) return rc;
+  }
   p.C = static_cast<uint32_t*>(C);
   p.row_scale = swap ? out.col_scale : out.row_scale;  // indexed by the kernel's rows
   p.col_scale = swap ? out.row_scale : out.col_scale;
-  p.lin = out.lin;
   if (swap) std::swap(p.lin.row_bias, p.lin.col_bias);
   p.status = s->status_ptr;
   p.trace = (g_trace_on & 1) ? s->trace_ptr : nullptr;
@@ -665,11 +671,11 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
     if constexpr (KIND == ptx::KIND_I8) {
       const int cb = 128 + epi_slot(EPI) * 2 + epi_bank(EPI);
       if (cfg.bn == 64)
-        return launch_variant<KIND, 64, 4, 1, 1, EPI, 2, 2>(s, cb + 1, ta, tb, tc, p, stream);
+        return launch_variant<KIND, 64, 4, 1, 1, EPI, 2, 2>(s, cb + 1, ta, tb, tc, tr, p, stream);
       if (!epi_out16(EPI) || swap) {
         if (cfg.splits == 4)
-          return launch_variant<KIND, 32, 4, 1, 1, EPI, 3, 4>(s, 136 + epi_slot(EPI) + epi_bank(EPI), ta, tb, tc, p, stream);
-        return launch_variant<KIND, 32, 4, 1, 1, EPI, 4, 2>(s, cb, ta, tb, tc, p, stream);
+          return launch_variant<KIND, 32, 4, 1, 1, EPI, 3, 4>(s, 136 + epi_slot(EPI) + epi_bank(EPI), ta, tb, tc, tr, p, stream);
+        return launch_variant<KIND, 32, 4, 1, 1, EPI, 4, 2>(s, cb, ta, tb, tc, tr, p, stream);
       }
     }
     return GEMM_ERR_INVALID_ARG;
@@ -677,14 +683,15 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   if (csplit) {  // attr_set bits 96..: kind, output mode, width
     const int cb = csplit_variant_base<KIND, EPI>();
     if (cfg.bn == 64)
-      return launch_variant<KIND, 64, 3, 1, 2, EPI, 0, 2>(s, cb + 1, ta, tb, tc, p, stream);
+      return launch_variant<KIND, 64, 3, 1, 2, EPI, 0, 2>(s, cb + 1, ta, tb, tc, tr, p, stream);
     if (!epi_out16(EPI) || swap) {
       if (cfg.splits == 4)
-        return launch_variant<KIND, 32, 3, 1, 2, EPI, 0, 4>(s, cb + 8, ta, tb, tc, p, stream);
-      return launch_variant<KIND, 32, 4, 1, 2, EPI, 0, 2>(s, cb, ta, tb, tc, p, stream);
+        return launch_variant<KIND, 32, 3, 1, 2, EPI, 0, 4>(s, cb + 8, ta, tb, tc, tr, p, stream);
+      return launch_variant<KIND, 32, 4, 1, 2, EPI, 0, 2>(s, cb, ta, tb, tc, tr, p, stream);
     }
     return GEMM_ERR_INVALID_ARG;
   }
+  constexpr bool LIN = epi_linear(EPI);  // eight epilogue warps' buffers take a ring slot (see epi_warps)
   const int vbase = ((KIND == ptx::KIND_F16) ? 0 : 32) + epi_slot(EPI) * 8 + epi_bank(EPI);  // bit index in attr_set
   if (packed_s4) {
     // fused INT4 variants: (int8 slots, packed slots) sized to fill shared memory; attr_set
@@ -693,26 +700,26 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
       const int fb = 64 + epi_slot(EPI) * 8 + epi_bank(EPI);
       if (hybrid) {  // (int8 slots, packed B slots) = (4, 4): two groups of expansion warps
         if (cfg.bn == 128) {
-          using L = SmemLayout<128, 4, 2, 1, 4, 1, true>;
+          using L = SmemLayout<128, 4, 2, 1, 4, 1, true, EPI>;
           return launch_kernel(s, gemm_kernel<KIND, 128, 4, 2, 1, EPI, 4, 1, false, false, true>, fb + 7,
-                               L::DYN_BYTES, NUM_THREADS_FUSED_A8, 2, ta, tb, tc, p, stream);
+                               L::DYN_BYTES, NUM_THREADS_FUSED_A8, 2, ta, tb, tc, tr, p, stream);
         }
-        using L = SmemLayout<256, 4, 2, 1, 4, 1, true>;
+        using L = SmemLayout<256, 4, 2, 1, 4, 1, true, EPI>;
         return launch_kernel(s, gemm_kernel<KIND, 256, 4, 2, 1, EPI, 4, 1, false, false, true>, fb + 6,
-                             L::DYN_BYTES, NUM_THREADS_FUSED_A8, 2, ta, tb, tc, p, stream);
+                             L::DYN_BYTES, NUM_THREADS_FUSED_A8, 2, ta, tb, tc, tr, p, stream);
       }
       if (cfg.cta_group == 2) {
         if (cfg.bn == 128)
-          return launch_variant<KIND, 128, 4, 2, 1, EPI, 3>(s, fb + 5, ta, tb, tc, p, stream);
-        return launch_variant<KIND, 256, 4, 2, 1, EPI, 2>(s, fb + 0, ta, tb, tc, p, stream);
+          return launch_variant<KIND, 128, 4, 2, 1, EPI, 3>(s, fb + 5, ta, tb, tc, tr, p, stream);
+        return launch_variant<KIND, 256, 4, 2, 1, EPI, 2>(s, fb + 0, ta, tb, tc, tr, p, stream);
       }
       switch (cfg.bn) {
-        case 256: return launch_variant<KIND, 256, 2, 1, 1, EPI, 2>(s, fb + 1, ta, tb, tc, p, stream);
-        case 128: return launch_variant<KIND, 128, 4, 1, 1, EPI, 2>(s, fb + 2, ta, tb, tc, p, stream);
-        case 64: return launch_variant<KIND, 64, 4, 1, 1, EPI, 4>(s, fb + 3, ta, tb, tc, p, stream);
+        case 256: return launch_variant<KIND, 256, 2, 1, 1, EPI, 2>(s, fb + 1, ta, tb, tc, tr, p, stream);
+        case 128: return launch_variant<KIND, 128, 4, 1, 1, EPI, 2>(s, fb + 2, ta, tb, tc, tr, p, stream);
+        case 64: return launch_variant<KIND, 64, 4, 1, 1, EPI, 4>(s, fb + 3, ta, tb, tc, tr, p, stream);
         case 32:
           if (!epi_out16(EPI) || swap)
-            return launch_variant<KIND, 32, 4, 1, 1, EPI, 5>(s, fb + 4, ta, tb, tc, p, stream);
+            return launch_variant<KIND, 32, 4, 1, 1, EPI, 5>(s, fb + 4, ta, tb, tc, tr, p, stream);
           return GEMM_ERR_INVALID_ARG;
         default: return GEMM_ERR_INVALID_ARG;
       }
@@ -727,29 +734,29 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
             t_last_s4_overlapped = 1;
             using L = SmemLayout<256, 6, 2, 1, 0, 1>;
             return launch_kernel(s, gemm_kernel<KIND, 256, 6, 2, 1, EPI, 0, 1, false, true>, 224 + EPI,
-                                 L::DYN_BYTES, NUM_THREADS_AHEAD, 2, ta, tb, tc, p, stream);
+                                 L::DYN_BYTES, NUM_THREADS_AHEAD, 2, ta, tb, tc, tr, p, stream);
           }
         }
         if constexpr (EPI == EPI_RAW32) {
           // ring depth as an ablation variable (gemm_set_stages_override); attr_set bits 216..
           const int sb = 216 + (KIND == ptx::KIND_F16 ? 0 : 4);
-          if (cfg.stages == 3) return launch_variant<KIND, 256, 3, 2, 1, EPI>(s, sb + 0, ta, tb, tc, p, stream);
-          if (cfg.stages == 4) return launch_variant<KIND, 256, 4, 2, 1, EPI>(s, sb + 1, ta, tb, tc, p, stream);
-          if (cfg.stages == 5) return launch_variant<KIND, 256, 5, 2, 1, EPI>(s, sb + 2, ta, tb, tc, p, stream);
+          if (cfg.stages == 3) return launch_variant<KIND, 256, 3, 2, 1, EPI>(s, sb + 0, ta, tb, tc, tr, p, stream);
+          if (cfg.stages == 4) return launch_variant<KIND, 256, 4, 2, 1, EPI>(s, sb + 1, ta, tb, tc, tr, p, stream);
+          if (cfg.stages == 5) return launch_variant<KIND, 256, 5, 2, 1, EPI>(s, sb + 2, ta, tb, tc, tr, p, stream);
         }
-        return launch_variant<KIND, 256, 6, 2, 1, EPI>(s, vbase + 4, ta, tb, tc, p, stream);
-      case 128: return launch_variant<KIND, 128, 4, 2, 2, EPI>(s, vbase + 5, ta, tb, tc, p, stream);
-      case 64: return launch_variant<KIND, 64, 4, 2, 2, EPI>(s, vbase + 6, ta, tb, tc, p, stream);
+        return launch_variant<KIND, 256, LIN ? 5 : 6, 2, 1, EPI>(s, vbase + 4, ta, tb, tc, tr, p, stream);
+      case 128: return launch_variant<KIND, 128, LIN ? 3 : 4, 2, 2, EPI>(s, vbase + 5, ta, tb, tc, tr, p, stream);
+      case 64: return launch_variant<KIND, 64, 4, 2, 2, EPI>(s, vbase + 6, ta, tb, tc, tr, p, stream);
       default: return GEMM_ERR_INVALID_ARG;
     }
   }
   switch (cfg.bn) {
-    case 256: return launch_variant<KIND, 256, 4, 1, 1, EPI>(s, vbase + 0, ta, tb, tc, p, stream);
-    case 128: return launch_variant<KIND, 128, 3, 1, 2, EPI>(s, vbase + 1, ta, tb, tc, p, stream);
-    case 64: return launch_variant<KIND, 64, 4, 1, 2, EPI>(s, vbase + 2, ta, tb, tc, p, stream);
+    case 256: return launch_variant<KIND, 256, LIN ? 3 : 4, 1, 1, EPI>(s, vbase + 0, ta, tb, tc, tr, p, stream);
+    case 128: return launch_variant<KIND, 128, LIN ? 2 : 3, 1, 2, EPI>(s, vbase + 1, ta, tb, tc, tr, p, stream);
+    case 64: return launch_variant<KIND, 64, 4, 1, 2, EPI>(s, vbase + 2, ta, tb, tc, tr, p, stream);
     case 32:
       if (!epi_out16(EPI) || swap)
-        return launch_variant<KIND, 32, 4, 1, 2, EPI>(s, vbase + 3, ta, tb, tc, p, stream);
+        return launch_variant<KIND, 32, 4, 1, 2, EPI>(s, vbase + 3, ta, tb, tc, tr, p, stream);
       return GEMM_ERR_INVALID_ARG;
     default: return GEMM_ERR_INVALID_ARG;
   }
@@ -1172,12 +1179,12 @@ int check_linear(int M, int N, const void* C, const gemm_epilogue_t* e, const fl
     case GEMM_ACT_GELU: l.act = LIN_ACT_ERF; break;
     case GEMM_ACT_GELU_TANH:  // 2 sqrt(2/pi) (x + 0.044715 x^3)
       l.act = LIN_ACT_GATE;
-      l.gate_a = 1.5957691216057308f;
-      l.gate_b = 0.07135481282635852f;
+      l.gate_a = 1.5957691216057308f * 1.4426950408889634f;
+      l.gate_b = 0.07135481282635852f * 1.4426950408889634f;
       break;
     case GEMM_ACT_SILU:
       l.act = LIN_ACT_GATE;
-      l.gate_a = 1.0f;
+      l.gate_a = 1.4426950408889634f;
       break;
     default: return GEMM_ERR_INVALID_ARG;
   }

@@ -9,8 +9,17 @@
 // Activations.  SiLU is x * s(x) with s the logistic function; the tanh form of GELU is
 // 0.5 x (1 + tanh z) = x * s(2 z), z = sqrt(2/pi) (x + 0.044715 x^3).  Both are therefore
 // x * s(x (a + b x^2)), one body for two constants, with s from one exponential and one division
-// (__expf, __fdividef): the exponential's relative error, about |u| 2^-22 + 2^-22 at argument u, is
-// weighed by s (1 - s), which leaves an absolute error below 1e-6 |x| everywhere.  GELU proper uses erff.
+// (ex2.approx, __fdividef): the exponential's relative error, about |u| 2^-22 + 2^-22 at argument u, is
+// weighed by s (1 - s), which leaves an absolute error below 1e-6 |x| everywhere.  GELU proper takes
+// erfc(z) = t (a1 + t (a2 + ... a5 t^3)) exp(-z^2), t = 1 / (1 + p z), for z >= 0 (Abramowitz and Stegun
+// 7.1.26, error below 1.5e-7) on the side where it is small: 0.5 |x| times that error.
+//
+// In the tile kernels a call of this epilogue meets a chain of latencies, not a throughput: with one
+// wave of tiles the whole of it lies behind the last product.  So it works on 16 columns at a time in a rolled loop
+// (an epilogue unrolled over 64 columns is some 2000 instructions that a CTA with one tile fetches cold, at about
+// ten cycles each), everything it reads is on its way one step ahead, and the residual arrives by the copy engine
+// in the very staging buffer the result leaves from: the residual's block is fetched there, each thread
+// reads its pieces, and writes the result over them.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -28,16 +37,30 @@ struct LinearEpilogue {
   const void* residual;   // element type of C, or null
   long long ldr;          // its row pitch in elements
   int r_vec_ok;           // 1: 16-byte loads along a row are aligned
+  int r_tma;              // 1: the tile kernel fetches it by the copy engine (C goes out the same way)
   int act;                // LinearAct
-  float gate_a, gate_b;   // LIN_ACT_GATE: x * s(x (a + b x^2))
+  float gate_a, gate_b;   // LIN_ACT_GATE: x * s(x (a + b x^2)), times log2 e
 };
 
+__device__ __forceinline__ float lin_exp2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float lin_gate(float x, float a, float b) {
-  const float u = x * fmaf(b * x, x, a);
-  return __fdividef(x, 1.0f + __expf(-u));
+  return __fdividef(x, 1.0f + lin_exp2(-x * fmaf(b * x, x, a)));
 }
 
-__device__ __forceinline__ float lin_erf(float x) { return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f)); }
+__device__ __forceinline__ float lin_erf(float x) {
+  const float z = fabsf(x) * 0.70710678118654752f;
+  const float t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
+  float q = fmaf(t, 1.061405429f, -1.453152027f);
+  q = fmaf(t, q, 1.421413741f);
+  q = fmaf(t, q, -0.284496736f);
+  q = fmaf(t, q, 0.254829592f);
+  const float erfc = q * t * lin_exp2(-1.4426950408889634f * z * z);
+  return 0.5f * x * (x < 0.0f ? erfc : 2.0f - erfc);
+}
 
 __device__ __forceinline__ float lin_activate(float x, const LinearEpilogue& e) {
   switch (e.act) {
@@ -85,13 +108,60 @@ __device__ __forceinline__ void lin_scale_bias(float (&x)[N], bool scaled, float
   }
 }
 
-// Asks the tile's part of a residual row into L2 while the products are still being summed.
+// Exchanged operands (lanes are consecutive elements of a row of C): the warp's 32 x COLS residual
+// values, asked into L2 while the products are still being summed.
+template <int BYTES, int COLS>
+__device__ __forceinline__ void lin_prefetch_transposed(const LinearEpilogue& e, int row0, int col0, int m,
+                                                        int n, int lane) {
+  if (row0 < m)
+    for (int c = col0 + lane; c < min(n, col0 + COLS); c += 32)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(e.residual) +
+                                                    (static_cast<long long>(c) * e.ldr + row0) * BYTES));
+}
+// A thread's part of a residual row, likewise.
 template <int BYTES, int COLS>
 __device__ __forceinline__ void lin_prefetch_row(const LinearEpilogue& e, int row, int col0, int n) {
   const char* at = static_cast<const char*>(e.residual) +
                    (static_cast<long long>(row) * e.ldr + col0) * BYTES;
   const int bytes = min(COLS, n - col0) * BYTES;
   for (int b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + b));
+}
+
+// Where 16-byte pieces of rows are not aligned: a block of 32 rows x COLS elements between global memory
+// and a staging buffer (rows of 128 bytes, 16-byte piece j of row r at j ^ (r & 7)), lanes along the rows.
+template <int BYTES, int COLS, bool TO_GLOBAL>
+__device__ __forceinline__ void lin_block_copy(uint32_t buf, void* global, long long pitch, int row0, int col0,
+                                               int m, int n, int lane) {
+  char* const base = static_cast<char*>(global);
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+#pragma unroll
+    for (int h = 0; h < COLS / 32; ++h) {
+      const int c = h * 32 + lane;
+      if (row0 + r >= m || col0 + c >= n) continue;
+      char* const at = base + (static_cast<long long>(row0 + r) * pitch + col0 + c) * BYTES;
+      const uint32_t s = buf + static_cast<uint32_t>(r * 128 + (((c * BYTES / 16) ^ (r & 7)) << 4) + c * BYTES % 16);
+      if constexpr (BYTES == 4) {
+        uint32_t v;
+        if constexpr (TO_GLOBAL) {
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(s) : "memory");
+          *reinterpret_cast<uint32_t*>(at) = v;
+        } else {
+          asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(at) : "memory");
+          asm volatile("st.shared.u32 [%0], %1;" ::"r"(s), "r"(v) : "memory");
+        }
+      } else {
+        uint16_t v;
+        if constexpr (TO_GLOBAL) {
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(s) : "memory");
+          *reinterpret_cast<uint16_t*>(at) = v;
+        } else {
+          asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(at) : "memory");
+          asm volatile("st.shared.u16 [%0], %1;" ::"r"(s), "h"(v) : "memory");
+        }
+      }
+    }
+  }
 }
 
 // Residual values of one row, columns col .. col + N - 1, as raw words (two halves or one float each).
