@@ -75,7 +75,9 @@ constexpr int AHEAD_WARPS = 4;    // overlapped INT4 pre-pass only: warps 6..9
 constexpr int NUM_THREADS_AHEAD = NUM_THREADS + 32 * AHEAD_WARPS;
 // Linear layers on tiles of 128 or 256 columns: two epilogue warps per lane quarter, taking the staging
 // blocks in turn (one warp per scheduler could not keep pace with K = 4096 int8: 16 k cycles of MMAs
-// per 256 x 256 tile against 1.5-2 k per 16 columns).  Their buffers cost a ring slot.
+// per 256 x 256 tile against 1.5-2 k per 16 columns).  A warp has two staging buffers, one to be filled
+// with the next block's residual, which costs the 256-wide tiles a ring slot; on 128 columns, where a warp has a
+// single block of 16-bit results per tile, one buffer (a slot fewer there: 512 x 4096 x 4096 20.4 -> 24.6 us).
 constexpr int epi_warps(int epi, int bn, int pstages, int csplit) {
   return epi >= 3 && bn >= 128 && pstages == 0 && csplit == 1 ? 8 : EPI_WARPS;
 }
@@ -199,7 +201,8 @@ struct SmemLayout {
   // Epilogue staging: per epilogue warp two buffers of 32 rows x 128 bytes (32 x 32 C values).
   static constexpr int EPI_BUF_BYTES = 32 * 128;
   static constexpr int EPI_OFFSET = RING_BYTES;
-  static constexpr int EPI_BYTES = EPI_W * 2 * EPI_BUF_BYTES;
+  static constexpr int EPI_NBUF = EPI_W == 8 && BN == 128 ? 1 : 2;  // buffers per warp
+  static constexpr int EPI_BYTES = EPI_W * EPI_NBUF * EPI_BUF_BYTES;
   // Cluster split-K: the CTA of cluster rank 0 receives the other CTAs' 128 x BN partial
   // accumulators (32-bit) here, one buffer per sender.
   static constexpr int X_OFFSET = EPI_OFFSET + EPI_BYTES;
@@ -892,7 +895,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     const int quarter = warp & 3;  // TMEM lane quarter this warp may read
     const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
     const uint32_t epi_base =
-        base + L::EPI_OFFSET + static_cast<uint32_t>((warp - 2) * 2 * L::EPI_BUF_BYTES);
+        base + L::EPI_OFFSET + static_cast<uint32_t>((warp - 2) * L::EPI_NBUF * L::EPI_BUF_BYTES);
     const uint64_t pol_c = p.c_evict_first ? ptx::policy_evict_first() : ptx::policy_evict_normal();
     int acc = 0;
     uint32_t acc_phase = 0;
@@ -933,18 +936,21 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         }
       }
     };
-    // The same for 16 columns from 16 * b16.
-    auto add_partial16 = [&](uint32_t (&r)[16], int b16) {
+    // Linear layers: columns per step (8 where the expansion warps leave an epilogue thread 128 registers)
+    constexpr int LIN_W = FUSED ? 8 : 16;
+    // The same for the LIN_W columns of step s.
+    [[maybe_unused]] auto add_partial_step = [&](uint32_t (&r)[LIN_W], int s) {
       if constexpr (CSPLIT > 1) {
 #pragma unroll
         for (int peer = 0; peer < CSPLIT - 1; ++peer) {
           const uint32_t xsrc = base + L::X_OFFSET +
                                 static_cast<uint32_t>(peer * L::X_PEER_BYTES + quarter * (32 * BN * 4) +
-                                                      (b16 >> 1) * 4096 + lane * 128);
+                                                      s * LIN_W / 32 * 4096 + lane * 128);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < LIN_W / 4; ++j) {
             uint32_t u[4];
-            ptx::ld_shared_v4(xsrc + static_cast<uint32_t>(((((b16 & 1) * 4 + j) ^ (lane & 7)) * 16)), u[0], u[1], u[2], u[3]);
+            ptx::ld_shared_v4(xsrc + static_cast<uint32_t>((((s % (32 / LIN_W)) * (LIN_W / 4) + j) ^ (lane & 7)) * 16), u[0],
+                              u[1], u[2], u[3]);
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
               if constexpr (KIND == ptx::KIND_F16)
@@ -960,26 +966,34 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     // One staging block = 32 rows x 128 bytes = 32 columns of 32-bit or 64 columns of 16-bit results.
     constexpr int LIN_COLS = (epi_out16(EPI) && BN >= 64) ? 64 : 32;
     constexpr int LIN_BYTES = epi_out16(EPI) ? 2 : 4;
-    constexpr int LIN_STEPS = LIN_COLS / 16, LIN_SIDES = EPI_W / 4;
+    constexpr int LIN_STEPS = LIN_COLS / LIN_W, LIN_SIDES = EPI_W / 4;
+    constexpr int LIN_PIECES = LIN_W * LIN_BYTES / 16, LIN_WORDS = 4 * LIN_PIECES;  // of a step in a staged row
     [[maybe_unused]] const int lin_side = (warp - 2) / 4;  // which of the quarter's warps
     [[maybe_unused]] const uint32_t res_bar = bar0 + 8u * static_cast<uint32_t>(L::RES_BAR + 2 * (warp - 2));
-    [[maybe_unused]] uint32_t res_phase = 0;   // parity of the two buffers' barriers
-    [[maybe_unused]] bool res_pending = false; // a residual block is on its way
+    constexpr int NBUF = L::EPI_NBUF;
+    [[maybe_unused]] uint32_t res_phase = 0;   // parity of the buffers' barriers
+    [[maybe_unused]] bool res_ahead = false;   // the next block's residual is in its buffer or on its way there
     [[maybe_unused]] float cs_next = 0.0f, cb_next = 0.0f;  // column factors of the next step
-    [[maybe_unused]] uint32_t res_next[4 * LIN_BYTES];      // ... and, with exchanged operands, its residual
-    // The residual's block of 32 rows from (row0, col) into the staging buffer of block number `block`.
+    [[maybe_unused]] uint32_t res_next[LIN_W];              // ... and, with exchanged operands, its residual
+    [[maybe_unused]] auto buf_of = [&](uint32_t block) { return epi_base + (block % NBUF) * static_cast<uint32_t>(L::EPI_BUF_BYTES); };
+    // The residual's block of 32 rows from (row0, col) into the staging buffer of block number `block`, whose
+    // last store has read it.
     [[maybe_unused]] auto lin_fetch_block = [&](uint32_t block, int row0, int col) {
       if (row0 >= p.M || col >= p.N) return;
-      res_pending = true;
-      if (lane == 0) {
-        const uint32_t bar = res_bar + 8u * (block & 1);
+      res_ahead = true;
+      if (!p.lin.r_tma) {
+        __syncwarp();
+        lin_block_copy<LIN_BYTES, LIN_COLS, false>(buf_of(block), const_cast<void*>(p.lin.residual), p.lin.ldr, row0, col, p.M,
+                                                   p.N, lane);
+        __syncwarp();
+      } else if (lane == 0) {
+        const uint32_t bar = res_bar + 8u * (block % NBUF);
         ptx::mbar_arrive_expect_tx(bar, L::EPI_BUF_BYTES);
-        ptx::tma_load_2d(epi_base + static_cast<uint32_t>((block & 1) * L::EPI_BUF_BYTES), &tmap_r, col, row0, bar,
-                         ptx::policy_evict_first());
+        ptx::tma_load_2d(buf_of(block), &tmap_r, col, row0, bar, ptx::policy_evict_first());
       }
     };
     [[maybe_unused]] auto lin_factors = [&](int col) {
-      const int cc = col + (lane & 15);
+      const int cc = col + (lane & (LIN_W - 1));
       cs_next = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
       cb_next = (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;
     };
@@ -990,9 +1004,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       if (!p.lin.residual) return;
       if (p.transpose_c) {
         lin_prefetch_transposed<LIN_BYTES, BN>(p.lin, row0, col0, p.M, p.N, lane);
-        lin_load_residual<LIN_BYTES, 16>(p.lin, row, col, p.M, p.N, 1, res_next);
-      } else if (p.lin.r_tma) {
-        if (lane == 0) ptx::bulk_wait_group_read<1>();  // the store two blocks ago has read the buffer
+        lin_load_transposed<LIN_BYTES>(p.lin, row, col, p.M, p.N, res_next);
+      } else {
+        if (lane == 0) ptx::bulk_wait_group_read<NBUF - 1>();
         lin_fetch_block(staged_blocks, row0, col);
       }
     };
@@ -1093,72 +1107,70 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       static_assert(BN % BLOCK_COLS == 0, "tile width must be a multiple of the store block");
       if constexpr (epi_linear(EPI)) {
         const uint32_t t_acc = tmem_base + lane_base + static_cast<uint32_t>(acc * BN);
-        uint32_t next[16];
-        if (!xpeer) ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>(lin_side * LIN_COLS), next);
+        uint32_t next[LIN_W];
+        if (!xpeer) ptx::tmem_ld_32x32b<LIN_W>(t_acc + static_cast<uint32_t>(lin_side * LIN_COLS), next);
 #pragma unroll 1
         for (int blk = lin_side; blk < BN / LIN_COLS && !xpeer; blk += LIN_SIDES) {
           const int bcol = col0 + blk * LIN_COLS;
-          const uint32_t buf = epi_base + static_cast<uint32_t>((staged_blocks & 1) * L::EPI_BUF_BYTES);
+          const uint32_t buf = buf_of(staged_blocks);
           const uint32_t row_addr = buf + static_cast<uint32_t>(lane * 128);
           const bool from_buf = p.lin.residual && !p.transpose_c;
           if (!p.transpose_c) {
-            if (from_buf && p.lin.r_tma) {
-              if (row0 < p.M && bcol < p.N) {
-                ok = wait_bounded(res_bar + 8u * (staged_blocks & 1), (res_phase >> (staged_blocks & 1)) & 1u, abort_flag,
-                                  p.status, DEV_TIMEOUT_EPILOGUE);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                res_phase ^= 1u << (staged_blocks & 1);
-                res_pending = false;
-              }
-            } else {
-              if (lane == 0) ptx::bulk_wait_group_read<1>();
+            if (!res_ahead) {
+              if (lane == 0) ptx::bulk_wait_group_read<NBUF - 1>();
               __syncwarp();
-              if (from_buf) {
-                lin_block_copy<LIN_BYTES, LIN_COLS, false>(buf, const_cast<void*>(p.lin.residual), p.lin.ldr, row0, bcol,
-                                                           p.M, p.N, lane);
-                __syncwarp();
-              }
+              if (from_buf) lin_fetch_block(staged_blocks, row0, bcol);
             }
+            if (res_ahead && p.lin.r_tma) {
+              ok = wait_bounded(res_bar + 8u * (staged_blocks % NBUF), (res_phase >> (staged_blocks % NBUF)) & 1u, abort_flag,
+                                p.status, DEV_TIMEOUT_EPILOGUE);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              res_phase ^= 1u << (staged_blocks % NBUF);
+            }
+            res_ahead = false;
           }
 #pragma unroll 1
           for (int g = 0; g < LIN_STEPS; ++g) {
-            const int col = bcol + g * 16;
-            const int ahead = g + 1 < LIN_STEPS ? blk * LIN_COLS + (g + 1) * 16 : (blk + LIN_SIDES) * LIN_COLS;
+            const int col = bcol + g * LIN_W;
+            const int ahead = g + 1 < LIN_STEPS ? blk * LIN_COLS + (g + 1) * LIN_W : (blk + LIN_SIDES) * LIN_COLS;
             const float cs_mine = cs_next, cb_mine = cb_next;
-            uint32_t res[4 * LIN_BYTES], r[16];
-            if (from_buf) {
+            uint32_t res[LIN_WORDS], res_t[LIN_W], r[LIN_W];
+            if (p.transpose_c) {
 #pragma unroll
-              for (int j = 0; j < LIN_BYTES; ++j)
-                ptx::ld_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_BYTES + j) ^ (lane & 7)) * 16), res[4 * j],
+              for (int v = 0; v < LIN_W; ++v) res_t[v] = res_next[v];
+            } else if (from_buf) {
+#pragma unroll
+              for (int j = 0; j < LIN_PIECES; ++j)
+                ptx::ld_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_PIECES + j) ^ (lane & 7)) * 16), res[4 * j],
                                   res[4 * j + 1], res[4 * j + 2], res[4 * j + 3]);
-            } else {
-#pragma unroll
-              for (int v = 0; v < 4 * LIN_BYTES; ++v) res[v] = res_next[v];
             }
             ptx::tmem_wait_ld();
 #pragma unroll
-            for (int v = 0; v < 16; ++v) r[v] = next[v];
+            for (int v = 0; v < LIN_W; ++v) r[v] = next[v];
             if (ahead < BN) {
-              ptx::tmem_ld_32x32b_x16(t_acc + static_cast<uint32_t>(ahead), next);
+              ptx::tmem_ld_32x32b<LIN_W>(t_acc + static_cast<uint32_t>(ahead), next);
               lin_factors(col0 + ahead);
               if (p.lin.residual && p.transpose_c)
-                lin_load_residual<LIN_BYTES, 16>(p.lin, row, col0 + ahead, p.M, p.N, 1, res_next);
-              if (from_buf && p.lin.r_tma && g == LIN_STEPS / 2 && blk + LIN_SIDES < BN / LIN_COLS) {
+                lin_load_transposed<LIN_BYTES>(p.lin, row, col0 + ahead, p.M, p.N, res_next);
+              if (NBUF == 2 && from_buf && p.lin.r_tma && g == LIN_STEPS / 2 && blk + LIN_SIDES < BN / LIN_COLS) {
                 if (lane == 0) ptx::bulk_wait_group_read<0>();  // the other buffer's store was issued half a block ago
                 lin_fetch_block(staged_blocks + 1, row0, bcol + LIN_SIDES * LIN_COLS);
               }
             }
-            add_partial16(r, blk * LIN_STEPS + g);
-            float x[16];
+            add_partial_step(r, blk * LIN_STEPS + g);
+            float x[LIN_W];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
+            for (int v = 0; v < LIN_W; ++v) x[v] = acc_to_float<KIND>(fix(r[v]));
             lin_scale_bias(x, KIND == ptx::KIND_I8, rs, cs_mine, rb, cb_mine, p.lin.col_bias != nullptr);
             lin_activate_all(x, p.lin);
-            if (p.lin.residual) lin_add_residual<LIN_BYTES, 16>(x, res);
-            uint32_t w[4 * LIN_BYTES];
+            if (from_buf)
+              lin_add_residual<LIN_BYTES, LIN_W>(x, res);
+            else if (p.lin.residual)
+              lin_add_transposed<LIN_BYTES>(x, res_t);
+            uint32_t w[LIN_WORDS];
 #pragma unroll
-            for (int v = 0; v < 4 * LIN_BYTES; ++v) {
+            for (int v = 0; v < LIN_WORDS; ++v) {
               if constexpr (LIN_BYTES == 2)
                 w[v] = pack_half2(x[2 * v], x[2 * v + 1]);
               else
@@ -1166,12 +1178,12 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             }
             if (!p.transpose_c) {
 #pragma unroll
-              for (int j = 0; j < LIN_BYTES; ++j)
-                ptx::st_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_BYTES + j) ^ (lane & 7)) * 16), w[4 * j],
+              for (int j = 0; j < LIN_PIECES; ++j)
+                ptx::st_shared_v4(row_addr + static_cast<uint32_t>(((g * LIN_PIECES + j) ^ (lane & 7)) * 16), w[4 * j],
                                   w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
             } else if (row < p.M) {
 #pragma unroll
-              for (int v = 0; v < 16; ++v) {
+              for (int v = 0; v < LIN_W; ++v) {
                 if (col + v >= p.N) continue;
                 const size_t at = static_cast<size_t>(row) + static_cast<size_t>(col + v) * static_cast<size_t>(p.ldc);
                 if constexpr (LIN_BYTES == 2)
@@ -1378,9 +1390,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       if (acc == 0) acc_phase ^= 1u;
     }
     if constexpr (epi_linear(EPI)) {
-      if (res_pending) {  // gave up: the residual block on its way must land before the CTA exits
+      if (res_ahead && p.lin.r_tma) {  // gave up: the residual block on its way must land before the CTA exits
         const uint64_t t0 = ptx::globaltimer_ns();
-        while (!ptx::mbar_try_wait(res_bar + 8u * (staged_blocks & 1), (res_phase >> (staged_blocks & 1)) & 1u) &&
+        while (!ptx::mbar_try_wait(res_bar + 8u * (staged_blocks % NBUF), (res_phase >> (staged_blocks % NBUF)) & 1u) &&
                ptx::globaltimer_ns() - t0 < WAIT_LIMIT_NS) {
         }
       }

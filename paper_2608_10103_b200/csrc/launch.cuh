@@ -745,14 +745,14 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
           if (cfg.stages == 5) return launch_variant<KIND, 256, 5, 2, 1, EPI>(s, sb + 2, ta, tb, tc, tr, p, stream);
         }
         return launch_variant<KIND, 256, LIN ? 5 : 6, 2, 1, EPI>(s, vbase + 4, ta, tb, tc, tr, p, stream);
-      case 128: return launch_variant<KIND, 128, LIN ? 3 : 4, 2, 2, EPI>(s, vbase + 5, ta, tb, tc, tr, p, stream);
+      case 128: return launch_variant<KIND, 128, 4, 2, 2, EPI>(s, vbase + 5, ta, tb, tc, tr, p, stream);
       case 64: return launch_variant<KIND, 64, 4, 2, 2, EPI>(s, vbase + 6, ta, tb, tc, tr, p, stream);
       default: return GEMM_ERR_INVALID_ARG;
     }
   }
   switch (cfg.bn) {
     case 256: return launch_variant<KIND, 256, LIN ? 3 : 4, 1, 1, EPI>(s, vbase + 0, ta, tb, tc, tr, p, stream);
-    case 128: return launch_variant<KIND, 128, LIN ? 2 : 3, 1, 2, EPI>(s, vbase + 1, ta, tb, tc, tr, p, stream);
+    case 128: return launch_variant<KIND, 128, 3, 1, 2, EPI>(s, vbase + 1, ta, tb, tc, tr, p, stream);
     case 64: return launch_variant<KIND, 64, 4, 1, 2, EPI>(s, vbase + 2, ta, tb, tc, tr, p, stream);
     case 32:
       if (!epi_out16(EPI) || swap)

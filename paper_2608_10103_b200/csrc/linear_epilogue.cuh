@@ -71,7 +71,7 @@ __device__ __forceinline__ float lin_activate(float x, const LinearEpilogue& e) 
   }
 }
 
-// The same for N values of a thread; the choice is the same for the whole grid.  (N = 16 in the tile
+// The same for N values of a thread; the choice is the same for the whole grid.  (N = 8 or 16 in the tile
 // kernels, in a rolled loop: an epilogue unrolled over 64 columns is some 2000 instructions that a CTA with
 // one tile fetches cold, at about ten cycles each.)
 template <int N>
@@ -125,6 +125,30 @@ __device__ __forceinline__ void lin_prefetch_row(const LinearEpilogue& e, int ro
                    (static_cast<long long>(row) * e.ldr + col0) * BYTES;
   const int bytes = min(COLS, n - col0) * BYTES;
   for (int b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + b));
+}
+
+// N values of one lane of it, one register each (packing them would wait for them).
+template <int BYTES, int N>
+__device__ __forceinline__ void lin_load_transposed(const LinearEpilogue& e, int row, int col, int m, int n,
+                                                    uint32_t (&r)[N]) {
+  const char* const base = static_cast<const char*>(e.residual) + static_cast<long long>(row) * BYTES;
+#pragma unroll
+  for (int v = 0; v < N; ++v) {
+    r[v] = 0;
+    if (row < m && col + v < n) {
+      const char* const at = base + static_cast<long long>(col + v) * e.ldr * BYTES;
+      if constexpr (BYTES == 4)
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(r[v]) : "l"(at) : "memory");
+      else
+        asm volatile("{\n\t.reg .u16 h;\n\tld.global.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(r[v]) : "l"(at) : "memory");
+    }
+  }
+}
+template <int BYTES, int N>
+__device__ __forceinline__ void lin_add_transposed(float (&x)[N], const uint32_t (&r)[N]) {
+#pragma unroll
+  for (int v = 0; v < N; ++v)
+    x[v] += BYTES == 4 ? __uint_as_float(r[v]) : __half2float(__ushort_as_half(static_cast<unsigned short>(r[v])));
 }
 
 // Where 16-byte pieces of rows are not aligned: a block of 32 rows x COLS elements between global memory
