@@ -241,9 +241,41 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
     }
   };
 
+  // Linear layers: scales, bias and residual of the LIN_U elements a thread finishes first are asked for
+  // before a block's products, not one after the other behind them.
+  constexpr int LIN_U = epi_linear(EPI) ? 4 : 1;
+  [[maybe_unused]] float lin_s[LIN_U], lin_l[LIN_U], lin_b[LIN_U];
+  constexpr int LIN_BYTES = EPI == EPI_LIN16 ? 2 : 4;
+  [[maybe_unused]] LinRaw<LIN_BYTES> lin_r[LIN_U];
+  [[maybe_unused]] auto lin_element = [&](int l0, int idx, int& s, int& l) {
+    const bool l_contiguous = p.c_stride_l == 1;
+    s = l_contiguous ? idx / BLOCK_ROWS : idx % (8 * NT);
+    l = l_contiguous ? idx % BLOCK_ROWS : idx / (8 * NT);
+    return idx < 8 * NT * BLOCK_ROWS && s < p.rows_s && l0 + l < p.rows_l;
+  };
+  [[maybe_unused]] auto lin_gather = [&](int l0, int first) {
+#pragma unroll
+    for (int u = 0; u < LIN_U; ++u) {
+      int s, l;
+      lin_s[u] = lin_l[u] = 1.0f;
+      lin_b[u] = 0.0f;
+      lin_r[u] = LinRaw<LIN_BYTES>();
+      if (!lin_element(l0, first + u * threads, s, l)) continue;
+      if constexpr (!F16) {
+        lin_s[u] = ld_f32(p.scale_s + s);
+        lin_l[u] = ld_f32(p.scale_l + l0 + l);
+      }
+      if (p.lin.row_bias) lin_b[u] = ld_f32(p.lin.row_bias + l0 + l);
+      if (p.lin.col_bias) lin_b[u] = ld_f32(p.lin.col_bias + s);
+      if (p.lin.residual)
+        lin_r[u].load(static_cast<const char*>(p.lin.residual) +
+                      (s * p.r_stride_s + static_cast<long long>(l0 + l) * p.r_stride_l) * LIN_BYTES);
+    }
+  };
   int c_slot = 0;
 #pragma unroll 1
   for (int blk = 0; blk < my_blocks; ++blk) {
+    if constexpr (epi_linear(EPI)) lin_gather((static_cast<int>(blockIdx.x) + blk * grid) * BLOCK_ROWS, tid);
     Acc acc[MT][NT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -289,6 +321,28 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
     __syncthreads();
     const int l0 = (static_cast<int>(blockIdx.x) + blk * grid) * BLOCK_ROWS;
     const bool l_contiguous = p.c_stride_l == 1;
+    if constexpr (epi_linear(EPI)) {
+      for (int first = tid; first < 8 * NT * BLOCK_ROWS; first += LIN_U * threads) {
+        if (first != tid) lin_gather(l0, first);
+#pragma unroll
+        for (int u = 0; u < LIN_U; ++u) {
+          int s, l;
+          if (!lin_element(l0, first + u * threads, s, l)) continue;
+          Acc sum = 0;
+          for (int w = 0; w < warps; ++w) sum += red[w * (8 * NT * RED_PITCH) + s * RED_PITCH + l];
+          float x = static_cast<float>(sum);
+          if constexpr (!F16) x = p.scale_s_first ? x * lin_s[u] * lin_l[u] : x * lin_l[u] * lin_s[u];
+          x = lin_activate(x + lin_b[u], p.lin) + lin_r[u].value();
+          const long long at = s * p.c_stride_s + static_cast<long long>(l0 + l) * p.c_stride_l;
+          if constexpr (EPI == EPI_LIN16)
+            static_cast<__half*>(p.C)[at] = __float2half_rn(x);
+          else
+            static_cast<float*>(p.C)[at] = x;
+        }
+      }
+      __syncthreads();  // the sums are read: the next block's may be written
+      continue;
+    }
     for (int idx = tid; idx < 8 * NT * BLOCK_ROWS; idx += threads) {
       // consecutive threads along whichever index is contiguous in C
       const int s = l_contiguous ? idx / BLOCK_ROWS : idx % (8 * NT);
@@ -297,27 +351,7 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
       Acc sum = 0;
       for (int w = 0; w < warps; ++w) sum += red[w * (8 * NT * RED_PITCH) + s * RED_PITCH + l];
       const long long at = s * p.c_stride_s + static_cast<long long>(l0 + l) * p.c_stride_l;
-      if constexpr (epi_linear(EPI)) {
-        float x = static_cast<float>(sum);
-        if constexpr (!F16) {
-          const float fs = ld_f32(p.scale_s + s), fl = ld_f32(p.scale_l + l0 + l);
-          x = p.scale_s_first ? x * fs * fl : x * fl * fs;
-        }
-        if (p.lin.row_bias) x += ld_f32(p.lin.row_bias + l0 + l);
-        if (p.lin.col_bias) x += ld_f32(p.lin.col_bias + s);
-        x = lin_activate(x, p.lin);
-        if (p.lin.residual) {
-          const long long rat = s * p.r_stride_s + static_cast<long long>(l0 + l) * p.r_stride_l;
-          if constexpr (EPI == EPI_LIN16)
-            x += __half2float(*(static_cast<const volatile __half*>(p.lin.residual) + rat));
-          else
-            x += ld_f32(static_cast<const float*>(p.lin.residual) + rat);
-        }
-        if constexpr (EPI == EPI_LIN16)
-          static_cast<__half*>(p.C)[at] = __float2half_rn(x);
-        else
-          static_cast<float*>(p.C)[at] = x;
-      } else if constexpr (EPI == EPI_RAW32) {
+      if constexpr (EPI == EPI_RAW32) {
         static_cast<Acc*>(p.C)[at] = sum;
       } else if constexpr (F16) {
         static_cast<__half*>(p.C)[at] = __float2half_rn(sum);  // EPI_OUT16: rounded once

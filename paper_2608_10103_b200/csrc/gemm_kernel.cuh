@@ -974,7 +974,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
     [[maybe_unused]] uint32_t res_phase = 0;   // parity of the buffers' barriers
     [[maybe_unused]] bool res_ahead = false;   // the next block's residual is in its buffer or on its way there
     [[maybe_unused]] float cs_next = 0.0f, cb_next = 0.0f;  // column factors of the next step
-    [[maybe_unused]] uint32_t res_next[LIN_W];              // ... and, with exchanged operands, its residual
+    [[maybe_unused]] LinRaw<LIN_BYTES> res_next[LIN_W];     // ... and, with exchanged operands, its residual
     [[maybe_unused]] auto buf_of = [&](uint32_t block) { return epi_base + (block % NBUF) * static_cast<uint32_t>(L::EPI_BUF_BYTES); };
     // The residual's block of 32 rows from (row0, col) into the staging buffer of block number `block`, whose
     // last store has read it.
@@ -1135,7 +1135,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
             const int col = bcol + g * LIN_W;
             const int ahead = g + 1 < LIN_STEPS ? blk * LIN_COLS + (g + 1) * LIN_W : (blk + LIN_SIDES) * LIN_COLS;
             const float cs_mine = cs_next, cb_mine = cb_next;
-            uint32_t res[LIN_WORDS], res_t[LIN_W], r[LIN_W];
+            uint32_t res[LIN_WORDS], r[LIN_W];
+            LinRaw<LIN_BYTES> res_t[LIN_W];
             if (p.transpose_c) {
 #pragma unroll
               for (int v = 0; v < LIN_W; ++v) res_t[v] = res_next[v];

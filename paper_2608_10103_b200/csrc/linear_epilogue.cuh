@@ -127,28 +127,37 @@ __device__ __forceinline__ void lin_prefetch_row(const LinearEpilogue& e, int ro
   for (int b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + b));
 }
 
-// N values of one lane of it, one register each (packing them would wait for them).
+// A value as it lies in memory: loaded without the conversion, which would wait for it.
+template <int BYTES>
+struct LinRaw;
+template <>
+struct LinRaw<4> {
+  uint32_t bits = 0;
+  __device__ __forceinline__ void load(const void* at) { asm volatile("ld.global.u32 %0, [%1];" : "=r"(bits) : "l"(at) : "memory"); }
+  __device__ __forceinline__ float value() const { return __uint_as_float(bits); }
+};
+template <>
+struct LinRaw<2> {
+  uint16_t bits = 0;
+  __device__ __forceinline__ void load(const void* at) { asm volatile("ld.global.u16 %0, [%1];" : "=h"(bits) : "l"(at) : "memory"); }
+  __device__ __forceinline__ float value() const { return __half2float(__ushort_as_half(bits)); }
+};
+// N values of one lane of such a block.
 template <int BYTES, int N>
 __device__ __forceinline__ void lin_load_transposed(const LinearEpilogue& e, int row, int col, int m, int n,
-                                                    uint32_t (&r)[N]) {
+                                                    LinRaw<BYTES> (&r)[N]) {
   const char* const base = static_cast<const char*>(e.residual) + static_cast<long long>(row) * BYTES;
 #pragma unroll
   for (int v = 0; v < N; ++v) {
-    r[v] = 0;
-    if (row < m && col + v < n) {
-      const char* const at = base + static_cast<long long>(col + v) * e.ldr * BYTES;
-      if constexpr (BYTES == 4)
-        asm volatile("ld.global.u32 %0, [%1];" : "=r"(r[v]) : "l"(at) : "memory");
-      else
-        asm volatile("{\n\t.reg .u16 h;\n\tld.global.u16 h, [%1];\n\tcvt.u32.u16 %0, h;\n\t}" : "=r"(r[v]) : "l"(at) : "memory");
-    }
+    r[v] = LinRaw<BYTES>();
+    if (row < m && col + v < n) r[v].load(base + static_cast<long long>(col + v) * e.ldr * BYTES);
   }
 }
 template <int BYTES, int N>
-__device__ __forceinline__ void lin_add_transposed(float (&x)[N], const uint32_t (&r)[N]) {
+__device__ __forceinline__ void lin_add_transposed(float (&x)[N], const LinRaw<BYTES> (&r)[N]) {
 #pragma unroll
   for (int v = 0; v < N; ++v)
-    x[v] += BYTES == 4 ? __uint_as_float(r[v]) : __half2float(__ushort_as_half(static_cast<unsigned short>(r[v])));
+    x[v] += r[v].value();
 }
 
 // Where 16-byte pieces of rows are not aligned: a block of 32 rows x COLS elements between global memory
