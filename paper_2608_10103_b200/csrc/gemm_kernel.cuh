@@ -936,8 +936,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         }
       }
     };
-    // Linear layers: columns per step (8 where the expansion warps leave an epilogue thread 128 registers)
-    constexpr int LIN_W = FUSED ? 8 : 16;
+    // Linear layers: columns per step (8 for FP32 results where the expansion warps leave a thread 128 registers: 16 would spill)
+    constexpr int LIN_W = FUSED && EPI == EPI_LIN32 ? 8 : 16;
     // The same for the LIN_W columns of step s.
     [[maybe_unused]] auto add_partial_step = [&](uint32_t (&r)[LIN_W], int s) {
       if constexpr (CSPLIT > 1) {
