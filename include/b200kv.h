@@ -22,9 +22,10 @@
  * are multiples of 8 elements.
  *
  * Lengths, counts and table entries are read on the device.  An entry outside
- * [0, num_pages), or a length that the table cannot hold, is not followed: the
- * call leaves those tokens out and the status word (gemm_last_device_status,
- * gemm_read_device_status) reads 6 afterwards.
+ * [0, num_pages), or a length that the table cannot hold, is not followed: nothing
+ * outside the arrays is read or written, the status word (gemm_last_device_status,
+ * gemm_read_device_status) reads 6 afterwards, and what the call gives for that
+ * sequence is undefined.
  */
 #ifndef B200KV_H_
 #define B200KV_H_

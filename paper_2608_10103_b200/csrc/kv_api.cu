@@ -87,7 +87,7 @@ int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stre
     if (per_sm < 1) return shared_cuda_fail(cudaErrorLaunchOutOfResources);
     resident[dev.device].store(per_sm);
   }
-  p.min_share = 8;
+  p.min_share = 4;
   const int grid = per_sm * dev.num_sms;
   const int rows = 8 * NR;
   const long long most = static_cast<long long>(p.max_q) * p.group;
@@ -130,7 +130,7 @@ int attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stream) {
   KvAttnParams few = p;
   const long long bound = rows < p.split_rows ? rows : p.split_rows;
   // ... and counts its steps of 16 tokens in 32 bits
-  const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1;
+  const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1 + KVA_UNIT_COST;
   if (rows + p.group + 512 >= (1ll << 31) || (bound + 7) / 8 * p.c.heads >= (1ll << 30) / steps / p.batch)
     return GEMM_ERR_TOO_LARGE;
   if (rows > p.split_rows) {

@@ -49,6 +49,10 @@ namespace b200gemm {
 constexpr int KVA_WARPS = 4;
 constexpr int KVA_THREADS = 32 * KVA_WARPS;
 constexpr int KVA_STEP = 16;  // tokens per step
+// What beginning a unit costs a CTA, in steps: the latencies of its q, page ids and first codes and the
+// exchange between the warps, some 8-10 k cycles where four warps take 3 k for four steps.  Without it in the
+// balance the CTAs with several short sequences were a fifth behind the others.
+constexpr int KVA_UNIT_COST = 12;
 
 struct KvAttnParams {
   KvCacheView c;
@@ -78,16 +82,20 @@ struct KvAttnParams {
 struct KvSeq {
   int row0, n, len;
 };
-__device__ __forceinline__ KvSeq kv_seq(const KvAttnParams& p, int b, bool report) {
+__device__ __forceinline__ KvSeq kv_seq_of(const KvAttnParams& p, int row0, int row1, int kv_len, bool report) {
   KvSeq s;
-  s.row0 = kv_ld(p.cu + b);
-  s.n = kv_ld(p.cu + b + 1) - s.row0;
-  s.len = kv_ld(p.kv_len + b);
+  s.row0 = row0;
+  s.n = row1 - row0;
+  s.len = kv_len;
   const int n = s.row0 < 0 ? 0 : min(max(s.n, 0), p.max_q), len = min(max(s.len, 0), p.max_len);
   if (report && (n != s.n || len != s.len)) kv_report(p.status);
   s.n = n;
   s.len = len;
   return s;
+}
+__device__ __forceinline__ KvSeq kv_seq(const KvAttnParams& p, int b, bool report) {
+  const int row0 = kv_ld(p.cu + b), row1 = kv_ld(p.cu + b + 1), len = kv_ld(p.kv_len + b);
+  return kv_seq_of(p, row0, row1, len, report);
 }
 // Tokens [lo, hi) that the queries [i0, i1) of a sequence see between them, lo rounded down to a step.
 __device__ __forceinline__ void kv_visible(const KvAttnParams& p, const KvSeq& s, int i0, int i1,
@@ -172,8 +180,12 @@ __device__ __forceinline__ uint32_t pack_halves(float a, float b) {
 
 }  // namespace kva
 
-// Bytes of one ring slot of a warp: 16 tokens of K and V, and each lane's copy of both scales.
-__host__ __device__ constexpr int kva_slot_bytes(int dim) { return KVA_STEP * 2 * dim + 256; }
+// Where a step's two scales travel: with its codes, a copy per lane (two more requests a step), or by lane, 32
+// pages at a time like the ids (two shuffles).  At 64 d, where a step has six other requests, the latter is
+// 27 % faster (16 x 131071 tokens: 79.5 -> 58 us); at 128 d the former by 2-8 %.
+__host__ __device__ constexpr bool kva_scales_in_ring(int dim) { return dim >= 128; }
+// Bytes of one ring slot of a warp: 16 tokens of K and V, and perhaps each lane's copy of both scales.
+__host__ __device__ constexpr int kva_slot_bytes(int dim) { return KVA_STEP * 2 * dim + (kva_scales_in_ring(dim) ? 256 : 0); }
 __host__ __device__ constexpr int kva_rows_floats(int rows, int dim) { return rows * (dim + 2); }
 // Dynamic shared memory: the rings, reused for the warps' results; Q fragments where they are kept there.
 // Fragments of q: 8 words a thread for 64 d and 8 rows; kept in registers up to 32 of them.
@@ -187,8 +199,10 @@ __host__ __device__ constexpr int kva_smem(int dim, int nr, int depth) {
   const int merge = KVA_WARPS * kva_rows_floats(8 * nr, dim) * 4;
   return (ring > merge ? ring : merge) + kva_q_bytes(dim, nr);
 }
-// CTAs an SM is meant to hold (registers: O takes dim * nr / 4 a thread).
-__host__ __device__ constexpr int kva_ctas(int dim, int nr) { return dim * nr <= 128 ? 4 : dim * nr <= 256 ? 3 : 2; }
+// CTAs an SM is meant to hold (registers: O takes dim * nr / 4 a thread).  At 128 d and 8 rows three with rings of
+// four steps and 168 registers run 2-6 % ahead of four with three steps and 128 (which spill); two CTAs of
+// six or eight warps behind them on long batches (64 x <= 8192 tokens: 127.6, 130.9, 136.9 us).
+__host__ __device__ constexpr int kva_ctas(int dim, int nr) { return dim * nr <= 64 ? 4 : dim * nr <= 256 ? 3 : 2; }
 
 template <int D, int NR, int DEPTH>
 __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_kernel(const KvAttnParams p) {
@@ -201,14 +215,12 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
   constexpr int VW = D == 64 ? 2 : 4;         // words of such a piece
   constexpr int OT = D / 16;                  // tiles of 16 d of the result
   constexpr int SUB = kva_sub(D, NR);
-  constexpr bool Q_REGS = kva_q_in_regs(D, NR);
+  constexpr bool Q_REGS = kva_q_in_regs(D, NR), SCALES_RING = kva_scales_in_ring(D);
   constexpr int SLOT = kva_slot_bytes(D);
   constexpr int PART = kva_rows_floats(ROWS, D);  // floats of a piece in scratch: O, then (m, l) a row
   constexpr int PITCH = D + 2;                    // floats of a row in the warps' exchange: O, m, l
   static_assert(DEPTH % SUB == 0 || SUB == 1 || DEPTH > SUB, "a ring holds the steps that are used together");
   extern __shared__ __align__(16) unsigned char kva_smem_raw[];
-  __shared__ int s_scan[KVA_WARPS];
-  __shared__ int s_find[3];
   __shared__ unsigned s_last;
 
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
@@ -216,85 +228,95 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
   if (tid == 0) ptx::grid_dep_launch_dependents();
   ptx::grid_dep_wait();
 
-  // ---- this CTA's share.  Thread i looks at the sequences [i * chunk, (i + 1) * chunk).
+  // ---- this CTA's share.  Every warp works it out for itself (no barriers): lane i looks at the sequences
+  // [i * chunk, (i + 1) * chunk).
   const int heads = p.c.heads;
   auto tiles_of = [&](const KvSeq& s) { return s.n * p.group > p.split_rows ? 0 : (s.n * p.group + ROWS - 1) / ROWS; };
   auto tile_steps = [&](const KvSeq& s, int qt, int& lo, int& hi) {
-    const int i0 = qt * ROWS / p.group, i1 = min(s.n, ((qt + 1) * ROWS + p.group - 1) / p.group);
+    int i0 = 0, i1 = s.n;
+    if (s.n * p.group > ROWS) {
+      i0 = qt * ROWS / p.group;
+      i1 = min(s.n, ((qt + 1) * ROWS + p.group - 1) / p.group);
+    }
     kv_visible(p, s, i0, i1, lo, hi);
     return kv_steps(lo, hi);
   };
-  // steps (share = 0) or pieces of at most `share` steps of a sequence, all heads and row tiles; units
-  auto seq_weight = [&](int b, int share, int& units) {
-    const KvSeq s = kv_seq(p, b, share == 0 && blockIdx.x == 0);
+  // A unit's weight: its pieces of at most `share` steps (one piece per CTA), or its steps and what beginning
+  // a unit costs besides.
+  int share = 0;
+  bool one_piece = false;
+  auto unit_weight_of = [&](int steps) { return one_piece ? (steps + share - 1) / share : steps + KVA_UNIT_COST; };
+  auto seq_weight = [&](const KvSeq& s, int& units) {  // all heads and row tiles
     int sum = 0, lo, hi;
 #pragma unroll 1
     for (int qt = tiles_of(s) - 1; qt >= 0; --qt) {
-      const int steps = tile_steps(s, qt, lo, hi);
-      sum += share ? (steps + share - 1) / share : steps;
+      sum += unit_weight_of(tile_steps(s, qt, lo, hi));
       ++units;
     }
     return sum * heads;
   };
-  const int chunk = (p.batch + KVA_THREADS - 1) / KVA_THREADS;
-  const int b_first = min(p.batch, tid * chunk), b_last = min(p.batch, b_first + chunk);
-  int share = 0, begin = 0, end = 0, mine = 0, before = 0, total = 0;
-  bool one_piece = false;
+  const int chunk = (p.batch + 31) / 32;
+  const int b_first = min(p.batch, lane * chunk), b_last = min(p.batch, b_first + chunk);
+  int begin = 0, end = 0, mine = 0, before = 0;
   // first pass: steps; second pass, with few units: pieces
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
     int units = 0;
     mine = 0;
 #pragma unroll 1
-    for (int b = b_first; b < b_last; ++b) mine += seq_weight(b, share, units);
+    for (int b = b_first; b < b_last; b += 4) {  // the loads of four sequences in flight together
+      int row[5], len[4];
+#pragma unroll
+      for (int u = 0; u < 5; ++u) row[u] = kv_ld(p.cu + min(b + u, p.batch));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) len[u] = kv_ld(p.kv_len + min(b + u, p.batch - 1));
+#pragma unroll 1
+      for (int u = 0; u < 4; ++u) {
+        if (b + u < b_last)
+          mine += seq_weight(kv_seq_of(p, row[0], row[1], len[0], pass == 0 && blockIdx.x == 0 && warp == 0), units);
+        row[0] = row[1]; row[1] = row[2]; row[2] = row[3]; row[3] = row[4];
+        len[0] = len[1]; len[1] = len[2]; len[2] = len[3];
+      }
+    }
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
-    const int all_units = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(units)));
-    if (lane == 31) {
-      s_scan[warp] = incl;
-      if (warp == 0 && pass == 0) s_find[0] = 0;
-    }
-    __syncthreads();
-    if (lane == 31 && pass == 0) atomicAdd(&s_find[0], all_units);
     before = incl - mine;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < KVA_WARPS; ++w) {
-      if (w < warp) before += s_scan[w];
-      total += s_scan[w];
-    }
-    __syncthreads();
+    const int total = __shfl_sync(0xffffffffu, incl, 31), grid = static_cast<int>(gridDim.x);
     if (pass == 1) {  // one piece per CTA
       begin = static_cast<int>(blockIdx.x);
       end = min(begin + 1, total);
       break;
     }
-    const int n_units = s_find[0] * heads, grid = static_cast<int>(gridDim.x);
     if (total == 0) return;
+    const int n_units = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(units))) * heads;
     one_piece = n_units * 4 <= grid;
-    share = max(p.min_share, (total - 1) / (one_piece ? grid - n_units : grid) + 1);
-    begin = min(static_cast<long long>(share) * blockIdx.x, static_cast<long long>(total));
+    // (few units: their steps without the extra cost, over the CTAs that are not needed for a unit's odd end)
+    share = max(p.min_share, one_piece ? (total - n_units * KVA_UNIT_COST - 1) / (grid - n_units) + 1 : (total - 1) / grid + 1);
+    if (one_piece) continue;
+    begin = static_cast<int>(min(static_cast<long long>(share) * blockIdx.x, static_cast<long long>(total)));
     end = min(begin + share, total);
-    if (!one_piece) break;
+    break;
   }
   if (begin >= end) return;
-  if (begin >= before && begin < before + mine) {  // the sequence that holds it is among this thread's
-    int b = b_first, at = begin - before, units = 0;
+  // the sequence that holds it, and where in that
+  int b = b_first, in_seq = begin - before;
+  const bool here = in_seq >= 0 && in_seq < mine;
+  if (here) {
+    int units = 0;
 #pragma unroll 1
     for (; b + 1 < b_last; ++b) {
-      const int w = seq_weight(b, one_piece ? share : 0, units);
-      if (at < w) break;
-      at -= w;
+      const int w = seq_weight(kv_seq(p, b, false), units);
+      if (in_seq < w) break;
+      in_seq -= w;
     }
-    s_find[1] = b;
-    s_find[2] = at;
   }
-  __syncthreads();
-  int b = s_find[1], in_seq = s_find[2];
+  const int holder = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+  b = __shfl_sync(0xffffffffu, b, holder);
+  in_seq = __shfl_sync(0xffffffffu, in_seq, holder);
 
   unsigned char* const rings = kva_smem_raw + kva_q_bytes(D, NR);
   const uint32_t ring_at = ptx::smem_addr(rings) + static_cast<uint32_t>(warp * DEPTH) * SLOT;
@@ -310,9 +332,10 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
     for (int qt = 0; qt < tiles && at < end; ++qt) {
       int lo, hi;
       const int unit_steps = tile_steps(s, qt, lo, hi);
-      // a unit counts as its pieces or as its steps; `per` steps of it go with one count
-      const int unit_weight = one_piece ? (unit_steps + share - 1) / share : unit_steps;
+      // count c of a unit: its c-th piece of per_count steps, or step c - KVA_UNIT_COST of it
+      const int unit_weight = unit_weight_of(unit_steps);
       const int per_count = one_piece ? (unit_steps + unit_weight - 1) / unit_weight : 1;
+      const int cost = one_piece ? 0 : KVA_UNIT_COST;
       if (in_seq >= unit_weight * heads) {
         in_seq -= unit_weight * heads;
         continue;
@@ -322,7 +345,11 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
 #pragma unroll 1
       for (; head < heads && at < end; ++head, c0 = 0) {
         const int c1 = min(unit_weight, c0 + (end - at));
-        const int s0 = c0 * per_count, s1 = min(unit_steps, c1 * per_count);
+        const int s0 = max(0, c0 - cost) * per_count, s1 = min(unit_steps, max(0, c1 - cost) * per_count);
+        if (cost && s1 == 0) {  // a share that ends inside what beginning the unit costs
+          at += c1 - c0;
+          continue;
+        }
         // ------------------------------------------------ piece: steps [s0, s1) of this unit
         const int row_first = qt * ROWS;  // row = query * group + head in group
         const int rows = min(ROWS, s.n * p.group - row_first);
@@ -334,7 +361,15 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
         const int last_page = (hi - 1) >> p.c.page_shift;  // (nothing visible: below every page)
         int id_first = (lo + w0 * KVA_STEP) >> p.c.page_shift;
         auto load_ids = [&](int first) { return first + lane <= last_page ? kv_ld(table + first + lane) : -1; };
+        // (and the scales of those pages, once their ids are there)
         int ids = load_ids(id_first);
+        [[maybe_unused]] float sks = 0.0f, svs = 0.0f, sks_next = 0.0f, svs_next = 0.0f;
+        [[maybe_unused]] auto load_scales = [&](int id, float& k, float& v) {
+          const bool ok = static_cast<uint32_t>(id) < static_cast<uint32_t>(p.c.num_pages);
+          const long long ph = ok ? static_cast<long long>(id) * heads + head : 0;
+          k = ok ? ptx::ld_global_f32(p.c.scales[0] + ph) : 0.0f;
+          v = ok ? ptx::ld_global_f32(p.c.scales[1] + ph) : 1.0f;
+        };
 
         // q: piece (group of rows, 64 d) i is converted by warp i % KVA_WARPS; its loads go out first
         float krow[NR];
@@ -362,6 +397,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
           }
         }
         int ids_next = load_ids(id_first + 32);
+        [[maybe_unused]] int s_first = id_first;  // the page of lane 0's scales
 
         // copies: one step of 16 tokens = rows g, g + 8 of K and rows 2t, 2t+1, 2t+8, 2t+9 of V
         const uint32_t page_bytes = static_cast<uint32_t>(heads) * p.c.page * D;  // of all heads: below 2^31
@@ -375,6 +411,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
             if (page - id_first >= 32) {
               id_first += 32;
               ids = ids_next;
+              if constexpr (!SCALES_RING) load_scales(ids, sks_next, svs_next);
               ids_next = load_ids(id_first + 32);
             }
             const uint32_t found = static_cast<uint32_t>(__shfl_sync(0xffffffffu, ids, page - id_first));
@@ -384,7 +421,6 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
             const uint32_t id = ok ? found : 0;
             const uint64_t off = static_cast<uint64_t>(id) * page_bytes +
                                  static_cast<uint32_t>((head_row + (tok & (p.c.page - 1))) * D);
-            const uint64_t ph = (static_cast<uint64_t>(id) * static_cast<uint32_t>(heads) + head) * 4;
             const int8_t* const kb = p.c.codes[0] + off + (g * D + t * 16);
             const int8_t* const vb = p.c.codes[1] + off + (2 * t * D + g * (D == 64 ? 8 : 16));
             each<2 * KC>([&](auto i) {
@@ -398,8 +434,11 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
               else
                 cp_async<KP * 512 + i * 512, tr * D + c * 128, 16>(f_at, vb, bytes);
             });
-            cp_async<KVA_STEP * 2 * D - KP * 512, 0, 4>(f_at8, reinterpret_cast<const char*>(p.c.scales[0]) + ph, bytes / 4);
-            cp_async<KVA_STEP * 2 * D - KP * 512 + 4, 0, 4>(f_at8, reinterpret_cast<const char*>(p.c.scales[1]) + ph, bytes / 4);
+            if constexpr (SCALES_RING) {
+              const uint64_t ph = (static_cast<uint64_t>(id) * static_cast<uint32_t>(heads) + head) * 4;
+              cp_async<KVA_STEP * 2 * D - KP * 512, 0, 4>(f_at8, reinterpret_cast<const char*>(p.c.scales[0]) + ph, bytes / 4);
+              cp_async<KVA_STEP * 2 * D - KP * 512 + 4, 0, 4>(f_at8, reinterpret_cast<const char*>(p.c.scales[1]) + ph, bytes / 4);
+            }
             ++f_step;
             const bool wrap = ++f_slot == DEPTH;
             f_slot = wrap ? 0 : f_slot;
@@ -411,6 +450,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
         };
 #pragma unroll 1
         for (int d = 0; d < DEPTH; ++d) fetch();
+        if constexpr (!SCALES_RING) load_scales(ids, sks, svs);  // (the ring spans fewer than 32 pages: these are still the first ones)
 
         // q as 254 q1 + q2 times a scale per row, in the d order of K's pieces
 #pragma unroll
@@ -514,16 +554,31 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
 #pragma unroll
                 for (int v = 0; v < 2; ++v)  // |254 q1 + q2| |k| D <= 32385 * 127 * 256 < 2^31
                   sc[sub][n][j][v] = static_cast<float>(sum[n][j][v] * 254 + sum[n][j][v + 2]);
-            uint32_t sk_bits, sv_bits;
-            lds_v2<KVA_STEP * 2 * D - KP * 512>(at8[sub], sk_bits, sv_bits);
             const bool dead = st + sub >= w1;  // the odd step out: nothing was fetched for it
-            float sv = __uint_as_float(sv_bits);
-            if (dead) sv = 1.0f;
+            const int tok0 = lo + (st + sub) * KVA_STEP;
+            float sv;
+            if constexpr (SCALES_RING) {
+              uint32_t sk_bits, sv_bits;
+              lds_v2<KVA_STEP * 2 * D - KP * 512>(at8[sub], sk_bits, sv_bits);
+              kk[sub] = __uint_as_float(sk_bits);
+              sv = __uint_as_float(sv_bits);
+            } else {
+              const int page = tok0 >> p.c.page_shift;
+              if (page - s_first >= 32) {  // the copies are ahead of this: the next 32 pages' scales are there
+                s_first += 32;
+                sks = sks_next;
+                svs = svs_next;
+              }
+              kk[sub] = __shfl_sync(0xffffffffu, sks, page - s_first);
+              sv = __shfl_sync(0xffffffffu, svs, page - s_first);
+            }
+            if (dead) {
+              kk[sub] = 0.0f;
+              sv = 1.0f;
+            }
             if (sv == 0.0f) sv = 1e-30f;  // a page of zeros: its codes are 0, its tokens still count in l
-            kk[sub] = dead ? 0.0f : __uint_as_float(sk_bits);
             lsv[sub] = __log2f(sv);
             inv_sv[sub] = __fdividef(1.0f, sv);
-            const int tok0 = lo + (st + sub) * KVA_STEP;
             masked |= dead || tok0 + KVA_STEP - 1 > all_hi || tok0 < all_lo;
           });
           if (masked) {
@@ -677,9 +732,9 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
             c_first = static_cast<int>(blockIdx.x) - c0;
             c_last = c_first + unit_weight - 1;
           } else {
-            const int u_begin = at - c0;
-            c_first = u_begin / share;
-            c_last = (u_begin + unit_steps - 1) / share;
+            const int u_begin = at - c0;  // of the unit; its first step counts `cost` later
+            c_first = (u_begin + cost) / share;
+            c_last = (u_begin + unit_weight - 1) / share;
             second = u_begin > share * c_first;
           }
           unsigned* const counter = p.arrived + (static_cast<long long>(b) * p.max_tiles + qt) * heads + head;
@@ -695,7 +750,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
               return p.partial + (2ll * (c_first + c) + (c == 0 && second ? 1 : 0)) * PART;
             };
             // weights of the pieces, JOIN of them at a time: [row][piece], and what their sum of l comes to
-            constexpr int JOIN = 64;
+            constexpr int JOIN = 128;
             constexpr int ACC = (ROWS * D / 4 + KVA_THREADS - 1) / KVA_THREADS;
             float4 acc[ACC];
 #pragma unroll
@@ -744,15 +799,25 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
                 if (r >= rows) continue;
                 const float f = state[4 * r + 2];
                 acc[a].x *= f; acc[a].y *= f; acc[a].z *= f; acc[a].w *= f;
-#pragma unroll 8
-                for (int c = 0; c < count; ++c) {
-                  const float4 x = __ldcg(reinterpret_cast<const float4*>(piece_at(first + c) + r * D + d));
-                  const float w = weight[r * JOIN + c];
-                  acc[a].x = fmaf(x.x, w, acc[a].x);
-                  acc[a].y = fmaf(x.y, w, acc[a].y);
-                  acc[a].z = fmaf(x.z, w, acc[a].z);
-                  acc[a].w = fmaf(x.w, w, acc[a].w);
-                }
+                // (weights beyond the last piece are 0)
+                auto add = [&](int c0, auto batch) {
+                  float4 x[batch];
+#pragma unroll
+                  for (int u = 0; u < batch; ++u)
+                    x[u] = __ldcg(reinterpret_cast<const float4*>(piece_at(first + min(c0 + u, count - 1)) + r * D + d));
+#pragma unroll
+                  for (int u = 0; u < batch; ++u) {
+                    const float w = weight[r * JOIN + c0 + u];
+                    acc[a].x = fmaf(x[u].x, w, acc[a].x);
+                    acc[a].y = fmaf(x[u].y, w, acc[a].y);
+                    acc[a].z = fmaf(x[u].z, w, acc[a].z);
+                    acc[a].w = fmaf(x[u].w, w, acc[a].w);
+                  }
+                };
+                int c0 = 0;
+#pragma unroll 1
+                for (; count - c0 > 8; c0 += 16) add(c0, Index<16>{});
+                if (c0 < count) add(c0, Index<8>{});
               }
             }
 #pragma unroll
