@@ -13,7 +13,7 @@
 // What bounds it: at 128 d, 1024 cycles of tensor pipe a tile pair of 128 x 128 against as many of exponentials
 // (16 a cycle and SM); the conversion takes a tenth of the issue slots.  O is rescaled in tensor memory only
 // when a row's maximum has grown by 2^8 (see kv_attention.cuh), so that it need not pass through registers.
-// Tiles of rows are launched with the longest of every sequence first.
+// Tiles of rows are taken longest first.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -54,8 +54,76 @@ struct KvTileShape {
   static_assert(O_COLUMN + QT * D <= 512, "tensor memory");
 };
 
+// The rank-th longest row tile of all sequences (sequence, tile), or (-1, 0) beyond the last: CTAs start in order,
+// and a long one that starts last leaves the rest of the chip idle (2 x 2048 queries over 8192 and 3130 tokens:
+// 358 -> 326 us).  A row tile's length is its number of token tiles (without a window; with one they are much
+// alike).  By one warp, a lane per sequence, searching for the length that `rank` tiles exceed.
+template <int ROWS, int TN>
+__device__ __noinline__ int2 kvt_item(const KvAttnParams& p, int rank) {
+  const int lane = static_cast<int>(threadIdx.x) & 31;
+  auto tiles_of = [&](const KvSeq& s) { return s.n * p.group <= p.split_rows ? 0 : (s.n * p.group + ROWS - 1) / ROWS; };
+  if (p.batch == 1) {  // its own order
+    const int tiles = tiles_of(kv_seq(p, 0, rank == 0 && lane == 0));
+    return rank < tiles ? make_int2(0, tiles - 1 - rank) : make_int2(-1, 0);
+  }
+  // row tiles of a sequence that are at least x token tiles long: their last query sees beyond (x - 1) TN
+  auto long_tiles = [&](const KvSeq& s, int x) {
+    const int all = tiles_of(s), need = (x - 1) * TN - (s.len - s.n);  // first query that sees so far
+    if (x <= 0 || need <= 0) return all;
+    return need < s.n ? all - static_cast<int>(static_cast<long long>(need) * p.group / ROWS) : 0;
+  };
+  int longest = 0, all = 0;
+  for (int i = lane; i < p.batch; i += 32) {
+    const KvSeq s = kv_seq(p, i, rank == 0);
+    longest = max(longest, (s.len + TN - 1) / TN);
+    all += tiles_of(s);
+  }
+  longest = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(longest)));
+  all = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(all)));
+  if (rank >= all) return make_int2(-1, 0);
+  int x_lo = 0, x_hi = longest + 1, beyond = 0;  // more than rank tiles are x_lo long, `beyond` <= rank are x_hi long
+#pragma unroll 1
+  while (x_hi - x_lo > 1) {
+    const int mid = (x_lo + x_hi) / 2;
+    int c = 0;
+    for (int i = lane; i < p.batch; i += 32) c += long_tiles(kv_seq(p, i, false), mid);
+    c = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
+    if (c > rank) {
+      x_lo = mid;
+    } else {
+      x_hi = mid;
+      beyond = c;
+    }
+  }
+  // the tiles of exactly that length, by sequence
+  int left = rank - beyond;
+#pragma unroll 1
+  for (int i0 = 0; i0 < p.batch; i0 += 32) {
+    int same = 0, qt = 0;
+    if (i0 + lane < p.batch) {
+      const KvSeq s = kv_seq(p, i0 + lane, false);
+      const int longer = long_tiles(s, x_hi);
+      same = long_tiles(s, x_lo) - longer;
+      qt = tiles_of(s) - 1 - longer;  // its longest tile of that length
+    }
+    int incl = same;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const unsigned holds = __ballot_sync(0xffffffffu, left < incl);
+    if (holds) {
+      const int from = __ffs(holds) - 1;
+      return make_int2(i0 + from, __shfl_sync(0xffffffffu, qt - (left - (incl - same)), from));
+    }
+    left -= __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return make_int2(-1, 0);  // (not reached: the tiles of that length are `rank - beyond` and more)
+}
+
 template <int D>
-__global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles_kernel(const KvAttnParams p) {
+__global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1)
+kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   using namespace kva;
   using T = KvTileShape<D>;
   constexpr int QT = T::QT, TN = T::TN, GROUPS = T::GROUPS, STAGES = T::STAGES;
@@ -83,16 +151,23 @@ __global__ void __launch_bounds__(KvTileShape<D>::THREADS, 1) kv_attention_tiles
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
   if (tid == 0) ptx::grid_dep_launch_dependents();
 
-  // ---- what this CTA works on: the longest row tile of every (sequence, head) first
+  // ---- what this CTA works on
   ptx::grid_dep_wait();
   const int heads = p.c.heads;
-  const int per_tile = heads * p.batch;
-  const int nth = static_cast<int>(blockIdx.x) / per_tile, rest = static_cast<int>(blockIdx.x) - nth * per_tile;
-  const int b = rest / heads, head = rest - b * heads;
-  const KvSeq s = kv_seq(p, b, tid == 0 && nth == 0 && head == 0);
+  const int rank = static_cast<int>(blockIdx.x) / heads, head = static_cast<int>(blockIdx.x) - rank * heads;
+  __shared__ int s_item[2];
+  if (warp == 0) {
+    const int2 item = kvt_item<T::ROWS, TN>(p, rank);
+    if (lane == 0) {
+      s_item[0] = item.x;
+      s_item[1] = item.y;
+    }
+  }
+  __syncthreads();
+  const int b = s_item[0], qt = s_item[1];
+  if (b < 0) return;
+  const KvSeq s = kv_seq(p, b, false);
   const int all_rows = s.n * p.group;
-  const int qt = (all_rows + T::ROWS - 1) / T::ROWS - 1 - nth;
-  if (all_rows <= p.split_rows || qt < 0) return;
   const int row_first = qt * T::ROWS, rows = min(T::ROWS, all_rows - row_first);
   const int active = QT == 2 && rows > 128 ? 2 : 1;  // row tiles with a row in them
   int lo, hi;
