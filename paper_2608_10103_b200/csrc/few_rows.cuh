@@ -340,10 +340,9 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
             static_cast<float*>(p.C)[at] = x;
         }
       }
-      __syncthreads();  // the sums are read: the next block's may be written
-      continue;
     }
-    for (int idx = tid; idx < 8 * NT * BLOCK_ROWS; idx += threads) {
+    const int rest = epi_linear(EPI) ? 0 : 8 * NT * BLOCK_ROWS;
+    for (int idx = tid; idx < rest; idx += threads) {
       // consecutive threads along whichever index is contiguous in C
       const int s = l_contiguous ? idx / BLOCK_ROWS : idx % (8 * NT);
       const int l = l_contiguous ? idx % BLOCK_ROWS : idx / (8 * NT);
@@ -351,7 +350,9 @@ __global__ void __launch_bounds__(512) few_rows_kernel(const FewRowsParams p) {
       Acc sum = 0;
       for (int w = 0; w < warps; ++w) sum += red[w * (8 * NT * RED_PITCH) + s * RED_PITCH + l];
       const long long at = s * p.c_stride_s + static_cast<long long>(l0 + l) * p.c_stride_l;
-      if constexpr (EPI == EPI_RAW32) {
+      if constexpr (epi_linear(EPI)) {
+        // done above
+      } else if constexpr (EPI == EPI_RAW32) {
         static_cast<Acc*>(p.C)[at] = sum;
       } else if constexpr (F16) {
         static_cast<__half*>(p.C)[at] = __float2half_rn(sum);  // EPI_OUT16: rounded once

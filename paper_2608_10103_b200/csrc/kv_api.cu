@@ -107,7 +107,7 @@ int launch_attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stre
 
 // Sequences with more than p.split_rows rows, on the tensor cores.
 template <int D>
-int launch_attention_tiles(const SharedDevice& dev, const KvAttnParams& p, cudaStream_t stream) {
+int launch_attention_tiles(const SharedDevice& dev, KvAttnParams p, cudaStream_t stream) {
   static std::atomic<bool> ready[MAX_DEV];
   using T = KvTileShape<D>;
   auto kernel = kv_attention_tiles_kernel<D>;
@@ -119,7 +119,26 @@ int launch_attention_tiles(const SharedDevice& dev, const KvAttnParams& p, cudaS
   const long long tiles = (static_cast<long long>(p.max_q) * p.group + T::ROWS - 1) / T::ROWS;
   const long long blocks = tiles * p.c.heads * p.batch;
   if (blocks > 0x7fffffffll) return GEMM_ERR_TOO_LARGE;
-  return launch(dev, kernel, dim3(static_cast<unsigned>(blocks)), T::THREADS, T::DYN_BYTES, stream, p);
+  // Fewer row tiles than half the SMs: as many parts of their tokens as fill the chip, two token tiles each if
+  // sequences are as long as their tables allow, sixteen at most (what is joined grows with them).
+  p.splits = 1;
+  if (2 * blocks <= dev.num_sms) {
+    long long most = dev.num_sms / blocks;
+    if (most > p.max_len / (2 * T::TN)) most = p.max_len / (2 * T::TN);
+    if (most > 16) most = 16;
+    if (most > 1) p.splits = static_cast<int>(most);
+  }
+  if (p.splits == 1)
+    return launch(dev, kernel, dim3(static_cast<unsigned>(blocks)), T::THREADS, T::DYN_BYTES, stream, p);
+  SharedLease lease;
+  const int rc = shared_scratch(dev.device, stream, static_cast<size_t>(blocks) * p.splits * T::ROWS * (D + 4) * 4,
+                                (static_cast<size_t>(blocks) * 4 + 255) / 256 * 256, &lease);
+  if (rc != GEMM_OK) return rc;
+  p.arrived = static_cast<unsigned*>(lease.head);
+  p.partial = static_cast<float*>(lease.data);
+  const int launched = launch(dev, kernel, dim3(static_cast<unsigned>(blocks * p.splits)), T::THREADS, T::DYN_BYTES, stream, p);
+  const int done = shared_scratch_done(dev.device, stream, lease);
+  return launched != GEMM_OK ? launched : done;
 }
 
 template <int D, int MAX_NR>

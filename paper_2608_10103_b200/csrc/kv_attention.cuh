@@ -76,6 +76,7 @@ struct KvAttnParams {
   int max_tiles;     // row tiles of a sequence at most
   float* partial;    // [2 * grid][rows * D + rows * 2]
   unsigned* arrived; // per unit, zero before and after
+  int splits;        // tile kernel: CTAs a row tile's tokens are divided over
 };
 
 // A sequence's rows and length, cut to what the table and the caller's bound allow.

@@ -121,6 +121,25 @@ def test_long_single_sequence(L):
     check([L], [4], 8, 8, 64, 16, seed=4)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("lens,news,q_heads,kv_heads", [
+    ([9000], [40], 4, 1), ([5000, 100, 4096], [70, 33, 300], 4, 2), ([20000, 3], [17, 1], 8, 1)])
+def test_chunks_over_long_sequences(dim, lens, news, q_heads, kv_heads):
+    """Few row tiles: their tokens are divided over CTAs; and a window that leaves most parts nothing."""
+    check(lens, news, q_heads, kv_heads, dim, 64, seed=7)
+    check(lens, news, q_heads, kv_heads, dim, 16, window=300, seed=8)
+
+
+def test_chunks_of_many_sequences():
+    """Row tiles of sequences of all lengths, longest first, beside sequences of single tokens."""
+    g = np.random.default_rng(11)
+    news = [int(x) for x in g.integers(0, 130, 45)]
+    lens = [n + int(x) for n, x in zip(news, g.integers(0, 1500, 45))]
+    news[7], news[20] = 1, 1
+    check(lens, news, 4, 1, 64, 16)
+    check(lens, news, 4, 4, 128, 32, window=77)
+
+
 def test_many_sequences():
     g = np.random.default_rng(5)
     lens = [int(x) for x in g.integers(0, 900, 300)]
