@@ -93,6 +93,16 @@ enum EpiMode {
   EPI_LIN32 = 4,       // ... as FP32
 };
 __host__ __device__ constexpr bool epi_linear(int epi) { return epi >= EPI_LIN16; }
+// FP32 results of FP16 linear layers are summed in parts of ACC_PART_BYTES of K.  The tensor core's FP32
+// accumulator drops the bits that do not fit instead of rounding, so the error grows with the length of the chain
+// and has one sign: 1.2e-9 K of the result's norm, 1.9e-5 at K = 16408, where a rounded FP32 sum leaves 2e-6.  A
+// tile's first part stays in one accumulator buffer, each later one goes to the other, and the epilogue adds it to
+// the first in FP32: 2.5e-6 however long K is, for 3-4 % of the time (4096 x 4096 x 4096: 102 -> 105 us, K = 16384:
+// 392 -> 409).  (Binary16 results, 2.4e-4 by their own rounding, need none of it.)
+constexpr int ACC_PART_BYTES = 4096;
+__host__ __device__ constexpr int acc_part_atoms(int kind, int epi) {
+  return kind == ptx::KIND_F16 && epi == EPI_LIN32 ? ACC_PART_BYTES / BK_BYTES : 0;
+}
 __host__ __device__ constexpr bool epi_out16(int epi) { return epi == EPI_OUT16 || epi == EPI_LIN16; }
 
 struct GemmParams {
@@ -281,6 +291,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   constexpr int BK_ELEMS = BK_BYTES / ELEM_BYTES;
   constexpr int TILE_M = BM * CTA_GROUP;
   constexpr uint32_t TMEM_COLS = (2 * BN <= 32) ? 32 : 2 * BN;  // two accumulator buffers
+  // Ring slots after which FP32 results of FP16 linear layers change accumulators (0: never).
+  constexpr int ACC_PART = acc_part_atoms(KIND, EPI) / KB;
   static_assert(CTA_GROUP == 1 || CTA_GROUP == 2, "CTA_GROUP is 1 or 2");
   static_assert(BN % 32 == 0 && BN >= 32 && BN <= 256, "BN must be a multiple of 32 up to 256");
   static_assert((TMEM_COLS & (TMEM_COLS - 1)) == 0 && TMEM_COLS <= 512, "TMEM columns: power of 2");
@@ -582,23 +594,47 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       int stage = 0;
       uint32_t phase = 0;
       int acc = 0;
-      uint32_t acc_phase = 0;
+      uint32_t acc_phase = 0;  // bit a: parity of buffer a's next use
       int astage = 0;          // hybrid fused INT4: the ring of A atoms
       uint32_t aphase = 0;
       bool ok = true;
       long long wait_full = 0, wait_acc = 0, t_issue = 0, t_commit = 0, wait_a = 0;
       for (int t = first_tile; t < num_tiles && ok; t += tile_stride) {
         const long long w0 = trace ? clock64() : 0;
-        ok = wait_bounded(acc_empty_bar(acc), acc_phase ^ 1u, abort_flag, p.status,
+        ok = wait_bounded(acc_empty_bar(acc), ((acc_phase >> acc) & 1u) ^ 1u, abort_flag, p.status,
                           DEV_TIMEOUT_MMA);
         if (trace) wait_acc += clock64() - w0;
         if (!ok) break;
         ptx::tc_fence_after_sync();
-        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
+        uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
         int tile, k_begin, k_end;
         bool add;
         decode_unit(t, tile, k_begin, k_end, add);
+        const int first_acc = acc;
+        auto commit_acc = [&]() {
+          if (elected) {
+            if constexpr (CTA_GROUP == 1) {
+              ptx::mma_commit<1>(acc_full_bar(acc));
+            } else {
+              ptx::mma_commit_pair(acc_full_bar(acc), 0x3);
+            }
+          }
+          acc_phase ^= 1u << acc;
+        };
+        int part_begin = k_begin;
         for (int ks = k_begin; ks < k_end; ++ks) {
+          if constexpr (ACC_PART > 0) {
+            if (ks == part_begin + ACC_PART) {  // the next part: into the other buffer, once its last one is added
+              commit_acc();
+              acc = first_acc ^ 1;
+              ok = wait_bounded(acc_empty_bar(acc), ((acc_phase >> acc) & 1u) ^ 1u, abort_flag, p.status,
+                                DEV_TIMEOUT_MMA);
+              if (!ok) break;
+              ptx::tc_fence_after_sync();
+              d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
+              part_begin = ks;
+            }
+          }
           const long long w1 = trace ? clock64() : 0;
           if constexpr (FUSED) {
             ok = wait_bounded(ready_bar(stage), phase, abort_flag, p.status, DEV_TIMEOUT_MMA);
@@ -631,7 +667,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
                 const uint64_t b_step =
                     static_cast<uint64_t>((a * L::B_BYTES + kk * MMA_K_BYTES) >> 4);
                 ptx::mma_ss<KIND, CTA_GROUP>(d_tmem, a_desc + a_step, b_desc + b_step, idesc,
-                                             (ks > k_begin || a > 0 || kk > 0) ? 1u : 0u);
+                                             (ks > part_begin || a > 0 || kk > 0) ? 1u : 0u);
               }
             }
           }
@@ -653,15 +689,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           }
         }
         if (!ok) break;
-        if (elected) {
-          if constexpr (CTA_GROUP == 1) {
-            ptx::mma_commit<1>(acc_full_bar(acc));
-          } else {
-            ptx::mma_commit_pair(acc_full_bar(acc), 0x3);
-          }
-        }
-        acc ^= 1;
-        if (acc == 0) acc_phase ^= 1u;
+        commit_acc();
+        acc = first_acc ^ 1;
       }
       if (trace && elected) {
         trace[TRACE_MMA_WAIT_FULL] = static_cast<unsigned long long>(wait_full);
@@ -898,7 +927,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         base + L::EPI_OFFSET + static_cast<uint32_t>((warp - 2) * L::EPI_NBUF * L::EPI_BUF_BYTES);
     const uint64_t pol_c = p.c_evict_first ? ptx::policy_evict_first() : ptx::policy_evict_normal();
     int acc = 0;
-    uint32_t acc_phase = 0;
+    uint32_t acc_phase = 0;  // bit a: parity of buffer a's next use
     bool ok = true;
     long long epi_wait = 0, epi_busy = 0, tiles_done = 0;
     uint32_t staged_blocks = 0;  // blocks sent through the staging buffers so far
@@ -1010,6 +1039,22 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         lin_fetch_block(staged_blocks, row0, col);
       }
     };
+    // Hand accumulator buffer a back to the (leader's) MMA issuer.
+    auto release_acc = [&](int a) {
+      ptx::tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if constexpr (CTA_GROUP == 1) {
+          ptx::mbar_arrive(acc_empty_bar(a));
+        } else {
+          // CTA-scope release on the leader's barrier: the accumulator reads above are complete
+          // (tcgen05.wait::ld) and ordered by the tcgen05 fence; nothing else has to be made
+          // visible cluster-wide, and a cluster-scope release would stall this lane for
+          // hundreds of cycles per tile.
+          ptx::mbar_arrive_remote(ptx::map_to_cta(acc_empty_bar(a), 0));
+        }
+      }
+    };
     for (int t = first_tile; t < num_tiles && ok; t += tile_stride) {
       int tm, tn, tile, k_begin, k_end;
       bool add;
@@ -1042,13 +1087,38 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         }
       }
       const long long w0 = trace ? clock64() : 0;
-      ok = wait_bounded<true>(acc_full_bar(acc), acc_phase, abort_flag, p.status,
+      ok = wait_bounded<true>(acc_full_bar(acc), (acc_phase >> acc) & 1u, abort_flag, p.status,
                               DEV_TIMEOUT_EPILOGUE, (ablate & 4) ? 500u : 0u);
       ok = __all_sync(0xffffffffu, ok);
       const long long w1 = trace ? clock64() : 0;
       epi_wait += w1 - w0;
       if (!ok) break;
       ptx::tc_fence_after_sync();
+      if constexpr (ACC_PART > 0) {  // the later parts of K: add each to the first, in the columns this warp reads below
+        for (int ks = k_begin + ACC_PART; ks < k_end; ks += ACC_PART) {
+          const int part = acc ^ 1;
+          ok = wait_bounded<true>(acc_full_bar(part), (acc_phase >> part) & 1u, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const uint32_t t_sum = tmem_base + lane_base + static_cast<uint32_t>(acc * BN);
+          const uint32_t t_part = tmem_base + lane_base + static_cast<uint32_t>(part * BN);
+#pragma unroll 1
+          for (int c = lin_side * LIN_COLS; c < BN; c += LIN_SIDES * LIN_COLS) {
+            uint32_t x[32], y[32];
+            ptx::tmem_ld_32x32b_x32(t_sum + static_cast<uint32_t>(c), x);
+            ptx::tmem_ld_32x32b_x32(t_part + static_cast<uint32_t>(c), y);
+            ptx::tmem_wait_ld();
+#pragma unroll
+            for (int v = 0; v < 32; ++v) x[v] = __float_as_uint(__uint_as_float(x[v]) + __uint_as_float(y[v]));
+            ptx::tmem_st_32x32b_x32(t_sum + static_cast<uint32_t>(c), x);
+          }
+          ptx::tmem_wait_st();
+          release_acc(part);
+          acc_phase ^= 1u << part;
+        }
+        if (!ok) break;
+      }
       if constexpr (CSPLIT > 1) {
         if (xpeer) {
           // Ranks 1..: write this tile's raw 32-bit accumulators (one 128-byte row piece per
@@ -1371,24 +1441,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
           }
         }
       }
-      // Hand the accumulator buffer back to the (leader's) MMA issuer.
-      ptx::tc_fence_before_sync();
-      __syncwarp();
-      if (lane == 0) {
-        if constexpr (CTA_GROUP == 1) {
-          ptx::mbar_arrive(acc_empty_bar(acc));
-        } else {
-          // CTA-scope release on the leader's barrier: the accumulator reads above are complete
-          // (tcgen05.wait::ld) and ordered by the tcgen05 fence; nothing else has to be made
-          // visible cluster-wide, and a cluster-scope release would stall this lane for
-          // hundreds of cycles per tile.
-          ptx::mbar_arrive_remote(ptx::map_to_cta(acc_empty_bar(acc), 0));
-        }
-      }
+      release_acc(acc);
       if (trace) epi_busy += clock64() - w1;
       ++tiles_done;
+      acc_phase ^= 1u << acc;
       acc ^= 1;
-      if (acc == 0) acc_phase ^= 1u;
     }
     if constexpr (epi_linear(EPI)) {
       if (res_ahead && p.lin.r_tma) {  // gave up: the residual block on its way must land before the CTA exits

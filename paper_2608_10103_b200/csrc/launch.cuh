@@ -494,7 +494,9 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   }
 
   // (a call that asks for the overlapped INT4 pre-pass stays on the kernel that has that role)
-  const bool wide = !req && wide_wanted(cfg, M, N, k_blocks, s->num_sms, swap, csplit, packed_s4,
+  // (the wide kernel's two accumulators fill TMEM: K that is summed in parts stays on the other tiles)
+  constexpr int PART = acc_part_atoms(KIND, EPI);
+  const bool wide = !req && (PART == 0 || k_blocks <= PART) && wide_wanted(cfg, M, N, k_blocks, s->num_sms, swap, csplit, packed_s4,
                                         KIND == ptx::KIND_F16);
   if (wide) {
     cfg.bn = WIDE_BN;

@@ -280,3 +280,24 @@ def test_quantize_rows_not_finite(bad):
         y = (binding.gemm_s8_linear if prec == "s8" else binding.gemm_s4_linear)(
             q, w, s, torch.ones(40, device="cuda"))
         assert torch.isnan(y[2]).all() and torch.isfinite(y[[0, 1, 3, 4, 5]]).all()
+
+
+# Long sums, FP32 results: parts of 2048 products are 128 accumulations, each cutting off 0.72 units of 2^-24 of an
+# accumulator that has on average 2/3 of its final size: 128 * 0.72 * 2/3 * 2^-24 = 3.7e-6 of the result's norm, plus
+# the rounded sums of up to nine parts (1e-6).  (One chain over all of K = 16408 would leave 3e-5.)
+@pytest.mark.parametrize("M,N,K", [(1, 640, 16400), (8, 4096, 8200), (40, 1000, 16384), (64, 512, 16408),
+                                   (333, 1001, 4104), (300, 512, 2056), (652, 176, 12536), (2000, 2000, 16408),
+                                   (2500, 4096, 6152), (4096, 4096, 4096)])
+@pytest.mark.parametrize("cfg", [None, (64, 1), (128, 1), (256, 1), (256, 2)])
+def test_long_sums_keep_fp32(M, N, K, cfg):
+    A, B, _, _ = operands("fp16", M, N, K, K + N)
+    bias = torch.randn(N, generator=rng(5), device="cuda")
+    res = torch.randn(M, N, generator=rng(6), device="cuda")
+    if cfg:
+        binding.gemm_set_config_override(*cfg, 1)
+    x = A.double() @ B.double().t()
+    y = binding.gemm_fp16_linear(A, B, out_dtype=torch.float32)
+    assert (y.double() - x).norm() <= 4.7e-6 * x.norm()
+    z = binding.gemm_fp16_linear(A, B, bias, "gelu", res, out_dtype=torch.float32)
+    want = activate(x + bias.double(), "gelu") + res.double()
+    assert (z.double() - want).norm() <= 4.7e-6 * 1.13 * x.norm() + 2e-6 * want.norm()
