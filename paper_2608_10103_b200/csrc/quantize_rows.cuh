@@ -33,52 +33,71 @@ struct QuantRowsParams {
   int row_threads; // threads per row: 32, 64, 128 or 256
 };
 
-// Eight values as floats.
+// Eight values as they are in memory.  Loading and converting are apart, so that all of a thread's loads are on their
+// way before the first is waited for.
 template <bool F16>
-__device__ __forceinline__ void qr_load(const QuantRowsParams& p, long long at, float (&v)[8]) {
-  if constexpr (F16) {
-    const __half* x = static_cast<const __half*>(p.x) + at;
-    uint32_t w[4];
-    if (p.vec_ok) {
-      const uint4 u = ptx::ld_global_stream_v4(x);
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-    } else {
+struct QrPiece {
+  uint4 w[F16 ? 1 : 2];
+
+  __device__ __forceinline__ void load(const QuantRowsParams& p, long long at) {
+    if constexpr (F16) {
+      const __half* x = static_cast<const __half*>(p.x) + at;
+      if (p.vec_ok) {
+        w[0] = ptx::ld_global_stream_v4(x);
+      } else {
+        uint32_t u[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const volatile uint16_t* h = reinterpret_cast<const volatile uint16_t*>(x) + 2 * i;
-        w[i] = h[0] | (static_cast<uint32_t>(h[1]) << 16);
+        for (int i = 0; i < 4; ++i) {
+          const volatile uint16_t* h = reinterpret_cast<const volatile uint16_t*>(x) + 2 * i;
+          u[i] = h[0] | (static_cast<uint32_t>(h[1]) << 16);
+        }
+        w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    } else {
+      const float* x = static_cast<const float*>(p.x) + at;
+      if (p.vec_ok) {
+        w[0] = ptx::ld_global_stream_v4(x);
+        w[1] = ptx::ld_global_stream_v4(x + 4);
+      } else {
+        uint32_t u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(ptx::ld_global_f32(x + i));
+        w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        w[1] = make_uint4(u[4], u[5], u[6], u[7]);
       }
     }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
-    }
-  } else {
-    const float* x = static_cast<const float*>(p.x) + at;
-    if (p.vec_ok) {
-      const uint4 a = ptx::ld_global_stream_v4(x), b = ptx::ld_global_stream_v4(x + 4);
-      v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y);
-      v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
-      v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y);
-      v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = ptx::ld_global_f32(x + i);
+    for (int i = 0; i < (F16 ? 4 : 2); ++i) {
+      if constexpr (F16) {
+        const uint32_t u = i == 0 ? w[0].x : i == 1 ? w[0].y : i == 2 ? w[0].z : w[0].w;
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+      } else {
+        v[4 * i] = __uint_as_float(w[i].x);
+        v[4 * i + 1] = __uint_as_float(w[i].y);
+        v[4 * i + 2] = __uint_as_float(w[i].z);
+        v[4 * i + 3] = __uint_as_float(w[i].w);
+      }
     }
   }
-}
-
-__device__ __forceinline__ uint32_t qr_max_bits(uint32_t m, const float (&v)[8]) {
+  // The larger of m and the magnitude bits (as FP32) of the eight values.
+  __device__ __forceinline__ uint32_t max_bits(uint32_t m) const {
+    float v[8];
+    values(v);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  return m;
-}
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+  }
+};
 
-template <bool S4>
+template <bool S4, bool F16>
 __device__ __forceinline__ void qr_store(const QuantRowsParams& p, int row, int piece, float inverse,
-                                         const float (&v)[8]) {
+                                         const QrPiece<F16>& x) {
+  float v[8];
+  x.values(v);
   int c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = __float2int_rn(v[i] * inverse);
@@ -106,20 +125,19 @@ __global__ void __launch_bounds__(QR_THREADS) quantize_rows_kernel(const QuantRo
   const int pieces = live ? p.K / 8 : 0;
   const long long at = static_cast<long long>(live ? row : 0) * p.ldx;
   ptx::grid_dep_wait();  // x may come from the grid in front, which may also still read q
-  float v[QR_PIECES][8];
+  QrPiece<F16> v[QR_PIECES] = {};  // (what is not loaded counts as zeros)
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < QR_PIECES; ++i) {
     const int piece = t + i * p.row_threads;
-    if (piece < pieces) {
-      qr_load<F16>(p, at + piece * 8, v[i]);
-      m = qr_max_bits(m, v[i]);
-    }
+    if (piece < pieces) v[i].load(p, at + piece * 8);
   }
+#pragma unroll
+  for (int i = 0; i < QR_PIECES; ++i) m = v[i].max_bits(m);
   for (int piece = t + QR_PIECES * p.row_threads; piece < pieces; piece += p.row_threads) {
-    float u[8];
-    qr_load<F16>(p, at + piece * 8, u);
-    m = qr_max_bits(m, u);
+    QrPiece<F16> u;
+    u.load(p, at + piece * 8);
+    m = u.max_bits(m);
   }
   m = __reduce_max_sync(0xffffffffu, m);
   if (p.row_threads > 32) {
@@ -141,8 +159,8 @@ __global__ void __launch_bounds__(QR_THREADS) quantize_rows_kernel(const QuantRo
     if (piece < pieces) qr_store<S4>(p, row, piece, inverse, v[i]);
   }
   for (int piece = t + QR_PIECES * p.row_threads; piece < pieces; piece += p.row_threads) {
-    float u[8];
-    qr_load<F16>(p, at + piece * 8, u);
+    QrPiece<F16> u;
+    u.load(p, at + piece * 8);
     qr_store<S4>(p, row, piece, inverse, u);
   }
 }
