@@ -1227,12 +1227,12 @@ int launch_quantize_rows(int rows, int K, const void* x, long long ldx, bool f16
   p.K = K;
   const int size = f16 ? 2 : 4;
   p.vec_ok = reinterpret_cast<uintptr_t>(x) % 16 == 0 && (rows == 1 || ldx * size % 16 == 0);
-  // two pieces per thread: enough loads in flight, and a row of up to 16 K values stays in registers
   p.row_threads = 32;
-  while (p.row_threads < QR_THREADS && p.row_threads * 16 < K) p.row_threads *= 2;
-  const int rows_per_cta = QR_THREADS / p.row_threads;
+  while (p.row_threads < QR_MAX_THREADS && p.row_threads * 8 * QR_PIECES < K) p.row_threads *= 2;
+  const int threads = p.row_threads > QR_THREADS ? p.row_threads : QR_THREADS;
+  const int rows_per_cta = threads / p.row_threads;
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = chained_config(dim3(ceil_div(rows, rows_per_cta)), dim3(QR_THREADS), 0, stream, &attr);
+  const cudaLaunchConfig_t cfg = chained_config(dim3(ceil_div(rows, rows_per_cta)), dim3(threads), 0, stream, &attr);
   const cudaError_t e =
       f16 ? (s4 ? cudaLaunchKernelEx(&cfg, quantize_rows_kernel<true, true>, p)
                 : cudaLaunchKernelEx(&cfg, quantize_rows_kernel<true, false>, p))
