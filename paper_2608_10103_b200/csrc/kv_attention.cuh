@@ -35,6 +35,11 @@
 // finishes a unit last joins its pieces in their order (no second launch, and no dependence on who was
 // last).  What runs once per CTA or piece is kept short and rolled up: between other kernels of a
 // model its instructions are fetched anew each time, at some ten cycles an instruction.
+//
+// Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 131 us, 4.1 TB/s of codes; one of 131072
+// tokens 72 us; one of 1000 tokens 10.6 us.  16 heads of 64 d, 131071 tokens, 4 queries: 58 us, 4.6 TB/s.  Two thirds of
+// the copy rate: the issue slots are 0.3 busy, and a step waits for its own bytes, its shuffles and its MMAs in
+// turn; the rings fill shared memory and the fragments the registers, so more warps would have shorter rings.
 #pragma once
 
 #include <cuda_fp16.h>

@@ -15,6 +15,12 @@
 // when a row's maximum has grown by 2^8 (see kv_attention.cuh), so that it need not pass through registers.
 // Tiles of rows are taken longest first.  With fewer of them than half the SMs the tokens are split too, and the
 // CTA that finishes a row tile last joins the parts (4 x 64 queries over <= 8192 tokens: 150 -> 78 us).
+// Measured: 2 x 2048 queries, 32 heads on 8, over <= 8192 tokens 326-331 us (0.55 of the cuBLAS bf16 rate), 4096
+// queries over themselves 187 us.  Per row tile the chain scores -> maximum -> exponentials -> both products is what
+// is left (2860 cycles alone, and the two row tiles share the exponential unit and shared memory's 128 bytes a cycle,
+// which the first product takes up by itself).  Slower: two buffers of 64 scores per row tile (421 against 358 us
+// then), part of the exponentials as a polynomial (383-510), weights handed over in two or four parts (353, 369
+// against 331: the issuing thread waits in order and holds back the other row tile's products).
 #pragma once
 
 #include <cuda_fp16.h>
