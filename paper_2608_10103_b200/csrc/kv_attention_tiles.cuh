@@ -16,11 +16,13 @@
 // Tiles of rows are taken longest first.  With fewer of them than half the SMs the tokens are split too, and the
 // CTA that finishes a row tile last joins the parts (4 x 64 queries over <= 8192 tokens: 150 -> 78 us).
 // Measured: 2 x 2048 queries, 32 heads on 8, over <= 8192 tokens 326-331 us (0.55 of the cuBLAS bf16 rate), 4096
-// queries over themselves 187 us.  Per row tile the chain scores -> maximum -> exponentials -> both products is what
-// is left (2860 cycles alone, and the two row tiles share the exponential unit and shared memory's 128 bytes a cycle,
-// which the first product takes up by itself).  Slower: two buffers of 64 scores per row tile (421 against 358 us
-// then), part of the exponentials as a polynomial (383-510), weights handed over in two or four parts (353, 369
-// against 331: the issuing thread waits in order and holds back the other row tile's products).
+// queries over themselves 187 us.  A pair of row tiles takes 4140 cycles per 128 tokens where its products and its
+// exponentials are 2048 each: per row tile scores -> maximum (600) -> weights (1580: the two row tiles share the
+// exponential unit) -> both products (1400: the first takes shared memory's 128 bytes a cycle up by itself, the conversion
+// wants some too) is a chain.  Slower: two buffers of 64 scores per row tile (421 against 358 us then), part of the
+// exponentials as a polynomial (383-510), weights handed over in two or four parts (353, 369 against 331: the
+// issuing thread waits in order and holds back the other row tile's products), weights without the maximum first,
+// checked afterwards (338).
 #pragma once
 
 #include <cuda_fp16.h>
