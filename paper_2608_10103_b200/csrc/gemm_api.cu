@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <mutex>
+#include <new>
 
 #include <chrono>
 #include "../../include/b200gemm.h"
@@ -41,7 +42,12 @@ int shared_cuda_fail(cudaError_t e) { return cuda_fail(e); }
 
 int shared_scratch(int device, cudaStream_t stream, size_t need, size_t head, SharedLease* out) {
   ScratchPool::Lease l;
-  const int rc = g_kv_pool[device].acquire(stream, need, head, &l);
+  int rc;
+  try {
+    rc = g_kv_pool[device].acquire(stream, need, head, &l);
+  } catch (const std::bad_alloc&) {  // the pool's list of buffers could not grow: no exception leaves the C entry
+    rc = cudaErrorMemoryAllocation;
+  }
   if (rc != 0) return pool_fail(rc);
   out->ptr = l.ptr;
   out->head = l.ptr;
