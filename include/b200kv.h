@@ -22,10 +22,13 @@
  * are multiples of 8 elements.
  *
  * Lengths, counts and table entries are read on the device.  An entry outside
- * [0, num_pages), or a length that the table cannot hold, is not followed: nothing
- * outside the arrays is read or written, the status word (gemm_last_device_status,
- * gemm_read_device_status) reads 6 afterwards, and what the call gives for that
- * sequence is undefined.
+ * [0, num_pages), a length that the table cannot hold, or a row outside the packed
+ * arrays is not followed: nothing outside the arrays is read or written, the status
+ * word (gemm_last_device_status, gemm_read_device_status) reads 6 afterwards, and what
+ * the call gives for that sequence is undefined.  The library knows how many rows the packed
+ * arrays have from the entry points' forms ..._rows, whose last argument before the
+ * stream is that number; the forms without it take cu at its word: the caller
+ * vouches that cu[batch] rows are there.
  */
 #ifndef B200KV_H_
 #define B200KV_H_
@@ -64,6 +67,10 @@ int kv_append_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int
                  const int* block_table, int table_stride, int max_new, const void* K,
                  const void* V, long long token_stride, long long head_stride,
                  gemm_stream_t stream);
+int kv_append_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* past,
+                      const int* block_table, int table_stride, int max_new, const void* K,
+                      const void* V, long long token_stride, long long head_stride, int rows,
+                      gemm_stream_t stream);
 
 /*
  * Reads tokens first[b] .. first[b] + (cu[b+1] - cu[b]) - 1 of each sequence back as
@@ -73,6 +80,9 @@ int kv_append_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int
 int kv_read_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* first,
                const int* block_table, int table_stride, int max_read, void* K, void* V,
                gemm_stream_t stream);
+int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* first,
+                    const int* block_table, int table_stride, int max_read, void* K, void* V,
+                    int rows, gemm_stream_t stream);
 
 /*
  * Attention over the cache.  Sequence b has kv_len[b] tokens in the cache and
@@ -96,6 +106,11 @@ int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const 
                     const void* Q, long long q_token_stride, long long q_head_stride,
                     float softmax_scale, int window, void* out, long long out_token_stride,
                     gemm_stream_t stream);
+int kv_attention_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* kv_len,
+                         const int* block_table, int table_stride, int max_q, int q_heads,
+                         const void* Q, long long q_token_stride, long long q_head_stride,
+                         float softmax_scale, int window, void* out, long long out_token_stride,
+                         int rows, gemm_stream_t stream);
 
 #ifdef __cplusplus
 }

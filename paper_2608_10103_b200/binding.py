@@ -29,7 +29,8 @@ EXPORTS = (
     "gemm_status_string", "gemm_version",
 )
 
-KV_EXPORTS = ("kv_append_s8", "kv_read_s8", "kv_attention_s8")   # include/b200kv.h
+KV_EXPORTS = ("kv_append_s8", "kv_read_s8", "kv_attention_s8",   # include/b200kv.h
+              "kv_append_s8_rows", "kv_read_s8_rows", "kv_attention_s8_rows")
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
@@ -88,6 +89,9 @@ def lib() -> ctypes.CDLL:
         L.kv_append_s8.argtypes = [kc, i, vp, vp, vp, i, i, vp, vp, ll, ll, vp]
         L.kv_read_s8.argtypes = [kc, i, vp, vp, vp, i, i, vp, vp, vp]
         L.kv_attention_s8.argtypes = [kc, i, vp, vp, vp, i, i, i, vp, ll, ll, ctypes.c_float, i, vp, ll, vp]
+        for name in KV_EXPORTS[:3]:      # ... and the forms with a row count in front of the stream
+            args = getattr(L, name).argtypes
+            getattr(L, name + "_rows").argtypes = args[:-1] + [i, args[-1]]
         L.gemm_s4_workspace_bytes.argtypes = [i, i, i]
         L.gemm_s4_workspace_bytes.restype = sz
         L.gemm_s4_static.argtypes = [i, i, i, vp, vp, vp, vp]
@@ -270,7 +274,7 @@ def _native():
             from . import _marshal as m
         except ImportError as e:
             raise ImportError("%s: build it with `python -m paper_2608_10103_b200.build`" % e) from e
-        names = ("gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows") + KV_EXPORTS
+        names = ("gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows") + KV_EXPORTS[3:]
         m.entries(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
         _marshal = m
     return _marshal
@@ -339,7 +343,8 @@ def kv_cache_s8(num_pages: int, kv_heads: int, page_size: int, head_dim: int, de
 
 def kv_append_s8(cache, k, v, cu, past, block_table, max_new: int, stream=None):
     """Quantises the rows of k and v (float16 (tokens, kv_heads, head_dim) views with one common pair of
-    strides) into the cache: rows cu[b] .. cu[b+1] become tokens past[b], past[b] + 1, ... of sequence b."""
+    strides) into the cache: rows cu[b] .. cu[b+1] become tokens past[b], past[b] + 1, ... of sequence b.  Rows
+    that cu names beyond those of k are left out (status 6), here as in the two functions below."""
     _checked((_marshal or _native()).kv_append(cache, k, v, cu, past, block_table, max_new,
                                                None if stream is None else stream.cuda_stream), "kv_append_s8")
 

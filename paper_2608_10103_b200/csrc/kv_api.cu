@@ -37,8 +37,8 @@ int check_cache(const kv_cache_s8_t* c, KvCacheView* v) {
 }
 
 int check_batch(int batch, const int* cu, const int* start, const int* table, int table_stride,
-                int max_rows, KvBatch* b) {
-  if (batch <= 0 || !cu || !start || !table || table_stride <= 0 || max_rows <= 0)
+                int max_rows, int rows, KvBatch* b) {
+  if (batch <= 0 || !cu || !start || !table || table_stride <= 0 || max_rows <= 0 || rows <= 0)
     return GEMM_ERR_INVALID_ARG;
   if (misaligned(cu, 4) || misaligned(start, 4) || misaligned(table, 4)) return GEMM_ERR_MISALIGNED;
   b->batch = batch;
@@ -47,6 +47,7 @@ int check_batch(int batch, const int* cu, const int* start, const int* table, in
   b->table = table;
   b->table_stride = table_stride;
   b->max_rows = max_rows;
+  b->rows = rows;
   return GEMM_OK;
 }
 
@@ -68,6 +69,7 @@ int launch(const SharedDevice& dev, Kernel kernel, dim3 grid, int threads, size_
 }
 
 constexpr int MAX_DEV = 64;
+constexpr int ANY_ROWS = 0x7fffffff;  // the entry points without a row count
 
 // D: head size, NR: groups of eight rows per tile.
 template <int D, int NR>
@@ -168,13 +170,13 @@ using namespace b200gemm;
 
 extern "C" {
 
-int kv_append_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* past,
-                 const int* block_table, int table_stride, int max_new, const void* K,
-                 const void* V, long long token_stride, long long head_stride,
-                 gemm_stream_t stream) {
+int kv_append_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* past,
+                      const int* block_table, int table_stride, int max_new, const void* K,
+                      const void* V, long long token_stride, long long head_stride, int rows,
+                      gemm_stream_t stream) {
   KvAppendParams p = {};
   int rc = check_cache(cache, &p.c);
-  if (rc == GEMM_OK) rc = check_batch(batch, cu, past, block_table, table_stride, max_new, &p.b);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, past, block_table, table_stride, max_new, rows, &p.b);
   if (rc != GEMM_OK) return rc;
   if (!K || !V || token_stride < 0 || head_stride < p.c.dim) return GEMM_ERR_INVALID_ARG;
   if (misaligned(K, 16) || misaligned(V, 16) || token_stride % 8 || head_stride % 8)
@@ -197,12 +199,20 @@ int kv_append_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int
                 reinterpret_cast<cudaStream_t>(stream), p);
 }
 
-int kv_read_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* first,
-               const int* block_table, int table_stride, int max_read, void* K, void* V,
-               gemm_stream_t stream) {
+int kv_append_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* past,
+                 const int* block_table, int table_stride, int max_new, const void* K,
+                 const void* V, long long token_stride, long long head_stride,
+                 gemm_stream_t stream) {
+  return kv_append_s8_rows(cache, batch, cu, past, block_table, table_stride, max_new, K, V, token_stride,
+                           head_stride, ANY_ROWS, stream);
+}
+
+int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* first,
+                    const int* block_table, int table_stride, int max_read, void* K, void* V,
+                    int rows, gemm_stream_t stream) {
   KvReadParams p = {};
   int rc = check_cache(cache, &p.c);
-  if (rc == GEMM_OK) rc = check_batch(batch, cu, first, block_table, table_stride, max_read, &p.b);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, first, block_table, table_stride, max_read, rows, &p.b);
   if (rc != GEMM_OK) return rc;
   if (!K && !V) return GEMM_ERR_INVALID_ARG;
   if (misaligned(K, 16) || misaligned(V, 16)) return GEMM_ERR_MISALIGNED;
@@ -219,15 +229,21 @@ int kv_read_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* 
                 reinterpret_cast<cudaStream_t>(stream), p);
 }
 
-int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* kv_len,
-                    const int* block_table, int table_stride, int max_q, int q_heads,
-                    const void* Q, long long q_token_stride, long long q_head_stride,
-                    float softmax_scale, int window, void* out, long long out_token_stride,
-                    gemm_stream_t stream) {
+int kv_read_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* first,
+               const int* block_table, int table_stride, int max_read, void* K, void* V,
+               gemm_stream_t stream) {
+  return kv_read_s8_rows(cache, batch, cu, first, block_table, table_stride, max_read, K, V, ANY_ROWS, stream);
+}
+
+int kv_attention_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const int* kv_len,
+                         const int* block_table, int table_stride, int max_q, int q_heads,
+                         const void* Q, long long q_token_stride, long long q_head_stride,
+                         float softmax_scale, int window, void* out, long long out_token_stride,
+                         int rows, gemm_stream_t stream) {
   KvAttnParams p = {};
   KvBatch b;
   int rc = check_cache(cache, &p.c);
-  if (rc == GEMM_OK) rc = check_batch(batch, cu, kv_len, block_table, table_stride, max_q, &b);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, kv_len, block_table, table_stride, max_q, rows, &b);
   if (rc != GEMM_OK) return rc;
   if (!Q || !out || q_heads <= 0 || q_heads % p.c.heads || window < 0 || q_token_stride < 0 ||
       q_head_stride < p.c.dim || out_token_stride < static_cast<long long>(q_heads) * p.c.dim ||
@@ -245,6 +261,7 @@ int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const 
   p.table = block_table;
   p.table_stride = table_stride;
   p.max_q = max_q;
+  p.rows = rows;
   p.group = q_heads / p.c.heads;
   p.q = static_cast<const __half*>(Q);
   p.q_token_stride = q_token_stride;
@@ -262,6 +279,16 @@ int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const 
     case 128: return attention<128, 4>(dev, p, st);
     default: return attention<256, 2>(dev, p, st);
   }
+}
+
+int kv_attention_s8(const kv_cache_s8_t* cache, int batch, const int* cu, const int* kv_len,
+                    const int* block_table, int table_stride, int max_q, int q_heads,
+                    const void* Q, long long q_token_stride, long long q_head_stride,
+                    float softmax_scale, int window, void* out, long long out_token_stride,
+                    gemm_stream_t stream) {
+  return kv_attention_s8_rows(cache, batch, cu, kv_len, block_table, table_stride, max_q, q_heads, Q,
+                              q_token_stride, q_head_stride, softmax_scale, window, out, out_token_stride,
+                              ANY_ROWS, stream);
 }
 
 }  // extern "C"

@@ -67,6 +67,7 @@ struct KvAttnParams {
   const int* table;
   int table_stride;
   int max_q;
+  int rows;     // rows of q and out
   int max_len;  // tokens a row of the table can name
   int group;    // query heads per KV head
   const __half* q;
@@ -84,7 +85,7 @@ struct KvAttnParams {
   int splits;        // tile kernel: CTAs a row tile's tokens are divided over
 };
 
-// A sequence's rows and length, cut to what the table and the caller's bound allow.
+// A sequence's rows and length, cut to what the packed arrays, the table and the caller's bound allow.
 struct KvSeq {
   int row0, n, len;
 };
@@ -93,7 +94,7 @@ __device__ __forceinline__ KvSeq kv_seq_of(const KvAttnParams& p, int row0, int 
   s.row0 = row0;
   s.n = row1 - row0;
   s.len = kv_len;
-  const int n = s.row0 < 0 ? 0 : min(max(s.n, 0), p.max_q), len = min(max(s.len, 0), p.max_len);
+  const int n = s.row0 < 0 ? 0 : max(0, min(s.n, min(p.max_q, p.rows - s.row0))), len = min(max(s.len, 0), p.max_len);
   if (report && (n != s.n || len != s.len)) kv_report(p.status);
   s.n = n;
   s.len = len;

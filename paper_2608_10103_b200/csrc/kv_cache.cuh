@@ -36,6 +36,7 @@ struct KvBatch {
   const int* table;
   int table_stride;    // entries per sequence
   int max_rows;        // upper bound of rows per sequence
+  int rows;            // rows of the packed arrays
   int* status;
 };
 
@@ -46,7 +47,7 @@ __device__ __forceinline__ int kv_ld(const int* p) {  // may have been written b
 }
 __device__ __forceinline__ void kv_report(int* status) { atomicCAS(status, 0, DEV_BAD_INDEX); }
 
-// Rows and positions of a sequence, cut to what the table and the caller's bound allow.
+// Rows and positions of a sequence, cut to what the packed arrays, the table and the caller's bound allow.
 struct KvRange {
   int row0;   // first row in the packed arrays
   int begin;  // first position
@@ -57,9 +58,9 @@ __device__ __forceinline__ KvRange kv_range(const KvBatch& b, int seq, int page,
   r.row0 = kv_ld(b.cu + seq);
   long long n = static_cast<long long>(kv_ld(b.cu + seq + 1)) - r.row0;
   long long first = kv_ld(b.start + seq);
-  const long long room = static_cast<long long>(b.table_stride) * page;
-  bool bad = n < 0 || n > b.max_rows || first < 0 || r.row0 < 0;
-  if (n > b.max_rows) n = b.max_rows;
+  const long long room = min(static_cast<long long>(b.table_stride) * page, 0x7fffffffll);
+  bool bad = n < 0 || n > b.max_rows || first < 0 || r.row0 < 0 || r.row0 + n > b.rows;
+  n = min(n, min(static_cast<long long>(b.max_rows), static_cast<long long>(b.rows) - r.row0));
   if (n < 0 || first < 0 || r.row0 < 0) n = first = 0;
   if (n > 0 && first + n > room) {
     bad = true;

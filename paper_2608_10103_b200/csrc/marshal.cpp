@@ -25,9 +25,9 @@ struct Entries {
   decltype(&gemm_s8_linear) s8_linear;
   decltype(&gemm_s4_linear) s4_linear;
   decltype(&gemm_quantize_rows) quantize_rows;
-  decltype(&kv_append_s8) kv_append;
-  decltype(&kv_read_s8) kv_read;
-  decltype(&kv_attention_s8) kv_attention;
+  decltype(&kv_append_s8_rows) kv_append;
+  decltype(&kv_read_s8_rows) kv_read;
+  decltype(&kv_attention_s8_rows) kv_attention;
 } g_entry = {};
 
 int g_device = -1;  // the current device, asked for once a call (with the first CUDA tensor)
@@ -276,7 +276,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Batch b = batch_of(a[3], a[4], a[5], "past");
     if (k.tokens == 0) Py_RETURN_NONE;
     const int rc = g_entry.kv_append(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[6])),
-                                     k.ptr, v.ptr, k.token, k.head, stream_of(a[7]).handle);
+                                     k.ptr, v.ptr, k.token, k.head, narrow(k.tokens, "tokens"), stream_of(a[7]).handle);
     if (rc) return code(rc);
     Py_RETURN_NONE;
   });
@@ -306,7 +306,7 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (out[0].size(0) > 0) {
       const int rc = g_entry.kv_read(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[4])),
-                                     out[0].data_ptr(), out[1].data_ptr(), s.handle);
+                                     out[0].data_ptr(), out[1].data_ptr(), narrow(out[0].size(0), "tokens"), s.handle);
       if (rc) return code(rc);
     }
     PyObject* const k = THPVariable_Wrap(out[0]);
@@ -339,7 +339,8 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (q.tokens > 0) {
       const int rc = g_entry.kv_attention(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[5])),
                                           narrow(q.heads, "heads"), q.ptr, q.token, q.head, static_cast<float>(PyFloat_AsDouble(a[6])),
-                                          static_cast<int>(PyLong_AsLong(a[7])), out.data_ptr(), o.token, s.handle);
+                                          static_cast<int>(PyLong_AsLong(a[7])), out.data_ptr(), o.token,
+                                          narrow(q.tokens, "tokens"), s.handle);
       if (rc) return code(rc);
     }
     return THPVariable_Wrap(out);
