@@ -70,6 +70,8 @@ void* rows_of(const at::Tensor& t, int64_t rows, int64_t cols, const char* what,
     throw Refused{PyExc_ValueError, std::string(what) + " must have shape (" + std::to_string(rows) + ", " +
                                         std::to_string(cols) + ")"};
   if (cols > 1 && t.stride(1) != 1) throw Refused{PyExc_ValueError, std::string(what) + " must have contiguous rows"};
+  // (a pitch of 0, a broadcast row, would read as "dense" in the entry points)
+  if (rows > 1 && t.stride(0) < cols) throw Refused{PyExc_ValueError, std::string(what) + " must have rows that do not overlap"};
   *pitch = rows > 1 ? t.stride(0) : cols;
   return t.data_ptr();
 }
