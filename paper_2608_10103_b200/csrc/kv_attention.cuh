@@ -583,6 +583,15 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
               kk[sub] = 0.0f;
               sv = 1.0f;
             }
+            // A page whose scale is not finite: NaN for the rows that see it, nothing (-inf below, which such factors
+            // would turn into a NaN) for those that do not.
+            if (!(fabsf(kk[sub]) < INFINITY && fabsf(sv) < INFINITY)) {
+              kk[sub] = sv = 1.0f;
+#pragma unroll
+              for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sc[sub][n][j][0] = sc[sub][n][j][1] = __int_as_float(0x7fffffff);
+            }
             if (sv == 0.0f) sv = 1e-30f;  // a page of zeros: its codes are 0, its tokens still count in l
             lsv[sub] = __log2f(sv);
             inv_sv[sub] = __fdividef(1.0f, sv);

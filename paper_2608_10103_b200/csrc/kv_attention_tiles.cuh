@@ -8,7 +8,8 @@
 // K and V arrive as int8, by bulk copies of whole pages of a head; four warps convert them
 // exactly to binary16 and write them as rows of 64 d in the 128-byte swizzle.  Such a tile is K-major for the
 // first product and, read the other way round, MN-major for the second: no transpose anywhere.
-// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own.
+// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own; a fourth word marks pages whose
+// scale is not finite, whose other factors are harmless: rows that see one become NaN by their l, others are left alone.
 //
 // What bounds it: at 128 d, 1024 cycles of tensor pipe a tile pair of 128 x 128 against as many of exponentials
 // (16 a cycle and SM); the conversion takes a tenth of the issue slots.  O is rescaled in tensor memory only
@@ -339,6 +340,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
             w[8 * g + v / 2] = pack_halves(e0, e1);
           }
           l = fmaf(sum0 + sum1, c.z, l);
+          const int first = tok0 + 32 * h + 16 * g;
+          if (c.w != 0.0f && first <= pos && first + 15 >= from) l = __int_as_float(0x7fffffff);
         }
         ptx::tmem_st_32x32b_x16(s_at + h * 16, w);
       }
@@ -482,7 +485,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           // scales by groups of 16 tokens.  (A page of zeros: its codes are 0, its tokens still count in l; a
           // hidden token's -inf must stay one.)
           const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
-          const float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
+          float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
+          if (!(fabsf(sk) < INFINITY && fabsf(sv) < INFINITY)) c = make_float4(1e-30f, 0.0f, 1.0f, 1.0f);
           if (lane < runs)
             for (int g = 0; g < run / 16; ++g)
               reinterpret_cast<float4*>(base_ptr + T::SCALE_OFFSET)[(j & 3) * GROUPS + lane * (run / 16) + g] = c;
