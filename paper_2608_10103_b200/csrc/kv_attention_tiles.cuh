@@ -8,8 +8,9 @@
 // K and V arrive as int8, by bulk copies of whole pages of a head; four warps convert them
 // exactly to binary16 and write them as rows of 64 d in the 128-byte swizzle.  Such a tile is K-major for the
 // first product and, read the other way round, MN-major for the second: no transpose anywhere.
-// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own; a fourth word marks pages whose
-// scale is not finite, whose other factors are harmless: rows that see one become NaN by their l, others are left alone.
+// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own;
+// A page whose scale is not finite gets harmless factors and raises a flag: the rows then look through the pages
+// that they see themselves, at the end, and become NaN by their l (a test per tile of tokens costs 2 %).
 //
 // What bounds it: at 128 d, 1024 cycles of tensor pipe a tile pair of 128 x 128 against as many of exponentials
 // (16 a cycle and SM); the conversion takes a tenth of the issue slots.  O is rescaled in tensor memory only
@@ -157,6 +158,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   static_assert(T::BARS == 24, "barrier numbering");
   volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
   volatile uint32_t* const abort_flag = tmem_holder + 1;
+  volatile uint32_t* const poison_flag = tmem_holder + 2;  // a page of this CTA's tokens has a scale that is not finite
+  auto not_finite = [](float sk, float sv) { return !(fabsf(sk) < INFINITY && fabsf(sv) < INFINITY); };
 
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
   if (tid == 0) ptx::grid_dep_launch_dependents();
@@ -212,6 +215,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
       ptx::mbar_init(raw_empty(i), 4);
     }
     *abort_flag = 0;
+    *poison_flag = 0;
     ptx::fence_mbar_init();
   }
   if (warp == T::SOFTMAX_WARPS + 4) {
@@ -340,8 +344,6 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
             w[8 * g + v / 2] = pack_halves(e0, e1);
           }
           l = fmaf(sum0 + sum1, c.z, l);
-          const int first = tok0 + 32 * h + 16 * g;
-          if (c.w != 0.0f && first <= pos && first + 15 >= from) l = __int_as_float(0x7fffffff);
         }
         ptx::tmem_st_32x32b_x16(s_at + h * 16, w);
       }
@@ -356,6 +358,18 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
         ok = wait_bounded(o_done(q), (tiles - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
         ok = __all_sync(0xffffffffu, ok);
         ptx::tc_fence_after_sync();
+      }
+      if (*poison_flag && live) {  // (written in front of the scale_full arrivals this thread has waited for)
+        const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
+        const int last = min(pos, hi - 1);
+#pragma unroll 1
+        for (int t = max(from, lo); t <= last; t = (t | (p.c.page - 1)) + 1) {
+          const int id = kv_ld(table + (t >> p.c.page_shift));
+          if (id < 0 || id >= p.c.num_pages) continue;
+          const long long ph = static_cast<long long>(id) * heads + head;
+          if (not_finite(ptx::ld_global_f32(p.c.scales[0] + ph), ptx::ld_global_f32(p.c.scales[1] + ph)))
+            l = __int_as_float(0x7fffffff);
+        }
       }
       const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
       float* const part = p.partial + (static_cast<long long>(blockIdx.x) * T::ROWS + r) * (D + 4);
@@ -486,7 +500,10 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           // hidden token's -inf must stay one.)
           const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
           float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
-          if (!(fabsf(sk) < INFINITY && fabsf(sv) < INFINITY)) c = make_float4(1e-30f, 0.0f, 1.0f, 1.0f);
+          if (not_finite(sk, sv)) {
+            c = make_float4(1e-30f, 0.0f, 1.0f, 0.0f);
+            *poison_flag = 1;
+          }
           if (lane < runs)
             for (int g = 0; g < run / 16; ++g)
               reinterpret_cast<float4*>(base_ptr + T::SCALE_OFFSET)[(j & 3) * GROUPS + lane * (run / 16) + g] = c;
