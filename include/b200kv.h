@@ -92,7 +92,8 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  * KV head h / (q_heads / kv_heads).
  *     out = sum_t softmax_t(softmax_scale * q . k_t) v_t
  * A query that sees nothing (position below 0) gives zeros, one that sees a page whose
- * scale is not finite NaN; pages that it does not see leave it alone, whatever they hold.
+ * scale is not finite, or that holds a NaN or an infinity itself, NaN; pages that it does
+ * not see leave it alone, whatever they hold.
  * Q, out: binary16, element (row, head, d) at row * token_stride + head * head_dim + d for
  * out, row * q_token_stride + head * q_head_stride + d for Q.  Scores, softmax
  * statistics and sums are FP32; the softmax weights are rounded to binary16 for the product with the

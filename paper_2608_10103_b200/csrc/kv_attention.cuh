@@ -380,6 +380,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
 
         // q: piece (group of rows, 64 d) i is converted by warp i % KVA_WARPS; its loads go out first
         float krow[NR];
+        uint32_t q_bad = 0;  // bit n: row g of group n holds a NaN or an infinity
         uint32_t qx[NR][KC][8];
         {
 #pragma unroll
@@ -472,8 +473,9 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
           const float amax = __half2float(__ushort_as_half(static_cast<unsigned short>(top)));
           const float inv = amax > 0.0f ? __fdividef(127.0f, amax) : 0.0f;
-          // a row with an infinity or a NaN gives NaN
-          krow[n] = p.scale_log2 * (top >= 0x7c00u ? __int_as_float(0x7fffffff) : amax * (1.0f / (127.0f * 254.0f)));
+          // (a row with an infinity or a NaN becomes NaN below, if it sees anything)
+          q_bad |= top >= 0x7c00u ? 1u << n : 0u;
+          krow[n] = p.scale_log2 * (top >= 0x7c00u ? 0.0f : amax * (1.0f / (127.0f * 254.0f)));
 #pragma unroll
           for (int c = 0; c < KC; ++c)
             if (warp == (n * KC + c) % KVA_WARPS) {
@@ -695,6 +697,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
         for (int n = 0; n < NR; ++n) {
           lrow[n] += __shfl_xor_sync(0xffffffffu, lrow[n], 1);
           lrow[n] += __shfl_xor_sync(0xffffffffu, lrow[n], 2);
+          if ((q_bad >> n & 1u) && base_pos + (row_first + 8 * n + g) / p.group >= 0) lrow[n] = __int_as_float(0x7fffffff);
           if (t == 0) *reinterpret_cast<float2*>(mine_out + (8 * n + g) * PITCH + D) = make_float2(mrow[n], lrow[n]);
 #pragma unroll
           for (int v = 0; v < 2; ++v) {

@@ -247,6 +247,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
     const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(q * 128);
     const uint32_t o_at = tmem + lane_base + T::O_COLUMN + static_cast<uint32_t>(q * D);
+    uint32_t q_top = 0;  // two maxima of magnitude bits of the row
     if (q < active) {  // this row of Q, in the 128-byte swizzle
       const __half* const src = p.q + (static_cast<long long>(s.row0) + (live ? qi : 0)) * p.q_token_stride +
                                 static_cast<long long>(live ? hq : 0) * p.q_head_stride;
@@ -255,6 +256,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
       for (int u = 0; u < D / 8; ++u) {
         uint4 x = make_uint4(0, 0, 0, 0);
         if (live) x = ptx::ld_global_stream_v4(src + u * 8);
+        q_top = __vmaxu2(q_top, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu),
+                                         __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
         ptx::st_shared_v4(dst + static_cast<uint32_t>((u >> 3) * 16384 + (((u & 7) ^ (r & 7)) << 4)), x.x, x.y, x.z, x.w);
       }
       ptx::fence_proxy_async_smem();
@@ -266,7 +269,9 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
     const int from = p.window > 0 ? pos - p.window + 1 : 0;
     const int all_hi = s.len - s.n + (row_first + q * 128) / p.group;
     const int all_lo = p.window > 0 ? s.len - s.n + (row_first + min(rows, q * 128 + 128) - 1) / p.group - p.window + 1 : 0;
-    float m = -INFINITY, l = 0.0f;
+    // A row with a NaN or an infinity is NaN if it sees anything, also where all its scores are -inf.
+    const bool q_bad = max(q_top & 0xffffu, q_top >> 16) >= 0x7c00u && pos >= 0;
+    float m = -INFINITY, l = q_bad ? __int_as_float(0x7fffffff) : 0.0f;
     bool ok = true;
     const int my_tiles = q < active ? tiles : 0;
 #pragma unroll 1
