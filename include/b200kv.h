@@ -9,7 +9,8 @@
  * the value of a code is code * scale.  The caller owns all four arrays and
  * hands pages to sequences through a block table, int32 [batch][table_stride]:
  * entry (b, j) is the page that holds tokens [j * page_size, (j+1) * page_size) of
- * sequence b.  Entries beyond a sequence's length are never read.  Different
+ * sequence b.  Entries beyond a sequence's length are never read, nor by attention those of
+ * pages that lie in front of every query's window.  Different
  * sequences may share pages that neither of them writes.
  *
  * Batches are ragged: sequence b has the rows cu[b] .. cu[b+1]-1 of a packed

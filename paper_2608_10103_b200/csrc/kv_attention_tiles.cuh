@@ -186,6 +186,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   const int active = QT == 2 && rows > 128 ? 2 : 1;  // row tiles with a row in them
   int lo, hi;
   kv_visible(p, s, row_first / p.group, (row_first + rows + p.group - 1) / p.group, lo, hi);
+  const int visible_lo = lo;  // pages wholly in front of it are not looked at: their owners may have given them away
   lo = lo / TN * TN;
   int tiles = (hi - lo + TN - 1) / TN;  // 0: nothing is visible
   if (p.splits > 1) {  // this CTA's part of the tokens
@@ -466,16 +467,19 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
     const uint32_t run_bytes = static_cast<uint32_t>(run * D);
     const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
     const uint64_t page_bytes = static_cast<uint64_t>(heads) * p.c.page * D;
-    auto load_id = [&](int j) {  // page of the lane's run of tile j, or -1
+    auto visible = [&](int j) {  // the lane's run of tile j, or a part of it
       const int tok = lo + j * TN + run * lane;
-      return lane < runs && j < tiles && tok < hi ? kv_ld(table + (tok >> p.c.page_shift)) : -1;
+      return lane < runs && j < tiles && tok < hi && tok + run > visible_lo;
+    };
+    auto load_id = [&](int j) {  // its page, or -1
+      return visible(j) ? kv_ld(table + ((lo + j * TN + run * lane) >> p.c.page_shift)) : -1;
     };
     bool ok = true;
     int id = load_id(0);
 #pragma unroll 1
     for (int j = 0; j < tiles && ok; ++j) {
       const int id_next = load_id(j + 1);
-      const bool in = lane < runs && lo + j * TN + run * lane < hi;
+      const bool in = visible(j);
       const bool good = in && id >= 0 && id < p.c.num_pages;
       if (in && !good) kv_report(p.status);
       const int tok = lo + j * TN + run * lane;
