@@ -97,8 +97,9 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  * not see leave it alone, whatever they hold.
  * Q, out: binary16, element (row, head, d) at row * token_stride + head * head_dim + d for
  * out, row * q_token_stride + head * q_head_stride + d for Q.  Scores, softmax
- * statistics and sums are FP32; the softmax weights are rounded to binary16 for the product with the
- * codes, which are exact there.  max_q: an upper bound of n over the batch (rows
+ * statistics and sums are FP32; the softmax weights (times their page's value scale) are rounded to binary16
+ * for the product with the codes, which are exact there: by 2^-11 of themselves, or up to 2^-32 of the row's
+ * largest where they are below 2^-21 of it.  max_q: an upper bound of n over the batch (rows
  * beyond it are not computed, status 6).
  * Work of long sequences is split over CTAs and joined in a fixed order: results
  * do not vary from run to run.  The library keeps grow-only scratch per stream for

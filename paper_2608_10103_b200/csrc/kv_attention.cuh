@@ -4,13 +4,15 @@
 // Mathematics.  The rows that share a KV head (queries x heads of its group) form one tile of
 // 8 NR rows, so the cache is read once for all of them.  With page scales sk, sv, codes K, V and
 // weights relative to a running reference m,
-//     t = c sk (q . K) + log2 sv,   w = 2^(t - m),   O = sum w V,   l = sum w / sv,   out = O / l,
+//     t = c sk (q . K) + log2 sv,   w = 2^(t - m + 7),   O = sum w V,   l = sum w / sv,   out = O / l,
 // c = softmax_scale log2 e: the value scale is folded into the exponent, so that O needs one
 // accumulator whatever the pages' scales are, and the softmax denominator takes it out again.  m is a
-// maximum seen earlier, renewed when a score passes it by 2^8 (w then stays below 2^8, O and l are
+// maximum seen earlier, renewed when a score passes it by 2^8 (O and l are
 // rescaled a few times per sequence instead of at every new maximum).  m, l, O and the scores are FP32;
-// w is rounded to binary16 for the product with V (relative 2^-11 a weight, the rounding of the
-// result itself; codes are exact in binary16).
+// w is rounded to binary16 for the product with V (codes are exact in binary16): off by 2^-11 of itself,
+// the rounding of the result, down to 2^-21 of the largest; a smaller one by up to 2^-32 of the largest.  The 2^7
+// uses what binary16 has above a maximum of 2^8: without it weights lose bits from 2^-14 of the
+// largest on and vanish at 2^-25, which long flat tails behind one large weight notice.
 //
 // q . K runs on the integer MMA, on the codes as they are: a row of q is held as
 // q = s (254 q1 + q2) with int8 q1, q2 and s = max|q| / (127 * 254), i.e. to 1.6e-5 of the row's
@@ -58,6 +60,12 @@ constexpr int KVA_STEP = 16;  // tokens per step
 // exchange between the warps, some 8-10 k cycles where four warps take 3 k for four steps.  Without it in the
 // balance the CTAs with several short sequences were a fifth behind the others.
 constexpr int KVA_UNIT_COST = 12;
+
+// A weight of the reference is 2^7: with scores up to 2^8 beyond it, weights reach 2^15 of binary16's 65504.
+constexpr float KVA_WEIGHT_BITS = 7.0f;
+// A value scale as the exponent takes it.  Pages of zeros have none, but their tokens count in l; and 1 / sv times a
+// weight must stay in FP32.  127 * 2^-40 = 1.2e-10 is nothing to a binary16 result (multiples of 6e-8).
+__device__ __forceinline__ float kva_value_scale(float sv) { return sv < 0x1p-40f ? 0x1p-40f : sv; }
 
 struct KvAttnParams {
   KvCacheView c;
@@ -594,7 +602,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
 #pragma unroll
                 for (int j = 0; j < 2; ++j) sc[sub][n][j][0] = sc[sub][n][j][1] = __int_as_float(0x7fffffff);
             }
-            if (sv == 0.0f) sv = 1e-30f;  // a page of zeros: its codes are 0, its tokens still count in l
+            sv = kva_value_scale(sv);
             lsv[sub] = __log2f(sv);
             inv_sv[sub] = __fdividef(1.0f, sv);
             masked |= dead || tok0 + KVA_STEP - 1 > all_hi || tok0 < all_lo;
@@ -642,7 +650,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
                 o[n][i][3] *= f1;
               }
             }
-            const float ref = mrow[n] == -INFINITY ? 0.0f : mrow[n];
+            const float ref = (mrow[n] == -INFINITY ? 0.0f : mrow[n]) - KVA_WEIGHT_BITS;
 #pragma unroll
             for (int sub = 0; sub < SUB; ++sub) {
               const float at_ref = lsv[sub] - ref;

@@ -331,7 +331,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           ptx::tmem_wait_st();
         }
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
+      const float ref = (m == -INFINITY ? 0.0f : m) - KVA_WEIGHT_BITS;
       // weights, two per column, over the scores: 32 tokens take 16 columns
 #pragma unroll
       for (int h = 0; h < TN / 32; ++h) {
@@ -505,9 +505,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           ptx::bulk_load(base + T::RAW_OFFSET + which * T::RAW_BYTES + lane * run_bytes,
                          (which ? p.c.codes[1] : p.c.codes[0]) + off, run_bytes, raw_full(which));
         if (which == 0) {
-          // scales by groups of 16 tokens.  (A page of zeros: its codes are 0, its tokens still count in l; a
-          // hidden token's -inf must stay one.)
-          const float v = sv == 0.0f ? 1e-30f : sv, k = p.scale_log2 * sk;
+          // scales by groups of 16 tokens (a hidden token's -inf must stay one)
+          const float v = kva_value_scale(sv), k = p.scale_log2 * sk;
           float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
           if (not_finite(sk, sv)) {
             c = make_float4(1e-30f, 0.0f, 1.0f, 0.0f);
