@@ -96,11 +96,17 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  * scale is not finite, or that holds a NaN or an infinity itself, NaN; pages that it does
  * not see leave it alone, whatever they hold.
  * Q, out: binary16, element (row, head, d) at row * token_stride + head * head_dim + d for
- * out, row * q_token_stride + head * q_head_stride + d for Q.  Scores, softmax
- * statistics and sums are FP32; the softmax weights (times their page's value scale) are rounded to binary16
- * for the product with the codes, which are exact there: by 2^-11 of themselves, or up to 2^-32 of the row's
- * largest where they are below 2^-21 of it.  max_q: an upper bound of n over the batch (rows
- * beyond it are not computed, status 6).
+ * out, row * q_token_stride + head * q_head_stride + d for Q.  max_q: an upper bound of n
+ * over the batch (rows beyond it are not computed, status 6).
+ * Scores, softmax statistics and sums are FP32.  Two operands have fewer bits:
+ *   - the softmax weights (times their page's value scale) are rounded to binary16 for the
+ *     product with the codes, which are exact there: by 2^-11 of themselves, or up to 2^-32 of
+ *     the row's largest where they are below 2^-21 of it;
+ *   - sequences of up to 32 rows (n * q_heads / kv_heads; 16 for head_dim 256) are scored on
+ *     the integer codes, with each row of Q in fixed point of 16 bits under one scale: a
+ *     value is off by up to max|q| / 64516 of its row, a score by up to softmax_scale *
+ *     sum|k| times that.  Longer ones take Q as it is.
+ * So what a token gets depends, within these bounds, on how many come with it.
  * Work of long sequences is split over CTAs and joined in a fixed order: results
  * do not vary from run to run.  The library keeps grow-only scratch per stream for
  * that, as for gemm_s4; gemm_release_workspaces frees it.
