@@ -107,6 +107,8 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  *     value is off by up to max|q| / 64516 of its row, a score by up to softmax_scale *
  *     sum|k| times that.  Longer ones take Q as it is.
  * So what a token gets depends, within these bounds, on how many come with it.
+ * GEMM_ERR_TOO_LARGE: batch * kv_heads * (tokens a row of the table can name / 16 + 13) of
+ * 2^30 or more, or max_q * q_heads / kv_heads near 2^31.
  * Work of long sequences is split over CTAs and joined in a fixed order: results
  * do not vary from run to run.  The library keeps grow-only scratch per stream for
  * that, as for gemm_s4; gemm_release_workspaces frees it.

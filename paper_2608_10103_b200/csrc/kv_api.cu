@@ -147,12 +147,12 @@ template <int D, int MAX_NR>
 int attention(const SharedDevice& dev, KvAttnParams& p, cudaStream_t stream) {
   const long long rows = static_cast<long long>(p.max_q) * p.group;
   p.split_rows = 8 * MAX_NR;
-  // the few-rows kernel counts a sequence's tiles by the bound it is given
   KvAttnParams few = p;
   const long long bound = rows < p.split_rows ? rows : p.split_rows;
-  // ... and counts its steps of 16 tokens in 32 bits
+  // The few-rows kernel takes a sequence's rows as one tile (its width goes by this bound) and counts the steps of
+  // 16 tokens of all of them in 32 bits.
   const long long steps = static_cast<long long>(p.max_len) / KVA_STEP + 1 + KVA_UNIT_COST;
-  if (rows + p.group + 512 >= (1ll << 31) || (bound + 7) / 8 * p.c.heads >= (1ll << 30) / steps / p.batch)
+  if (rows + p.group + 512 >= (1ll << 31) || static_cast<long long>(p.batch) * p.c.heads >= (1ll << 30) / steps)
     return GEMM_ERR_TOO_LARGE;
   if (rows > p.split_rows) {
     const int rc = launch_attention_tiles<D>(dev, p, stream);
