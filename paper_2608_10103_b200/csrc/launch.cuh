@@ -1185,7 +1185,7 @@ int check_linear(int M, int N, const void* C, const gemm_epilogue_t* e, const fl
       l.gate_b = 0.07135481282635852f * 1.4426950408889634f;
       break;
     case GEMM_ACT_SILU:
-      l.act = LIN_ACT_GATE;
+      l.act = LIN_ACT_SILU;
       l.gate_a = 1.4426950408889634f;
       break;
     default: return GEMM_ERR_INVALID_ARG;

@@ -8,7 +8,7 @@
 //
 // Activations.  SiLU is x * s(x) with s the logistic function; the tanh form of GELU is
 // 0.5 x (1 + tanh z) = x * s(2 z), z = sqrt(2/pi) (x + 0.044715 x^3).  Both are therefore
-// x * s(x (a + b x^2)), one body for two constants, with s from one exponential and one division
+// x * s(x (a + b x^2)), with b = 0 for SiLU (which leaves the term out: 0 * inf is a NaN), with s from one exponential and one division
 // (ex2.approx, __fdividef): the exponential's relative error, about |u| 2^-22 + 2^-22 at argument u, is
 // weighed by s (1 - s), which leaves an absolute error below 1e-6 |x| everywhere.  GELU proper takes
 // erfc(z) = t (a1 + t (a2 + ... a5 t^3)) exp(-z^2), t = 1 / (1 + p z), for z >= 0 (Abramowitz and Stegun
@@ -32,7 +32,7 @@
 
 namespace b200gemm {
 
-enum LinearAct { LIN_ACT_NONE = 0, LIN_ACT_RELU = 1, LIN_ACT_GATE = 2, LIN_ACT_ERF = 3 };
+enum LinearAct { LIN_ACT_NONE = 0, LIN_ACT_RELU = 1, LIN_ACT_GATE = 2, LIN_ACT_ERF = 3, LIN_ACT_SILU = 4 };
 
 struct LinearEpilogue {
   const float* row_bias;  // indexed by the kernel's rows / columns; at most one of them is set
@@ -42,7 +42,7 @@ struct LinearEpilogue {
   int r_vec_ok;           // 1: 16-byte loads along a row are aligned
   int r_tma;              // 1: the tile kernel fetches it by the copy engine (C goes out the same way)
   int act;                // LinearAct
-  float gate_a, gate_b;   // LIN_ACT_GATE: x * s(x (a + b x^2)), times log2 e
+  float gate_a, gate_b;   // LIN_ACT_GATE: x * s(x (a + b x^2)), LIN_ACT_SILU: x * s(a x); times log2 e
 };
 
 __device__ __forceinline__ float lin_exp2(float x) {
@@ -53,6 +53,8 @@ __device__ __forceinline__ float lin_exp2(float x) {
 __device__ __forceinline__ float lin_gate(float x, float a, float b) {
   return __fdividef(x, 1.0f + lin_exp2(-x * fmaf(b * x, x, a)));
 }
+
+__device__ __forceinline__ float lin_silu(float x, float a) { return __fdividef(x, 1.0f + lin_exp2(-x * a)); }
 
 __device__ __forceinline__ float lin_erf(float x) {
   const float z = fabsf(x) * 0.70710678118654752f;
@@ -70,6 +72,7 @@ __device__ __forceinline__ float lin_activate(float x, const LinearEpilogue& e) 
     case LIN_ACT_RELU: return x < 0.0f ? 0.0f : x;  // (a NaN stays one)
     case LIN_ACT_GATE: return lin_gate(x, e.gate_a, e.gate_b);
     case LIN_ACT_ERF: return lin_erf(x);
+    case LIN_ACT_SILU: return lin_silu(x, e.gate_a);
     default: return x;
   }
 }
@@ -84,6 +87,10 @@ __device__ __forceinline__ void lin_activate_all(float (&x)[N], const LinearEpil
     const float a = e.gate_a, b = e.gate_b;
 #pragma unroll
     for (int v = 0; v < N; ++v) x[v] = lin_gate(x[v], a, b);
+  } else if (e.act == LIN_ACT_SILU) {
+    const float a = e.gate_a;
+#pragma unroll
+    for (int v = 0; v < N; ++v) x[v] = lin_silu(x[v], a);
   } else if (e.act == LIN_ACT_ERF) {
 #pragma unroll
     for (int v = 0; v < N; ++v) x[v] = lin_erf(x[v]);
