@@ -232,7 +232,8 @@ int gemm_s4_linear(int M, int N, int K, const uint8_t* A, const uint8_t* B, cons
  *
  *     row_scale = amax / T,   q[k] = rint(x[k] * (T / amax))
  *
- * in FP32 (IEEE divisions, ties to even).  X: `rows` rows of K binary16
+ * in FP32 (IEEE divisions, ties to even; rows with amax below 2^-64 as if multiplied by
+ * 2^64, which keeps T / amax in range).  X: `rows` rows of K binary16
  * (x_is_fp16 = 1) or FP32 values, row pitch ldx elements (0 = K).  Q: K int8 or
  * K / 2 bytes of packed INT4 per row, as gemm_s8 / gemm_s4 take them; 16-byte
  * aligned.  A row of zeros gets scale 0 and codes 0; a row that holds an infinity

@@ -6,7 +6,8 @@
 // and |q| <= T without a clamp.  A row of zeros gives scale 0 and codes 0.  A row with an infinity
 // or a NaN gives that as its scale and codes of 0 where x * (T / amax) is not a number, so that
 // every result of the product that uses it is NaN rather than plausible: the maximum is taken over
-// the magnitude bits, where infinities and NaN compare above every finite value.
+// the magnitude bits, where infinities and NaN compare above every finite value.  FP32 rows below 2^-64, whose T / amax
+// may leave the type, are multiplied by 2^64 first, which is exact.
 //
 // Bound by reading X once and writing the codes.  A row is kept in registers between its two
 // passes (eight values per piece, QR_PIECES pieces per thread, as they are in memory: all loads are under way
@@ -100,9 +101,10 @@ struct QrPiece {
 };
 
 // The codes of a piece.  FINITE: |x * inverse| <= T for all of the row, and adding 1.5 * 2^23 in FP32 rounds to the nearest
-// even integer and leaves it in the low bits (a conversion instruction per value runs at a quarter of the rate).
+// even integer and leaves it in the low bits (a conversion instruction per value runs at a quarter of the rate).  Rows that
+// are not finite or are tiny go the other way, with a factor `lift` in front.
 template <bool S4, bool FINITE, bool F16>
-__device__ __forceinline__ void qr_store(const QuantRowsParams& p, int row, int piece, float inverse,
+__device__ __forceinline__ void qr_store(const QuantRowsParams& p, int row, int piece, float lift, float inverse,
                                          const QrPiece<F16>& x) {
   float v[8];
   x.values(v);
@@ -110,7 +112,7 @@ __device__ __forceinline__ void qr_store(const QuantRowsParams& p, int row, int 
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     c[i] = FINITE ? __float_as_uint(__fadd_rn(__fmul_rn(v[i], inverse), 12582912.0f))
-                  : static_cast<uint32_t>(__float2int_rn(__fmul_rn(v[i], inverse)));
+                  : static_cast<uint32_t>(__float2int_rn(__fmul_rn(__fmul_rn(v[i], lift), inverse)));
   if constexpr (S4) {
     uint32_t w = 0;
 #pragma unroll
@@ -162,23 +164,24 @@ __global__ void __maxnreg__(F16 ? 48 : 64) quantize_rows_kernel(const QuantRowsP
   if (!live) return;
   constexpr float TOP = S4 ? 7.0f : 127.0f;
   const float amax = __uint_as_float(m);
-  // (FP32 rows whose largest value is below 4e-37: the inverse stays finite, codes come out smaller)
-  const float inverse = m == 0 ? 0.0f : fminf(__fdiv_rn(TOP, amax), 3.402823466e38f);
+  const bool tiny = !F16 && m < 0x1f800000u;  // below 2^-64 (the least binary16 value is 2^-24)
+  const float lift = tiny ? 0x1p64f : 1.0f;
+  const float inverse = m == 0 ? 0.0f : __fdiv_rn(TOP, __fmul_rn(amax, lift));
   if (t == 0) p.scale[row] = __fdiv_rn(amax, TOP);
   auto store = [&](auto finite) {
     constexpr bool FINITE = decltype(finite)::value;
 #pragma unroll
     for (int i = 0; i < QR_PIECES; ++i) {
       const int piece = t + i * p.row_threads;
-      if (piece < pieces) qr_store<S4, FINITE>(p, row, piece, inverse, v[i]);
+      if (piece < pieces) qr_store<S4, FINITE>(p, row, piece, lift, inverse, v[i]);
     }
     for (int piece = t + QR_PIECES * p.row_threads; piece < pieces; piece += p.row_threads) {
       QrPiece<F16> u;
       u.load(p, at + piece * 8);
-      qr_store<S4, FINITE>(p, row, piece, inverse, u);
+      qr_store<S4, FINITE>(p, row, piece, lift, inverse, u);
     }
   };
-  if (m < 0x7f800000u)
+  if (m < 0x7f800000u && !tiny)
     store(std::true_type());
   else
     store(std::false_type());
