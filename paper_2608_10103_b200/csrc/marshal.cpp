@@ -20,6 +20,8 @@ struct Refused {
   std::string text;
 };
 
+struct Raised {};  // a Python error is set already
+
 struct Entries {
   decltype(&gemm_fp16_linear) fp16_linear;
   decltype(&gemm_s8_linear) s8_linear;
@@ -64,6 +66,19 @@ int narrow(int64_t v, const char* what) {
   return static_cast<int>(v);
 }
 
+// Python numbers.  What is no integer (or number) raises Python's own TypeError.
+int integer(PyObject* o, const char* what) {
+  int overflow = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+  if (v == -1 && !overflow && PyErr_Occurred()) throw Raised{};
+  return narrow(overflow ? INT64_MAX : v, what);
+}
+float number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw Raised{};
+  return static_cast<float>(v);
+}
+
 // A matrix whose rows are contiguous: pointer and row pitch.
 void* rows_of(const at::Tensor& t, int64_t rows, int64_t cols, const char* what, long long* pitch) {
   if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols)
@@ -103,6 +118,7 @@ PyObject* guarded(F&& f) {
   try {
     g_device = -1;
     return f();
+  } catch (const Raised&) {
   } catch (const Refused& r) {
     PyErr_SetString(r.type, r.text.c_str());
   } catch (const std::exception& e) {
@@ -123,7 +139,7 @@ bool arity(Py_ssize_t n, Py_ssize_t want) {
 PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 11)) return nullptr;
   return guarded([&]() -> PyObject* {
-    const long precision = PyLong_AsLong(a[0]);
+    const int precision = integer(a[0], "precision");
     const at::ScalarType in = precision == GEMM_PREC_FP16 ? at::kHalf : precision == GEMM_PREC_S8 ? at::kChar : at::kByte;
     const at::Tensor &A = typed(a[1], in, "A"), &B = typed(a[2], in, "B");
     if (A.dim() != 2 || B.dim() != 2 || A.size(1) != B.size(1))
@@ -131,7 +147,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int M = narrow(A.size(0), "M"), N = narrow(B.size(0), "N");
     const int K = narrow(A.size(1) * (precision == GEMM_PREC_S4 ? 2 : 1), "K");
     gemm_epilogue_t e = {};
-    e.activation = static_cast<int>(PyLong_AsLong(a[6]));
+    e.activation = integer(a[6], "activation");
     const Launch s = stream_of(a[10]);
     at::ScalarType out = PyObject_IsTrue(a[9]) ? at::kHalf : at::kFloat;
     at::Tensor C;
@@ -172,7 +188,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 5)) return nullptr;
   return guarded([&]() -> PyObject* {
-    const int precision = static_cast<int>(PyLong_AsLong(a[0]));
+    const int precision = integer(a[0], "precision");
     const at::Tensor& X = tensor(a[1], "X");
     if (X.dim() != 2 || (X.scalar_type() != at::kHalf && X.scalar_type() != at::kFloat))
       throw Refused{PyExc_TypeError, "X must be a float16 or float32 matrix"};
@@ -276,8 +292,9 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k.tokens != v.tokens || k.token != v.token || k.head != v.head)
       throw Refused{PyExc_ValueError, "k and v must have the same shape and strides"};
     const Batch b = batch_of(a[3], a[4], a[5], "past");
+    const int max_new = integer(a[6], "max_new");
     if (k.tokens == 0) Py_RETURN_NONE;
-    const int rc = g_entry.kv_append(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[6])),
+    const int rc = g_entry.kv_append(&c, b.batch, b.cu, b.start, b.table, b.width, max_new,
                                      k.ptr, v.ptr, k.token, k.head, narrow(k.tokens, "tokens"), stream_of(a[7]).handle);
     if (rc) return code(rc);
     Py_RETURN_NONE;
@@ -290,6 +307,7 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     const kv_cache_s8_t c = cache_of(a[0]);
     const Batch b = batch_of(a[1], a[2], a[3], "first");
+    const int max_read = integer(a[4], "max_read");
     const Launch s = stream_of(a[7]);
     at::Tensor out[2];
     if (a[6] != Py_None) {
@@ -302,12 +320,12 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
     } else {
       // (not given: cu[-1], which waits for the device)
-      const int64_t tokens = a[5] == Py_None ? THPVariable_Unpack(a[1]).select(0, b.batch).item<int>() : PyLong_AsLongLong(a[5]);
+      const int64_t tokens = a[5] == Py_None ? THPVariable_Unpack(a[1]).select(0, b.batch).item<int>() : integer(a[5], "tokens");
       if (tokens < 0) throw Refused{PyExc_ValueError, "tokens must not be negative"};
       for (auto& t : out) t = new_out({tokens, c.kv_heads, c.head_dim}, at::kHalf, s);
     }
     if (out[0].size(0) > 0) {
-      const int rc = g_entry.kv_read(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[4])),
+      const int rc = g_entry.kv_read(&c, b.batch, b.cu, b.start, b.table, b.width, max_read,
                                      out[0].data_ptr(), out[1].data_ptr(), narrow(out[0].size(0), "tokens"), s.handle);
       if (rc) return code(rc);
     }
@@ -328,6 +346,8 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& qt = typed(a[0], at::kHalf, "q");
     const Rows q = heads_of(qt, 0, c.head_dim, "q");
     const Batch b = batch_of(a[2], a[3], a[4], "kv_len");
+    const int max_q = integer(a[5], "max_q"), window = integer(a[7], "window");
+    const float scale = number(a[6]);
     const Launch s = stream_of(a[9]);
     at::Tensor out;
     if (a[8] != Py_None) {
@@ -339,9 +359,8 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows o = heads_of(out, 0, c.head_dim, "out");
     if (o.head != c.head_dim) throw Refused{PyExc_ValueError, "the heads of a row of out must be contiguous"};
     if (q.tokens > 0) {
-      const int rc = g_entry.kv_attention(&c, b.batch, b.cu, b.start, b.table, b.width, static_cast<int>(PyLong_AsLong(a[5])),
-                                          narrow(q.heads, "heads"), q.ptr, q.token, q.head, static_cast<float>(PyFloat_AsDouble(a[6])),
-                                          static_cast<int>(PyLong_AsLong(a[7])), out.data_ptr(), o.token,
+      const int rc = g_entry.kv_attention(&c, b.batch, b.cu, b.start, b.table, b.width, max_q, narrow(q.heads, "heads"), q.ptr,
+                                          q.token, q.head, scale, window, out.data_ptr(), o.token,
                                           narrow(q.tokens, "tokens"), s.handle);
       if (rc) return code(rc);
     }
