@@ -6,6 +6,7 @@
 // Every function returns its result, or the negative GEMM_ERR_* code of the entry point as an int.
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -103,12 +104,15 @@ Launch stream_of(PyObject* o) {
   return {reinterpret_cast<gemm_stream_t>(s), s != current};
 }
 
+c10::cuda::CUDAStream torch_stream(const Launch& s) {
+  return c10::cuda::getStreamFromExternal(reinterpret_cast<cudaStream_t>(s.handle), device());
+}
+
 // An output of our own: if the work runs on another stream than the current one, the allocator must
 // not hand its memory on before that stream is done with it.
 at::Tensor new_out(at::IntArrayRef shape, at::ScalarType type, const Launch& s) {
   at::Tensor t = at::empty(shape, at::TensorOptions().dtype(type).device(at::kCUDA, device()));
-  if (s.foreign)
-    t.record_stream(c10::cuda::getStreamFromExternal(reinterpret_cast<cudaStream_t>(s.handle), device()).unwrap());
+  if (s.foreign) t.record_stream(torch_stream(s).unwrap());
   return t;
 }
 
@@ -319,8 +323,14 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
           throw Refused{PyExc_ValueError, "outputs are two (tokens, kv_heads, head_dim)"};
       }
     } else {
-      // (not given: cu[-1], which waits for the device)
-      const int64_t tokens = a[5] == Py_None ? THPVariable_Unpack(a[1]).select(0, b.batch).item<int>() : integer(a[5], "tokens");
+      int64_t tokens;
+      if (a[5] == Py_None) {  // cu[-1], in the order of the stream, which is waited for
+        c10::cuda::OptionalCUDAStreamGuard on;
+        if (s.foreign) on.reset_stream(torch_stream(s));
+        tokens = THPVariable_Unpack(a[1]).reshape(-1).select(0, b.batch).item<int>();
+      } else {
+        tokens = integer(a[5], "tokens");
+      }
       if (tokens < 0) throw Refused{PyExc_ValueError, "tokens must not be negative"};
       for (auto& t : out) t = new_out({tokens, c.kv_heads, c.head_dim}, at::kHalf, s);
     }
