@@ -33,7 +33,9 @@ struct Entries {
   decltype(&kv_attention_s8_rows) kv_attention;
 } g_entry = {};
 
-int g_device = -1;  // the current device, asked for once a call (with the first CUDA tensor)
+// The current device, asked for once a call (with the first CUDA tensor).  Per thread: kv_read lets other threads run
+// while it waits for a count.
+thread_local int g_device = -1;
 int device() {
   if (g_device < 0) g_device = c10::cuda::current_device();
   return g_device;
