@@ -1,4 +1,5 @@
-"""ctypes binding of libb200gemm.so: argument marshalling only.
+"""Binding of libb200gemm.so: argument marshalling only, by ctypes or, for the linear layers, row
+quantisation and the key/value cache, by a compiled module (csrc/marshal.cpp).
 
 Every function here has the name and meaning of the C entry point it calls
 (see include/b200gemm.h); tensors are torch CUDA tensors used purely as device

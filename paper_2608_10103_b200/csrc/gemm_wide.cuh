@@ -422,7 +422,7 @@ gemm_wide_kernel(const __grid_constant__ CUtensorMap tmap_a,
             for (int h = 0; h < BLOCK_COLS / 32; ++h) {
               const int c32 = col + h * 32, cc = c32 + lane;
               uint32_t res[C_ELEM * 8];
-              if (p.lin.residual) lin_load_residual<C_ELEM, 32>(p.lin, row, c32, p.M, p.N, 0, res);
+              if (p.lin.residual) lin_load_residual<C_ELEM, 32>(p.lin, row, c32, p.M, p.N, res);
               const float cs_mine = (p.col_scale && cc < p.N) ? ptx::ld_global_f32(p.col_scale + cc) : 0.0f;
               const float cb_mine =
                   (p.lin.col_bias && cc < p.N) ? ptx::ld_global_f32(p.lin.col_bias + cc) : 0.0f;

@@ -805,6 +805,8 @@ bool few_rows_wanted(int M, int N, int K, bool packed_s4, const OutputSpec& out,
   if (packed_s4) return true;
   // A CTA's time grows with the length of a row (its 16 warps share it), the tile kernels
   // split K over as many CTAs as it takes: few row blocks against long rows stay on tiles.
+  // (Both rules were measured with raw results.  Linear layers go by them too, unmeasured; their
+  // tiles can only share K inside a cluster of up to four.)
   const long long row_bytes = fp16 ? 2LL * K : K;
   if (ceil_div(longer, 16 * FEW_ROWS_MT) < 6 * ceil_div(row_bytes, 1024)) return false;
   if (fp16) return static_cast<long long>(longer) * K <= (32LL << 20);

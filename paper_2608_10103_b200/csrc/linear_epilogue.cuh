@@ -212,11 +212,11 @@ __device__ __forceinline__ void lin_block_copy(uint32_t buf, void* global, long 
 // from the grid in front, whose end the caller has awaited.
 template <int BYTES, int N>
 __device__ __forceinline__ void lin_load_residual(const LinearEpilogue& e, int row, int col, int m,
-                                                  int n, int transposed, uint32_t (&r)[BYTES * N / 4]) {
+                                                  int n, uint32_t (&r)[BYTES * N / 4]) {
 #pragma unroll
   for (int v = 0; v < BYTES * N / 4; ++v) r[v] = 0;
   if (row >= m) return;
-  if (!transposed && e.r_vec_ok && col + N <= n) {
+  if (e.r_vec_ok && col + N <= n) {
     const char* at = static_cast<const char*>(e.residual) +
                      (static_cast<long long>(row) * e.ldr + col) * BYTES;
 #pragma unroll
@@ -227,12 +227,10 @@ __device__ __forceinline__ void lin_load_residual(const LinearEpilogue& e, int r
                    : "memory");
     return;
   }
-  const long long base = transposed ? row : static_cast<long long>(row) * e.ldr;
-  const long long step = transposed ? e.ldr : 1;
 #pragma unroll
   for (int v = 0; v < N; ++v) {
     if (col + v >= n) continue;
-    const long long at = base + (col + v) * step;
+    const long long at = static_cast<long long>(row) * e.ldr + col + v;
     if constexpr (BYTES == 4) {
       asm volatile("ld.global.u32 %0, [%1];"
                    : "=r"(r[v])
