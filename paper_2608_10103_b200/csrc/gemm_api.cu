@@ -8,7 +8,6 @@
 #include <string.h>
 
 #include <mutex>
-#include <new>
 
 #include <chrono>
 #include "../../include/b200gemm.h"
@@ -42,12 +41,7 @@ int shared_cuda_fail(cudaError_t e) { return cuda_fail(e); }
 
 int shared_scratch(int device, cudaStream_t stream, size_t need, size_t head, SharedLease* out) {
   ScratchPool::Lease l;
-  int rc;
-  try {
-    rc = g_kv_pool[device].acquire(stream, need, head, &l);
-  } catch (const std::bad_alloc&) {  // the pool's list of buffers could not grow: no exception leaves the C entry
-    rc = cudaErrorMemoryAllocation;
-  }
+  const int rc = g_kv_pool[device].acquire(stream, need, head, &l);
   if (rc != 0) return pool_fail(rc);
   out->ptr = l.ptr;
   out->head = l.ptr;

@@ -234,6 +234,7 @@ ScratchPool g_pool[MAX_DEVICES];
 
 int pool_fail(int rc) {
   if (rc == ScratchPool::kNoAllocInCapture) return cuda_fail(cudaErrorStreamCaptureUnsupported);
+  if (rc == ScratchPool::kNoHostMemory) return cuda_fail(cudaErrorMemoryAllocation);
   return cuda_fail(static_cast<cudaError_t>(rc));
 }
 }  // namespace

@@ -29,6 +29,7 @@
 #include <stddef.h>
 
 #include <mutex>
+#include <new>
 #include <vector>
 
 namespace b200gemm {
@@ -52,7 +53,9 @@ class WorkspacePool {
   // zeroed when the buffer was allocated (and is never cleared again by the pool: whatever
   // lives there must leave it consistent).  0 = ok, else the backend's error code;
   // kNoAllocInCapture when the stream is being captured and no buffer is large enough.
+  // kNoHostMemory when the list of buffers cannot grow; nothing is thrown.
   static constexpr int kNoAllocInCapture = -1000;
+  static constexpr int kNoHostMemory = -1001;
   int acquire(Stream s, size_t need, size_t head, Lease* out) {
     std::lock_guard<std::mutex> lock(mutex_);
     const bool cap = backend_.capturing(s);
@@ -83,6 +86,13 @@ class WorkspacePool {
           mine = static_cast<int>(i);
       for (size_t i = 0; i < entries_.size() && mine < 0; ++i)  // or an emptied slot
         if (!entries_[i].leased && !entries_[i].ptr) mine = static_cast<int>(i);
+      if (mine < 0) {
+        try {
+          entries_.reserve(entries_.size() + 1);
+        } catch (const std::bad_alloc&) {
+          return kNoHostMemory;
+        }
+      }
       // a replacement is never smaller than what it replaces, in either part
       if (mine >= 0 && entries_[mine].ptr) {
         if (entries_[mine].bytes > need) need = entries_[mine].bytes;
