@@ -93,16 +93,15 @@ enum EpiMode {
   EPI_LIN32 = 4,       // ... as FP32
 };
 __host__ __device__ constexpr bool epi_linear(int epi) { return epi >= EPI_LIN16; }
-// FP32 results of FP16 linear layers are summed in parts of ACC_PART_BYTES of K.  The tensor core's FP32
+// FP32 results of FP16 linear layers are summed in parts of K (GemmParams::acc_part).  The tensor core's FP32
 // accumulator drops the bits that do not fit instead of rounding, so the error grows with the length of the chain
-// and has one sign: 1.2e-9 K of the result's norm, 1.9e-5 at K = 16408, where a rounded FP32 sum leaves 2e-6.  A
+// and has one sign: 1.2e-9 a product of the result's norm, 1.9e-5 at K = 16408, where a rounded FP32 sum leaves 2e-6.  A
 // tile's first part stays in one accumulator buffer, each later one goes to the other, and the epilogue adds it to
-// the first in FP32: 2.5e-6 however long K is, for 3-4 % of the time (4096 x 4096 x 4096: 102 -> 105 us, K = 16384:
-// 392 -> 409).  (Binary16 results, 2.4e-4 by their own rounding, need none of it.)
-constexpr int ACC_PART_BYTES = 4096;
-__host__ __device__ constexpr int acc_part_atoms(int kind, int epi) {
-  return kind == ptx::KIND_F16 && epi == EPI_LIN32 ? ACC_PART_BYTES / BK_BYTES : 0;
-}
+// the first in FP32, while the products wait.  How long a part is: acc_part_atoms.  Keeping the sum in registers, so that
+// both buffers are free for the products, took longer (4096 x 4096 x 4096 in parts of 640: 141 us against 138): its
+// unrolled code is fetched cold and the registers spill.  (Binary16 results, 2.4e-4 by their own rounding, need none
+// of it.)
+__host__ __device__ constexpr bool acc_parts(int kind, int epi) { return kind == ptx::KIND_F16 && epi == EPI_LIN32; }
 __host__ __device__ constexpr bool epi_out16(int epi) { return epi == EPI_OUT16 || epi == EPI_LIN16; }
 
 struct GemmParams {
@@ -143,6 +142,7 @@ struct GemmParams {
   const float* row_scale;  // EPI_OUT16 (integer kinds) / EPI_F32_SCALED: M per-row factors
   const float* col_scale;  // and N per-column factors; both null = no scaling (FP16 kind)
   LinearEpilogue lin;      // EPI_LIN16 / EPI_LIN32: bias, activation, residual
+  int acc_part;            // FP32 results of FP16 linear layers: ring slots of K in a part
   int* status;           // device status word (0 = ok)
   // Optional per-CTA cycle accounting (TRACE_SLOTS 64-bit words per CTA), or null.
   unsigned long long* trace;
@@ -291,8 +291,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
   constexpr int BK_ELEMS = BK_BYTES / ELEM_BYTES;
   constexpr int TILE_M = BM * CTA_GROUP;
   constexpr uint32_t TMEM_COLS = (2 * BN <= 32) ? 32 : 2 * BN;  // two accumulator buffers
-  // Ring slots after which FP32 results of FP16 linear layers change accumulators (0: never).
-  constexpr int ACC_PART = acc_part_atoms(KIND, EPI) / KB;
+  constexpr bool ACC_PARTS = acc_parts(KIND, EPI);
   static_assert(CTA_GROUP == 1 || CTA_GROUP == 2, "CTA_GROUP is 1 or 2");
   static_assert(BN % 32 == 0 && BN >= 32 && BN <= 256, "BN must be a multiple of 32 up to 256");
   static_assert((TMEM_COLS & (TMEM_COLS - 1)) == 0 && TMEM_COLS <= 512, "TMEM columns: power of 2");
@@ -623,8 +622,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
         };
         int part_begin = k_begin;
         for (int ks = k_begin; ks < k_end; ++ks) {
-          if constexpr (ACC_PART > 0) {
-            if (ks == part_begin + ACC_PART) {  // the next part: into the other buffer, once its last one is added
+          if constexpr (ACC_PARTS) {
+            if (ks == part_begin + p.acc_part) {  // the next part: into the other buffer, once its last one is added
               commit_acc();
               acc = first_acc ^ 1;
               ok = wait_bounded(acc_empty_bar(acc), ((acc_phase >> acc) & 1u) ^ 1u, abort_flag, p.status,
@@ -1094,8 +1093,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ 
       epi_wait += w1 - w0;
       if (!ok) break;
       ptx::tc_fence_after_sync();
-      if constexpr (ACC_PART > 0) {  // the later parts of K: add each to the first, in the columns this warp reads below
-        for (int ks = k_begin + ACC_PART; ks < k_end; ks += ACC_PART) {
+      if constexpr (ACC_PARTS) {  // the later parts of K: add each to the first, in the columns this warp reads below
+        for (int ks = k_begin + p.acc_part; ks < k_end; ks += p.acc_part) {
           const int part = acc ^ 1;
           ok = wait_bounded<true>(acc_full_bar(part), (acc_phase >> part) & 1u, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
           ok = __all_sync(0xffffffffu, ok);

@@ -2,6 +2,8 @@
 // shared by the entry points, the INT4 pre-pass and its workspaces.
 #pragma once
 
+#include <math.h>
+
 #include <utility>
 
 #include "few_rows.cuh"
@@ -407,6 +409,19 @@ bool swap_ab_wanted(int M, int N, bool integer_kind, const OutputSpec& out) {
   return N >= 1024 && M <= ((integer_kind || epi_out16(out.epi) || N >= 16384) ? 64 : 32);
 }
 
+// FP32 results of FP16 linear layers: atoms (64 values) of K that an accumulator sums before its part is added to the
+// rest.  A chain of L products cuts off 1.2e-9 L of the result's norm; the roundings of an FP32 sum over K leave 1.8e-8
+// sqrt(K).  L = 20 sqrt(K) keeps the former within 1.4 times the latter; 640 at least (0.8e-6) and 2048 at most.  Narrow
+// problems, where library sums split K and are off by less, always take 640.  Measured, against parts of 2048
+// throughout (2.5e-6): 4096 x 4096 x 4096 in 1280 120 -> 128 us (960: 132, 640: 138), 2000 x 2000 x 2048 25.8 -> 26.8,
+// 40 x 2048 x 4096 11.9 -> 12.5; K = 16384 as before.
+int acc_part_atoms(int K, bool narrow) {
+  constexpr int LEAST = 10, MOST = 32;
+  if (narrow) return LEAST;
+  const int atoms = static_cast<int>(20.0 / 64.0 * sqrt(static_cast<double>(K)));
+  return atoms < LEAST ? LEAST : atoms > MOST ? MOST : atoms;
+}
+
 // Returned (never to the caller of the library) when the fused INT4 kernel does not cover the
 // shape the selector picked: the entry point then takes the pre-pass route.
 constexpr int GEMM_NOT_FUSED = 1;
@@ -495,9 +510,10 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
 
   // (a call that asks for the overlapped INT4 pre-pass stays on the kernel that has that role)
   // (the wide kernel's two accumulators fill TMEM: K that is summed in parts stays on the other tiles)
-  constexpr int PART = acc_part_atoms(KIND, EPI);
-  const bool wide = !req && (PART == 0 || k_blocks <= PART) && wide_wanted(cfg, M, N, k_blocks, s->num_sms, swap, csplit, packed_s4,
-                                        KIND == ptx::KIND_F16);
+  constexpr bool PARTS = acc_parts(KIND, EPI);
+  const int part_atoms = acc_part_atoms(K, M <= 128 || N <= 128);
+  const bool wide = !req && (!PARTS || k_blocks <= part_atoms) &&
+                    wide_wanted(cfg, M, N, k_blocks, s->num_sms, swap, csplit, packed_s4, KIND == ptx::KIND_F16);
   if (wide) {
     cfg.bn = WIDE_BN;
     cfg.cta_group = 2;
@@ -551,6 +567,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   // policy bit 32: plain stream order; so are traced launches, whose cycle counts would
   // otherwise include the time spent waiting for the predecessor's tail
   p.wait_prior_grid = ((g_l2_policy & 32) || (g_trace_on & 1)) ? 0 : 1;
+  if (PARTS) p.acc_part = part_atoms / (cfg.bn <= 128 ? 2 : 1);  // (tiles of up to 128 columns: two atoms a slot)
   p.c_vec_ok = !swap && (ldc % (16 / C_ELEM) == 0) && (reinterpret_cast<uintptr_t>(C) % 16 == 0);
   // 16-byte stores must end on a row's end (the copy engine clips a box at N, but writes whole
   // 16-byte pieces: with a pitch beyond N, N = 1100 binary16 columns had zeros put behind them)
