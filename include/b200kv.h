@@ -98,7 +98,9 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  * Q, out: binary16, element (row, head, d) at row * token_stride + head * head_dim + d for
  * out, row * q_token_stride + head * q_head_stride + d for Q.  max_q: an upper bound of n
  * over the batch (rows beyond it are not computed, status 6).
- * Scores, softmax statistics and sums are FP32.  Two operands have fewer bits:
+ * Scores, softmax statistics and sums are FP32.  The tensor cores' sums of weighted values cut
+ * off what does not fit, up to 2e-9 of the result per token of one sum: 16384 tokens at most, or for
+ * sequences of few rows (below) up to a quarter of the sequence.  Two operands have fewer bits:
  *   - the softmax weights (times their page's value scale) are rounded to binary16 for the
  *     product with the codes, which are exact there: by 2^-11 of themselves, or up to 2^-32 of
  *     the row's largest where they are below 2^-21 of it;

@@ -130,14 +130,23 @@ int launch_attention_tiles(const SharedDevice& dev, KvAttnParams p, cudaStream_t
     if (most > 16) most = 16;
     if (most > 1) p.splits = static_cast<int>(most);
   }
-  if (p.splits == 1)
+  // Sums of long sequences: one CTA is resident per SM (its registers are all of them), so as many slots do.
+  const bool long_sums = p.max_len > T::SUM_TILES * T::TN;
+  if (p.splits == 1 && !long_sums)
     return launch(dev, kernel, dim3(static_cast<unsigned>(blocks)), T::THREADS, T::DYN_BYTES, stream, p);
+  const size_t parts = p.splits > 1 ? static_cast<size_t>(blocks) * p.splits * T::ROWS * (D + 4) * 4 : 0;
+  const size_t counters = p.splits > 1 ? static_cast<size_t>(blocks) : 0;
+  p.slots = long_sums ? dev.num_sms : 0;
   SharedLease lease;
-  const int rc = shared_scratch(dev.device, stream, static_cast<size_t>(blocks) * p.splits * T::ROWS * (D + 4) * 4,
-                                (static_cast<size_t>(blocks) * 4 + 255) / 256 * 256, &lease);
+  const int rc = shared_scratch(dev.device, stream, parts + static_cast<size_t>(p.slots) * T::ROWS * D * 4,
+                                ((counters + p.slots) * 4 + 255) / 256 * 256, &lease);
   if (rc != GEMM_OK) return rc;
   p.arrived = static_cast<unsigned*>(lease.head);
   p.partial = static_cast<float*>(lease.data);
+  if (long_sums) {
+    p.taken = p.arrived + counters;
+    p.long_sums = p.partial + parts / 4;
+  }
   const int launched = launch(dev, kernel, dim3(static_cast<unsigned>(blocks * p.splits)), T::THREADS, T::DYN_BYTES, stream, p);
   const int done = shared_scratch_done(dev.device, stream, lease);
   return launched != GEMM_OK ? launched : done;

@@ -91,6 +91,9 @@ struct KvAttnParams {
   float* partial;    // [2 * grid][rows * D + rows * 2]
   unsigned* arrived; // per unit, zero before and after
   int splits;        // tile kernel: CTAs a row tile's tokens are divided over
+  float* long_sums;  // tile kernel: [slots][rows of a CTA][D] for CTAs with many tokens, or null
+  unsigned* taken;   // per slot, zero before and after
+  int slots;         // as many as CTAs can be resident
 };
 
 // A sequence's rows and length, cut to what the packed arrays, the table and the caller's bound allow.

@@ -61,6 +61,10 @@ struct KvTileShape {
   static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
   static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
   static constexpr uint32_t O_COLUMN = 256;        // S (and P) of tile q at 128 q, O behind both
+  // O is summed in tensor memory over this many tiles of tokens at most, 16384 tokens: the accumulator cuts off what does
+  // not fit, 1e-9 to 2e-9 of the result a token, all with one sign (131072 tokens in one sum: 1.3e-4 to 2.8e-4, as much
+  // as the rounding to binary16).  Then the rows' threads add it to a sum in scratch.
+  static constexpr int SUM_TILES = 16384 / TN;
   static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");
   static_assert(O_COLUMN + QT * D <= 512, "tensor memory");
 };
@@ -196,7 +200,20 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
     hi = min(hi, lo + tiles * TN);
   }
 
+  __shared__ int s_slot;  // of the sums in scratch; -1 = none needed
   if (tid == 0) {
+    s_slot = -1;
+    if (p.long_sums && tiles > T::SUM_TILES) {
+      // There are as many slots as CTAs at a time, so one is free at any time; which one may change while this looks
+      // at them, hence the (limited) rounds.  The one that the SM's last CTA had is as a rule free at once.
+      uint32_t sm;
+      asm volatile("mov.u32 %0, %%smid;" : "=r"(sm));
+      for (int i = 0; i < 1000 * p.slots && s_slot < 0; ++i) {
+        const int slot = static_cast<int>((sm + static_cast<uint32_t>(i)) % static_cast<uint32_t>(p.slots));
+        if (atomicCAS(p.taken + slot, 0u, 1u) == 0u) s_slot = slot;
+      }
+      __threadfence();
+    }
     ptx::mbar_init(q_full, T::SOFTMAX_WARPS);
     for (int i = 0; i < STAGES; ++i) {
       ptx::mbar_init(k_full(i), 4);
@@ -227,6 +244,9 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   __syncthreads();
   ptx::tc_fence_after_sync();
   const uint32_t tmem = *tmem_holder;
+  const int slot = s_slot;
+  // the tile whose products start a new sum in tensor memory
+  auto new_sum = [&](int j) { return j == 0 || (slot >= 0 && (j & (T::SUM_TILES - 1)) == 0); };
 
   if constexpr (QT == 2) {
     // Register shares of the four groups of four warps, which sum up to the 4 x 128 they were launched with:
@@ -273,6 +293,9 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
     // A row with a NaN or an infinity is NaN if it sees anything, also where all its scores are -inf.
     const bool q_bad = max(q_top & 0xffffu, q_top >> 16) >= 0x7c00u && pos >= 0;
     float m = -INFINITY, l = q_bad ? __int_as_float(0x7fffffff) : 0.0f;
+    float* const long_sum = p.long_sums + (static_cast<long long>(max(slot, 0)) * T::ROWS + r) * D;
+    float long_m = -INFINITY;  // reference of the sum in scratch
+    auto long_factor = [&]() { return long_m == -INFINITY ? 0.0f : exp2_approx(long_m - m); };
     bool ok = true;
     const int my_tiles = q < active ? tiles : 0;
 #pragma unroll 1
@@ -309,7 +332,8 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
         top = fmaxf(top, fmaf(mx, c.x, c.y));
       }
       const bool grow = top > m + 8.0f;
-      if (__any_sync(0xffffffffu, grow)) {
+      const bool move = j > 0 && new_sum(j);
+      if (__any_sync(0xffffffffu, grow) || move) {
         const float now = grow ? top : m;
         const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
         m = now;
@@ -319,6 +343,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           ptx::tc_fence_after_sync();
+          const float of_old = long_factor();
 #pragma unroll 1
           for (int c = 0; c < D; c += 16) {
             uint32_t y[16];  // (few registers: the scores are in the others)
@@ -326,8 +351,20 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
             ptx::tmem_wait_ld();
 #pragma unroll
             for (int v = 0; v < 16; ++v) y[v] = __float_as_uint(__uint_as_float(y[v]) * f);
-            ptx::tmem_st_32x32b_x16(o_at + c, y);
+            if (move) {
+#pragma unroll 1
+              for (int v = 0; v < 16; ++v) {
+                float sum = __uint_as_float(y[0]);
+#pragma unroll
+                for (int u = 0; u < 15; ++u) y[u] = y[u + 1];
+                if (j > T::SUM_TILES) sum = fmaf(__ldcg(long_sum + c + v), of_old, sum);
+                __stcg(long_sum + c + v, sum);
+              }
+            } else {
+              ptx::tmem_st_32x32b_x16(o_at + c, y);
+            }
           }
+          if (move) long_m = m;
           ptx::tmem_wait_st();
         }
       }
@@ -387,6 +424,11 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
         if (tiles > 0) {
           ptx::tmem_ld_32x32b_x32(o_at + c, x);
           ptx::tmem_wait_ld();
+          if (slot >= 0) {
+            const float of_old = long_factor();
+#pragma unroll
+            for (int v = 0; v < 32; ++v) x[v] = __float_as_uint(fmaf(__ldcg(long_sum + c + v), of_old, __uint_as_float(x[v])));
+          }
         }
         if (!live) continue;
         if (p.splits > 1) {  // O as it stands, to be joined
@@ -549,7 +591,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
 #pragma unroll
         for (int kk = 0; kk < TN / 16; ++kk) {
           const uint64_t v = ptx::smem_desc_sw128_mn(base + T::V_OFFSET + (j & 1) * T::KV_BYTES + kk * 2048, T::CHUNK);
-          ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + q * 128 + kk * 8, v, idesc_pv, j > 0 || kk > 0);
+          ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + q * 128 + kk * 8, v, idesc_pv, !new_sum(j) || kk > 0);
         }
         ptx::mma_commit<1>(o_done(q));
       }
@@ -603,6 +645,10 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   if (warp == T::SOFTMAX_WARPS + 4) {
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc<1>(tmem, 512);
+  }
+  if (tid == 0 && slot >= 0) {  // (the rows' threads are done with it)
+    __threadfence();
+    atomicExch(p.taken + slot, 0u);
   }
   if (p.splits > 1) {
     // ---- the CTA that finishes a row tile last joins its parts, in their order
