@@ -194,8 +194,8 @@ int gemm_s4_dequant(int M, int N, int K, const uint8_t* A, const uint8_t* B,
  * computed in FP32 and rounded once where C is binary16.  (The tensor cores' FP32
  * accumulators cut off what does not fit instead of rounding: a sum of L binary16 products
  * is off by about 1.2e-9 L of the result's norm.  Where results are FP32 their K is summed in parts
- * of 640 to 20 sqrt(K), at most 2048, so that they are off by 1e-6 or 1.4 times what the
- * roundings of an FP32 sum leave, whichever is more.)  A, B, K rules, scales
+ * of 640, for results of a million and more up to 20 sqrt(K) and at most 2048, so that they are
+ * off by 1e-6 or 1.4 times what the roundings of an FP32 sum leave, whichever is more.)  A, B, K rules, scales
  * and (INT4) the internal workspace are those of gemm_fp16, gemm_s8_dequant and
  * gemm_s4_dequant.  C and residual have the same element type and may have row
  * pitches of their own (a column block of a larger matrix); they need only the

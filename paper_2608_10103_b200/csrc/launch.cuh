@@ -411,13 +411,14 @@ bool swap_ab_wanted(int M, int N, bool integer_kind, const OutputSpec& out) {
 
 // FP32 results of FP16 linear layers: atoms (64 values) of K that an accumulator sums before its part is added to the
 // rest.  A chain of L products cuts off 1.2e-9 L of the result's norm; the roundings of an FP32 sum over K leave 1.8e-8
-// sqrt(K).  L = 20 sqrt(K) keeps the former within 1.4 times the latter; 640 at least (0.8e-6) and 2048 at most.  Narrow
-// problems, where library sums split K and are off by less, always take 640.  Measured, against parts of 2048
+// sqrt(K).  L = 20 sqrt(K) keeps the former within 1.4 times the latter; 640 at least (0.8e-6) and 2048 at most.  Where a
+// library's FP32 product would split a long K for want of tiles and be off by less (narrow results, and up to a
+// million: 652 x 176 x 12536 2.4e-6 against 0.8e-6), it is always 640.  Measured, against parts of 2048
 // throughout (2.5e-6): 4096 x 4096 x 4096 in 1280 120 -> 128 us (960: 132, 640: 138), 2000 x 2000 x 2048 25.8 -> 26.8,
 // 40 x 2048 x 4096 11.9 -> 12.5; K = 16384 as before.
-int acc_part_atoms(int K, bool narrow) {
+int acc_part_atoms(int M, int N, int K) {
   constexpr int LEAST = 10, MOST = 32;
-  if (narrow) return LEAST;
+  if (M <= 128 || N <= 128 || static_cast<long long>(M) * N < (1 << 20)) return LEAST;
   const int atoms = static_cast<int>(20.0 / 64.0 * sqrt(static_cast<double>(K)));
   return atoms < LEAST ? LEAST : atoms > MOST ? MOST : atoms;
 }
@@ -511,7 +512,7 @@ int launch_gemm_epi(int M, int N, int K, const void* A, size_t a_pitch, const vo
   // (a call that asks for the overlapped INT4 pre-pass stays on the kernel that has that role)
   // (the wide kernel's two accumulators fill TMEM: K that is summed in parts stays on the other tiles)
   constexpr bool PARTS = acc_parts(KIND, EPI);
-  const int part_atoms = acc_part_atoms(K, M <= 128 || N <= 128);
+  const int part_atoms = acc_part_atoms(M, N, K);
   const bool wide = !req && (!PARTS || k_blocks <= part_atoms) &&
                     wide_wanted(cfg, M, N, k_blocks, s->num_sms, swap, csplit, packed_s4, KIND == ptx::KIND_F16);
   if (wide) {
