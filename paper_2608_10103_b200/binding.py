@@ -36,6 +36,7 @@ KV_EXPORTS = ("kv_append_s8", "kv_read_s8", "kv_attention_s8",   # include/b200k
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
+# Structures of the C entry points, for calls by ctypes (the functions below go through the compiled module).
 class _Epilogue(ctypes.Structure):        # gemm_epilogue_t
     _fields_ = [("bias", ctypes.c_void_p), ("activation", ctypes.c_int), ("c_is_fp16", ctypes.c_int),
                 ("residual", ctypes.c_void_p), ("ldr", ctypes.c_longlong), ("ldc", ctypes.c_longlong)]

@@ -21,8 +21,8 @@
 // in the very staging buffer the result leaves from: the residual's block is fetched there, each thread
 // reads its pieces, and writes the result over them.
 //
-// Measured: 4096 x 16384 x 4096 FP16 with bias and GELU 378 us (0.88 of the burst rate), 512 x 8192 x 8192 with bias, SiLU and
-// residual 59 us, 333 x 1001 x 1096 FP32 with all stages 11 us; one row against 4096 x 4096 with bias and residual 7.1 us.
+// Measured: 4096 x 16384 x 4096 FP16 with bias and GELU 378-390 us (0.87 of the burst rate), 512 x 8192 x 8192 with bias, SiLU and
+// residual 60.5 us, 333 x 1001 x 1096 FP32 with all stages 11.5 us; one row against 4096 x 4096 with bias and residual 7.1 us.
 #pragma once
 
 #include <cuda_fp16.h>
