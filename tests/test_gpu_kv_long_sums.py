@@ -56,3 +56,30 @@ def test_sums_in_scratch(length, new, kv_heads, window, dim):
     group = 1 if kv_heads == 80 else 4
     for got, ref, tol in run(length, new, kv_heads, group, dim, slope=3.0, window=window):
         assert ((got - ref).abs() <= tol).all()
+
+
+def test_captured_into_a_graph():
+    """The scratch of both kernels exists after one call of the same size; lengths are read when the graph runs."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    page, pages, heads, dim, new = 64, 600, 40, 64, 300
+    cache = tuple([torch.randint(-100, 100, (pages, heads, page, dim), generator=g, device="cuda").to(torch.int8) for _ in range(2)] +
+                  [0.02 + 0.02 * torch.rand(pages, heads, generator=g, device="cuda") for _ in range(2)])
+    table = torch.randperm(pages, generator=g, device="cuda").to(torch.int32)[None]
+    q = torch.randn(new, heads * 2, dim, generator=g, device="cuda").half()
+    cu, lens, out = dev([0, new]), dev([pages * page]), torch.empty_like(q)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        binding.kv_attention_s8(q, cache, cu, lens, table, new, out=out)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            binding.kv_attention_s8(q, cache, cu, lens, table, new, out=out)
+    for length in (pages * page, 20000, 700, pages * page):
+        lens.fill_(length)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = binding.kv_attention_s8(q, cache, cu, lens, table, new)
+        assert torch.equal(out, want)
