@@ -126,6 +126,56 @@ int kv_attention_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, c
                          float softmax_scale, int window, void* out, long long out_token_stride,
                          int rows, gemm_stream_t stream);
 
+/*
+ * The same cache in 4 bits: half the bytes, and a scale and an offset for every token and head, so that
+ * writing never touches older tokens and a token is held the same whichever call brings it.
+ * K and V are uint8 arrays [num_pages][kv_heads][page_size][head_dim / 2], code d of a token in bits
+ * [4 (d & 1), 4 (d & 1) + 4) of byte d >> 1; k_scale and v_scale are pairs of binary16 (scale, offset),
+ * [num_pages][kv_heads][page_size][2], 16-byte aligned like the codes.  The value of a code is
+ * offset + code * scale; pages, tables, batches and what is done about bad ones are as above.
+ */
+typedef struct kv_cache_u4 {
+  uint8_t* k;
+  uint8_t* v;
+  void* k_scale;
+  void* v_scale;
+  int num_pages;
+  int kv_heads;
+  int page_size;
+  int head_dim;
+} kv_cache_u4_t;
+
+/*
+ * Writes new tokens, as kv_append_s8_rows does.  Per token and head, over its head_dim values x,
+ *     offset = min x,   scale = (max x - min x) / 15 rounded to binary16,
+ *     code(x) = min(rint((x - offset) * (1 / scale)), 15),
+ * in FP32, ties to even; scale = 0 gives codes 0.  (Where offset + 15 scale would pass the largest binary16, scale is
+ * the next smaller one.)  A row of values with a NaN or an infinity has a NaN for its scale.
+ */
+int kv_append_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* past,
+                 const int* block_table, int table_stride, int max_new, const void* K,
+                 const void* V, long long token_stride, long long head_stride, int rows,
+                 gemm_stream_t stream);
+
+/* Reads tokens back as binary16, as kv_read_s8_rows does. */
+int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* first,
+               const int* block_table, int table_stride, int max_read, void* K, void* V, int rows,
+               gemm_stream_t stream);
+
+/*
+ * Attention over it, as kv_attention_s8_rows; q_heads / kv_heads: up to 128.  A query that sees a token whose scale
+ * or offset (of K or of V) is not finite gives NaN, as does one that holds a NaN or an infinity itself; tokens that it
+ * does not see leave it alone.
+ * Scores, softmax statistics and sums are FP32, and the softmax weights are rounded as for kv_attention_s8.
+ * Sequences of many rows multiply keys and values that are rounded to binary16, by 2^-12 of themselves.
+ * The tensor cores' sums cut off what does not fit, up to 2e-9 of the result per token of one sum.
+ */
+int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,
+                    const int* block_table, int table_stride, int max_q, int q_heads,
+                    const void* Q, long long q_token_stride, long long q_head_stride,
+                    float softmax_scale, int window, void* out, long long out_token_stride,
+                    int rows, gemm_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,8 +31,11 @@ EXPORTS = (
 )
 
 KV_EXPORTS = ("kv_append_s8", "kv_read_s8", "kv_attention_s8",   # include/b200kv.h
-              "kv_append_s8_rows", "kv_read_s8_rows", "kv_attention_s8_rows")
+              "kv_append_s8_rows", "kv_read_s8_rows", "kv_attention_s8_rows",
+              "kv_append_u4", "kv_read_u4", "kv_attention_u4")
+ATTN_EXPORTS = ("attention_fp16", "rotary_fp16")                 # include/b200attn.h
 
+ROTARY_PAIRS = {"halves": 0, "neighbours": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
@@ -42,7 +45,12 @@ class _Epilogue(ctypes.Structure):        # gemm_epilogue_t
                 ("residual", ctypes.c_void_p), ("ldr", ctypes.c_longlong), ("ldc", ctypes.c_longlong)]
 
 
-class _KvCache(ctypes.Structure):         # kv_cache_s8_t
+class _RotaryRows(ctypes.Structure):      # rotary_rows_t
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("heads", ctypes.c_int)] + [
+        (name, ctypes.c_longlong) for name in ("x_token_stride", "x_head_stride", "y_token_stride", "y_head_stride")]
+
+
+class _KvCache(ctypes.Structure):         # kv_cache_s8_t, kv_cache_u4_t
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("num_pages", ctypes.c_int), ("kv_heads", ctypes.c_int),
                 ("page_size", ctypes.c_int), ("head_dim", ctypes.c_int)]
@@ -94,6 +102,10 @@ def lib() -> ctypes.CDLL:
         for name in KV_EXPORTS[:3]:      # ... and the forms with a row count in front of the stream
             args = getattr(L, name).argtypes
             getattr(L, name + "_rows").argtypes = args[:-1] + [i, args[-1]]
+            getattr(L, name[:-2] + "u4").argtypes = args[:-1] + [i, args[-1]]
+        rr = ctypes.POINTER(_RotaryRows)
+        L.rotary_fp16.argtypes = [i, i, i, i, rr, rr, vp, i, ll, ctypes.POINTER(ctypes.c_int), vp, vp]
+        L.attention_fp16.argtypes = [i, vp, i, i, i, i, i, vp, ll, ll, vp, vp, ll, ll, ctypes.c_float, i, i, vp, ll, vp]
         L.gemm_s4_workspace_bytes.argtypes = [i, i, i]
         L.gemm_s4_workspace_bytes.restype = sz
         L.gemm_s4_static.argtypes = [i, i, i, vp, vp, vp, vp]
@@ -116,7 +128,7 @@ def lib() -> ctypes.CDLL:
         L.gemm_trace_read.argtypes = [ctypes.POINTER(ctypes.c_ulonglong), i]
         L.gemm_status_string.argtypes = [i]
         L.gemm_status_string.restype = ctypes.c_char_p
-        for name in EXPORTS + KV_EXPORTS:
+        for name in EXPORTS + KV_EXPORTS + ATTN_EXPORTS:
             fn = getattr(L, name)
             if name not in ("gemm_s4_workspace_bytes", "gemm_s4_static_capacity",
                             "gemm_status_string"):
@@ -276,7 +288,7 @@ def _native():
             from . import _marshal as m
         except ImportError as e:
             raise ImportError("%s: build it with `python -m paper_2608_10103_b200.build`" % e) from e
-        names = ("gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows") + KV_EXPORTS[3:]
+        names = ("gemm_fp16_linear", "gemm_s8_linear", "gemm_s4_linear", "gemm_quantize_rows") + KV_EXPORTS[3:] + ATTN_EXPORTS
         m.entries(*(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
         _marshal = m
     return _marshal
@@ -367,6 +379,60 @@ def kv_attention_s8(q, cache, cu, kv_len, block_table, max_q: int, softmax_scale
     return _checked((_marshal or _native()).kv_attention(q, cache, cu, kv_len, block_table, max_q, scale, window, out,
                                                          None if stream is None else stream.cuda_stream),
                     "kv_attention_s8")
+
+
+# ---------------------------------------------------------------- 4-bit key/value cache
+def kv_cache_u4(num_pages: int, kv_heads: int, page_size: int, head_dim: int, device="cuda"):
+    """(k, v, k_scale, v_scale) of an empty cache in 4 bits: uint8 (num_pages, kv_heads, page_size, head_dim / 2)
+    and float16 (num_pages, kv_heads, page_size, 2), a scale and an offset per token and head."""
+    shape = (num_pages, kv_heads, page_size)
+    return (torch.zeros(shape + (head_dim // 2,), dtype=torch.uint8, device=device),
+            torch.zeros(shape + (head_dim // 2,), dtype=torch.uint8, device=device),
+            torch.zeros(shape + (2,), dtype=torch.float16, device=device),
+            torch.zeros(shape + (2,), dtype=torch.float16, device=device))
+
+
+def kv_append_u4(cache, k, v, cu, past, block_table, max_new: int, stream=None):
+    """kv_append_s8 into a cache of 4 bits."""
+    _checked((_marshal or _native()).kv_append4(cache, k, v, cu, past, block_table, max_new,
+                                                  None if stream is None else stream.cuda_stream), "kv_append_u4")
+
+
+def kv_read_u4(cache, cu, first, block_table, max_read: int, tokens: int | None = None, out=None, stream=None):
+    """kv_read_s8 from a cache of 4 bits."""
+    return _checked((_marshal or _native()).kv_read4(cache, cu, first, block_table, max_read, tokens, out,
+                                                       None if stream is None else stream.cuda_stream), "kv_read_u4")
+
+
+def kv_attention_u4(q, cache, cu, kv_len, block_table, max_q: int, softmax_scale: float | None = None,
+                    window: int = 0, out=None, stream=None):
+    """kv_attention_s8 over a cache of 4 bits; up to 128 query heads per KV head."""
+    scale = q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale
+    return _checked((_marshal or _native()).kv_attention4(q, cache, cu, kv_len, block_table, max_q, scale, window, out,
+                                                            None if stream is None else stream.cuda_stream),
+                    "kv_attention_u4")
+
+
+# ------------------------------------------------------- rotary positions, prompt attention
+def rotary_fp16(q, k, positions, inv_freq, sections=None, pairs: str = "halves", out=None, stream=None):
+    """Turns the first 2 * len(inv_freq) values of every head of q and k (float16 (tokens, heads, head_dim) views; k
+    may be None) by positions (int32 (axes, tokens), or (tokens,) for one axis) times inv_freq (float32); the
+    first sections[0] frequencies go by axis 0, the next sections[1] by axis 1 and so on.  pairs: a key of
+    ROTARY_PAIRS.  Returns new tensors (q, k), or q alone without k; out: where to put them, which may be (q, k)."""
+    if pairs not in ROTARY_PAIRS:
+        raise ValueError("pairs is one of %s" % ", ".join(ROTARY_PAIRS))
+    return _checked((_marshal or _native()).rotary(q, k, positions, inv_freq, sections, ROTARY_PAIRS[pairs], out,
+                                                   None if stream is None else stream.cuda_stream), "rotary_fp16")
+
+
+def attention_fp16(q, k, v, cu, max_len: int, softmax_scale: float | None = None, causal: bool = True,
+                   window: int = 0, out=None, stream=None):
+    """Attention of packed sequences over themselves: rows cu[b] .. cu[b+1] of q (float16 (tokens, q_heads,
+    head_dim)), k and v ((tokens, kv_heads, head_dim) views with one common pair of strides) are sequence b, of at
+    most max_len rows; causal, perhaps over the last `window` tokens only, or over all of its tokens."""
+    scale = q.shape[-1] ** -0.5 if softmax_scale is None else softmax_scale
+    return _checked((_marshal or _native()).attention(q, k, v, cu, max_len, scale, causal, window, out,
+                                                      None if stream is None else stream.cuda_stream), "attention_fp16")
 
 
 def gemm_s4_workspace_bytes(M: int, N: int, K: int) -> int:

@@ -1,0 +1,906 @@
+// Attention for many query rows per KV head on the 5th-generation tensor cores, over binary16 keys and values of packed
+// prompts or over the pages of the 4-bit cache.
+//
+// A CTA stays on its SM and takes row tiles one after another, longest first. A row tile is QT times 128 rows (queries x heads
+// of a group) of one KV head, which walk the tokens in tiles of TN. Per tile: S = Q K^T (tcgen05.mma, operands in shared
+// memory) into tensor memory; four warps, a thread per row, turn S into weights w = 2^(c s - m + 7), rounded to binary16, in the
+// same place; O += w V (A operand in tensor memory). out = O / l with l the FP32 sum of the weights before rounding; m is
+// a maximum seen earlier, renewed when a score passes it by 2^8 (see kv_attention.cuh), so that O rarely passes through
+// registers. Scores, sums and statistics are FP32.
+//
+// Roles: a scheduler works out the next row tile while this one runs; a loader brings Q and, through a ring of tiles that runs
+// on from one row tile into the next, K and V; two issuers, one for each 128 rows, so that neither waits for the
+// other's softmax; the softmax warps hand their weights over in two halves, the first of which is multiplied while the second is
+// computed. One row tile at 256 d has two score buffers instead: the scores of the next tokens are computed meanwhile.
+//
+// Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
+// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; four warps expand a code c to offset + c scale,
+// rounded to binary16 once (a sixteenth-bit nibble becomes a binary16 by placing it under the exponent of 1024 or of 64),
+// and write the same tiles.
+//
+// What a masked place holds must not matter, but weight 0 times an infinity is NaN. 4-bit tokens whose scale or offset is not
+// finite get zeros for values and NaN for keys: a NaN score for the rows that see them, and nothing for those that mask it.
+// Binary16 values are not looked at on their way; a row whose result is not finite looks through the tokens that its
+// masked tiles hide from it and, if one of them is not finite, is computed again, alone.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "bounded_wait.cuh"
+#include "kv_attention.cuh"
+#include "kv_common.cuh"
+#include "ptx.cuh"
+
+namespace b200gemm {
+
+struct AttnTilesParams {
+  int batch;
+  const int* cu;
+  const int* kv_len;  // null: each sequence's tokens are its rows
+  int max_q, max_len, rows;
+  int group, heads;   // query heads per KV head, KV heads
+  const __half* q;
+  long long q_token_stride, q_head_stride;
+  __half* out;
+  long long out_token_stride;
+  float scale_log2;  // softmax_scale * log2(e)
+  int causal, window;
+  int split_rows;    // sequences of up to so many rows belong to another kernel
+  int* status;
+  // prompts
+  const __half *k, *v;
+  long long kv_token_stride, kv_head_stride;
+  // 4-bit cache
+  KvCacheU4View c;
+  const int* table;
+  int table_stride;
+  // tokens of a row tile divided over several CTAs
+  int splits;
+  float* partial;     // [units][splits][ROWS][D + 4]
+  unsigned* arrived;  // per unit, zero before and after
+};
+
+template <int D, bool U4>
+struct AttnTileShape {
+  static constexpr int QT = D <= 128 ? 2 : 1;    // row tiles of 128 per CTA
+  static constexpr int TN = D <= 128 ? 128 : 64; // tokens per tile
+  static constexpr int ROWS = 128 * QT;
+  static constexpr int SOFTMAX_WARPS = 4 * QT;
+  static constexpr int CONVERT_WARPS = U4 ? 4 : 0;
+  static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
+  static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
+  static constexpr int TILE_BYTES = (D / 64) * CHUNK;
+  static constexpr int Q_BYTES = QT * (D / 64) * 16384;
+  static constexpr int SLOTS = U4 ? (D == 64 ? 6 : 4) : (D == 64 ? 8 : 5);  // K and V tiles in the ring
+  static constexpr int SLOT_OFFSET = Q_BYTES;
+  static constexpr int RAW_BYTES = U4 ? TN * D / 2 : 0;  // codes of a K or V tile
+  static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
+  static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_BYTES;
+  static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // of a K or V tile; two tiles of both
+  static constexpr int ITEM_OFFSET = SCALE_OFFSET + 4 * SCALE_BYTES;
+  static constexpr int ITEM_INTS = 16;
+  static constexpr int BAR_OFFSET = ITEM_OFFSET + 2 * ITEM_INTS * 4;
+  // item_full[2], item_empty[2], q_full, q_empty, s_full[2], p_full[2][2], o_done[2], drain[2], raw_full[2], raw_empty[2],
+  // parts_written, parts_counted, slot_full[], slot_empty[]
+  static constexpr int BARS = 22 + 2 * SLOTS;
+  static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
+  static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
+  static constexpr uint32_t O_COLUMN = 256;      // S (and its weights) of tile i at TN i, O behind both
+  static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");
+  static_assert(O_COLUMN + QT * D <= 512, "tensor memory");
+};
+
+// What a CTA works on next.
+struct AttnItem {
+  int tiles;     // tiles of TN tokens; -1 = there is nothing more
+  int row0;      // first row of the sequence in the packed arrays
+  int n, base;   // its queries, the position of the first of them
+  int seq, head;
+  int query;     // first query of the row tile
+  int active;    // tiles of 128 rows with a row in them
+  int lo, hi;    // tokens
+  int from;      // first token that any row sees
+  int unit, split;
+};
+static_assert(sizeof(AttnItem) <= AttnTileShape<64, true>::ITEM_INTS * 4, "fits its place in shared memory");
+
+__device__ __forceinline__ KvSeq attn_seq(const AttnTilesParams& p, int b, bool report) {
+  KvSeq s;
+  s.row0 = kv_ld(p.cu + b);
+  s.n = kv_ld(p.cu + b + 1) - s.row0;
+  s.len = p.kv_len ? kv_ld(p.kv_len + b) : 0;
+  const int n = s.row0 < 0 ? 0 : max(0, min(s.n, min(p.max_q, p.rows - s.row0)));
+  const int len = p.kv_len ? min(max(s.len, 0), p.max_len) : 0;
+  if (report && (n != s.n || len != s.len)) kv_report(p.status);
+  s.n = n;
+  s.len = p.kv_len ? len : n;
+  return s;
+}
+
+// The row tiles of all sequences, longest first (see kvt_item in kv_attention_tiles.cuh), by one warp, a lane per sequence.
+template <int TN>
+struct AttnOrder {
+  const AttnTilesParams& p;
+  int queries;  // of a row tile
+  int all, longest;
+
+  __device__ int tiles_of(const KvSeq& s) const {
+    return static_cast<long long>(s.n) * p.group <= p.split_rows ? 0 : (s.n + queries - 1) / queries;
+  }
+  // row tiles of a sequence that are at least x token tiles long: their last query sees beyond (x - 1) TN
+  __device__ int long_tiles(const KvSeq& s, int x) const {
+    const int count = tiles_of(s);
+    if (x <= 0) return count;
+    if (!p.causal) return s.len > (x - 1) * TN ? count : 0;
+    const int need = (x - 1) * TN - (s.len - s.n);  // first query that sees so far
+    if (need <= 0) return count;
+    return need < s.n ? count - need / queries : 0;
+  }
+  __device__ AttnOrder(const AttnTilesParams& params, int queries, bool report) : p(params), queries(queries) {
+    const int lane = static_cast<int>(threadIdx.x) & 31;
+    all = longest = 0;
+    for (int i = lane; i < p.batch; i += 32) {
+      const KvSeq s = attn_seq(p, i, report);
+      longest = max(longest, s.len / TN + 1);
+      all += tiles_of(s);
+    }
+    longest = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(longest)));
+    all = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(all)));
+  }
+  // (sequence, row tile) of a rank below `all`
+  __device__ int2 at(int rank) const {
+    const int lane = static_cast<int>(threadIdx.x) & 31;
+    if (p.batch == 1) return make_int2(0, all - 1 - rank);
+    int x_lo = 0, x_hi = longest + 1, beyond = 0;  // more than rank tiles are x_lo long, `beyond` <= rank are x_hi long
+#pragma unroll 1
+    while (x_hi - x_lo > 1) {
+      const int mid = (x_lo + x_hi) / 2;
+      int c = 0;
+      for (int i = lane; i < p.batch; i += 32) c += long_tiles(attn_seq(p, i, false), mid);
+      c = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
+      if (c > rank) {
+        x_lo = mid;
+      } else {
+        x_hi = mid;
+        beyond = c;
+      }
+    }
+    int left = rank - beyond;  // among the tiles of exactly that length, by sequence
+#pragma unroll 1
+    for (int i0 = 0; i0 < p.batch; i0 += 32) {
+      int same = 0, qt = 0;
+      if (i0 + lane < p.batch) {
+        const KvSeq s = attn_seq(p, i0 + lane, false);
+        const int longer = long_tiles(s, x_hi);
+        same = long_tiles(s, x_lo) - longer;
+        qt = tiles_of(s) - 1 - longer;  // its longest tile of that length
+      }
+      int incl = same;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      const unsigned holds = __ballot_sync(0xffffffffu, left < incl);
+      if (holds) {
+        const int from = __ffs(holds) - 1;
+        return make_int2(i0 + from, __shfl_sync(0xffffffffu, qt - (left - (incl - same)), from));
+      }
+      left -= __shfl_sync(0xffffffffu, incl, 31);
+    }
+    return make_int2(0, 0);  // (not reached: there are `rank - beyond` and more tiles of that length)
+  }
+};
+
+namespace attn {
+
+// Pairs of FP32 values in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 64 d of box_heads x box_tokens rows (see shared_row_map): coordinates d, head, row.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, int d, int head, int row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(d), "r"(head), "r"(row), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ bool not_finite2(uint32_t w) {  // either of two binary16
+  return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
+}
+__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// Eight codes as binary16 values offset + code * scale, in order; scale and offset twice in their words.
+__device__ __forceinline__ uint4 expand(uint32_t w, uint32_t scale, uint32_t offset) {
+  const uint32_t u = w >> 8;
+  const uint32_t a = fma_h2(sub_h2((w & 0x000f000fu) | 0x64006400u, 0x64006400u), scale, offset);  // 1024 + code: d 0, 4
+  const uint32_t b = fma_h2(sub_h2((w & 0x00f000f0u) | 0x54005400u, 0x54005400u), scale, offset);  // 64 + code: d 1, 5
+  const uint32_t c = fma_h2(sub_h2((u & 0x000f000fu) | 0x64006400u, 0x64006400u), scale, offset);
+  const uint32_t d = fma_h2(sub_h2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u), scale, offset);
+  return make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(c, d, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x7632));
+}
+// One row of a prompt by itself: query `row` of head hq over tokens [first, last] of the packed arrays.
+template <int D>
+__device__ __forceinline__ void lone_row(const AttnTilesParams& p, int row, int hq, int head, int first, int last) {
+  const __half* const q = p.q + row * p.q_token_stride + hq * p.q_head_stride;
+  float o[D], m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+  for (int d = 0; d < D; ++d) o[d] = 0.0f;
+#pragma unroll 1
+  for (int t = first; t <= last; ++t) {
+    const __half* const k = p.k + t * p.kv_token_stride + head * p.kv_head_stride;
+    const __half* const v = p.v + t * p.kv_token_stride + head * p.kv_head_stride;
+    float s = 0.0f;
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) s = fmaf(__half2float(q[d]), __half2float(k[d]), s);
+    s *= p.scale_log2;
+    if (s == -INFINITY) continue;
+    if (!(s <= m)) {
+      const float f = m == -INFINITY ? 0.0f : exp2f(m - s);
+      m = s;
+      l *= f;
+#pragma unroll 1
+      for (int d = 0; d < D; ++d) o[d] *= f;
+    }
+    const float w = exp2f(s - m);
+    l += w;
+#pragma unroll 1
+    for (int d = 0; d < D; ++d) o[d] = fmaf(w, __half2float(v[d]), o[d]);
+  }
+  __half* const out = p.out + row * p.out_token_stride + static_cast<long long>(hq) * D;
+#pragma unroll 1
+  for (int d = 0; d < D; ++d) out[d] = __float2half_rn(o[d] / l);
+}
+// Whether a value of tokens [first, last] of the packed arrays is not finite.
+template <int D>
+__device__ __forceinline__ bool any_not_finite(const AttnTilesParams& p, int head, int first, int last) {
+#pragma unroll 1
+  for (int t = max(first, 0); t <= min(last, p.rows - 1); ++t)
+#pragma unroll 1
+    for (int d = 0; d < D; d += 8) {
+      const uint4 x = ptx::ld_global_stream_v4(p.v + t * p.kv_token_stride + head * p.kv_head_stride + d);
+      if (not_finite2(x.x) || not_finite2(x.y) || not_finite2(x.z) || not_finite2(x.w)) return true;
+    }
+  return false;
+}
+
+}  // namespace attn
+
+template <int D, bool U4>
+__global__ void __launch_bounds__(AttnTileShape<D, U4>::THREADS, 1)
+attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                       const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttnTilesParams p) {
+  using namespace kva;
+  using namespace attn;
+  using T = AttnTileShape<D, U4>;
+  constexpr int QT = T::QT, TN = T::TN, SLOTS = T::SLOTS;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = ptx::smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* const base_ptr = smem_raw + (base - raw);
+  const uint32_t bar0 = base + T::BAR_OFFSET;
+  auto item_full = [&](int i) { return bar0 + 8u * i; };
+  auto item_empty = [&](int i) { return bar0 + 8u * (2 + i); };
+  const uint32_t q_full = bar0 + 8u * 4, q_empty = bar0 + 8u * 5;
+  auto s_full = [&](int i) { return bar0 + 8u * (6 + i); };
+  auto p_full = [&](int i, int part) { return bar0 + 8u * (8 + 2 * i + part); };
+  auto o_done = [&](int q) { return bar0 + 8u * (12 + q); };
+  auto drain = [&](int q) { return bar0 + 8u * (14 + q); };
+  auto raw_full = [&](int w) { return bar0 + 8u * (16 + w); };
+  auto raw_empty = [&](int w) { return bar0 + 8u * (18 + w); };
+  const uint32_t parts_written = bar0 + 8u * 20, parts_counted = bar0 + 8u * 21;
+  auto slot_full = [&](int s) { return bar0 + 8u * (22 + s); };
+  auto slot_empty = [&](int s) { return bar0 + 8u * (22 + SLOTS + s); };
+  volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
+  volatile uint32_t* const abort_flag = tmem_holder + 1;
+  volatile uint32_t* const last_flag = tmem_holder + 2;
+
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
+  constexpr int W_LOAD = T::SOFTMAX_WARPS, W_SCHEDULE = W_LOAD + 1, W_MMA = W_LOAD + 2;  // two issuers
+  constexpr int CONSUMERS = T::SOFTMAX_WARPS + 1 + QT + T::CONVERT_WARPS;  // warps that read the items
+  if (tid == 0) {
+    ptx::grid_dep_launch_dependents();
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(item_full(i), 1);
+      ptx::mbar_init(item_empty(i), CONSUMERS);
+      ptx::mbar_init(s_full(i), 1);
+      ptx::mbar_init(p_full(i, 0), 4);
+      ptx::mbar_init(p_full(i, 1), 4);
+      ptx::mbar_init(o_done(i), 1);
+      ptx::mbar_init(drain(i), 1);
+      ptx::mbar_init(raw_full(i), 1);
+      ptx::mbar_init(raw_empty(i), 4);
+    }
+    ptx::mbar_init(q_full, 1);
+    ptx::mbar_init(q_empty, QT);
+    ptx::mbar_init(parts_written, T::SOFTMAX_WARPS);
+    ptx::mbar_init(parts_counted, 1);
+    for (int i = 0; i < SLOTS; ++i) {
+      ptx::mbar_init(slot_full(i), U4 ? 4 : 1);
+      ptx::mbar_init(slot_empty(i), QT);
+    }
+    *abort_flag = 0;
+    ptx::fence_mbar_init();
+  }
+  if (warp == W_MMA) {
+    ptx::tmem_alloc<1>(ptx::smem_addr(const_cast<uint32_t*>(tmem_holder)), 512);
+    ptx::tmem_relinquish<1>();
+  }
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  ptx::tc_fence_after_sync();
+  const uint32_t tmem = *tmem_holder;
+  ptx::grid_dep_wait();
+
+  const int per_tile = 128 / p.group;  // queries of 128 rows
+  // The k-th item; false: give up.
+  auto next_item = [&](int k, AttnItem& it) {
+    bool ok = wait_bounded(item_full(k & 1), (k >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+    ok = __all_sync(0xffffffffu, ok);
+    if (ok) it = *reinterpret_cast<const AttnItem*>(base_ptr + T::ITEM_OFFSET + (k & 1) * T::ITEM_INTS * 4);
+    __syncwarp();
+    if (ok && lane == 0) ptx::mbar_arrive(item_empty(k & 1));
+    return ok;
+  };
+
+  // Register shares by group of four warps; they sum up to no more than the block was launched with (384 x 168
+  // resp. 512 x 128): a row's scores stay in registers between the maximum and the weights.
+  if constexpr (QT == 2) {
+    if (warp < T::SOFTMAX_WARPS) {
+      if constexpr (U4)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+      else
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    } else if (warp < T::SOFTMAX_WARPS + 4) {
+      if constexpr (U4)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+      else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    }
+  }
+
+  if (warp < T::SOFTMAX_WARPS) {
+    // ------------------------------------------------------------------ softmax, one thread per row
+    const int q = warp >> 2, r = (warp & 3) * 32 + lane;  // row of the 128
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t o_at = tmem + lane_base + T::O_COLUMN + static_cast<uint32_t>(q * D);
+    const int in_tile = r / p.group, in_group = r - in_tile * p.group;
+    const float c = p.scale_log2;
+    const uint64_t c2 = pair(c, c);
+    int done = 0;  // token tiles of this tile of rows so far
+    int joins = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0; ok; ++k) {
+      AttnItem it;
+      ok = next_item(k, it);
+      if (!ok || it.tiles < 0) break;
+      if (q >= it.active) {
+        // (the joining below is for all of these warps)
+      } else {
+        const int qi = it.query + q * per_tile + in_tile;  // query of the sequence
+        const bool live = in_tile < per_tile && qi < it.n;
+        const int hq = it.head * p.group + in_group;
+        const int pos = p.causal ? it.base + qi : it.base + it.n - 1;  // sees tokens from .. pos
+        const int from = p.window > 0 ? pos - p.window + 1 : 0;
+        const int q0 = it.query + q * per_tile;
+        const int all_hi = p.causal ? it.base + q0 : pos;
+        const int all_lo = p.window > 0 ? it.base + min(it.n, q0 + per_tile) - p.window : 0;
+        float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
+        for (int j = 0; j < it.tiles; ++j, ++done) {
+          const int sb = QT == 2 ? q : done & 1;  // score buffer
+          const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(sb * TN);
+          ok = wait_bounded(s_full(sb), (QT == 2 ? done : done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          uint32_t x[TN / 32][32];
+#pragma unroll
+          for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
+          ptx::tmem_wait_ld();
+          const int tok0 = it.lo + j * TN;
+          if (tok0 + TN - 1 > all_hi || tok0 < all_lo) {
+            const int last = pos - tok0, first = from - tok0;
+#pragma unroll
+            for (int h = 0; h < TN / 32; ++h)
+#pragma unroll
+              for (int v = 0; v < 32; ++v)
+                if (h * 32 + v > last || h * 32 + v < first) x[h][v] = 0xff800000u;  // -inf
+          }
+          float mx[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) mx[u] = __uint_as_float(x[0][u]);
+#pragma unroll
+          for (int h = 0; h < TN / 32; ++h)
+#pragma unroll
+            for (int v = h == 0 ? 4 : 0; v < 32; v += 8)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                mx[u] = v + u + 4 < 32 ? fmaxf(fmaxf(mx[u], __uint_as_float(x[h][v + u])), __uint_as_float(x[h][v + u + 4]))
+                                       : fmaxf(mx[u], __uint_as_float(x[h][v + u]));
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+          const bool grow = top > m + 8.0f;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float now = grow ? top : m;
+            const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
+            m = now;
+            l *= f;
+            if (j > 0) {  // O of the tiles before, once their products are done
+              ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              ptx::tc_fence_after_sync();
+#pragma unroll 1
+              for (int d = 0; d < D; d += 16) {
+                uint32_t y[16];  // (few registers: the scores are in the others)
+                ptx::tmem_ld_32x32b_x16(o_at + d, y);
+                ptx::tmem_wait_ld();
+#pragma unroll
+                for (int v = 0; v < 16; ++v) y[v] = __float_as_uint(__uint_as_float(y[v]) * f);
+                ptx::tmem_st_32x32b_x16(o_at + d, y);
+              }
+              ptx::tmem_wait_st();
+            }
+          }
+          // weights, two per column, over the scores: 32 tokens take 16 columns
+          const float at_ref = KVA_WEIGHT_BITS - (m == -INFINITY ? 0.0f : m);
+          const uint64_t at2 = pair(at_ref, at_ref);
+          uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+          for (int h = 0; h < TN / 32; ++h) {
+            uint32_t w[16];
+#pragma unroll
+            for (int v = 0; v < 32; v += 2) {
+              const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), c2, at2));
+              const float e0 = exp2_approx(t.x), e1 = exp2_approx(t.y);
+              sum[(v / 2) & 1] = add2(sum[(v / 2) & 1], pair(e0, e1));
+              w[v / 2] = pack_halves(e0, e1);
+            }
+            ptx::tmem_st_32x32b_x16(s_at + h * 16, w);
+            if (h % (TN / 64) == TN / 64 - 1) {  // half of the tokens
+              ptx::tmem_wait_st();
+              ptx::tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) ptx::mbar_arrive(p_full(sb, h / (TN / 64)));
+            }
+          }
+          const float2 total = unpair(add2(sum[0], sum[1]));
+          l += total.x + total.y;
+          if (QT == 1 && j > 0) {  // (with two score buffers nothing else says that those are done: a phase that is not waited for is
+                                   // taken for the next but one)
+            ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+          }
+        }
+        if (!ok) break;
+        // ---- the rows' results
+        if (it.tiles > 0) {
+          ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+        }
+        // (a row that sees a token has l > 0, or NaN; or all its scores are -inf, which makes it NaN)
+        if (l == 0.0f && pos >= max(from, 0) && it.split < 0) l = __int_as_float(0x7fffffff);
+        const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
+        float* const part = U4 && it.split >= 0
+                                ? p.partial + ((static_cast<long long>(it.unit) * p.splits + it.split) * T::ROWS + q * 128 + r) * (D + 4)
+                                : nullptr;
+        if (U4 && part && live) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
+        __half* const dst = p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
+        uint32_t worst = 0;  // magnitude bits of the results
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+          uint32_t x[32];
+          if (it.tiles > 0) {
+            ptx::tmem_ld_32x32b_x32(o_at + d, x);
+            ptx::tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int v = 0; v < 32; ++v) x[v] = 0;
+          }
+          if (!live) continue;
+          if (U4 && part) {  // O as it stands, to be joined
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+              *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
+            continue;
+          }
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            uint32_t y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              y[u] = pack_halves(__uint_as_float(x[8 * v + 2 * u]) * inv, __uint_as_float(x[8 * v + 2 * u + 1]) * inv);
+              if constexpr (!U4) worst = __vmaxu2(worst, y[u] & 0x7fff7fffu);
+            }
+            *reinterpret_cast<uint4*>(dst + d + 8 * v) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        }
+        ptx::tc_fence_before_sync();
+        if constexpr (!U4) {
+          if (live && max(worst & 0xffffu, worst >> 16) >= 0x7c00u) {
+            // Was it a value that this row does not see?  Tiles wholly visible to it hide none.
+            const int end = it.lo + it.tiles * TN - 1;
+            if (any_not_finite<D>(p, it.head, it.row0 + max(pos + 1, it.lo), it.row0 + end) ||
+                any_not_finite<D>(p, it.head, it.row0 + it.lo, it.row0 + from - 1))
+              lone_row<D>(p, it.row0 + qi, hq, it.head, it.row0 + max(from, 0), it.row0 + pos);
+          }
+        }
+        __syncwarp();
+      }
+      if (U4 && it.split >= 0) {
+        // ---- the CTA that finishes a row tile last joins its parts, in their order
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(parts_written);
+        ok = wait_bounded(parts_written, joins & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        if (tid == 0) {
+          *last_flag = atomicAdd(p.arrived + it.unit, 1u) == static_cast<unsigned>(p.splits - 1);
+          ptx::mbar_arrive(parts_counted);
+        }
+        ok = wait_bounded(parts_counted, joins & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ++joins;
+        if (!*last_flag) continue;
+        __threadfence();
+        if (tid == 0) p.arrived[it.unit] = 0;
+        const float* const parts = p.partial + static_cast<long long>(it.unit) * p.splits * T::ROWS * (D + 4);
+#pragma unroll 1
+        for (int i = tid; i < T::ROWS * (D / 4); i += 32 * T::SOFTMAX_WARPS) {
+          const int rr = i / (D / 4), d = i % (D / 4) * 4;
+          const int row = rr & 127, tile = rr >> 7, qin = row / p.group, qi = it.query + tile * per_tile + qin;
+          if (tile >= it.active || qin >= per_tile || qi >= it.n) continue;
+          const float* const mine = parts + rr * (D + 4);
+          float top = -INFINITY, l = 0.0f;
+          float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          for (int s = 0; s < p.splits; ++s) top = fmaxf(top, __ldcg(mine + static_cast<long long>(s) * T::ROWS * (D + 4) + D));
+          const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+          for (int s = 0; s < p.splits; ++s) {
+            const float* const at = mine + static_cast<long long>(s) * T::ROWS * (D + 4);
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(at + D));
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + d));
+            const float f = exp2_approx(ml.x - ref);
+            l = fmaf(ml.y, f, l);
+            o.x = fmaf(x.x, f, o.x);
+            o.y = fmaf(x.y, f, o.y);
+            o.z = fmaf(x.z, f, o.z);
+            o.w = fmaf(x.w, f, o.w);
+          }
+          if (l == 0.0f && it.base + qi >= 0) l = __int_as_float(0x7fffffff);
+          const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
+          __half2* const dst = reinterpret_cast<__half2*>(
+              p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride +
+              (static_cast<long long>(it.head) * p.group + (row - qin * p.group)) * D + d);
+          dst[0] = __floats2half2_rn(o.x * inv, o.y * inv);
+          dst[1] = __floats2half2_rn(o.z * inv, o.w * inv);
+        }
+      }
+    }
+  } else if (warp == W_SCHEDULE) {
+    // ------------------------------------------------------------------ scheduler
+    const AttnOrder<TN> order(p, QT * per_tile, blockIdx.x == 0);
+    const int grid = static_cast<int>(gridDim.x), total = order.all * p.heads * p.splits;
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0, round = 0; ok; ++k, ++round) {
+      // every other round backwards: who got the longest of one gets the shortest of the next
+      const int at = round * grid + (round & 1 ? grid - 1 - static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x));
+      AttnItem it = {};
+      it.tiles = -1;
+      const bool more = at < total;  // (only the last round has gaps)
+      if (more) {
+        it.unit = at / p.splits;
+        it.split = at - it.unit * p.splits;
+        const int rank = it.unit / p.heads;
+        it.head = it.unit - rank * p.heads;
+        const int2 where = order.at(rank);
+        const KvSeq s = attn_seq(p, where.x, false);
+        it.seq = where.x;
+        it.row0 = s.row0;
+        it.n = s.n;
+        it.base = s.len - s.n;
+        it.query = where.y * QT * per_tile;
+        const int queries = min(QT * per_tile, s.n - it.query);
+        it.active = QT == 2 && queries > per_tile ? 2 : 1;
+        it.hi = p.causal ? max(0, it.base + it.query + queries) : s.len;
+        it.from = p.window > 0 ? max(0, it.base + it.query - p.window + 1) : 0;
+        it.lo = it.from / TN * TN;
+        it.tiles = max(0, (it.hi - it.lo + TN - 1) / TN);
+        if (p.splits > 1) {  // this CTA's part of the tokens
+          const int per = (it.tiles + p.splits - 1) / p.splits, first = min(it.tiles, it.split * per);
+          it.tiles = min(it.tiles, first + per) - first;
+          it.lo += first * TN;
+          it.hi = min(it.hi, it.lo + it.tiles * TN);
+        } else {
+          it.split = -1;
+        }
+      }
+      ok = wait_bounded(item_empty(k & 1), ((k >> 1) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok && lane == 0) {
+        *reinterpret_cast<AttnItem*>(base_ptr + T::ITEM_OFFSET + (k & 1) * T::ITEM_INTS * 4) = it;
+        ptx::mbar_arrive(item_full(k & 1));
+      }
+      __syncwarp();
+      if (!more) break;
+    }
+  } else if (warp == W_LOAD) {
+    // ------------------------------------------------------------------ loader
+    const uint32_t q_box = static_cast<uint32_t>(per_tile * p.group) * 128u;
+    int tile = 0;  // tiles in the ring so far (FP16), tiles of tokens (4-bit)
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0, used = 0; ok; ++k) {
+      AttnItem it;
+      ok = next_item(k, it);
+      if (!ok || it.tiles < 0) break;
+      if (it.tiles == 0) continue;
+      ok = wait_bounded(q_empty, (used & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      ++used;
+      if (lane == 0) {
+        ptx::mbar_arrive_expect_tx(q_full, q_box * static_cast<uint32_t>(it.active * (D / 64)));
+        for (int q = 0; q < it.active; ++q)
+          for (int d = 0; d < D / 64; ++d)
+            load_rows(base + (q * (D / 64) + d) * 16384, &q_map, d * 64, it.head * p.group, it.row0 + it.query + q * per_tile, q_full);
+      }
+      __syncwarp();
+      if constexpr (!U4) {
+#pragma unroll 1
+        for (int j = 0; j < 2 * it.tiles; ++j, ++tile) {  // K, V by turns
+          const int slot = tile % SLOTS;
+          ok = wait_bounded(slot_empty(slot), ((tile / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          if (lane == 0) {
+            ptx::mbar_arrive_expect_tx(slot_full(slot), T::TILE_BYTES);
+            for (int d = 0; d < D / 64; ++d)
+              load_rows(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + d * T::CHUNK, j & 1 ? &v_map : &k_map, d * 64, it.head,
+                        it.row0 + it.lo + (j >> 1) * TN, slot_full(slot));
+          }
+          __syncwarp();
+        }
+      } else {
+        // Lane g looks after the tile's g-th run of `run` tokens: one page, or half a tile's worth of a longer one.
+        const int run = min(p.c.page, TN), runs = TN / run;
+        const uint32_t run_bytes = static_cast<uint32_t>(run * D / 2);
+        const int* const table = p.table + static_cast<long long>(it.seq) * p.table_stride;
+        auto visible = [&](int j) {  // the lane's run of tile j, or a part of it
+          const int tok = it.lo + j * TN + run * lane;
+          return lane < runs && j < it.tiles && tok < it.hi && tok + run > it.from;
+        };
+        auto load_id = [&](int j) {  // its page, or -1
+          return visible(j) ? kv_ld(table + ((it.lo + j * TN + run * lane) >> p.c.page_shift)) : -1;
+        };
+        int id = load_id(0);
+#pragma unroll 1
+        for (int j = 0; j < it.tiles && ok; ++j, ++tile) {
+          const int id_next = load_id(j + 1);
+          const bool in = visible(j);
+          const bool good = in && id >= 0 && id < p.c.num_pages;
+          if (in && !good) kv_report(p.status);
+          const int tok = it.lo + j * TN + run * lane;
+          const uint64_t token = good ? (static_cast<uint64_t>(id) * p.heads + it.head) * p.c.page + (tok & (p.c.page - 1)) : 0;
+          const uint32_t count = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, good)));
+#pragma unroll 1
+          for (int which = 0; which < 2; ++which) {
+            ok = wait_bounded(raw_empty(which), (tile & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            // (scales and offsets of both come with K; runs that are left out keep what the buffers held)
+            if (lane == 0) ptx::mbar_arrive_expect_tx(raw_full(which), count * (run_bytes + (which ? 0u : static_cast<uint32_t>(run) * 8u)));
+            __syncwarp();
+            if (good) {
+              ptx::bulk_load(base + T::RAW_OFFSET + which * T::RAW_BYTES + lane * run_bytes, (which ? p.c.codes[1] : p.c.codes[0]) + token * (D / 2),
+                             run_bytes, raw_full(which));
+              if (which == 0) {
+                const uint32_t to = base + T::SCALE_OFFSET + (tile & 1) * 2 * T::SCALE_BYTES + lane * run * 4;
+                ptx::bulk_load(to, p.c.scales[0] + token, run * 4, raw_full(0));
+                ptx::bulk_load(to + T::SCALE_BYTES, p.c.scales[1] + token, run * 4, raw_full(0));
+              }
+            }
+          }
+          id = id_next;
+        }
+      }
+    }
+    if (!ok) {
+      // Gave up: let the copies in flight land before the CTA exits.
+      const uint64_t start = ptx::globaltimer_ns();
+      while (ptx::globaltimer_ns() - start < 1000000ull) {
+      }
+    }
+  } else if (warp < W_MMA + QT && warp >= W_MMA) {
+    // ------------------------------------------------------------------ MMA issuer of tile q of the rows
+    const int q = warp - W_MMA;
+    const bool elected = ptx::elect_one();
+    constexpr uint32_t idesc_qk = ptx::make_idesc<ptx::KIND_F16>(128, TN);
+    constexpr uint32_t idesc_pv = ptx::make_idesc<ptx::KIND_F16>(128, D) | ptx::IDESC_B_MN_MAJOR;
+    constexpr int AHEAD = QT == 2 ? 1 : 2;  // score buffers of these rows
+    int tile = 0;  // K and V tiles in the ring before this item
+    int done = 0;  // token tiles of these rows
+    bool ok = true;
+    auto wait_slot = [&](int i) {
+      const bool there = wait_bounded(slot_full(i % SLOTS), (i / SLOTS) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+      if (there) ptx::tc_fence_after_sync();
+      return there;
+    };
+#pragma unroll 1
+    for (int k = 0, used = 0; ok; ++k) {
+      AttnItem it;
+      ok = next_item(k, it);
+      if (!ok || it.tiles < 0) break;
+      if (it.tiles == 0) continue;
+      if (q >= it.active) {  // nothing to do but to let the ring go round
+        ok = wait_bounded(q_full, used & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+        if (ok && elected) ptx::mbar_arrive(q_empty);
+#pragma unroll 1
+        for (int j = 0; j < 2 * it.tiles && ok; ++j) {
+          ok = wait_slot(tile + j);
+          if (ok && elected) ptx::mbar_arrive(slot_empty((tile + j) % SLOTS));
+        }
+        __syncwarp();
+        tile += 2 * it.tiles;
+        ++used;
+        continue;
+      }
+      ok = wait_bounded(q_full, used & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+      if (!ok) break;
+      ++used;
+      auto qk = [&](int j) {  // scores of token tile j
+        if (!wait_slot(tile + 2 * j)) return false;
+        const int slot = (tile + 2 * j) % SLOTS, sb = QT == 2 ? q : (done + j) & 1;
+        if (elected) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = static_cast<uint32_t>((kk & 3) * 32);
+            const uint64_t a = ptx::smem_desc_sw128(base + (q * (D / 64) + (kk >> 2)) * 16384 + off);
+            const uint64_t b = ptx::smem_desc_sw128(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + (kk >> 2) * T::CHUNK + off);
+            ptx::mma_ss<ptx::KIND_F16, 1>(tmem + sb * TN, a, b, idesc_qk, kk > 0);
+          }
+          ptx::mma_commit<1>(s_full(sb));
+          ptx::mma_commit<1>(slot_empty(slot));
+          if (j == it.tiles - 1) ptx::mma_commit<1>(q_empty);
+        }
+        __syncwarp();
+        return true;
+      };
+      for (int j = 0; j < AHEAD && j < it.tiles && ok; ++j) ok = qk(j);
+#pragma unroll 1
+      for (int j = 0; j < it.tiles && ok; ++j) {
+        const int sb = QT == 2 ? q : (done + j) & 1;
+        const uint32_t parity = (QT == 2 ? done + j : (done + j) >> 1) & 1;
+        const int slot = (tile + 2 * j + 1) % SLOTS;
+        ok = wait_slot(tile + 2 * j + 1);
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          ok = ok && wait_bounded(p_full(sb, part), parity, abort_flag, p.status, DEV_TIMEOUT_MMA);
+          if (ok) {
+            ptx::tc_fence_after_sync();
+            if (elected) {
+#pragma unroll
+              for (int kk = part * (TN / 32); kk < (part + 1) * (TN / 32); ++kk) {
+                const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
+                ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || kk > 0);
+              }
+              if (part == 1) {
+                ptx::mma_commit<1>(o_done(q));
+                ptx::mma_commit<1>(slot_empty(slot));
+              }
+            }
+            __syncwarp();
+          }
+        }
+        // (the scores go where the weights are: the MMAs of this thread run in order)
+        if (ok && j + AHEAD < it.tiles) ok = qk(j + AHEAD);
+      }
+      tile += 2 * it.tiles;
+      done += it.tiles;
+    }
+    if (!ok && elected) {
+      // Gave up: wait for the MMAs already issued before tensor memory is released.
+      ptx::mma_commit<1>(drain(q));
+      const uint64_t start = ptx::globaltimer_ns();
+      while (!ptx::mbar_try_wait(drain(q), 0) && ptx::globaltimer_ns() - start < WAIT_LIMIT_NS) {
+      }
+    }
+    __syncwarp();
+  } else if (U4 && warp >= W_LOAD + 4) {
+    // ------------------------------------------------------------------ K and V: 4-bit codes to binary16 tiles
+    const int ct = tid - 32 * (W_LOAD + 4);         // 0 .. 127
+    constexpr int PER_TOKEN = D / 32;               // 16-byte pieces of a token's codes: 32 d, 64 bytes of a row of a chunk
+    constexpr int N = TN * PER_TOKEN / 128;         // pieces per thread and tile
+    constexpr int TOKENS_AT_ONCE = 128 / PER_TOKEN; // tokens the 128 threads cover together
+    const int piece = ct % PER_TOKEN, t0 = ct / PER_TOKEN;
+    int tile = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int k = 0; ok; ++k) {
+      AttnItem it;
+      ok = next_item(k, it);
+      if (!ok || it.tiles < 0) break;
+#pragma unroll 1
+      for (int j = 0; j < 2 * it.tiles; ++j, ++tile) {
+        const int which = j & 1, slot = tile % SLOTS, nth = tile >> 1;
+        ok = wait_bounded(raw_full(which), nth & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
+             wait_bounded(slot_empty(slot), ((tile / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        const uint32_t codes = base + T::RAW_OFFSET + which * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
+        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + (nth & 1) * 2 * T::SCALE_BYTES);
+        const uint32_t to = base + T::SLOT_OFFSET + slot * T::TILE_BYTES + static_cast<uint32_t>((piece >> 1) * T::CHUNK);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int tok = i * TOKENS_AT_ONCE + t0;
+          uint32_t w[4];
+          ptx::ld_shared_v4(codes + i * 2048, w[0], w[1], w[2], w[3]);
+          // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
+          const int place = it.lo + (j >> 1) * TN + tok;
+          const bool seen = place < it.hi && place >= it.from;
+          const uint32_t mine = seen ? scales[which * TN + tok] : 0u, other = which || !seen ? 0u : scales[TN + tok];
+          const bool bad = not_finite2(mine) || not_finite2(other);
+          const uint32_t scale = bad ? (which ? 0u : 0x7fff7fffu) : __byte_perm(mine, 0, 0x1010);
+          const uint32_t offset = bad && which ? 0u : __byte_perm(mine, 0, 0x3232);
+          const uint32_t at = to + static_cast<uint32_t>(tok * 128), sw = static_cast<uint32_t>(tok & 7);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const uint4 x = expand(w[v], scale, offset);
+            ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), x.x, x.y, x.z, x.w);
+          }
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(slot_full(slot));
+          ptx::mbar_arrive(raw_empty(which));
+        }
+      }
+    }
+  }
+
+  // Every role gets here: all waits are bounded, and the last products have been waited for above.
+  ptx::tc_fence_before_sync();
+  __syncthreads();
+  if (warp == W_MMA) {
+    ptx::tc_fence_after_sync();
+    ptx::tmem_dealloc<1>(tmem, 512);
+  }
+}
+
+}  // namespace b200gemm

@@ -61,6 +61,18 @@ int shared_scratch_done(int device, cudaStream_t stream, const SharedLease& leas
   const int rc = g_kv_pool[device].release(l, stream);
   return rc == 0 ? GEMM_OK : pool_fail(rc);
 }
+
+int shared_row_map(CUtensorMap* out, const void* base, int dim, int heads, int tokens, long long token_stride,
+                   long long head_stride, int box_heads, int box_tokens) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(head_stride) * 2, static_cast<cuuint64_t>(token_stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_tokens)};
+  const cuuint32_t unit[3] = {1, 1, 1};
+  const CUresult r = g_encode.load()(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(base), dims, strides, box,
+                                     unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? GEMM_OK : cuda_fail(cudaErrorInvalidValue);
+}
 }  // namespace b200gemm
 
 extern "C" {

@@ -1,0 +1,191 @@
+// C-ABI of the 4-bit key/value cache (include/b200kv.h): argument checks and launches.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "../../include/b200kv.h"
+#include "attention_tiles.cuh"
+#include "kv_cache_u4.cuh"
+#include "kv_host.cuh"
+#include "shared_state.h"
+
+namespace b200gemm {
+namespace {
+
+int check_cache(const kv_cache_u4_t* c, KvCacheU4View* v) {
+  if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return GEMM_ERR_INVALID_ARG;
+  if (c->num_pages <= 0 || c->kv_heads <= 0 || c->kv_heads > 65535) return GEMM_ERR_INVALID_ARG;
+  int shift = 4;
+  while (shift < 7 && (1 << shift) != c->page_size) ++shift;
+  if ((1 << shift) != c->page_size) return GEMM_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return GEMM_ERR_INVALID_ARG;
+  if (misaligned(c->k, 16) || misaligned(c->v, 16) || misaligned(c->k_scale, 16) || misaligned(c->v_scale, 16))
+    return GEMM_ERR_MISALIGNED;
+  v->codes[0] = c->k;
+  v->codes[1] = c->v;
+  v->scales[0] = static_cast<__half2*>(c->k_scale);
+  v->scales[1] = static_cast<__half2*>(c->v_scale);
+  v->num_pages = c->num_pages;
+  v->heads = c->kv_heads;
+  v->page = c->page_size;
+  v->page_shift = shift;
+  v->dim = c->head_dim;
+  return GEMM_OK;
+}
+
+// Blocks of KV4_TOKENS tokens of every sequence; 0 = too many.
+int blocks_of(int max_rows, int batch, int* per_seq) {
+  *per_seq = static_cast<int>((static_cast<long long>(max_rows) + KV4_TOKENS - 1) / KV4_TOKENS);
+  const long long blocks = static_cast<long long>(*per_seq) * batch;
+  return blocks > 0x7fffffffll ? 0 : static_cast<int>(blocks);
+}
+
+// Sequences with more than p.split_rows rows, on the tensor cores.
+template <int D>
+int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream) {
+  static std::atomic<bool> ready[MAX_DEV];
+  using T = AttnTileShape<D, true>;
+  auto kernel = attention_tiles_kernel<D, true>;
+  if (!ready[dev.device].load()) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::DYN_BYTES);
+    if (e != cudaSuccess) return shared_cuda_fail(e);
+    ready[dev.device].store(true);
+  }
+  const int per_tile = 128 / p.group, per_cta = T::QT * per_tile;
+  const int longest = p.max_q < p.rows ? p.max_q : p.rows;
+  // row tiles: one more a sequence than its rows would fill, and no more than the longest allows
+  const long long by_rows = static_cast<long long>(p.rows) / per_cta + p.batch;
+  const long long by_longest = (static_cast<long long>(longest) + per_cta - 1) / per_cta * p.batch;
+  const long long units = (by_rows < by_longest ? by_rows : by_longest) * p.heads;
+  if (units > 0x3fffffffll) return GEMM_ERR_TOO_LARGE;
+  CUtensorMap q;
+  int rc = shared_row_map(&q, p.q, D, p.heads * p.group, p.rows, p.q_token_stride, p.q_head_stride, p.group, per_tile);
+  if (rc != GEMM_OK) return rc;
+  // Fewer row tiles than half the SMs: as many parts of their tokens as fill the chip, two token tiles each if
+  // sequences are as long as their tables allow, sixteen at most (what is joined grows with them).
+  p.splits = 1;
+  if (2 * units <= dev.num_sms) {
+    long long most = dev.num_sms / units;
+    if (most > p.max_len / (2 * T::TN)) most = p.max_len / (2 * T::TN);
+    if (most > 16) most = 16;
+    if (most > 1) p.splits = static_cast<int>(most);
+  }
+  const long long items = units * p.splits;
+  const int grid = items < dev.num_sms ? static_cast<int>(items) : dev.num_sms;
+  if (p.splits == 1) return launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, q, q, p);
+  SharedLease lease;
+  rc = shared_scratch(dev.device, stream, static_cast<size_t>(items) * T::ROWS * (D + 4) * 4,
+                      (static_cast<size_t>(units) * 4 + 255) / 256 * 256, &lease);
+  if (rc != GEMM_OK) return rc;
+  p.arrived = static_cast<unsigned*>(lease.head);
+  p.partial = static_cast<float*>(lease.data);
+  rc = launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, q, q, p);
+  const int done = shared_scratch_done(dev.device, stream, lease);
+  return rc != GEMM_OK ? rc : done;
+}
+
+}  // namespace
+}  // namespace b200gemm
+
+using namespace b200gemm;
+
+extern "C" {
+
+int kv_append_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* past,
+                 const int* block_table, int table_stride, int max_new, const void* K,
+                 const void* V, long long token_stride, long long head_stride, int rows,
+                 gemm_stream_t stream) {
+  KvAppendU4Params p = {};
+  int rc = check_cache(cache, &p.c);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, past, block_table, table_stride, max_new, rows, &p.b);
+  if (rc != GEMM_OK) return rc;
+  if (!K || !V || token_stride < 0 || head_stride < p.c.dim) return GEMM_ERR_INVALID_ARG;
+  if (misaligned(K, 16) || misaligned(V, 16) || token_stride % 8 || head_stride % 8)
+    return GEMM_ERR_MISALIGNED;
+  const int blocks = blocks_of(max_new < rows ? max_new : rows, batch, &p.blocks_per_seq);
+  if (!blocks) return GEMM_ERR_TOO_LARGE;
+  SharedDevice dev;
+  rc = shared_device(&dev);
+  if (rc != GEMM_OK) return rc;
+  p.b.status = dev.status;
+  p.x[0] = static_cast<const __half*>(K);
+  p.x[1] = static_cast<const __half*>(V);
+  p.token_stride = token_stride;
+  p.head_stride = head_stride;
+  return launch(dev, kv_append_u4_kernel, dim3(static_cast<unsigned>(blocks), 2), KV4_THREADS, 0,
+                reinterpret_cast<cudaStream_t>(stream), p);
+}
+
+int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* first,
+               const int* block_table, int table_stride, int max_read, void* K, void* V, int rows,
+               gemm_stream_t stream) {
+  KvReadU4Params p = {};
+  int rc = check_cache(cache, &p.c);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, first, block_table, table_stride, max_read, rows, &p.b);
+  if (rc != GEMM_OK) return rc;
+  if (!K && !V) return GEMM_ERR_INVALID_ARG;
+  if (misaligned(K, 16) || misaligned(V, 16)) return GEMM_ERR_MISALIGNED;
+  const int blocks = blocks_of(max_read < rows ? max_read : rows, batch, &p.blocks_per_seq);
+  if (!blocks) return GEMM_ERR_TOO_LARGE;
+  SharedDevice dev;
+  rc = shared_device(&dev);
+  if (rc != GEMM_OK) return rc;
+  p.b.status = dev.status;
+  p.out[0] = static_cast<__half*>(K);
+  p.out[1] = static_cast<__half*>(V);
+  return launch(dev, kv_read_u4_kernel, dim3(static_cast<unsigned>(blocks), 2), KV4_THREADS, 0,
+                reinterpret_cast<cudaStream_t>(stream), p);
+}
+
+int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,
+                    const int* block_table, int table_stride, int max_q, int q_heads,
+                    const void* Q, long long q_token_stride, long long q_head_stride,
+                    float softmax_scale, int window, void* out, long long out_token_stride,
+                    int rows, gemm_stream_t stream) {
+  AttnTilesParams p = {};
+  KvBatch b;
+  int rc = check_cache(cache, &p.c);
+  if (rc == GEMM_OK) rc = check_batch(batch, cu, kv_len, block_table, table_stride, max_q, rows, &b);
+  if (rc != GEMM_OK) return rc;
+  if (!Q || !out || q_heads <= 0 || q_heads % p.c.heads || window < 0 || q_token_stride < p.c.dim ||
+      q_head_stride < p.c.dim || out_token_stride < static_cast<long long>(q_heads) * p.c.dim ||
+      !(softmax_scale > 0.0f && softmax_scale < 1e30f))
+    return GEMM_ERR_INVALID_ARG;
+  if (misaligned(Q, 16) || misaligned(out, 16) || q_token_stride % 8 || q_head_stride % 8 ||
+      out_token_stride % 8)
+    return GEMM_ERR_MISALIGNED;
+  p.group = q_heads / p.c.heads;
+  constexpr long long FAR = 1ll << 38;  // (strides of tensor maps stay below 2^40 bytes)
+  if (p.group > 128 || q_token_stride > FAR || q_head_stride > FAR || rows > 0x7fffffff - 1024) return GEMM_ERR_TOO_LARGE;
+  SharedDevice dev;
+  rc = shared_device(&dev);
+  if (rc != GEMM_OK) return rc;
+  p.batch = batch;
+  p.cu = cu;
+  p.kv_len = kv_len;
+  p.table = block_table;
+  p.table_stride = table_stride;
+  p.max_q = max_q;
+  p.rows = rows;
+  p.heads = p.c.heads;
+  p.q = static_cast<const __half*>(Q);
+  p.q_token_stride = q_token_stride;
+  p.q_head_stride = q_head_stride;
+  p.out = static_cast<__half*>(out);
+  p.out_token_stride = out_token_stride;
+  p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.causal = 1;
+  p.window = window;
+  p.status = dev.status;
+  const long long max_len = static_cast<long long>(table_stride) * p.c.page;
+  p.max_len = max_len < 0x7fffffff - 256 ? static_cast<int>(max_len) : 0x7fffffff - 256;
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  switch (p.c.dim) {
+    case 64: return launch_tiles<64>(dev, p, st);
+    case 128: return launch_tiles<128>(dev, p, st);
+    default: return launch_tiles<256>(dev, p, st);
+  }
+}
+
+}  // extern "C"

@@ -8,12 +8,11 @@
 #include "kv_attention.cuh"
 #include "kv_attention_tiles.cuh"
 #include "kv_cache.cuh"
+#include "kv_host.cuh"
 #include "shared_state.h"
 
 namespace b200gemm {
 namespace {
-
-bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
 int check_cache(const kv_cache_s8_t* c, KvCacheView* v) {
   if (!c || !c->k || !c->v || !c->k_scale || !c->v_scale) return GEMM_ERR_INVALID_ARG;
@@ -36,39 +35,6 @@ int check_cache(const kv_cache_s8_t* c, KvCacheView* v) {
   return GEMM_OK;
 }
 
-int check_batch(int batch, const int* cu, const int* start, const int* table, int table_stride,
-                int max_rows, int rows, KvBatch* b) {
-  if (batch <= 0 || !cu || !start || !table || table_stride <= 0 || max_rows <= 0 || rows <= 0)
-    return GEMM_ERR_INVALID_ARG;
-  if (misaligned(cu, 4) || misaligned(start, 4) || misaligned(table, 4)) return GEMM_ERR_MISALIGNED;
-  b->batch = batch;
-  b->cu = cu;
-  b->start = start;
-  b->table = table;
-  b->table_stride = table_stride;
-  b->max_rows = max_rows;
-  b->rows = rows;
-  return GEMM_OK;
-}
-
-template <class Kernel, class Params>
-int launch(const SharedDevice& dev, Kernel kernel, dim3 grid, int threads, size_t smem,
-           cudaStream_t stream, const Params& p) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(static_cast<unsigned>(threads));
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = dev.plain_order ? 0 : 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
-  return e == cudaSuccess ? GEMM_OK : shared_cuda_fail(e);
-}
-
-constexpr int MAX_DEV = 64;
 constexpr int ANY_ROWS = 0x7fffffff;  // the entry points without a row count
 
 // D: head size, NR: groups of eight rows per tile.

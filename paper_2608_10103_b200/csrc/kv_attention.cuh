@@ -47,7 +47,7 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
-#include "kv_cache.cuh"
+#include "kv_common.cuh"
 #include "ptx.cuh"
 #include "warp_pieces.cuh"
 

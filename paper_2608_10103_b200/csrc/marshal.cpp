@@ -1,4 +1,4 @@
-// Argument marshalling of the linear-layer, row-quantisation and cache entry points, for the calls
+// Argument marshalling of the linear-layer, row-quantisation, cache and attention entry points, for the calls
 // whose own time is a few microseconds: tensors are looked at and outputs allocated here instead of
 // attribute by attribute from Python (11 us of a 7 us single-token linear layer were spent there,
 // 4 of them in the library).  No arithmetic, no CUDA: the C entry points are called by address.
@@ -11,7 +11,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <string>
+#include <type_traits>
 
+#include "../../include/b200attn.h"
 #include "../../include/b200kv.h"
 
 namespace {
@@ -31,6 +33,11 @@ struct Entries {
   decltype(&kv_append_s8_rows) kv_append;
   decltype(&kv_read_s8_rows) kv_read;
   decltype(&kv_attention_s8_rows) kv_attention;
+  decltype(&kv_append_u4) kv_append4;
+  decltype(&kv_read_u4) kv_read4;
+  decltype(&kv_attention_u4) kv_attention4;
+  decltype(&attention_fp16) attention;
+  decltype(&rotary_fp16) rotary;
 } g_entry = {};
 
 // The current device, asked for once a call (with the first CUDA tensor).  Per thread: kv_read lets other threads run
@@ -231,25 +238,30 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-kv_cache_s8_t cache_of(PyObject* o) {
+// A cache of either kind: int8 codes with FP32 scales per page and head, or 4-bit codes with pairs of FP16 per token and head.
+template <class Cache>
+Cache cache_of(PyObject* o) {
+  constexpr bool u4 = std::is_same<Cache, kv_cache_u4_t>::value;
+  constexpr at::ScalarType code = u4 ? at::kByte : at::kChar, scale = u4 ? at::kHalf : at::kFloat;
   if (!PyTuple_Check(o) && !PyList_Check(o))
     throw Refused{PyExc_TypeError, "cache is (k, v, k_scale, v_scale)"};
   if (PySequence_Fast_GET_SIZE(o) != 4) throw Refused{PyExc_ValueError, "cache is (k, v, k_scale, v_scale)"};
   PyObject** const i = PySequence_Fast_ITEMS(o);
-  kv_cache_s8_t c = {};
-  c.k = static_cast<int8_t*>(dense(i[0], at::kChar, "k"));
-  c.v = static_cast<int8_t*>(dense(i[1], at::kChar, "v"));
-  c.k_scale = static_cast<float*>(dense(i[2], at::kFloat, "k_scale"));
-  c.v_scale = static_cast<float*>(dense(i[3], at::kFloat, "v_scale"));
+  Cache c = {};
+  c.k = static_cast<decltype(c.k)>(dense(i[0], code, "k"));
+  c.v = static_cast<decltype(c.v)>(dense(i[1], code, "v"));
+  c.k_scale = static_cast<decltype(c.k_scale)>(dense(i[2], scale, "k_scale"));
+  c.v_scale = static_cast<decltype(c.v_scale)>(dense(i[3], scale, "v_scale"));
   const auto shape = THPVariable_Unpack(i[0]).sizes();
   const auto ks = THPVariable_Unpack(i[2]).sizes();
-  if (shape.size() != 4 || THPVariable_Unpack(i[1]).sizes() != shape || ks != shape.slice(0, 2) ||
-      THPVariable_Unpack(i[3]).sizes() != ks)
-    throw Refused{PyExc_ValueError, "cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim), two (pages, heads)"};
+  if (shape.size() != 4 || THPVariable_Unpack(i[1]).sizes() != shape || THPVariable_Unpack(i[3]).sizes() != ks ||
+      (u4 ? ks.size() != 4 || ks.slice(0, 3) != shape.slice(0, 3) || ks[3] != 2 : ks != shape.slice(0, 2)))
+    throw Refused{PyExc_ValueError, u4 ? "cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim / 2), two (pages, heads, page, 2)"
+                                       : "cache is (k, v, k_scale, v_scale): two (pages, heads, page, dim), two (pages, heads)"};
   c.num_pages = narrow(shape[0], "pages");
   c.kv_heads = narrow(shape[1], "heads");
   c.page_size = narrow(shape[2], "page");
-  c.head_dim = narrow(shape[3], "dim");
+  c.head_dim = narrow(u4 ? 2 * shape[3] : shape[3], "dim");
   return c;
 }
 
@@ -289,10 +301,11 @@ Rows heads_of(const at::Tensor& t, int heads, int dim, const char* what) {
 }
 
 // kv_append(cache, k, v, cu, past, table, max_new, stream)
-PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+template <class Cache, class Entry>
+PyObject* kv_append_of(Entry entry, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 8)) return nullptr;
   return guarded([&]() -> PyObject* {
-    const kv_cache_s8_t c = cache_of(a[0]);
+    const Cache c = cache_of<Cache>(a[0]);
     const Rows k = heads_of(typed(a[1], at::kHalf, "k"), c.kv_heads, c.head_dim, "k");
     const Rows v = heads_of(typed(a[2], at::kHalf, "v"), c.kv_heads, c.head_dim, "v");
     if (k.tokens != v.tokens || k.token != v.token || k.head != v.head)
@@ -300,7 +313,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Batch b = batch_of(a[3], a[4], a[5], "past");
     const int max_new = integer(a[6], "max_new");
     if (k.tokens == 0) Py_RETURN_NONE;
-    const int rc = g_entry.kv_append(&c, b.batch, b.cu, b.start, b.table, b.width, max_new,
+    const int rc = entry(&c, b.batch, b.cu, b.start, b.table, b.width, max_new,
                                      k.ptr, v.ptr, k.token, k.head, narrow(k.tokens, "tokens"), stream_of(a[7]).handle);
     if (rc) return code(rc);
     Py_RETURN_NONE;
@@ -308,10 +321,11 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // kv_read(cache, cu, first, table, max_read, tokens, out, stream)
-PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+template <class Cache, class Entry>
+PyObject* kv_read_of(Entry entry, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 8)) return nullptr;
   return guarded([&]() -> PyObject* {
-    const kv_cache_s8_t c = cache_of(a[0]);
+    const Cache c = cache_of<Cache>(a[0]);
     const Batch b = batch_of(a[1], a[2], a[3], "first");
     const int max_read = integer(a[4], "max_read");
     const Launch s = stream_of(a[7]);
@@ -337,7 +351,7 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
       for (auto& t : out) t = new_out({tokens, c.kv_heads, c.head_dim}, at::kHalf, s);
     }
     if (out[0].size(0) > 0) {
-      const int rc = g_entry.kv_read(&c, b.batch, b.cu, b.start, b.table, b.width, max_read,
+      const int rc = entry(&c, b.batch, b.cu, b.start, b.table, b.width, max_read,
                                      out[0].data_ptr(), out[1].data_ptr(), narrow(out[0].size(0), "tokens"), s.handle);
       if (rc) return code(rc);
     }
@@ -351,10 +365,11 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // kv_attention(q, cache, cu, kv_len, table, max_q, softmax_scale, window, out, stream)
-PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+template <class Cache, class Entry>
+PyObject* kv_attention_of(Entry entry, PyObject* const* a, Py_ssize_t n) {
   if (!arity(n, 10)) return nullptr;
   return guarded([&]() -> PyObject* {
-    const kv_cache_s8_t c = cache_of(a[1]);
+    const Cache c = cache_of<Cache>(a[1]);
     const at::Tensor& qt = typed(a[0], at::kHalf, "q");
     const Rows q = heads_of(qt, 0, c.head_dim, "q");
     const Batch b = batch_of(a[2], a[3], a[4], "kv_len");
@@ -371,7 +386,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Rows o = heads_of(out, 0, c.head_dim, "out");
     if (o.head != c.head_dim) throw Refused{PyExc_ValueError, "the heads of a row of out must be contiguous"};
     if (q.tokens > 0) {
-      const int rc = g_entry.kv_attention(&c, b.batch, b.cu, b.start, b.table, b.width, max_q, narrow(q.heads, "heads"), q.ptr,
+      const int rc = entry(&c, b.batch, b.cu, b.start, b.table, b.width, max_q, narrow(q.heads, "heads"), q.ptr,
                                           q.token, q.head, scale, window, out.data_ptr(), o.token,
                                           narrow(q.tokens, "tokens"), s.handle);
       if (rc) return code(rc);
@@ -380,11 +395,126 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The arguments are those of the functions above.
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_append_of<kv_cache_s8_t>(g_entry.kv_append, a, n); }
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_read_of<kv_cache_s8_t>(g_entry.kv_read, a, n); }
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return kv_attention_of<kv_cache_s8_t>(g_entry.kv_attention, a, n);
+}
+PyObject* kv_append4(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_append_of<kv_cache_u4_t>(g_entry.kv_append4, a, n); }
+PyObject* kv_read4(PyObject*, PyObject* const* a, Py_ssize_t n) { return kv_read_of<kv_cache_u4_t>(g_entry.kv_read4, a, n); }
+PyObject* kv_attention4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return kv_attention_of<kv_cache_u4_t>(g_entry.kv_attention4, a, n);
+}
+
+// attention(q, k, v, cu, max_len, softmax_scale, causal, window, out, stream)
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 10)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const at::Tensor& qt = typed(a[0], at::kHalf, "q");
+    if (qt.dim() != 3) throw Refused{PyExc_ValueError, "q must be (tokens, heads, dim)"};
+    const int dim = narrow(qt.size(2), "dim");
+    const Rows q = heads_of(qt, 0, dim, "q");
+    const Rows k = heads_of(typed(a[1], at::kHalf, "k"), 0, dim, "k");
+    const Rows v = heads_of(typed(a[2], at::kHalf, "v"), 0, dim, "v");
+    if (k.tokens != v.tokens || k.heads != v.heads || k.token != v.token || k.head != v.head)
+      throw Refused{PyExc_ValueError, "k and v must have the same shape and strides"};
+    if (k.tokens != q.tokens) throw Refused{PyExc_ValueError, "q, k and v must have the same tokens"};
+    const int* const cu = static_cast<const int*>(dense(a[3], at::kInt, "cu"));
+    const int batch = narrow(THPVariable_Unpack(a[3]).numel() - 1, "batch");
+    const int max_len = integer(a[4], "max_len"), causal = PyObject_IsTrue(a[6]), window = integer(a[7], "window");
+    const float scale = number(a[5]);
+    const Launch s = stream_of(a[9]);
+    at::Tensor out;
+    if (a[8] != Py_None) {
+      out = typed(a[8], at::kHalf, "out");
+      if (out.sizes() != qt.sizes()) throw Refused{PyExc_ValueError, "out must have the shape of q"};
+    } else {
+      out = new_out(qt.sizes(), at::kHalf, s);
+    }
+    const Rows o = heads_of(out, 0, dim, "out");
+    if (o.head != dim) throw Refused{PyExc_ValueError, "the heads of a row of out must be contiguous"};
+    if (q.tokens > 0) {
+      const int rc = g_entry.attention(batch, cu, max_len, narrow(q.tokens, "tokens"), narrow(q.heads, "heads"),
+                                       narrow(k.heads, "heads"), dim, q.ptr, q.token, q.head, k.ptr, v.ptr, k.token, k.head, scale,
+                                       causal, window, out.data_ptr(), o.token, s.handle);
+      if (rc) return code(rc);
+    }
+    return THPVariable_Wrap(out);
+  });
+}
+
+// rotary(q, k, positions, inv_freq, sections, pairs, out, stream): k, sections and out may be None
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!arity(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const int given = a[1] == Py_None ? 1 : 2;
+    for (int i = 0; i < given; ++i) typed(a[i], at::kHalf, i ? "k" : "q");
+    const Launch s = stream_of(a[7]);
+    if (a[6] != Py_None && (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != given))
+      throw Refused{PyExc_TypeError, "out is a tuple of one tensor for each of q and k"};
+    rotary_rows_t rows[2] = {};
+    at::Tensor out[2];
+    int64_t tokens = 0;
+    int dim = 0;
+    for (int i = 0; i < given; ++i) {
+      const char* const what = i ? "k" : "q";
+      const at::Tensor& x = THPVariable_Unpack(a[i]);
+      if (x.dim() != 3) throw Refused{PyExc_ValueError, std::string(what) + " must be (tokens, heads, dim)"};
+      if (i == 0) {
+        tokens = x.size(0);
+        dim = narrow(x.size(2), "dim");
+      } else if (x.size(0) != tokens) {
+        throw Refused{PyExc_ValueError, "q and k must have the same tokens"};
+      }
+      const Rows r = heads_of(x, 0, dim, what);
+      if (a[6] != Py_None) {
+        out[i] = typed(PyTuple_GET_ITEM(a[6], i), at::kHalf, "out");
+        if (out[i].sizes() != x.sizes()) throw Refused{PyExc_ValueError, "out must have the shapes of q and k"};
+      } else {
+        out[i] = new_out(x.sizes(), at::kHalf, s);
+      }
+      const Rows o = heads_of(out[i], 0, dim, "out");
+      rows[i] = {r.ptr, o.ptr, narrow(r.heads, "heads"), r.token, r.head, o.token, o.head};
+    }
+    const int* const positions = static_cast<const int*>(dense(a[2], at::kInt, "positions"));
+    const at::Tensor& pt = THPVariable_Unpack(a[2]);
+    if (pt.dim() < 1 || pt.dim() > 2 || pt.size(pt.dim() - 1) != tokens)
+      throw Refused{PyExc_ValueError, "positions must be (axes, tokens) or (tokens,)"};
+    const int axes = pt.dim() == 2 ? narrow(pt.size(0), "axes") : 1;
+    const float* const inv_freq = static_cast<const float*>(dense(a[3], at::kFloat, "inv_freq"));
+    const int64_t count = THPVariable_Unpack(a[3]).numel();
+    int sections[4] = {};
+    if (a[4] != Py_None) {
+      if (!PyTuple_Check(a[4]) && !PyList_Check(a[4])) throw Refused{PyExc_TypeError, "sections is a tuple of integers"};
+      const Py_ssize_t size = PySequence_Fast_GET_SIZE(a[4]);
+      if (size != axes || size > 4) throw Refused{PyExc_ValueError, "sections needs one entry per axis, four at most"};
+      for (Py_ssize_t i = 0; i < size; ++i) sections[i] = integer(PySequence_Fast_GET_ITEM(a[4], i), "sections");
+    } else if (axes != 1) {
+      throw Refused{PyExc_ValueError, "positions of several axes need sections"};
+    }
+    if (tokens > 0) {
+      const int rc = g_entry.rotary(narrow(tokens, "tokens"), dim, narrow(2 * count, "inv_freq"), integer(a[5], "pairs"), &rows[0],
+                                    given > 1 ? &rows[1] : nullptr, positions, axes, tokens, a[4] == Py_None ? nullptr : sections,
+                                    inv_freq, s.handle);
+      if (rc) return code(rc);
+    }
+    PyObject* const q = THPVariable_Wrap(out[0]);
+    if (given == 1) return q;
+    PyObject* const k = THPVariable_Wrap(out[1]);
+    PyObject* const both = PyTuple_Pack(2, q, k);
+    Py_XDECREF(q);
+    Py_XDECREF(k);
+    return both;
+  });
+}
+
 // entries(address, ...): in the order of the struct above
 PyObject* entries(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!arity(n, 7)) return nullptr;
-  void* p[7];
-  for (int i = 0; i < 7; ++i) {
+  constexpr int COUNT = 12;
+  if (!arity(n, COUNT)) return nullptr;
+  void* p[COUNT];
+  for (int i = 0; i < COUNT; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "an entry point is missing");
@@ -398,12 +528,18 @@ PyObject* entries(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_entry.kv_append = reinterpret_cast<decltype(g_entry.kv_append)>(p[4]);
   g_entry.kv_read = reinterpret_cast<decltype(g_entry.kv_read)>(p[5]);
   g_entry.kv_attention = reinterpret_cast<decltype(g_entry.kv_attention)>(p[6]);
+  g_entry.kv_append4 = reinterpret_cast<decltype(g_entry.kv_append4)>(p[7]);
+  g_entry.kv_read4 = reinterpret_cast<decltype(g_entry.kv_read4)>(p[8]);
+  g_entry.kv_attention4 = reinterpret_cast<decltype(g_entry.kv_attention4)>(p[9]);
+  g_entry.attention = reinterpret_cast<decltype(g_entry.attention)>(p[10]);
+  g_entry.rotary = reinterpret_cast<decltype(g_entry.rotary)>(p[11]);
   Py_RETURN_NONE;
 }
 
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(entries),   METHOD(linear),  METHOD(quantize_rows), METHOD(kv_append),
-                         METHOD(kv_read),   METHOD(kv_attention), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(kv_read),   METHOD(kv_attention), METHOD(kv_append4), METHOD(kv_read4),
+                         METHOD(kv_attention4), METHOD(attention), METHOD(rotary), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

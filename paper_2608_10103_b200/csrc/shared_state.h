@@ -2,6 +2,7 @@
 // Internal: not exported in any header of include/.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 
@@ -29,5 +30,11 @@ struct SharedLease {
 };
 int shared_scratch(int device, cudaStream_t stream, size_t need, size_t head, SharedLease* out);
 int shared_scratch_done(int device, cudaStream_t stream, const SharedLease& lease);
+
+
+// Tensor map of binary16 rows [tokens][heads][dim] with strides in elements: boxes of 64 d x box_heads x box_tokens, in the
+// 128-byte swizzle; places beyond the tensor read as zeros.
+int shared_row_map(CUtensorMap* out, const void* base, int dim, int heads, int tokens, long long token_stride,
+                   long long head_stride, int box_heads, int box_tokens);
 
 }  // namespace b200gemm
