@@ -14,12 +14,13 @@
 // computed. One row tile at 256 d has two score buffers instead: the scores of the next tokens are computed meanwhile.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
-// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; four warps expand a code c to offset + c scale,
-// rounded to binary16 once (a sixteenth-bit nibble becomes a binary16 by placing it under the exponent of 1024 or of 64),
-// and write the same tiles.
+// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; four warps write the same tiles: keys as
+// their codes, which are exact in binary16, and values as offset + c scale, rounded to it once. A score of such
+// keys is scale (q . codes) + offset sum(q), by a table of two factors per token (keys rounded to binary16 too would make the results'
+// distance from the exact ones 6e-4 of their norm instead of 3e-4, 2e-4 being that of the rounded exact ones).
 //
 // What a masked place holds must not matter, but weight 0 times an infinity is NaN. 4-bit tokens whose scale or offset is not
-// finite get zeros for values and NaN for keys: a NaN score for the rows that see them, and nothing for those that mask it.
+// finite get zeros for values and NaN for the scores' factor: NaN for the rows that see them, and nothing for those that mask it.
 // Binary16 values are not looked at on their way; a row whose result is not finite looks through the tokens that its
 // masked tiles hide from it and, if one of them is not finite, is computed again, alone.
 #pragma once
@@ -79,12 +80,15 @@ struct AttnTileShape {
   static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
   static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_BYTES;
   static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // of a K or V tile; two tiles of both
-  static constexpr int ITEM_OFFSET = SCALE_OFFSET + 4 * SCALE_BYTES;
+  static constexpr int TABLES = 4;               // ring of the scores' factors, four floats for two tokens
+  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 4 * SCALE_BYTES;
+  static constexpr int TABLE_BYTES = U4 ? TN * 8 : 0;
+  static constexpr int ITEM_OFFSET = TABLE_OFFSET + TABLES * TABLE_BYTES;
   static constexpr int ITEM_INTS = 16;
   static constexpr int BAR_OFFSET = ITEM_OFFSET + 2 * ITEM_INTS * 4;
   // item_full[2], item_empty[2], q_full, q_empty, s_full[2], p_full[2][2], o_done[2], drain[2], raw_full[2], raw_empty[2],
-  // parts_written, parts_counted, slot_full[], slot_empty[]
-  static constexpr int BARS = 22 + 2 * SLOTS;
+  // parts_written, parts_counted, table_full[4], slot_full[], slot_empty[]
+  static constexpr int BARS = 26 + 2 * SLOTS;
   static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
   static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
   static constexpr uint32_t O_COLUMN = 256;      // S (and its weights) of tile i at TN i, O behind both
@@ -211,6 +215,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
@@ -236,15 +245,20 @@ __device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// Eight codes as binary16 values offset + code * scale, in order; scale and offset twice in their words.
-__device__ __forceinline__ uint4 expand(uint32_t w, uint32_t scale, uint32_t offset) {
+// Eight codes in binary16, in the order of pairs d (0, 4), (1, 5), (2, 6), (3, 7): a nibble under the exponent of 1024 or of 64.
+__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&h)[4]) {
   const uint32_t u = w >> 8;
-  const uint32_t a = fma_h2(sub_h2((w & 0x000f000fu) | 0x64006400u, 0x64006400u), scale, offset);  // 1024 + code: d 0, 4
-  const uint32_t b = fma_h2(sub_h2((w & 0x00f000f0u) | 0x54005400u, 0x54005400u), scale, offset);  // 64 + code: d 1, 5
-  const uint32_t c = fma_h2(sub_h2((u & 0x000f000fu) | 0x64006400u, 0x64006400u), scale, offset);
-  const uint32_t d = fma_h2(sub_h2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u), scale, offset);
-  return make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(c, d, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x7632));
+  h[0] = sub_h2((w & 0x000f000fu) | 0x64006400u, 0x64006400u);
+  h[1] = sub_h2((w & 0x00f000f0u) | 0x54005400u, 0x54005400u);
+  h[2] = sub_h2((u & 0x000f000fu) | 0x64006400u, 0x64006400u);
+  h[3] = sub_h2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u);
 }
+// ... brought into the order of d
+__device__ __forceinline__ uint4 in_order(const uint32_t (&h)[4]) {
+  return make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[0], h[1], 0x7632),
+                    __byte_perm(h[2], h[3], 0x7632));
+}
+
 // One row of a prompt by itself: query `row` of head hq over tokens [first, last] of the packed arrays.
 template <int D>
 __device__ __forceinline__ void lone_row(const AttnTilesParams& p, int row, int hq, int head, int first, int last) {
@@ -315,8 +329,9 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   auto raw_full = [&](int w) { return bar0 + 8u * (16 + w); };
   auto raw_empty = [&](int w) { return bar0 + 8u * (18 + w); };
   const uint32_t parts_written = bar0 + 8u * 20, parts_counted = bar0 + 8u * 21;
-  auto slot_full = [&](int s) { return bar0 + 8u * (22 + s); };
-  auto slot_empty = [&](int s) { return bar0 + 8u * (22 + SLOTS + s); };
+  auto table_full = [&](int i) { return bar0 + 8u * (22 + i); };
+  auto slot_full = [&](int s) { return bar0 + 8u * (26 + s); };
+  auto slot_empty = [&](int s) { return bar0 + 8u * (26 + SLOTS + s); };
   volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
   volatile uint32_t* const abort_flag = tmem_holder + 1;
   volatile uint32_t* const last_flag = tmem_holder + 2;
@@ -341,6 +356,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     ptx::mbar_init(q_empty, QT);
     ptx::mbar_init(parts_written, T::SOFTMAX_WARPS);
     ptx::mbar_init(parts_counted, 1);
+    for (int i = 0; i < T::TABLES; ++i) ptx::mbar_init(table_full(i), 4);
     for (int i = 0; i < SLOTS; ++i) {
       ptx::mbar_init(slot_full(i), U4 ? 4 : 1);
       ptx::mbar_init(slot_empty(i), QT);
@@ -396,6 +412,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     const float c = p.scale_log2;
     const uint64_t c2 = pair(c, c);
     int done = 0;  // token tiles of this tile of rows so far
+    int ring = 0;  // token tiles of the CTA before this item
     int joins = 0;
     bool ok = true;
 #pragma unroll 1
@@ -403,6 +420,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       AttnItem it;
       ok = next_item(k, it);
       if (!ok || it.tiles < 0) break;
+      const int ring0 = ring;
+      ring += it.tiles;
       if (q >= it.active) {
         // (the joining below is for all of these warps)
       } else {
@@ -415,6 +434,24 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const int all_hi = p.causal ? it.base + q0 : pos;
         const int all_lo = p.window > 0 ? it.base + min(it.n, q0 + per_tile) - p.window : 0;
         float m = -INFINITY, l = 0.0f;
+        uint64_t q_sum2 = 0;  // the sum of the row's values, twice
+        if constexpr (U4) {
+          float sum = 0.0f;
+          if (live) {
+            const __half* const src = p.q + (static_cast<long long>(it.row0) + qi) * p.q_token_stride + hq * p.q_head_stride;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 8) {
+              uint32_t w[4];
+              asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(src + d) : "memory");
+#pragma unroll
+              for (int v = 0; v < 4; ++v) {
+                const float2 f = half2_of(w[v]);
+                sum += f.x + f.y;
+              }
+            }
+          }
+          q_sum2 = pair(sum, sum);
+        }
 #pragma unroll 1
         for (int j = 0; j < it.tiles; ++j, ++done) {
           const int sb = QT == 2 ? q : done & 1;  // score buffer
@@ -427,6 +464,22 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 #pragma unroll
           for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
           ptx::tmem_wait_ld();
+          if constexpr (U4) {  // scores in the units of the exponent: scale (q . codes) + offset sum(q)
+            ok = wait_bounded(table_full((ring0 + j) % T::TABLES), ((ring0 + j) / T::TABLES) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
+#pragma unroll
+            for (int h = 0; h < TN / 32; ++h)
+#pragma unroll
+              for (int v = 0; v < 32; v += 2) {
+                uint64_t scale, offset;
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(scale), "=l"(offset) : "r"(table + (h * 32 + v) * 8) : "memory");
+                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), scale, mul2(offset, q_sum2)));
+                x[h][v] = __float_as_uint(t.x);
+                x[h][v + 1] = __float_as_uint(t.y);
+              }
+          }
           const int tok0 = it.lo + j * TN;
           if (tok0 + TN - 1 > all_hi || tok0 < all_lo) {
             const int last = pos - tok0, first = from - tok0;
@@ -447,7 +500,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               for (int u = 0; u < 4; ++u)
                 mx[u] = v + u + 4 < 32 ? fmaxf(fmaxf(mx[u], __uint_as_float(x[h][v + u])), __uint_as_float(x[h][v + u + 4]))
                                        : fmaxf(mx[u], __uint_as_float(x[h][v + u]));
-          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+          float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          if constexpr (!U4) top *= c;
           const bool grow = top > m + 8.0f;
           if (__any_sync(0xffffffffu, grow)) {
             const float now = grow ? top : m;
@@ -480,7 +534,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             uint32_t w[16];
 #pragma unroll
             for (int v = 0; v < 32; v += 2) {
-              const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), c2, at2));
+              const uint64_t x2 = pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1]));
+              const float2 t = unpair(U4 ? add2(x2, at2) : fma2(x2, c2, at2));
               const float e0 = exp2_approx(t.x), e1 = exp2_approx(t.y);
               sum[(v / 2) & 1] = add2(sum[(v / 2) & 1], pair(e0, e1));
               w[v / 2] = pack_halves(e0, e1);
@@ -865,28 +920,50 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const uint32_t codes = base + T::RAW_OFFSET + which * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
         const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + (nth & 1) * 2 * T::SCALE_BYTES);
         const uint32_t to = base + T::SLOT_OFFSET + slot * T::TILE_BYTES + static_cast<uint32_t>((piece >> 1) * T::CHUNK);
+        // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
+        const int first = it.lo + (j >> 1) * TN;
+        auto seen = [&](int tok) { return first + tok < it.hi && first + tok >= it.from; };
+        if (which == 0 && ct < TN) {  // factors of the scores; NaN for a token whose key or value is not finite
+          const uint32_t mine = scales[ct];
+          const float2 f = half2_of(mine);
+          float a = 0.0f, b = 0.0f;
+          if (seen(ct)) {
+            a = not_finite2(mine) || not_finite2(scales[TN + ct]) ? __int_as_float(0x7fffffff) : p.scale_log2 * f.x;
+            b = p.scale_log2 * f.y;
+          }
+          float* const table = reinterpret_cast<float*>(base_ptr + T::TABLE_OFFSET + (nth % T::TABLES) * T::TABLE_BYTES) + (ct >> 1) * 4 + (ct & 1);
+          table[0] = a;
+          table[2] = b;
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int tok = i * TOKENS_AT_ONCE + t0;
           uint32_t w[4];
           ptx::ld_shared_v4(codes + i * 2048, w[0], w[1], w[2], w[3]);
-          // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
-          const int place = it.lo + (j >> 1) * TN + tok;
-          const bool seen = place < it.hi && place >= it.from;
-          const uint32_t mine = seen ? scales[which * TN + tok] : 0u, other = which || !seen ? 0u : scales[TN + tok];
-          const bool bad = not_finite2(mine) || not_finite2(other);
-          const uint32_t scale = bad ? (which ? 0u : 0x7fff7fffu) : __byte_perm(mine, 0, 0x1010);
-          const uint32_t offset = bad && which ? 0u : __byte_perm(mine, 0, 0x3232);
+          uint32_t scale = 0, offset = 0;  // twice in their words; of V
+          if (which) {
+            const uint32_t mine = scales[TN + tok];
+            const bool good = seen(tok) && !not_finite2(mine);
+            scale = good ? __byte_perm(mine, 0, 0x1010) : 0u;
+            offset = good ? __byte_perm(mine, 0, 0x3232) : 0u;
+          }
           const uint32_t at = to + static_cast<uint32_t>(tok * 128), sw = static_cast<uint32_t>(tok & 7);
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const uint4 x = expand(w[v], scale, offset);
+            uint32_t h[4];
+            codes_of(w[v], h);
+            if (which) {
+#pragma unroll
+              for (int u = 0; u < 4; ++u) h[u] = fma_h2(h[u], scale, offset);
+            }
+            const uint4 x = in_order(h);
             ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), x.x, x.y, x.z, x.w);
           }
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
+          if (which == 0) ptx::mbar_arrive(table_full(nth % T::TABLES));
           ptx::mbar_arrive(slot_full(slot));
           ptx::mbar_arrive(raw_empty(which));
         }

@@ -6,6 +6,7 @@
 
 #include "../../include/b200kv.h"
 #include "attention_tiles.cuh"
+#include "kv_attention_u4.cuh"
 #include "kv_cache_u4.cuh"
 #include "kv_host.cuh"
 #include "shared_state.h"
@@ -83,6 +84,75 @@ int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream
   rc = launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, q, q, p);
   const int done = shared_scratch_done(dev.device, stream, lease);
   return rc != GEMM_OK ? rc : done;
+}
+
+// Sequences of up to p.split_rows rows.  D: head size, NR: groups of eight rows.
+template <int D, int NR>
+int launch_few_rows(const SharedDevice& dev, KvAttn4Params p, cudaStream_t stream) {
+  static std::atomic<int> resident[MAX_DEV];
+  constexpr int room = 227 * 1024 / kva4_ctas(D, NR) - 2048 - kva4_q_bytes(D, NR);
+  constexpr int slots = room / (KVA_WARPS * kva4_slot_bytes(D));
+  constexpr int depth = slots < 8 ? slots : 8;
+  static_assert(depth >= 2, "the ring holds two steps at least");
+  constexpr int smem = kva4_smem(D, NR, depth);
+  auto kernel = kv_attention_u4_kernel<D, NR, depth>;
+  int per_sm = resident[dev.device].load();
+  if (per_sm == 0) {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, KVA_THREADS, smem);
+    if (e != cudaSuccess) return shared_cuda_fail(e);
+    if (per_sm < 1) return shared_cuda_fail(cudaErrorLaunchOutOfResources);
+    resident[dev.device].store(per_sm);
+  }
+  p.min_share = 4;
+  const int grid = per_sm * dev.num_sms;
+  const size_t counters = static_cast<size_t>(p.batch) * p.c.heads * 4;
+  const size_t bytes = 2ull * grid * kva_rows_floats(8 * NR, D) * 4;
+  SharedLease lease;
+  int rc = shared_scratch(dev.device, stream, bytes, (counters + 255) / 256 * 256, &lease);
+  if (rc != GEMM_OK) return rc;
+  p.arrived = static_cast<unsigned*>(lease.head);
+  p.partial = static_cast<float*>(lease.data);
+  rc = launch(dev, kernel, dim3(grid), KVA_THREADS, smem, stream, p);
+  const int done = shared_scratch_done(dev.device, stream, lease);
+  return rc != GEMM_OK ? rc : done;
+}
+
+constexpr int FEW_ROWS = 16;  // most rows of a sequence that the few-rows kernel takes
+
+template <int D>
+int attention(const SharedDevice& dev, AttnTilesParams& p, cudaStream_t stream) {
+  const long long most = static_cast<long long>(p.max_q < p.rows ? p.max_q : p.rows) * p.group;
+  p.split_rows = FEW_ROWS;
+  // The few-rows kernel counts the steps of all sequences in 32 bits.
+  const long long steps = static_cast<long long>(p.max_len) / kva4_step(D) + 1 + kva4_unit_cost(D);
+  if (most + p.group + 512 >= (1ll << 31) || static_cast<long long>(p.batch) * p.heads >= (1ll << 30) / steps)
+    return GEMM_ERR_TOO_LARGE;
+  if (most > FEW_ROWS) {
+    const int rc = launch_tiles<D>(dev, p, stream);
+    if (rc != GEMM_OK || p.group > FEW_ROWS) return rc;
+  }
+  KvAttn4Params few = {};
+  few.c = p.c;
+  few.batch = p.batch;
+  few.cu = p.cu;
+  few.kv_len = p.kv_len;
+  few.table = p.table;
+  few.table_stride = p.table_stride;
+  few.max_q = p.max_q;
+  few.rows = p.rows;
+  few.max_len = p.max_len;
+  few.group = p.group;
+  few.q = p.q;
+  few.q_token_stride = p.q_token_stride;
+  few.q_head_stride = p.q_head_stride;
+  few.out = p.out;
+  few.out_token_stride = p.out_token_stride;
+  few.scale_log2 = p.scale_log2;
+  few.window = p.window;
+  few.split_rows = p.split_rows;
+  few.status = p.status;
+  return most <= 8 ? launch_few_rows<D, 1>(dev, few, stream) : launch_few_rows<D, 2>(dev, few, stream);
 }
 
 }  // namespace
@@ -182,9 +252,9 @@ int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const 
   p.max_len = max_len < 0x7fffffff - 256 ? static_cast<int>(max_len) : 0x7fffffff - 256;
   const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   switch (p.c.dim) {
-    case 64: return launch_tiles<64>(dev, p, st);
-    case 128: return launch_tiles<128>(dev, p, st);
-    default: return launch_tiles<256>(dev, p, st);
+    case 64: return attention<64>(dev, p, st);
+    case 128: return attention<128>(dev, p, st);
+    default: return attention<256>(dev, p, st);
   }
 }
 

@@ -2,9 +2,9 @@
 
 Tolerance, per output value, with p the softmax weights, v the values and c the softmax scale: rounding of a weight to
 binary16 2^-11 p |v| -- codes count with their distance from the middle of the range, so |v| stands for up to
-max(|v|, |offset| + 15 scale) -- (below its normal range 2^-32 of the largest a token); FP32 scores 2^-20 of c sum|q k|,
-twice (numerator and denominator); q in 16 bits of fixed point, max|q| / 64516 a value (few rows), or k and v rounded to
-binary16, 2^-11 of c sum |q k| and of p |v| (many rows); sums cut off 2e-9 a token; binary16 result 2^-11 (2^-25)."""
+max(|v|, |offset| + 15 scale) -- (below its normal range 2^-32 of the largest a token); FP32 scores 2^-20 of c sum |q| (|offset|
++ 15 scale), twice (numerator and denominator); q in 16 bits of fixed point, max|q| / 64516 a value (few rows), or v rounded to
+binary16, 2^-11 of p |v| (many rows); sums cut off 2e-9 a token; binary16 result 2^-11 (2^-25)."""
 import math
 
 import numpy as np
@@ -63,7 +63,7 @@ def reference(q, cache, table, lens, news, window, scale):
         for lo in range(0, n, 256):
             xs = x[lo:lo + 256]
             sc = torch.einsum("nhgd,htd->nhgt", xs, kk) * scale
-            mag = (torch.einsum("nhgd,htd->nhgt", xs.abs(), kk.abs()) * scale).amax(3, keepdim=True)
+            mag = (torch.einsum("nhgd,htd->nhgt", xs.abs(), ktop) * scale).amax(3, keepdim=True)
             pos = L - n + lo + torch.arange(xs.shape[0], device="cuda")[:, None]
             tok = torch.arange(L, device="cuda")[None]
             hidden = tok > pos
@@ -72,7 +72,7 @@ def reference(q, cache, table, lens, news, window, scale):
             w = torch.nan_to_num(torch.softmax(sc.masked_fill(hidden[:, None, None, :], -math.inf), dim=3), nan=0.0)
             o = torch.einsum("nhgt,htd->nhgd", w, vv)
             mass = torch.einsum("nhgt,htd->nhgd", w, vtop)
-            rel = 2.0 ** -11 + (2 * 2.0 ** -20 + 2 * 2.0 ** -11) * mag + 2 * held[lo:lo + 256] + 4e-6 + 2e-9 * L
+            rel = 2.0 ** -11 + 2 * 2.0 ** -20 * mag + 2 * held[lo:lo + 256] + 4e-6 + 2e-9 * L
             t = rel * mass + 2.0 ** -11 * torch.einsum("nhgt,htd->nhgd", w, vv.abs()) + 2.0 ** -11 * o.abs()
             t = t + 2.0 ** -25 + L * 2.0 ** -32 * vtop.amax()
             out.append(o.reshape(-1, q.shape[1], dim))
