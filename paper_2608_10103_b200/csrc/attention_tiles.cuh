@@ -66,7 +66,7 @@ struct AttnTilesParams {
 template <int D, bool U4>
 struct AttnTileShape {
   static constexpr int QT = D <= 128 ? 2 : 1;    // row tiles of 128 per CTA
-  static constexpr int TN = D <= 128 ? 128 : 64; // tokens per tile
+  static constexpr int TN = 64;                  // tokens per tile
   static constexpr int ROWS = 128 * QT;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
   static constexpr int CONVERT_WARPS = U4 ? 4 : 0;
@@ -74,24 +74,33 @@ struct AttnTileShape {
   static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
   static constexpr int TILE_BYTES = (D / 64) * CHUNK;
   static constexpr int Q_BYTES = QT * (D / 64) * 16384;
-  static constexpr int SLOTS = U4 ? (D == 64 ? 6 : 4) : (D == 64 ? 8 : 5);  // K and V tiles in the ring
+  static constexpr int SLOTS = U4 ? (D == 64 ? 8 : D == 128 ? 6 : 4) : (D == 64 ? 12 : D == 128 ? 8 : 4);  // K and V tiles in the ring
   static constexpr int SLOT_OFFSET = Q_BYTES;
   static constexpr int RAW_BYTES = U4 ? TN * D / 2 : 0;  // codes of a K or V tile
   static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
-  static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_BYTES;
-  static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // of a K or V tile; two tiles of both
-  static constexpr int TABLES = 4;               // ring of the scores' factors, four floats for two tokens
-  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 4 * SCALE_BYTES;
+  static constexpr int RAW_STAGES = D == 256 ? 1 : 4;    // rings of such tiles
+  static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_STAGES * RAW_BYTES;
+  static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // scales and offsets of a K or V tile
+  // One tile of both more than of codes: V's are needed longer than K's codes, with which they come.
+  static constexpr int SCALE_STAGES = RAW_STAGES + 1;
+  // Ring of the scores' factors, four floats for two tokens.  They are written with a tile of K, up to SLOTS / 2 tiles ahead of
+  // the first product, and that up to two ahead of the softmax that reads them.
+  static constexpr int TABLES = 8;
+  static_assert(TABLES >= SLOTS / 2 + 2 || !U4, "no factor is replaced before it is read");
+  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 2 * SCALE_STAGES * SCALE_BYTES;
   static constexpr int TABLE_BYTES = U4 ? TN * 8 : 0;
   static constexpr int ITEM_OFFSET = TABLE_OFFSET + TABLES * TABLE_BYTES;
   static constexpr int ITEM_INTS = 16;
   static constexpr int BAR_OFFSET = ITEM_OFFSET + 2 * ITEM_INTS * 4;
-  // item_full[2], item_empty[2], q_full, q_empty, s_full[2], p_full[2][2], o_done[2], drain[2], raw_full[2], raw_empty[2],
-  // parts_written, parts_counted, table_full[4], slot_full[], slot_empty[]
-  static constexpr int BARS = 26 + 2 * SLOTS;
+  // item_full[2], item_empty[2], q_full, q_empty, s_full[4], p_full[4], o_done[2], drain[2], parts_written, parts_counted,
+  // raw_full[2][4], raw_empty[2][4], table_full[8], turn_done[2][4], slot_full[], slot_empty[]
+  static constexpr int BARS = 52 + 2 * SLOTS;
   static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
-  static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
-  static constexpr uint32_t O_COLUMN = 256;      // S (and its weights) of tile i at TN i, O behind both
+  // 32 rows of 32 results for each softmax warp, which leave as runs of 64 bytes: a row pitch of 80 keeps them off one another's banks
+  static constexpr int OUT_PITCH = 80;
+  static constexpr int OUT_OFFSET = MISC_OFFSET + 16;
+  static constexpr int DYN_BYTES = OUT_OFFSET + SOFTMAX_WARPS * 32 * OUT_PITCH + 1024;
+  static constexpr uint32_t O_COLUMN = 256;      // score (and weight) buffer i at TN i, two for each tile of rows; O behind them
   static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");
   static_assert(O_COLUMN + QT * D <= 512, "tensor memory");
 };
@@ -197,6 +206,21 @@ struct AttnOrder {
   }
 };
 
+#ifndef ATTN_TURN
+#define ATTN_TURN 1
+#endif
+#ifndef ATTN_LAG
+#define ATTN_LAG 4
+#endif
+#ifndef ATTN_PASS
+#define ATTN_PASS 31
+#endif
+#ifndef ATTN_SPIN
+#define ATTN_SPIN 0
+#endif
+#ifndef ATTN_FMA_OF
+#define ATTN_FMA_OF 64
+#endif
 namespace attn {
 
 // Pairs of FP32 values in one instruction.
@@ -224,6 +248,51 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+// The same, where they stand: the order of a pipeline written by hand.
+__device__ __forceinline__ uint64_t fma2_here(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm volatile("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2_here(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm volatile("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float exp2_here(float x) {
+  float r;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_here(float a, float b) {
+  uint32_t r;
+  asm volatile("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two values x below 127 by the FMA units: x = i + f with i the nearest whole number, 2^f by the polynomial of
+// degree 4 with the smallest largest relative error on [-1/2, 1/2] (Remez exchange; 2.6e-6), 2^i by its bits.  What is below
+// -126 counts as that; NaN stays.
+__device__ __forceinline__ float2 exp2_fma(uint64_t x2) {
+  constexpr float ROUND = 12582912.0f + 127.0f;  // its sum with x has i + 127 in the low bits
+  float2 x = unpair(x2);
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.0f));
+  x2 = pair(x.x, x.y);
+  const uint64_t whole = add2(x2, pair(ROUND, ROUND));
+  const uint64_t f = fma2(add2(whole, pair(-ROUND, -ROUND)), pair(-1.0f, -1.0f), x2);
+  uint64_t y = fma2(f, pair(9.570102207e-3f, 9.570102207e-3f), pair(5.591785908e-2f, 5.591785908e-2f));
+  y = fma2(f, y, pair(2.402474433e-1f, 2.402474433e-1f));
+  y = fma2(f, y, pair(6.931217909e-1f, 6.931217909e-1f));
+  y = fma2(f, y, pair(9.999992847e-1f, 9.999992847e-1f));
+  const float2 w = unpair(whole);
+  const uint64_t scale = pair(__uint_as_float(__float_as_uint(w.x) << 23), __uint_as_float(__float_as_uint(w.y) << 23));
+  return unpair(mul2(y, scale));
 }
 // 64 d of box_heads x box_tokens rows (see shared_row_map): coordinates d, head, row.
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, int d, int head, int row, uint32_t bar) {
@@ -323,15 +392,16 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   auto item_empty = [&](int i) { return bar0 + 8u * (2 + i); };
   const uint32_t q_full = bar0 + 8u * 4, q_empty = bar0 + 8u * 5;
   auto s_full = [&](int i) { return bar0 + 8u * (6 + i); };
-  auto p_full = [&](int i, int part) { return bar0 + 8u * (8 + 2 * i + part); };
-  auto o_done = [&](int q) { return bar0 + 8u * (12 + q); };
-  auto drain = [&](int q) { return bar0 + 8u * (14 + q); };
-  auto raw_full = [&](int w) { return bar0 + 8u * (16 + w); };
-  auto raw_empty = [&](int w) { return bar0 + 8u * (18 + w); };
-  const uint32_t parts_written = bar0 + 8u * 20, parts_counted = bar0 + 8u * 21;
-  auto table_full = [&](int i) { return bar0 + 8u * (22 + i); };
-  auto slot_full = [&](int s) { return bar0 + 8u * (26 + s); };
-  auto slot_empty = [&](int s) { return bar0 + 8u * (26 + SLOTS + s); };
+  auto p_full = [&](int i) { return bar0 + 8u * (10 + i); };
+  auto o_done = [&](int q) { return bar0 + 8u * (14 + q); };
+  auto drain = [&](int q) { return bar0 + 8u * (16 + q); };
+  const uint32_t parts_written = bar0 + 8u * 18, parts_counted = bar0 + 8u * 19;
+  auto raw_full = [&](int which, int stage) { return bar0 + 8u * (20 + 4 * which + stage); };
+  auto raw_empty = [&](int which, int stage) { return bar0 + 8u * (28 + 4 * which + stage); };
+  auto table_full = [&](int i) { return bar0 + 8u * (36 + i); };
+  auto turn_done = [&](int q, int w) { return bar0 + 8u * (44 + 4 * q + w); };
+  auto slot_full = [&](int s) { return bar0 + 8u * (52 + s); };
+  auto slot_empty = [&](int s) { return bar0 + 8u * (52 + SLOTS + s); };
   volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
   volatile uint32_t* const abort_flag = tmem_holder + 1;
   volatile uint32_t* const last_flag = tmem_holder + 2;
@@ -344,19 +414,23 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(item_full(i), 1);
       ptx::mbar_init(item_empty(i), CONSUMERS);
-      ptx::mbar_init(s_full(i), 1);
-      ptx::mbar_init(p_full(i, 0), 4);
-      ptx::mbar_init(p_full(i, 1), 4);
+      ptx::mbar_init(s_full(2 * i), 1);
+      ptx::mbar_init(s_full(2 * i + 1), 1);
+      ptx::mbar_init(p_full(2 * i), 4);
+      ptx::mbar_init(p_full(2 * i + 1), 4);
       ptx::mbar_init(o_done(i), 1);
       ptx::mbar_init(drain(i), 1);
-      ptx::mbar_init(raw_full(i), 1);
-      ptx::mbar_init(raw_empty(i), 4);
+      for (int stage = 0; stage < 4; ++stage) {
+        ptx::mbar_init(raw_full(i, stage), 1);
+        ptx::mbar_init(raw_empty(i, stage), 4);
+      }
     }
     ptx::mbar_init(q_full, 1);
     ptx::mbar_init(q_empty, QT);
     ptx::mbar_init(parts_written, T::SOFTMAX_WARPS);
     ptx::mbar_init(parts_counted, 1);
     for (int i = 0; i < T::TABLES; ++i) ptx::mbar_init(table_full(i), 4);
+    for (int i = 0; i < 8; ++i) ptx::mbar_init(turn_done(i >> 2, i & 3), 1);
     for (int i = 0; i < SLOTS; ++i) {
       ptx::mbar_init(slot_full(i), U4 ? 4 : 1);
       ptx::mbar_init(slot_empty(i), QT);
@@ -385,24 +459,6 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     return ok;
   };
 
-  // Register shares by group of four warps; they sum up to no more than the block was launched with (384 x 168
-  // resp. 512 x 128): a row's scores stay in registers between the maximum and the weights.
-  if constexpr (QT == 2) {
-    if (warp < T::SOFTMAX_WARPS) {
-      if constexpr (U4)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
-      else
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    } else if (warp < T::SOFTMAX_WARPS + 4) {
-      if constexpr (U4)
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-      else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    } else {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    }
-  }
-
   if (warp < T::SOFTMAX_WARPS) {
     // ------------------------------------------------------------------ softmax, one thread per row
     const int q = warp >> 2, r = (warp & 3) * 32 + lane;  // row of the 128
@@ -414,6 +470,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     int done = 0;  // token tiles of this tile of rows so far
     int ring = 0;  // token tiles of the CTA before this item
     int joins = 0;
+    int turns = 0;  // of this warp at the exponentials
     bool ok = true;
 #pragma unroll 1
     for (int k = 0; ok; ++k) {
@@ -454,9 +511,9 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         }
 #pragma unroll 1
         for (int j = 0; j < it.tiles; ++j, ++done) {
-          const int sb = QT == 2 ? q : done & 1;  // score buffer
+          const int sb = 2 * q + (done & 1);  // score buffer
           const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(sb * TN);
-          ok = wait_bounded(s_full(sb), (QT == 2 ? done : done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = wait_bounded(s_full(sb), (done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           ptx::tc_fence_after_sync();
@@ -489,18 +546,15 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               for (int v = 0; v < 32; ++v)
                 if (h * 32 + v > last || h * 32 + v < first) x[h][v] = 0xff800000u;  // -inf
           }
-          float mx[4];
+          float mx[8];  // (chains of their own)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) mx[u] = __uint_as_float(x[0][u]);
+          for (int u = 0; u < 8; ++u) mx[u] = fmaxf(__uint_as_float(x[0][u]), __uint_as_float(x[0][u + 8]));
 #pragma unroll
-          for (int h = 0; h < TN / 32; ++h)
+          for (int i = 16; i < TN; i += 16)
 #pragma unroll
-            for (int v = h == 0 ? 4 : 0; v < 32; v += 8)
-#pragma unroll
-              for (int u = 0; u < 4; ++u)
-                mx[u] = v + u + 4 < 32 ? fmaxf(fmaxf(mx[u], __uint_as_float(x[h][v + u])), __uint_as_float(x[h][v + u + 4]))
-                                       : fmaxf(mx[u], __uint_as_float(x[h][v + u]));
-          float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+            for (int u = 0; u < 8; ++u)
+              mx[u] = max3(mx[u], __uint_as_float(x[(i + u) / 32][(i + u) % 32]), __uint_as_float(x[(i + u + 8) / 32][(i + u + 8) % 32]));
+          float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
           if constexpr (!U4) top *= c;
           const bool grow = top > m + 8.0f;
           if (__any_sync(0xffffffffu, grow)) {
@@ -525,37 +579,63 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               ptx::tmem_wait_st();
             }
           }
+          // The warps of an SM quarter that have a row tile each take turns at the exponentials, which one warp keeps busy.
+          // (Left alone they fall into step: both at the exponentials, then both at everything else.)
+          if (ATTN_TURN && it.active == 2) {
+            if (q == 1 || turns > 0)
+              ok = wait_bounded<false, ATTN_SPIN>(turn_done(q ^ 1, warp & 3), (q == 1 ? turns : turns - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            ++turns;
+          }
           // weights, two per column, over the scores: 32 tokens take 16 columns
           const float at_ref = KVA_WEIGHT_BITS - (m == -INFINITY ? 0.0f : m);
           const uint64_t at2 = pair(at_ref, at_ref);
           uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-#pragma unroll
-          for (int h = 0; h < TN / 32; ++h) {
+          {
+            // Pair i is summed up and packed LAG pairs after its exponentials were asked for.
+            constexpr int PAIRS = TN / 2, LAG = ATTN_LAG;
+            auto exponent = [&](int i) {
+              const uint64_t x2 = pair(__uint_as_float(x[i / 16][i % 16 * 2]), __uint_as_float(x[i / 16][i % 16 * 2 + 1]));
+              return unpair(U4 ? add2_here(x2, at2) : fma2_here(x2, c2, at2));
+            };
+            float2 e[LAG + 1], t = exponent(0);
             uint32_t w[16];
 #pragma unroll
-            for (int v = 0; v < 32; v += 2) {
-              const uint64_t x2 = pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1]));
-              const float2 t = unpair(U4 ? add2(x2, at2) : fma2(x2, c2, at2));
-              const float e0 = exp2_approx(t.x), e1 = exp2_approx(t.y);
-              sum[(v / 2) & 1] = add2(sum[(v / 2) & 1], pair(e0, e1));
-              w[v / 2] = pack_halves(e0, e1);
-            }
-            ptx::tmem_st_32x32b_x16(s_at + h * 16, w);
-            if (h % (TN / 64) == TN / 64 - 1) {  // half of the tokens
-              ptx::tmem_wait_st();
-              ptx::tc_fence_before_sync();
-              __syncwarp();
-              if (lane == 0) ptx::mbar_arrive(p_full(sb, h / (TN / 64)));
+            for (int i = 0; i < PAIRS + LAG; ++i) {
+              if (i < PAIRS) {
+                if (i % (ATTN_FMA_OF / 2) == ATTN_FMA_OF / 2 - 1) {
+                  e[i % (LAG + 1)] = exp2_fma(pair(t.x, t.y));
+                } else {
+                  e[i % (LAG + 1)].x = exp2_here(t.x);
+                  e[i % (LAG + 1)].y = exp2_here(t.y);
+                }
+                if (i + 1 < PAIRS) t = exponent(i + 1);
+              }
+              if (i == ATTN_PASS && ATTN_TURN && it.active == 2 && lane == 0) ptx::mbar_arrive(turn_done(q, warp & 3));
+              if (i >= LAG) {
+                const int o = i - LAG;
+                const float2 v = e[o % (LAG + 1)];
+                sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
+                w[o % 16] = pack_here(v.x, v.y);
+                if (o % 16 == 15) ptx::tmem_st_32x32b_x16(s_at + (o / 16) * 16, w);
+              }
             }
           }
-          const float2 total = unpair(add2(sum[0], sum[1]));
-          l += total.x + total.y;
-          if (QT == 1 && j > 0) {  // (with two score buffers nothing else says that those are done: a phase that is not waited for is
-                                   // taken for the next but one)
+          ptx::tmem_wait_st();
+          if (j > 0 && j == it.tiles - 1) {
+            // A barrier tells a phase from the one before or behind it only.  That S was there says that the products of the tile before
+            // the last are done (they were issued earlier, by the same thread); the last one's are seen to here, in front of this one's,
+            // so that the wait for these, below, is not taken in by them.
             ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
           }
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(p_full(sb));
+          const float2 total = unpair(add2(sum[0], sum[1]));
+          l += total.x + total.y;
         }
         if (!ok) break;
         // ---- the rows' results
@@ -574,6 +654,12 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         if (U4 && part && live) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         __half* const dst = p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
         uint32_t worst = 0;  // magnitude bits of the results
+        const unsigned alive = __ballot_sync(0xffffffffu, live);
+        const uint32_t stage = base + T::OUT_OFFSET + static_cast<uint32_t>(warp * 32 * T::OUT_PITCH);
+        __half* run[4];  // of rows lane / 4 + 8 i
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          run[i] = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), lane / 4 + 8 * i)) + (lane & 3) * 8;
 #pragma unroll 1
         for (int d = 0; d < D; d += 32) {
           uint32_t x[32];
@@ -584,23 +670,30 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 #pragma unroll
             for (int v = 0; v < 32; ++v) x[v] = 0;
           }
-          if (!live) continue;
           if (U4 && part) {  // O as it stands, to be joined
 #pragma unroll
             for (int v = 0; v < 8; ++v)
-              *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
-            continue;
-          }
+              if (live) *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
+          } else {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            uint32_t y[4];
+            for (int v = 0; v < 4; ++v) {
+              uint32_t y[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              y[u] = pack_halves(__uint_as_float(x[8 * v + 2 * u]) * inv, __uint_as_float(x[8 * v + 2 * u + 1]) * inv);
-              if constexpr (!U4) worst = __vmaxu2(worst, y[u] & 0x7fff7fffu);
+              for (int u = 0; u < 4; ++u) {
+                y[u] = pack_halves(__uint_as_float(x[8 * v + 2 * u]) * inv, __uint_as_float(x[8 * v + 2 * u + 1]) * inv);
+                if constexpr (!U4) worst = __vmaxu2(worst, y[u] & 0x7fff7fffu);
+              }
+              ptx::st_shared_v4(stage + lane * T::OUT_PITCH + v * 16, y[0], y[1], y[2], y[3]);
             }
-            *reinterpret_cast<uint4*>(dst + d + 8 * v) = make_uint4(y[0], y[1], y[2], y[3]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t y[4];
+              ptx::ld_shared_v4(stage + (lane / 4 + 8 * i) * T::OUT_PITCH + (lane & 3) * 16, y[0], y[1], y[2], y[3]);
+              if (alive >> (lane / 4 + 8 * i) & 1u) *reinterpret_cast<uint4*>(run[i] + d) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
           }
+          __syncwarp();
         }
         ptx::tc_fence_before_sync();
         if constexpr (!U4) {
@@ -775,19 +868,21 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const uint32_t count = static_cast<uint32_t>(__popc(__ballot_sync(0xffffffffu, good)));
 #pragma unroll 1
           for (int which = 0; which < 2; ++which) {
-            ok = wait_bounded(raw_empty(which), (tile & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+            const int stage = tile % T::RAW_STAGES;
+            const uint32_t full = raw_full(which, stage);
+            ok = wait_bounded(raw_empty(which, stage), ((tile / T::RAW_STAGES) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             // (scales and offsets of both come with K; runs that are left out keep what the buffers held)
-            if (lane == 0) ptx::mbar_arrive_expect_tx(raw_full(which), count * (run_bytes + (which ? 0u : static_cast<uint32_t>(run) * 8u)));
+            if (lane == 0) ptx::mbar_arrive_expect_tx(full, count * (run_bytes + (which ? 0u : static_cast<uint32_t>(run) * 8u)));
             __syncwarp();
             if (good) {
-              ptx::bulk_load(base + T::RAW_OFFSET + which * T::RAW_BYTES + lane * run_bytes, (which ? p.c.codes[1] : p.c.codes[0]) + token * (D / 2),
-                             run_bytes, raw_full(which));
+              ptx::bulk_load(base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + lane * run_bytes,
+                             (which ? p.c.codes[1] : p.c.codes[0]) + token * (D / 2), run_bytes, full);
               if (which == 0) {
-                const uint32_t to = base + T::SCALE_OFFSET + (tile & 1) * 2 * T::SCALE_BYTES + lane * run * 4;
-                ptx::bulk_load(to, p.c.scales[0] + token, run * 4, raw_full(0));
-                ptx::bulk_load(to + T::SCALE_BYTES, p.c.scales[1] + token, run * 4, raw_full(0));
+                const uint32_t to = base + T::SCALE_OFFSET + (tile % T::SCALE_STAGES) * 2 * T::SCALE_BYTES + lane * run * 4;
+                ptx::bulk_load(to, p.c.scales[0] + token, run * 4, full);
+                ptx::bulk_load(to + T::SCALE_BYTES, p.c.scales[1] + token, run * 4, full);
               }
             }
           }
@@ -807,7 +902,6 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     const bool elected = ptx::elect_one();
     constexpr uint32_t idesc_qk = ptx::make_idesc<ptx::KIND_F16>(128, TN);
     constexpr uint32_t idesc_pv = ptx::make_idesc<ptx::KIND_F16>(128, D) | ptx::IDESC_B_MN_MAJOR;
-    constexpr int AHEAD = QT == 2 ? 1 : 2;  // score buffers of these rows
     int tile = 0;  // K and V tiles in the ring before this item
     int done = 0;  // token tiles of these rows
     bool ok = true;
@@ -840,7 +934,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       ++used;
       auto qk = [&](int j) {  // scores of token tile j
         if (!wait_slot(tile + 2 * j)) return false;
-        const int slot = (tile + 2 * j) % SLOTS, sb = QT == 2 ? q : (done + j) & 1;
+        const int slot = (tile + 2 * j) % SLOTS, sb = 2 * q + ((done + j) & 1);
         if (elected) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
@@ -856,34 +950,25 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         __syncwarp();
         return true;
       };
-      for (int j = 0; j < AHEAD && j < it.tiles && ok; ++j) ok = qk(j);
+      for (int j = 0; j < 2 && j < it.tiles && ok; ++j) ok = qk(j);
 #pragma unroll 1
       for (int j = 0; j < it.tiles && ok; ++j) {
-        const int sb = QT == 2 ? q : (done + j) & 1;
-        const uint32_t parity = (QT == 2 ? done + j : (done + j) >> 1) & 1;
-        const int slot = (tile + 2 * j + 1) % SLOTS;
-        ok = wait_slot(tile + 2 * j + 1);
+        const int sb = 2 * q + ((done + j) & 1), slot = (tile + 2 * j + 1) % SLOTS;
+        ok = wait_slot(tile + 2 * j + 1) && wait_bounded(p_full(sb), ((done + j) >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        if (elected) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          ok = ok && wait_bounded(p_full(sb, part), parity, abort_flag, p.status, DEV_TIMEOUT_MMA);
-          if (ok) {
-            ptx::tc_fence_after_sync();
-            if (elected) {
-#pragma unroll
-              for (int kk = part * (TN / 32); kk < (part + 1) * (TN / 32); ++kk) {
-                const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
-                ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || kk > 0);
-              }
-              if (part == 1) {
-                ptx::mma_commit<1>(o_done(q));
-                ptx::mma_commit<1>(slot_empty(slot));
-              }
-            }
-            __syncwarp();
+          for (int kk = 0; kk < TN / 16; ++kk) {
+            const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
+            ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || kk > 0);
           }
+          ptx::mma_commit<1>(o_done(q));
+          ptx::mma_commit<1>(slot_empty(slot));
         }
+        __syncwarp();
         // (the scores go where the weights are: the MMAs of this thread run in order)
-        if (ok && j + AHEAD < it.tiles) ok = qk(j + AHEAD);
+        if (j + 2 < it.tiles) ok = qk(j + 2);
       }
       tile += 2 * it.tiles;
       done += it.tiles;
@@ -912,13 +997,13 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       if (!ok || it.tiles < 0) break;
 #pragma unroll 1
       for (int j = 0; j < 2 * it.tiles; ++j, ++tile) {
-        const int which = j & 1, slot = tile % SLOTS, nth = tile >> 1;
-        ok = wait_bounded(raw_full(which), nth & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
+        const int which = j & 1, slot = tile % SLOTS, nth = tile >> 1, stage = nth % T::RAW_STAGES;
+        ok = wait_bounded(raw_full(which, stage), (nth / T::RAW_STAGES) & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
              wait_bounded(slot_empty(slot), ((tile / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint32_t codes = base + T::RAW_OFFSET + which * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
-        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + (nth & 1) * 2 * T::SCALE_BYTES);
+        const uint32_t codes = base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
+        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + (nth % T::SCALE_STAGES) * 2 * T::SCALE_BYTES);
         const uint32_t to = base + T::SLOT_OFFSET + slot * T::TILE_BYTES + static_cast<uint32_t>((piece >> 1) * T::CHUNK);
         // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
         const int first = it.lo + (j >> 1) * TN;
@@ -965,7 +1050,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         if (lane == 0) {
           if (which == 0) ptx::mbar_arrive(table_full(nth % T::TABLES));
           ptx::mbar_arrive(slot_full(slot));
-          ptx::mbar_arrive(raw_empty(which));
+          ptx::mbar_arrive(raw_empty(which, stage));
         }
       }
     }
