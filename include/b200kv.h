@@ -167,7 +167,6 @@ int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* 
  * or offset (of K or of V) is not finite gives NaN, as does one that holds a NaN or an infinity itself; tokens that it
  * does not see leave it alone.
  * Scores, softmax statistics and sums are FP32, and the softmax weights are rounded as for kv_attention_s8.
- * Sequences of many rows multiply values that are rounded to binary16, by 2^-12 of themselves.
  * The tensor cores' sums cut off what does not fit, up to 2e-9 of the result per token of one sum.
  */
 int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,

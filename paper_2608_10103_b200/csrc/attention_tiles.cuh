@@ -14,13 +14,15 @@
 // computed. One row tile at 256 d has two score buffers instead: the scores of the next tokens are computed meanwhile.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
-// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; four warps write the same tiles: keys as
-// their codes, which are exact in binary16, and values as offset + c scale, rounded to it once. A score of such
-// keys is scale (q . codes) + offset sum(q), by a table of two factors per token (keys rounded to binary16 too would make the results'
-// distance from the exact ones 6e-4 of their norm instead of 3e-4, 2e-4 being that of the rounded exact ones).
+// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; warps write the same tiles from them, keys as
+// their codes and values as theirs less 8, which both are exact in binary16. Scales and offsets go another way, through a table of
+// five factors a token: with sk, ok, sv, ov those of key and value
+//     t = c sk (q . K) + c ok sum(q) + log2 sv,   w = 2^(t - m + 7),   l = sum w / sv,   out = (sum w (V - 8) + sum w (ov + 8 sv) / sv) / l
+// as in kv_attention_u4.cuh. (Keys and values rounded to binary16 instead would need no table, but are 6e-4 of their norm away from the
+// exact results, where this is 2.5e-4, and the rounded exact ones are 2e-4.)
 //
-// What a masked place holds must not matter, but weight 0 times an infinity is NaN. 4-bit tokens whose scale or offset is not
-// finite get zeros for values and NaN for the scores' factor: NaN for the rows that see them, and nothing for those that mask it.
+// What a masked place holds must not matter, but weight 0 times an infinity is NaN. Codes are always finite, and a 4-bit token whose scale or
+// offset is not gets a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
 // Binary16 values are not looked at on their way; a row whose result is not finite looks through the tokens that its
 // masked tiles hide from it and, if one of them is not finite, is computed again, alone.
 #pragma once
@@ -69,7 +71,10 @@ struct AttnTileShape {
   static constexpr int TN = 64;                  // tokens per tile
   static constexpr int ROWS = 128 * QT;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
-  static constexpr int CONVERT_WARPS = U4 ? 4 : 0;
+  static constexpr int CONVERT_WARPS = U4 ? 8 : 0;
+  // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
+  // at a time, as far as there is room for their codes: tile by tile by all warps took 1.4 times as long.
+  static constexpr int TILE_WARPS = D == 256 ? 4 : 1;
   static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
   static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
   static constexpr int TILE_BYTES = (D / 64) * CHUNK;
@@ -78,17 +83,20 @@ struct AttnTileShape {
   static constexpr int SLOT_OFFSET = Q_BYTES;
   static constexpr int RAW_BYTES = U4 ? TN * D / 2 : 0;  // codes of a K or V tile
   static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
-  static constexpr int RAW_STAGES = D == 256 ? 1 : 4;    // rings of such tiles
+  static constexpr int RAW_STAGES = D == 256 ? 1 : D == 128 ? 3 : 4;  // rings of such tiles
+  // The warps that expand into a place of the ring of tiles are always the same ones: they wait for it once for every time that it
+  // is used, as a barrier that tells a phase only from its neighbours needs it.
+  static_assert(!U4 || SLOTS % (2 * RAW_STAGES) == 0, "a place belongs to one group of warps");
+  static_assert(!U4 || 2 * RAW_STAGES * TILE_WARPS <= CONVERT_WARPS, "a group for every place of the ring of codes");
   static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_STAGES * RAW_BYTES;
   static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // scales and offsets of a K or V tile
-  // One tile of both more than of codes: V's are needed longer than K's codes, with which they come.
-  static constexpr int SCALE_STAGES = RAW_STAGES + 1;
-  // Ring of the scores' factors, four floats for two tokens.  They are written with a tile of K, up to SLOTS / 2 tiles ahead of
+  // Ring of the tokens' factors, twelve floats for two of them: of the scores a, a, b, b, L, L and two places; of the sums i, i, r, r.
+  // They are written with a tile of K, up to SLOTS / 2 tiles ahead of
   // the first product, and that up to two ahead of the softmax that reads them.
-  static constexpr int TABLES = 8;
+  static constexpr int TABLES = D == 256 ? 4 : 8;
   static_assert(TABLES >= SLOTS / 2 + 2 || !U4, "no factor is replaced before it is read");
-  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 2 * SCALE_STAGES * SCALE_BYTES;
-  static constexpr int TABLE_BYTES = U4 ? TN * 8 : 0;
+  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 2 * RAW_STAGES * SCALE_BYTES;
+  static constexpr int TABLE_BYTES = U4 ? TN * 24 : 0;
   static constexpr int ITEM_OFFSET = TABLE_OFFSET + TABLES * TABLE_BYTES;
   static constexpr int ITEM_INTS = 16;
   static constexpr int BAR_OFFSET = ITEM_OFFSET + 2 * ITEM_INTS * 4;
@@ -151,11 +159,14 @@ struct AttnOrder {
     if (need <= 0) return count;
     return need < s.n ? count - need / queries : 0;
   }
-  __device__ AttnOrder(const AttnTilesParams& params, int queries, bool report) : p(params), queries(queries) {
+  KvSeq mine;  // sequence `lane`
+  __device__ KvSeq seq(int i) const { return i < 32 ? mine : attn_seq(p, i, false); }
+  __device__ AttnOrder(const AttnTilesParams& params, int queries, bool report) : p(params), queries(queries), mine{} {
     const int lane = static_cast<int>(threadIdx.x) & 31;
     all = longest = 0;
     for (int i = lane; i < p.batch; i += 32) {
       const KvSeq s = attn_seq(p, i, report);
+      if (i < 32) mine = s;
       longest = max(longest, s.len / TN + 1);
       all += tiles_of(s);
     }
@@ -171,7 +182,7 @@ struct AttnOrder {
     while (x_hi - x_lo > 1) {
       const int mid = (x_lo + x_hi) / 2;
       int c = 0;
-      for (int i = lane; i < p.batch; i += 32) c += long_tiles(attn_seq(p, i, false), mid);
+      for (int i = lane; i < p.batch; i += 32) c += long_tiles(seq(i), mid);
       c = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
       if (c > rank) {
         x_lo = mid;
@@ -185,7 +196,7 @@ struct AttnOrder {
     for (int i0 = 0; i0 < p.batch; i0 += 32) {
       int same = 0, qt = 0;
       if (i0 + lane < p.batch) {
-        const KvSeq s = attn_seq(p, i0 + lane, false);
+        const KvSeq s = seq(i0 + lane);
         const int longer = long_tiles(s, x_hi);
         same = long_tiles(s, x_lo) - longer;
         qt = tiles_of(s) - 1 - longer;  // its longest tile of that length
@@ -208,18 +219,6 @@ struct AttnOrder {
 
 #ifndef ATTN_TURN
 #define ATTN_TURN 1
-#endif
-#ifndef ATTN_LAG
-#define ATTN_LAG 4
-#endif
-#ifndef ATTN_PASS
-#define ATTN_PASS 31
-#endif
-#ifndef ATTN_SPIN
-#define ATTN_SPIN 0
-#endif
-#ifndef ATTN_FMA_OF
-#define ATTN_FMA_OF 64
 #endif
 namespace attn {
 
@@ -275,25 +274,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x of two values x below 127 by the FMA units: x = i + f with i the nearest whole number, 2^f by the polynomial of
-// degree 4 with the smallest largest relative error on [-1/2, 1/2] (Remez exchange; 2.6e-6), 2^i by its bits.  What is below
-// -126 counts as that; NaN stays.
-__device__ __forceinline__ float2 exp2_fma(uint64_t x2) {
-  constexpr float ROUND = 12582912.0f + 127.0f;  // its sum with x has i + 127 in the low bits
-  float2 x = unpair(x2);
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.0f));
-  x2 = pair(x.x, x.y);
-  const uint64_t whole = add2(x2, pair(ROUND, ROUND));
-  const uint64_t f = fma2(add2(whole, pair(-ROUND, -ROUND)), pair(-1.0f, -1.0f), x2);
-  uint64_t y = fma2(f, pair(9.570102207e-3f, 9.570102207e-3f), pair(5.591785908e-2f, 5.591785908e-2f));
-  y = fma2(f, y, pair(2.402474433e-1f, 2.402474433e-1f));
-  y = fma2(f, y, pair(6.931217909e-1f, 6.931217909e-1f));
-  y = fma2(f, y, pair(9.999992847e-1f, 9.999992847e-1f));
-  const float2 w = unpair(whole);
-  const uint64_t scale = pair(__uint_as_float(__float_as_uint(w.x) << 23), __uint_as_float(__float_as_uint(w.y) << 23));
-  return unpair(mul2(y, scale));
-}
 // 64 d of box_heads x box_tokens rows (see shared_row_map): coordinates d, head, row.
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, int d, int head, int row, uint32_t bar) {
   asm volatile(
@@ -304,28 +284,21 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, in
 __device__ __forceinline__ bool not_finite2(uint32_t w) {  // either of two binary16
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
-__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t r;
-  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
-  return r;
-}
 __device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-// Eight codes in binary16, in the order of pairs d (0, 4), (1, 5), (2, 6), (3, 7): a nibble under the exponent of 1024 or of 64.
-__device__ __forceinline__ void codes_of(uint32_t w, uint32_t (&h)[4]) {
-  const uint32_t u = w >> 8;
-  h[0] = sub_h2((w & 0x000f000fu) | 0x64006400u, 0x64006400u);
-  h[1] = sub_h2((w & 0x00f000f0u) | 0x54005400u, 0x54005400u);
-  h[2] = sub_h2((u & 0x000f000fu) | 0x64006400u, 0x64006400u);
-  h[3] = sub_h2((u & 0x00f000f0u) | 0x54005400u, 0x54005400u);
+// Eight codes of a key as binary16 numbers, the subnormals c 2^-24 that they are as they stand, in the order of d.
+__device__ __forceinline__ uint4 key_codes(uint32_t w) {
+  const uint32_t a = w & 0x000f000fu, b = (w >> 4) & 0x000f000fu, c = (w >> 8) & 0x000f000fu, d = (w >> 12) & 0x000f000fu;
+  return make_uint4(__byte_perm(a, b, 0x5410), __byte_perm(c, d, 0x5410), __byte_perm(a, b, 0x7632), __byte_perm(c, d, 0x7632));
 }
-// ... brought into the order of d
-__device__ __forceinline__ uint4 in_order(const uint32_t (&h)[4]) {
-  return make_uint4(__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[2], h[3], 0x5410), __byte_perm(h[0], h[1], 0x7632),
-                    __byte_perm(h[2], h[3], 0x7632));
+// Eight codes of a value less 8, in the order d 0, 4, 1, 5, 2, 6, 3, 7: a nibble under the exponent of 1024 or of 64.
+__device__ __forceinline__ uint4 value_codes(uint32_t w) {
+  const uint32_t u = w >> 8;
+  return make_uint4(sub_h2((w & 0x000f000fu) | 0x64006400u, 0x64086408u), sub_h2((w & 0x00f000f0u) | 0x54005400u, 0x54805480u),
+                    sub_h2((u & 0x000f000fu) | 0x64006400u, 0x64086408u), sub_h2((u & 0x00f000f0u) | 0x54005400u, 0x54805480u));
 }
 
 // One row of a prompt by itself: query `row` of head hq over tokens [first, last] of the packed arrays.
@@ -422,17 +395,17 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       ptx::mbar_init(drain(i), 1);
       for (int stage = 0; stage < 4; ++stage) {
         ptx::mbar_init(raw_full(i, stage), 1);
-        ptx::mbar_init(raw_empty(i, stage), 4);
+        ptx::mbar_init(raw_empty(i, stage), T::TILE_WARPS);
       }
     }
     ptx::mbar_init(q_full, 1);
     ptx::mbar_init(q_empty, QT);
     ptx::mbar_init(parts_written, T::SOFTMAX_WARPS);
     ptx::mbar_init(parts_counted, 1);
-    for (int i = 0; i < T::TABLES; ++i) ptx::mbar_init(table_full(i), 4);
+    for (int i = 0; i < T::TABLES; ++i) ptx::mbar_init(table_full(i), T::TILE_WARPS);
     for (int i = 0; i < 8; ++i) ptx::mbar_init(turn_done(i >> 2, i & 3), 1);
     for (int i = 0; i < SLOTS; ++i) {
-      ptx::mbar_init(slot_full(i), U4 ? 4 : 1);
+      ptx::mbar_init(slot_full(i), U4 ? T::TILE_WARPS : 1);
       ptx::mbar_init(slot_empty(i), QT);
     }
     *abort_flag = 0;
@@ -459,6 +432,12 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     return ok;
   };
 
+  if constexpr (U4 && QT == 2) {  // register shares: 256 x 128 + 384 x 72, of the 640 x 96 the block was launched with
+    if (warp < T::SOFTMAX_WARPS)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  }
   if (warp < T::SOFTMAX_WARPS) {
     // ------------------------------------------------------------------ softmax, one thread per row
     const int q = warp >> 2, r = (warp & 3) * 32 + lane;  // row of the 128
@@ -490,7 +469,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const int q0 = it.query + q * per_tile;
         const int all_hi = p.causal ? it.base + q0 : pos;
         const int all_lo = p.window > 0 ? it.base + min(it.n, q0 + per_tile) - p.window : 0;
-        float m = -INFINITY, l = 0.0f;
+        float m = -INFINITY, l = 0.0f, z = 0.0f;  // z: what the offsets of values add to every one of the row's
         uint64_t q_sum2 = 0;  // the sum of the row's values, twice
         if constexpr (U4) {
           float sum = 0.0f;
@@ -521,18 +500,19 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 #pragma unroll
           for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
           ptx::tmem_wait_ld();
-          if constexpr (U4) {  // scores in the units of the exponent: scale (q . codes) + offset sum(q)
+          [[maybe_unused]] const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
+          if constexpr (U4) {  // scores in the units of the exponent, a (q . codes) + b sum(q), and log2 of the value's scale
             ok = wait_bounded(table_full((ring0 + j) % T::TABLES), ((ring0 + j) / T::TABLES) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
 #pragma unroll
             for (int h = 0; h < TN / 32; ++h)
 #pragma unroll
               for (int v = 0; v < 32; v += 2) {
-                uint64_t scale, offset;
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(scale), "=l"(offset) : "r"(table + (h * 32 + v) * 8) : "memory");
-                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), scale, mul2(offset, q_sum2)));
+                uint64_t a, b, logs;
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(table + (h * 32 + v) * 24) : "memory");
+                asm volatile("ld.shared.b64 %0, [%1];" : "=l"(logs) : "r"(table + (h * 32 + v) * 24 + 16) : "memory");
+                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), a, fma2(b, q_sum2, logs)));
                 x[h][v] = __float_as_uint(t.x);
                 x[h][v + 1] = __float_as_uint(t.y);
               }
@@ -562,6 +542,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
             m = now;
             l *= f;
+            z *= f;
             if (j > 0) {  // O of the tiles before, once their products are done
               ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
               ok = __all_sync(0xffffffffu, ok);
@@ -581,9 +562,9 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           }
           // The warps of an SM quarter that have a row tile each take turns at the exponentials, which one warp keeps busy.
           // (Left alone they fall into step: both at the exponentials, then both at everything else.)
-          if (ATTN_TURN && it.active == 2) {
+          if (it.active == 2) {
             if (q == 1 || turns > 0)
-              ok = wait_bounded<false, ATTN_SPIN>(turn_done(q ^ 1, warp & 3), (q == 1 ? turns : turns - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+              ok = wait_bounded(turn_done(q ^ 1, warp & 3), (q == 1 ? turns : turns - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             ++turns;
@@ -594,29 +575,33 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
           {
             // Pair i is summed up and packed LAG pairs after its exponentials were asked for.
-            constexpr int PAIRS = TN / 2, LAG = ATTN_LAG;
+            constexpr int PAIRS = TN / 2, LAG = U4 ? 2 : 4;
             auto exponent = [&](int i) {
               const uint64_t x2 = pair(__uint_as_float(x[i / 16][i % 16 * 2]), __uint_as_float(x[i / 16][i % 16 * 2 + 1]));
               return unpair(U4 ? add2_here(x2, at2) : fma2_here(x2, c2, at2));
             };
             float2 e[LAG + 1], t = exponent(0);
+            [[maybe_unused]] uint64_t of_l[LAG + 1], of_z[LAG + 1];
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < PAIRS + LAG; ++i) {
               if (i < PAIRS) {
-                if (i % (ATTN_FMA_OF / 2) == ATTN_FMA_OF / 2 - 1) {
-                  e[i % (LAG + 1)] = exp2_fma(pair(t.x, t.y));
-                } else {
-                  e[i % (LAG + 1)].x = exp2_here(t.x);
-                  e[i % (LAG + 1)].y = exp2_here(t.y);
-                }
+                if constexpr (U4)
+                  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(of_l[i % (LAG + 1)]), "=l"(of_z[i % (LAG + 1)]) : "r"(table + i * 48 + 32) : "memory");
+                e[i % (LAG + 1)].x = exp2_here(t.x);
+                e[i % (LAG + 1)].y = exp2_here(t.y);
                 if (i + 1 < PAIRS) t = exponent(i + 1);
               }
-              if (i == ATTN_PASS && ATTN_TURN && it.active == 2 && lane == 0) ptx::mbar_arrive(turn_done(q, warp & 3));
+              if (i == PAIRS - 1 && it.active == 2 && lane == 0) ptx::mbar_arrive(turn_done(q, warp & 3));
               if (i >= LAG) {
                 const int o = i - LAG;
                 const float2 v = e[o % (LAG + 1)];
-                sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
+                if constexpr (U4) {
+                  sum[0] = fma2_here(pair(v.x, v.y), of_l[o % (LAG + 1)], sum[0]);
+                  sum[1] = fma2_here(pair(v.x, v.y), of_z[o % (LAG + 1)], sum[1]);
+                } else {
+                  sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
+                }
                 w[o % 16] = pack_here(v.x, v.y);
                 if (o % 16 == 15) ptx::tmem_st_32x32b_x16(s_at + (o / 16) * 16, w);
               }
@@ -634,8 +619,14 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full(sb));
-          const float2 total = unpair(add2(sum[0], sum[1]));
-          l += total.x + total.y;
+          if constexpr (U4) {
+            const float2 of_l = unpair(sum[0]), of_z = unpair(sum[1]);
+            l += of_l.x + of_l.y;
+            z += of_z.x + of_z.y;
+          } else {
+            const float2 total = unpair(add2(sum[0], sum[1]));
+            l += total.x + total.y;
+          }
         }
         if (!ok) break;
         // ---- the rows' results
@@ -669,6 +660,16 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           } else {
 #pragma unroll
             for (int v = 0; v < 32; ++v) x[v] = 0;
+          }
+          if constexpr (U4) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {  // (columns of values lie in the order in which words of codes come apart: 0, 4, 1, 5, ...)
+              float y[8];
+#pragma unroll
+              for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[8 * v + (u < 4 ? 2 * u : 2 * u - 7)]) + z;
+#pragma unroll
+              for (int u = 0; u < 8; ++u) x[8 * v + u] = __float_as_uint(y[u]);
+            }
           }
           if (U4 && part) {  // O as it stands, to be joined
 #pragma unroll
@@ -880,7 +881,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               ptx::bulk_load(base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + lane * run_bytes,
                              (which ? p.c.codes[1] : p.c.codes[0]) + token * (D / 2), run_bytes, full);
               if (which == 0) {
-                const uint32_t to = base + T::SCALE_OFFSET + (tile % T::SCALE_STAGES) * 2 * T::SCALE_BYTES + lane * run * 4;
+                const uint32_t to = base + T::SCALE_OFFSET + (tile % T::RAW_STAGES) * 2 * T::SCALE_BYTES + lane * run * 4;
                 ptx::bulk_load(to, p.c.scales[0] + token, run * 4, full);
                 ptx::bulk_load(to + T::SCALE_BYTES, p.c.scales[1] + token, run * 4, full);
               }
@@ -983,12 +984,16 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     __syncwarp();
   } else if (U4 && warp >= W_LOAD + 4) {
     // ------------------------------------------------------------------ K and V: 4-bit codes to binary16 tiles
-    const int ct = tid - 32 * (W_LOAD + 4);         // 0 .. 127
+    // A group of TILE_WARPS warps has a place of the ring of codes for itself, of K or of V.
+    constexpr int AT_ONCE = 32 * T::TILE_WARPS;     // threads of a tile
+    const int group = (warp - (W_LOAD + 4)) / T::TILE_WARPS, which = group & 1, stage = group >> 1;
+    const int ct = tid % AT_ONCE;
     constexpr int PER_TOKEN = D / 32;               // 16-byte pieces of a token's codes: 32 d, 64 bytes of a row of a chunk
-    constexpr int N = TN * PER_TOKEN / 128;         // pieces per thread and tile
-    constexpr int TOKENS_AT_ONCE = 128 / PER_TOKEN; // tokens the 128 threads cover together
-    const int piece = ct % PER_TOKEN, t0 = ct / PER_TOKEN;
-    int tile = 0;
+    constexpr int N = TN * PER_TOKEN / AT_ONCE;     // pieces per thread and tile
+    constexpr int WARP_TOKENS = 32 / PER_TOKEN;     // tokens that a warp covers at a time (its lanes: neighbouring tokens, whose
+                                                    // rows the swizzle keeps off one another's banks)
+    const int piece = lane / WARP_TOKENS, t0 = ct / 32 * WARP_TOKENS + lane % WARP_TOKENS;
+    int nth = 0;  // token tile of the CTA
     bool ok = true;
 #pragma unroll 1
     for (int k = 0; ok; ++k) {
@@ -996,52 +1001,44 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       ok = next_item(k, it);
       if (!ok || it.tiles < 0) break;
 #pragma unroll 1
-      for (int j = 0; j < 2 * it.tiles; ++j, ++tile) {
-        const int which = j & 1, slot = tile % SLOTS, nth = tile >> 1, stage = nth % T::RAW_STAGES;
+      for (int j = 0; j < it.tiles; ++j, ++nth) {
+        if (nth % T::RAW_STAGES != stage) continue;
+        const int tile = 2 * nth + which, slot = tile % SLOTS;
         ok = wait_bounded(raw_full(which, stage), (nth / T::RAW_STAGES) & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
              wait_bounded(slot_empty(slot), ((tile / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        const uint32_t codes = base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + static_cast<uint32_t>(ct * 16);
-        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + (nth % T::SCALE_STAGES) * 2 * T::SCALE_BYTES);
+        const uint32_t codes = base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + static_cast<uint32_t>(piece * 16);
+        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + stage * 2 * T::SCALE_BYTES);
         const uint32_t to = base + T::SLOT_OFFSET + slot * T::TILE_BYTES + static_cast<uint32_t>((piece >> 1) * T::CHUNK);
-        // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
-        const int first = it.lo + (j >> 1) * TN;
-        auto seen = [&](int tok) { return first + tok < it.hi && first + tok >= it.from; };
-        if (which == 0 && ct < TN) {  // factors of the scores; NaN for a token whose key or value is not finite
-          const uint32_t mine = scales[ct];
-          const float2 f = half2_of(mine);
-          float a = 0.0f, b = 0.0f;
-          if (seen(ct)) {
-            a = not_finite2(mine) || not_finite2(scales[TN + ct]) ? __int_as_float(0x7fffffff) : p.scale_log2 * f.x;
-            b = p.scale_log2 * f.y;
-          }
-          float* const table = reinterpret_cast<float*>(base_ptr + T::TABLE_OFFSET + (nth % T::TABLES) * T::TABLE_BYTES) + (ct >> 1) * 4 + (ct & 1);
-          table[0] = a;
-          table[2] = b;
-        }
+        const int first = it.lo + j * TN;
+        if (which == 0) {  // the tokens' factors; a NaN for one whose key or value is not finite
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int tok = i * TOKENS_AT_ONCE + t0;
-          uint32_t w[4];
-          ptx::ld_shared_v4(codes + i * 2048, w[0], w[1], w[2], w[3]);
-          uint32_t scale = 0, offset = 0;  // twice in their words; of V
-          if (which) {
-            const uint32_t mine = scales[TN + tok];
-            const bool good = seen(tok) && !not_finite2(mine);
-            scale = good ? __byte_perm(mine, 0, 0x1010) : 0u;
-            offset = good ? __byte_perm(mine, 0, 0x3232) : 0u;
+          for (int tok = ct; tok < TN; tok += AT_ONCE) {
+            const uint32_t k_scale = scales[tok], v_scale = scales[TN + tok];
+            const float2 f = half2_of(k_scale), g = half2_of(v_scale);
+            const bool good = !not_finite2(k_scale) && !not_finite2(v_scale);
+            float* const table = reinterpret_cast<float*>(base_ptr + T::TABLE_OFFSET + (nth % T::TABLES) * T::TABLE_BYTES) + (tok >> 1) * 12 + (tok & 1);
+            const float sv = good ? kva_value_scale(g.x) : 1.0f;
+            const float inv = __fdividef(1.0f, sv);
+            // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
+            const bool seen = first + tok < it.hi && first + tok >= it.from;
+            table[0] = !seen ? 0.0f : good ? p.scale_log2 * f.x * 0x1p24f : __int_as_float(0x7fffffff);
+            table[2] = seen && good ? p.scale_log2 * f.y : 0.0f;
+            table[4] = seen ? __log2f(sv) : 0.0f;
+            table[8] = seen ? inv : 0.0f;
+            table[10] = seen && good ? fmaf(8.0f, g.x, g.y) * inv : 0.0f;
           }
+        }
+#pragma unroll 4
+        for (int i = 0; i < N; ++i) {
+          const int tok = i * (AT_ONCE / PER_TOKEN) + t0;
+          uint32_t w[4];
+          ptx::ld_shared_v4(codes + tok * (D / 2), w[0], w[1], w[2], w[3]);
           const uint32_t at = to + static_cast<uint32_t>(tok * 128), sw = static_cast<uint32_t>(tok & 7);
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            uint32_t h[4];
-            codes_of(w[v], h);
-            if (which) {
-#pragma unroll
-              for (int u = 0; u < 4; ++u) h[u] = fma_h2(h[u], scale, offset);
-            }
-            const uint4 x = in_order(h);
+            const uint4 x = which ? value_codes(w[v]) : key_codes(w[v]);
             ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), x.x, x.y, x.z, x.w);
           }
         }

@@ -3,15 +3,16 @@
 // Mathematics.  With a token's scale and offset (sk, ok) of its key, (sv, ov) of its value, codes K, V in 0 .. 15 and weights
 // relative to a running reference m,
 //     t = c (sk (q . K) + ok sum(q)) + log2 sv,   w = 2^(t - m + 7),   u = w / sv,   l = sum u,
-//     O = sum w (V - 7.5) + sum u (ov + 7.5 sv),   out = O / l,
+//     O = sum w (V - 8) + sum u (ov + 8 sv),   out = O / l,
 // c = softmax_scale log2 e.  The value scale is folded into the exponent, as in kv_attention.cuh (see there for m, the 2^7 and
 // the bits of a weight), so that one accumulator serves tokens of any scale; the offsets are a single sum per row, in FP32.
-// w is rounded to binary16 for the product with V; counting codes from the middle of their range halves what that rounding does.
+// w is rounded to binary16 for the product with V; counting codes from the middle of their range halves what that rounding does,
+// and keeps the sums small: a mean of many tokens is far below its terms, and the MMA's sums cut off what does not fit.
 //
 // q . K runs on the integer MMA, q held as 254 q1 + q2 in int8 each (kv_attention.cuh): eight codes of a word are two masks and a
 // shift away from the int8 of two registers.  V has to meet fractional weights: a code in the low bits of a binary16 IS one, the
-// subnormal c 2^-24, and its left neighbour 16 c 2^-24, so that eight registers of V fragments take two byte permutes, two
-// shifts and eight masks; results are scaled by 2^24 or 2^20 at the end.  An MMA with ones for codes gives sum w as rounded.
+// subnormal c 2^-24, and its left neighbour 16 c 2^-24, so that one fused product each makes them (c - 8) 2^-9: eight registers of V
+// fragments take two byte permutes, two shifts, eight masks and eight products.
 //
 // What bounds it: reading the codes once (D + 8 bytes a token and KV head), and issuing some 400 instructions per 32 tokens
 // while they arrive.  As in kv_attention.cuh a warp fetches its own tokens, by cp.async, into a ring nobody else reads; here the
@@ -89,6 +90,17 @@ template <int OFF>
 __device__ __forceinline__ uint32_t lds(uint32_t at) {
   uint32_t r;
   asm volatile("ld.shared.b32 %0, [%1+%2];" : "=r"(r) : "r"(at), "n"(OFF) : "memory");
+  return r;
+}
+// Codes in the lowest four bits of two binary16, or in the next four: (c - 8) 2^-9.
+__device__ __forceinline__ uint32_t low_codes(uint32_t w) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w & 0x000f000fu), "r"(0x78007800u), "r"(0xa400a400u));  // 2^15, -2^-6
+  return r;
+}
+__device__ __forceinline__ uint32_t high_codes(uint32_t w) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w & 0x00f000f0u), "r"(0x68006800u), "r"(0xa400a400u));  // 2^11, -2^-6
   return r;
 }
 
@@ -387,15 +399,13 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
         q_sum[n] = static_cast<float>(sum);
       }
 
-      // O^T: o[n][i] = d (two per lane, see the exchange below) x rows 2t, 2t + 1 of group n; ones: sums of the weights as
-      // they are multiplied, of the same rows; m, l and z (what the offsets add) of row g of group n
-      float o[NR][OT][4], ones[NR][4], mrow[NR], lrow[NR], zrow[NR];
+      // O^T: o[n][i] = d (two per lane, see the exchange below) x rows 2t, 2t + 1 of group n; m, l and z (what the
+      // offsets add) of row g of group n
+      float o[NR][OT][4], mrow[NR], lrow[NR], zrow[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         mrow[n] = -INFINITY;
         lrow[n] = zrow[n] = 0.0f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) ones[n][v] = 0.0f;
 #pragma unroll
         for (int i = 0; i < OT; ++i)
 #pragma unroll
@@ -485,7 +495,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
             const float sv = kva_value_scale(x.x);
             lsv[j][v] = __log2f(sv);
             inv_sv[j][v] = __fdividef(1.0f, sv);
-            mid[j][v] = fmaf(7.5f, x.x, x.y);
+            mid[j][v] = fmaf(8.0f, x.x, x.y);
 #pragma unroll
             for (int n = 0; n < NR; ++n)
               sc[n][j][v] = fmaf(fmaf(k.y, q_sum[n], k.x * sc[n][j][v]), krow[n], lsv[j][v]);
@@ -519,8 +529,6 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
             lrow[n] *= f;
             zrow[n] *= f;
             const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4);
-            ones[n][0] *= f0;
-            ones[n][1] *= f1;
 #pragma unroll
             for (int i = 0; i < OT; ++i) {
               o[n][i][0] *= f0;
@@ -565,15 +573,11 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
 #pragma unroll
             for (int u = 0; u < 4; ++u) {  // d 2u and 2u + 1 of the word
               const uint32_t a = u & 1 ? x[0][u >> 1] >> 8 : x[0][u >> 1], bb = u & 1 ? x[1][u >> 1] >> 8 : x[1][u >> 1];
+              const uint32_t a0 = low_codes(a), a1 = high_codes(a), a2 = low_codes(bb), a3 = high_codes(bb);
 #pragma unroll
-              for (int n = 0; n < NR; ++n)
-                mma_f16_m16n8k16(o[n][4 * w + u], a & 0x000f000fu, a & 0x00f000f0u, bb & 0x000f000fu, bb & 0x00f000f0u, pw[n][2 * h],
-                                 pw[n][2 * h + 1]);
+              for (int n = 0; n < NR; ++n) mma_f16_m16n8k16(o[n][4 * w + u], a0, a1, a2, a3, pw[n][2 * h], pw[n][2 * h + 1]);
             }
           }
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-            mma_f16_m16n8k16(ones[n], 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u, pw[n][2 * h], pw[n][2 * h + 1]);
         });
       }
       cp_async_wait<0>();
@@ -596,11 +600,10 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
         for (int v = 0; v < 2; ++v) {
           if (8 * n + 2 * t + v >= rows) continue;
           float* const dst = mine_out + (8 * n + 2 * t + v) * PITCH + g * (D / 8);
-          const float middle = -7.5f * ones[n][v];
           // tile i holds d = g D / 8 + 2 i and the one behind it
 #pragma unroll
           for (int i = 0; i < OT; ++i)
-            *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(fmaf(o[n][i][v], 0x1p24f, middle), fmaf(o[n][i][v + 2], 0x1p20f, middle));
+            *reinterpret_cast<float2*>(dst + 2 * i) = make_float2(o[n][i][v] * 512.0f, o[n][i][v + 2] * 512.0f);
         }
       }
       __syncthreads();
