@@ -183,8 +183,13 @@ int kv_append_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int
   p.x[1] = static_cast<const __half*>(V);
   p.token_stride = token_stride;
   p.head_stride = head_stride;
-  return launch(dev, kv_append_u4_kernel, dim3(static_cast<unsigned>(blocks), 2), KV4_THREADS, 0,
-                reinterpret_cast<cudaStream_t>(stream), p);
+  const dim3 grid(static_cast<unsigned>(blocks), 2);
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  switch (p.c.dim) {
+    case 64: return launch(dev, kv_append_u4_kernel<64>, grid, KV4_THREADS, 0, st, p);
+    case 128: return launch(dev, kv_append_u4_kernel<128>, grid, KV4_THREADS, 0, st, p);
+    default: return launch(dev, kv_append_u4_kernel<256>, grid, KV4_THREADS, 0, st, p);
+  }
 }
 
 int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* first,
@@ -204,8 +209,13 @@ int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* 
   p.b.status = dev.status;
   p.out[0] = static_cast<__half*>(K);
   p.out[1] = static_cast<__half*>(V);
-  return launch(dev, kv_read_u4_kernel, dim3(static_cast<unsigned>(blocks), 2), KV4_THREADS, 0,
-                reinterpret_cast<cudaStream_t>(stream), p);
+  const dim3 grid(static_cast<unsigned>(blocks), 2);
+  const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  switch (p.c.dim) {
+    case 64: return launch(dev, kv_read_u4_kernel<64>, grid, KV4_THREADS, 0, st, p);
+    case 128: return launch(dev, kv_read_u4_kernel<128>, grid, KV4_THREADS, 0, st, p);
+    default: return launch(dev, kv_read_u4_kernel<256>, grid, KV4_THREADS, 0, st, p);
+  }
 }
 
 int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,

@@ -4,9 +4,11 @@
 // Every token and head has a scale and an offset of its own, so that writing looks at nothing that is there
 // already, and what a token is held as does not depend on the call that brought it.
 //
-// Both kernels move 16 bytes of binary16 a lane, a row of head_dim values being 8 to 32 lanes side by side; the
-// extrema of a row travel between them as one pair (max, -min), four or five shuffles. Bound by 2 bytes read and 0.53 written
-// per value (reading back: the reverse), and in single-token calls by a launch and two dependent loads.
+// Eight lanes share a row (a token's head), head_dim / 64 pieces of eight values each: 16 bytes of binary16 or 4 of codes, side by
+// side. The extrema of a row travel between them as one pair (max, -min), three shuffles. What a row costs besides its values
+// (where it lies, two divisions) is a third of the instructions so, instead of two thirds with one piece per lane
+// (4 x 8192 tokens written and 4 x 9192 read back: 104 -> 62 us). Bound by 2 bytes read and 0.53 written per value (reading
+// back: the reverse), and in single-token calls by a launch and two dependent loads.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -27,7 +29,9 @@ struct KvAppendU4Params {
 
 constexpr int KV4_THREADS = 256;
 constexpr int KV4_TOKENS = 16;  // tokens per CTA
-constexpr int KV4_UNITS = 4;    // 16-byte pieces a thread has in flight
+constexpr int KV4_ROWS = KV4_THREADS / 8;  // rows a CTA works on at a time
+// Rows a thread has in flight: four pieces of 16 bytes.
+__host__ __device__ constexpr int kv4_units(int dim) { return 256 / dim; }
 
 // Two halves' larger one each, a NaN on either side staying.
 __device__ __forceinline__ uint32_t kv4_max2(uint32_t a, uint32_t b) {
@@ -35,9 +39,29 @@ __device__ __forceinline__ uint32_t kv4_max2(uint32_t a, uint32_t b) {
   asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// Rows in the order of tokens, then heads, KV4_ROWS apart: no division per row.
+struct Kv4Row {
+  int token, head, step_token, step_head, heads;
+  __device__ Kv4Row(int first, int heads) : heads(heads) {
+    token = first / heads;
+    head = first - token * heads;
+    step_token = KV4_ROWS / heads;
+    step_head = KV4_ROWS - step_token * heads;
+  }
+  __device__ void next() {
+    token += step_token;
+    head += step_head;
+    if (head >= heads) {
+      head -= heads;
+      ++token;
+    }
+  }
+};
 
 // grid: (batch * blocks_per_seq, 2)
+template <int D>
 __global__ void __launch_bounds__(KV4_THREADS) kv_append_u4_kernel(const KvAppendU4Params p) {
+  constexpr int PIECES = D / 64, UNITS = kv4_units(D);
   if (threadIdx.x == 0) ptx::grid_dep_launch_dependents();
   const int seq = static_cast<int>(blockIdx.x) / p.blocks_per_seq;
   const int nth = static_cast<int>(blockIdx.x) % p.blocks_per_seq;
@@ -47,42 +71,46 @@ __global__ void __launch_bounds__(KV4_THREADS) kv_append_u4_kernel(const KvAppen
   const int t0 = nth * KV4_TOKENS;
   const int tokens = min(KV4_TOKENS, r.end - r.begin - t0);
   if (tokens <= 0) return;
-  const int per_row = p.c.dim / 8;  // lanes of a row: 8, 16 or 32
-  const int rows = tokens * p.c.heads, at_once = KV4_THREADS / per_row;
-  const int lane = static_cast<int>(threadIdx.x) & (per_row - 1), first = static_cast<int>(threadIdx.x) / per_row;
-  const __half* const x = (which ? p.x[1] : p.x[0]) + lane * 8;
+  const int lane = static_cast<int>(threadIdx.x) & 7;
+  const __half* const x = (which ? p.x[1] : p.x[0]) + (static_cast<long long>(r.row0) + t0) * p.token_stride + lane * 8;
   const int* const table = p.b.table + static_cast<long long>(seq) * p.b.table_stride;
-  uint8_t* const codes = which ? p.c.codes[1] : p.c.codes[0];
+  uint8_t* const codes = (which ? p.c.codes[1] : p.c.codes[0]) + lane * 4;
   __half2* const scales = which ? p.c.scales[1] : p.c.scales[0];
+  Kv4Row row(static_cast<int>(threadIdx.x) >> 3, p.c.heads);
 #pragma unroll 1
-  for (int row0 = 0; row0 < rows; row0 += KV4_UNITS * at_once) {
-    uint4 v[KV4_UNITS];
-    int slot[KV4_UNITS], head[KV4_UNITS], pos[KV4_UNITS];  // pos -1 = none
+  for (int done = 0; done < tokens * p.c.heads; done += UNITS * KV4_ROWS) {
+    uint4 v[UNITS][PIECES];
+    int slot[UNITS], at[UNITS];  // page, place of the row in it; -1 = no row
 #pragma unroll
-    for (int i = 0; i < KV4_UNITS; ++i) {
-      const int row = row0 + first + i * at_once;
-      const bool in = row < rows;
-      const int t = in ? row / p.c.heads : 0;
-      head[i] = in ? row - t * p.c.heads : 0;
-      pos[i] = in ? r.begin + t0 + t : -1;
-      v[i] = make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < UNITS; ++i) {
+      at[i] = -1;
       slot[i] = -1;
-      if (in) {
-        slot[i] = kv_ld(table + (pos[i] >> p.c.page_shift));
-        v[i] = ptx::ld_global_stream_v4(x + (static_cast<long long>(r.row0) + t0 + t) * p.token_stride + head[i] * p.head_stride);
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) v[i][k] = make_uint4(0, 0, 0, 0);
+      if (row.token < tokens) {
+        const int pos = r.begin + t0 + row.token;
+        at[i] = row.head * p.c.page + (pos & (p.c.page - 1));
+        slot[i] = kv_ld(table + (pos >> p.c.page_shift));
+        const __half* const from = x + row.token * p.token_stride + row.head * p.head_stride;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) v[i][k] = ptx::ld_global_stream_v4(from + k * 64);
       }
+      row.next();
     }
 #pragma unroll
-    for (int i = 0; i < KV4_UNITS; ++i) {
-      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+    for (int i = 0; i < UNITS; ++i) {
       // (max, -min) of the row; the sign bit turned makes a minimum a maximum
-      uint32_t most = kv4_max2(kv4_max2(w[0], w[1]), kv4_max2(w[2], w[3]));
-      uint32_t least = kv4_max2(kv4_max2(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u),
-                                kv4_max2(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u));
+      uint32_t most = 0xfc00fc00u, least = 0xfc00fc00u;
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        const uint32_t w[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+        most = kv4_max2(most, kv4_max2(kv4_max2(w[0], w[1]), kv4_max2(w[2], w[3])));
+        least = kv4_max2(least, kv4_max2(kv4_max2(w[0] ^ 0x80008000u, w[1] ^ 0x80008000u),
+                                         kv4_max2(w[2] ^ 0x80008000u, w[3] ^ 0x80008000u)));
+      }
       uint32_t both = kv4_max2(__byte_perm(most, least, 0x5410), __byte_perm(most, least, 0x7632));
 #pragma unroll
-      for (int o = 16; o; o >>= 1)
-        if (o < per_row) both = kv4_max2(both, __shfl_xor_sync(0xffffffffu, both, o));
+      for (int o = 4; o; o >>= 1) both = kv4_max2(both, __shfl_xor_sync(0xffffffffu, both, o));
       const __half hi = __ushort_as_half(static_cast<unsigned short>(both & 0xffffu));
       const __half lo = __ushort_as_half(static_cast<unsigned short>((both >> 16) ^ 0x8000u));
       const float low = __half2float(lo);
@@ -94,27 +122,31 @@ __global__ void __launch_bounds__(KV4_THREADS) kv_append_u4_kernel(const KvAppen
       if (low + 15.0f * __half2float(step) >= 65520.0f) step = __ushort_as_half(static_cast<unsigned short>(__half_as_ushort(step) - 1));
       const float s = __half2float(step);
       const float inverse = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
-      // Codes as whole FP32 numbers by adding 2^23 (rounded to even by the addition), four of them as one number below 2^16:
-      // conversions to integers run at a quarter of the rate of all this.
-      float four[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[2 * j]));
-        const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&w[2 * j + 1]));
-        auto code = [&](float x) {  // (16 bits of scale may leave the largest value a little beyond 15)
-          return __fadd_rn(__fadd_rn(fminf(__fmul_rn(__fsub_rn(x, low), inverse), 15.0f), 8388608.0f), -8388608.0f);
-        };
-        four[j] = fmaf(code(g.y), 4096.0f, fmaf(code(g.x), 256.0f, fmaf(code(f.y), 16.0f, code(f.x)))) + 8388608.0f;
-      }
-      const uint32_t word = bad ? 0u : __byte_perm(__float_as_uint(four[0]), __float_as_uint(four[1]), 0x5410);
-      if (pos[i] < 0) continue;
+      if (at[i] < 0) continue;
       if (slot[i] < 0 || slot[i] >= p.c.num_pages) {
         if (lane == 0) kv_report(p.b.status);
         continue;
       }
-      const long long token = (static_cast<long long>(slot[i]) * p.c.heads + head[i]) * p.c.page + (pos[i] & (p.c.page - 1));
-      *reinterpret_cast<uint32_t*>(codes + token * (p.c.dim / 2) + lane * 4) = word;
+      const long long token = static_cast<long long>(slot[i]) * (p.c.heads * p.c.page) + at[i];
       if (lane == 0) scales[token] = __halves2half2(step, lo);
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        const uint32_t w[4] = {v[i][k].x, v[i][k].y, v[i][k].z, v[i][k].w};
+        // Codes as whole FP32 numbers by adding 2^23 (rounded to even by the addition), four of them as one number below 2^16:
+        // conversions to integers run at a quarter of the rate of all this.
+        float four[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[2 * j]));
+          const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&w[2 * j + 1]));
+          auto code = [&](float y) {  // (16 bits of scale may leave the largest value a little beyond 15)
+            return __fadd_rn(__fadd_rn(fminf(__fmul_rn(__fsub_rn(y, low), inverse), 15.0f), 8388608.0f), -8388608.0f);
+          };
+          four[j] = fmaf(code(g.y), 4096.0f, fmaf(code(g.x), 256.0f, fmaf(code(f.y), 16.0f, code(f.x)))) + 8388608.0f;
+        }
+        const uint32_t word = bad ? 0u : __byte_perm(__float_as_uint(four[0]), __float_as_uint(four[1]), 0x5410);
+        *reinterpret_cast<uint32_t*>(codes + token * (D / 2) + k * 32) = word;
+      }
     }
   }
 }
@@ -127,7 +159,9 @@ struct KvReadU4Params {
 };
 
 // grid: (batch * blocks_per_seq, 2)
+template <int D>
 __global__ void __launch_bounds__(KV4_THREADS) kv_read_u4_kernel(const KvReadU4Params p) {
+  constexpr int PIECES = D / 64, UNITS = 2 * kv4_units(D);
   if (threadIdx.x == 0) ptx::grid_dep_launch_dependents();
   const int seq = static_cast<int>(blockIdx.x) / p.blocks_per_seq;
   const int nth = static_cast<int>(blockIdx.x) % p.blocks_per_seq;
@@ -139,52 +173,62 @@ __global__ void __launch_bounds__(KV4_THREADS) kv_read_u4_kernel(const KvReadU4P
   const int t0 = nth * KV4_TOKENS;
   const int tokens = min(KV4_TOKENS, r.end - r.begin - t0);
   if (tokens <= 0) return;
-  const int per_row = p.c.dim / 8, per_token = p.c.heads * per_row;
+  const int lane = static_cast<int>(threadIdx.x) & 7;
   const int* const table = p.b.table + static_cast<long long>(seq) * p.b.table_stride;
-  const uint8_t* const codes = which ? p.c.codes[1] : p.c.codes[0];
+  const uint8_t* const codes = (which ? p.c.codes[1] : p.c.codes[0]) + lane * 4;
   const __half2* const scales = which ? p.c.scales[1] : p.c.scales[0];
-  const int units = tokens * per_token;
+  // rows of a token are dense: heads x dim, and so are those of neighbouring tokens
+  __half* to = out + ((static_cast<long long>(r.row0) + t0) * p.c.heads + (threadIdx.x >> 3)) * D + lane * 8;
+  Kv4Row row(static_cast<int>(threadIdx.x) >> 3, p.c.heads);
 #pragma unroll 1
-  for (int first = static_cast<int>(threadIdx.x); first < units; first += KV4_UNITS * KV4_THREADS) {
-    // the ids of all pieces, then their codes and scales, then the results: three latencies for all
-    int slot[KV4_UNITS], pos[KV4_UNITS], rest[KV4_UNITS];
-    uint32_t q[KV4_UNITS], s[KV4_UNITS];
+  for (int done = 0; done < tokens * p.c.heads; done += UNITS * KV4_ROWS) {
+    // the ids of all rows, then their codes and scales, then the results: three latencies for all
+    int slot[UNITS], at[UNITS];
+    uint32_t q[UNITS][PIECES], s[UNITS];
 #pragma unroll
-    for (int i = 0; i < KV4_UNITS; ++i) {
-      const int u = first + i * KV4_THREADS;
-      const int t = u / per_token;
-      rest[i] = u - t * per_token;
-      pos[i] = u < units ? t : -1;
-      slot[i] = u < units ? kv_ld(table + ((r.begin + t0 + t) >> p.c.page_shift)) : -1;
+    for (int i = 0; i < UNITS; ++i) {
+      at[i] = slot[i] = -1;
+      if (row.token < tokens) {
+        const int pos = r.begin + t0 + row.token;
+        at[i] = row.head * p.c.page + (pos & (p.c.page - 1));
+        slot[i] = kv_ld(table + (pos >> p.c.page_shift));
+      }
+      row.next();
     }
 #pragma unroll
-    for (int i = 0; i < KV4_UNITS; ++i) {
-      q[i] = s[i] = 0;
+    for (int i = 0; i < UNITS; ++i) {
+      s[i] = 0;
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) q[i][k] = 0;
       if (slot[i] < 0 || slot[i] >= p.c.num_pages) {
-        if (pos[i] >= 0) kv_report(p.b.status);
+        if (at[i] >= 0) kv_report(p.b.status);
         continue;
       }
-      const int head = rest[i] / per_row;
-      const long long token = (static_cast<long long>(slot[i]) * p.c.heads + head) * p.c.page + ((r.begin + t0 + pos[i]) & (p.c.page - 1));
-      asm volatile("ld.global.u32 %0, [%1];" : "=r"(q[i]) : "l"(codes + token * (p.c.dim / 2) + (rest[i] - head * per_row) * 4) : "memory");
+      const long long token = static_cast<long long>(slot[i]) * (p.c.heads * p.c.page) + at[i];
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k)
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(q[i][k]) : "l"(codes + token * (D / 2) + k * 32) : "memory");
       asm volatile("ld.global.u32 %0, [%1];" : "=r"(s[i]) : "l"(scales + token) : "memory");
     }
 #pragma unroll
-    for (int i = 0; i < KV4_UNITS; ++i) {
-      if (pos[i] < 0) continue;
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&s[i]));
-      uint32_t h[4];
+    for (int i = 0; i < UNITS; ++i) {
+      if (at[i] >= 0) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&s[i]));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // (a code under the exponent of 2^23; code times scale is exact in FP32, so that a fused product changes nothing)
-        const float a = fmaf(__uint_as_float(0x4b000000u | ((q[i] >> (8 * j)) & 15u)) - 8388608.0f, f.x, f.y);
-        const float b = fmaf(__uint_as_float(0x4b000000u | ((q[i] >> (8 * j + 4)) & 15u)) - 8388608.0f, f.x, f.y);
-        const __half2 v = __floats2half2_rn(a, b);
-        h[j] = *reinterpret_cast<const uint32_t*>(&v);
+        for (int k = 0; k < PIECES; ++k) {
+          uint32_t h[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // (a code under the exponent of 2^23; code times scale is exact in FP32, so that a fused product changes nothing)
+            const float a = fmaf(__uint_as_float(0x4b000000u | ((q[i][k] >> (8 * j)) & 15u)) - 8388608.0f, f.x, f.y);
+            const float b = fmaf(__uint_as_float(0x4b000000u | ((q[i][k] >> (8 * j + 4)) & 15u)) - 8388608.0f, f.x, f.y);
+            const __half2 y = __floats2half2_rn(a, b);
+            h[j] = *reinterpret_cast<const uint32_t*>(&y);
+          }
+          *reinterpret_cast<uint4*>(to + k * 64) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
       }
-      // rows of a token are dense: heads x dim
-      *reinterpret_cast<uint4*>(out + ((static_cast<long long>(r.row0) + t0 + pos[i]) * per_token + rest[i]) * 8) =
-          make_uint4(h[0], h[1], h[2], h[3]);
+      to += KV4_ROWS * D;
     }
   }
 }
