@@ -14,15 +14,16 @@
 // computed. One row tile at 256 d has two score buffers instead: the scores of the next tokens are computed meanwhile.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
-// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies; warps write the same tiles from them, keys as
-// their codes and values as theirs less 8, which both are exact in binary16. Scales and offsets go another way, through a table of
-// five factors a token: with sk, ok, sv, ov those of key and value
-//     t = c sk (q . K) + c ok sum(q) + log2 sv,   w = 2^(t - m + 7),   l = sum w / sv,   out = (sum w (V - 8) + sum w (ov + 8 sv) / sv) / l
-// as in kv_attention_u4.cuh. (Keys and values rounded to binary16 instead would need no table, but are 6e-4 of their norm away from the
-// exact results, where this is 2.5e-4, and the rounded exact ones are 2e-4.)
+// other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies, and warps write the same tiles from them. Keys
+// are their codes, exact in binary16: a score is then scale (q . codes) + offset sum(q), by a table of two factors per token. Values are two
+// tiles, multiplied one after the other: with the scale's first seven bits, and the middle of the range rounded to units of that, a value is
+// exact in binary16; the second tile holds what is left. (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
+// results, only values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in
+// kv_attention_u4.cuh, need five factors a token for every row: what shared memory then hands to registers took longer, 340 us against
+// 250 for 2 x 1024 queries over up to 8192 tokens.)
 //
-// What a masked place holds must not matter, but weight 0 times an infinity is NaN. Codes are always finite, and a 4-bit token whose scale or
-// offset is not gets a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
+// What a masked place holds must not matter, but weight 0 times an infinity is NaN. A 4-bit token whose scale or
+// offset is not finite gets zeros for values and a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
 // Binary16 values are not looked at on their way; a row whose result is not finite looks through the tokens that its
 // masked tiles hide from it and, if one of them is not finite, is computed again, alone.
 #pragma once
@@ -74,29 +75,30 @@ struct AttnTileShape {
   static constexpr int CONVERT_WARPS = U4 ? 8 : 0;
   // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
   // at a time, as far as there is room for their codes: tile by tile by all warps took 1.4 times as long.
-  static constexpr int TILE_WARPS = D == 256 ? 4 : 1;
+  static constexpr int TILE_WARPS = D == 256 ? 8 : 1;
+  static constexpr int GROUPS = D == 256 ? 1 : 6;
+  static constexpr int KINDS = U4 ? 3 : 2;       // tiles of the ring for TN tokens: K, V, and what V's binary16 leaves of it
   static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
   static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
   static constexpr int TILE_BYTES = (D / 64) * CHUNK;
   static constexpr int Q_BYTES = QT * (D / 64) * 16384;
-  static constexpr int SLOTS = U4 ? (D == 64 ? 8 : D == 128 ? 6 : 4) : (D == 64 ? 12 : D == 128 ? 8 : 4);  // K and V tiles in the ring
+  static constexpr int SLOTS = U4 ? (D == 64 ? 12 : D == 128 ? 6 : 4) : (D == 64 ? 12 : D == 128 ? 8 : 4);  // tiles in the ring
   static constexpr int SLOT_OFFSET = Q_BYTES;
   static constexpr int RAW_BYTES = U4 ? TN * D / 2 : 0;  // codes of a K or V tile
   static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
-  static constexpr int RAW_STAGES = D == 256 ? 1 : D == 128 ? 3 : 4;  // rings of such tiles
-  // The warps that expand into a place of the ring of tiles are always the same ones: they wait for it once for every time that it
-  // is used, as a barrier that tells a phase only from its neighbours needs it.
-  static_assert(!U4 || SLOTS % (2 * RAW_STAGES) == 0, "a place belongs to one group of warps");
-  static_assert(!U4 || 2 * RAW_STAGES * TILE_WARPS <= CONVERT_WARPS, "a group for every place of the ring of codes");
+  static constexpr int RAW_STAGES = D == 256 ? 1 : 4;  // rings of such tiles
+  // A place of the ring of tiles, or of codes, belongs to one group of warps: it waits for every time that it is used, one by one, as a
+  // barrier that tells a phase only from its neighbours needs it.
+  static_assert(!U4 || (SLOTS % GROUPS == 0 && (GROUPS == 1 || (GROUPS % KINDS == 0 && RAW_STAGES % (GROUPS / KINDS) == 0))), "places and groups");
+  static_assert(!U4 || GROUPS * TILE_WARPS <= CONVERT_WARPS, "warps of the groups");
   static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_STAGES * RAW_BYTES;
   static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // scales and offsets of a K or V tile
-  // Ring of the tokens' factors, twelve floats for two of them: of the scores a, a, b, b, L, L and two places; of the sums i, i, r, r.
-  // They are written with a tile of K, up to SLOTS / 2 tiles ahead of
+  // Ring of the scores' factors, four floats for two tokens.  They are written with a tile of K, up to SLOTS / KINDS tiles ahead of
   // the first product, and that up to two ahead of the softmax that reads them.
   static constexpr int TABLES = D == 256 ? 4 : 8;
-  static_assert(TABLES >= SLOTS / 2 + 2 || !U4, "no factor is replaced before it is read");
-  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 2 * RAW_STAGES * SCALE_BYTES;
-  static constexpr int TABLE_BYTES = U4 ? TN * 24 : 0;
+  static_assert(TABLES >= SLOTS / KINDS + 2 || !U4, "no factor is replaced before it is read");
+  static constexpr int TABLE_OFFSET = SCALE_OFFSET + 3 * RAW_STAGES * SCALE_BYTES;  // (of K and V with K's codes, of V with V's)
+  static constexpr int TABLE_BYTES = U4 ? TN * 8 : 0;
   static constexpr int ITEM_OFFSET = TABLE_OFFSET + TABLES * TABLE_BYTES;
   static constexpr int ITEM_INTS = 16;
   static constexpr int BAR_OFFSET = ITEM_OFFSET + 2 * ITEM_INTS * 4;
@@ -284,6 +286,11 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* m, in
 __device__ __forceinline__ bool not_finite2(uint32_t w) {  // either of two binary16
   return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u;
 }
+__device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
 __device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -395,7 +402,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       ptx::mbar_init(drain(i), 1);
       for (int stage = 0; stage < 4; ++stage) {
         ptx::mbar_init(raw_full(i, stage), 1);
-        ptx::mbar_init(raw_empty(i, stage), T::TILE_WARPS);
+        ptx::mbar_init(raw_empty(i, stage), i ? 2 * T::TILE_WARPS : T::TILE_WARPS);
       }
     }
     ptx::mbar_init(q_full, 1);
@@ -469,7 +476,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const int q0 = it.query + q * per_tile;
         const int all_hi = p.causal ? it.base + q0 : pos;
         const int all_lo = p.window > 0 ? it.base + min(it.n, q0 + per_tile) - p.window : 0;
-        float m = -INFINITY, l = 0.0f, z = 0.0f;  // z: what the offsets of values add to every one of the row's
+        float m = -INFINITY, l = 0.0f;
         uint64_t q_sum2 = 0;  // the sum of the row's values, twice
         if constexpr (U4) {
           float sum = 0.0f;
@@ -500,19 +507,18 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
 #pragma unroll
           for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
           ptx::tmem_wait_ld();
-          [[maybe_unused]] const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
-          if constexpr (U4) {  // scores in the units of the exponent, a (q . codes) + b sum(q), and log2 of the value's scale
+          if constexpr (U4) {  // scores in the units of the exponent: scale (q . codes) + offset sum(q)
             ok = wait_bounded(table_full((ring0 + j) % T::TABLES), ((ring0 + j) / T::TABLES) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
+            const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
 #pragma unroll
             for (int h = 0; h < TN / 32; ++h)
 #pragma unroll
               for (int v = 0; v < 32; v += 2) {
-                uint64_t a, b, logs;
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(table + (h * 32 + v) * 24) : "memory");
-                asm volatile("ld.shared.b64 %0, [%1];" : "=l"(logs) : "r"(table + (h * 32 + v) * 24 + 16) : "memory");
-                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), a, fma2(b, q_sum2, logs)));
+                uint64_t a, b;
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(table + (h * 32 + v) * 8) : "memory");
+                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), a, mul2(b, q_sum2)));
                 x[h][v] = __float_as_uint(t.x);
                 x[h][v + 1] = __float_as_uint(t.y);
               }
@@ -542,7 +548,6 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
             m = now;
             l *= f;
-            z *= f;
             if (j > 0) {  // O of the tiles before, once their products are done
               ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
               ok = __all_sync(0xffffffffu, ok);
@@ -575,19 +580,16 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
           {
             // Pair i is summed up and packed LAG pairs after its exponentials were asked for.
-            constexpr int PAIRS = TN / 2, LAG = U4 ? 2 : 4;
+            constexpr int PAIRS = TN / 2, LAG = 4;
             auto exponent = [&](int i) {
               const uint64_t x2 = pair(__uint_as_float(x[i / 16][i % 16 * 2]), __uint_as_float(x[i / 16][i % 16 * 2 + 1]));
               return unpair(U4 ? add2_here(x2, at2) : fma2_here(x2, c2, at2));
             };
             float2 e[LAG + 1], t = exponent(0);
-            [[maybe_unused]] uint64_t of_l[LAG + 1], of_z[LAG + 1];
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < PAIRS + LAG; ++i) {
               if (i < PAIRS) {
-                if constexpr (U4)
-                  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(of_l[i % (LAG + 1)]), "=l"(of_z[i % (LAG + 1)]) : "r"(table + i * 48 + 32) : "memory");
                 e[i % (LAG + 1)].x = exp2_here(t.x);
                 e[i % (LAG + 1)].y = exp2_here(t.y);
                 if (i + 1 < PAIRS) t = exponent(i + 1);
@@ -596,12 +598,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               if (i >= LAG) {
                 const int o = i - LAG;
                 const float2 v = e[o % (LAG + 1)];
-                if constexpr (U4) {
-                  sum[0] = fma2_here(pair(v.x, v.y), of_l[o % (LAG + 1)], sum[0]);
-                  sum[1] = fma2_here(pair(v.x, v.y), of_z[o % (LAG + 1)], sum[1]);
-                } else {
-                  sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
-                }
+                sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
                 w[o % 16] = pack_here(v.x, v.y);
                 if (o % 16 == 15) ptx::tmem_st_32x32b_x16(s_at + (o / 16) * 16, w);
               }
@@ -619,14 +616,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           ptx::tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(p_full(sb));
-          if constexpr (U4) {
-            const float2 of_l = unpair(sum[0]), of_z = unpair(sum[1]);
-            l += of_l.x + of_l.y;
-            z += of_z.x + of_z.y;
-          } else {
-            const float2 total = unpair(add2(sum[0], sum[1]));
-            l += total.x + total.y;
-          }
+          const float2 total = unpair(add2(sum[0], sum[1]));
+          l += total.x + total.y;
         }
         if (!ok) break;
         // ---- the rows' results
@@ -666,7 +657,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             for (int v = 0; v < 4; ++v) {  // (columns of values lie in the order in which words of codes come apart: 0, 4, 1, 5, ...)
               float y[8];
 #pragma unroll
-              for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[8 * v + (u < 4 ? 2 * u : 2 * u - 7)]) + z;
+              for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[8 * v + (u < 4 ? 2 * u : 2 * u - 7)]);
 #pragma unroll
               for (int u = 0; u < 8; ++u) x[8 * v + u] = __float_as_uint(y[u]);
             }
@@ -874,17 +865,15 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             ok = wait_bounded(raw_empty(which, stage), ((tile / T::RAW_STAGES) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            // (scales and offsets of both come with K; runs that are left out keep what the buffers held)
-            if (lane == 0) ptx::mbar_arrive_expect_tx(full, count * (run_bytes + (which ? 0u : static_cast<uint32_t>(run) * 8u)));
+            // (runs that are left out keep what the buffers held)
+            if (lane == 0) ptx::mbar_arrive_expect_tx(full, count * (run_bytes + static_cast<uint32_t>(run) * (which ? 4u : 8u)));
             __syncwarp();
             if (good) {
               ptx::bulk_load(base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + lane * run_bytes,
                              (which ? p.c.codes[1] : p.c.codes[0]) + token * (D / 2), run_bytes, full);
-              if (which == 0) {
-                const uint32_t to = base + T::SCALE_OFFSET + (tile % T::RAW_STAGES) * 2 * T::SCALE_BYTES + lane * run * 4;
-                ptx::bulk_load(to, p.c.scales[0] + token, run * 4, full);
-                ptx::bulk_load(to + T::SCALE_BYTES, p.c.scales[1] + token, run * 4, full);
-              }
+              const uint32_t scales = base + T::SCALE_OFFSET + stage * 3 * T::SCALE_BYTES + lane * run * 4;
+              if (which == 0) ptx::bulk_load(scales, p.c.scales[0] + token, run * 4, full);
+              ptx::bulk_load(scales + (which ? 2 : 1) * T::SCALE_BYTES, p.c.scales[1] + token, run * 4, full);
             }
           }
           id = id_next;
@@ -921,12 +910,12 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         ok = wait_bounded(q_full, used & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
         if (ok && elected) ptx::mbar_arrive(q_empty);
 #pragma unroll 1
-        for (int j = 0; j < 2 * it.tiles && ok; ++j) {
+        for (int j = 0; j < T::KINDS * it.tiles && ok; ++j) {
           ok = wait_slot(tile + j);
           if (ok && elected) ptx::mbar_arrive(slot_empty((tile + j) % SLOTS));
         }
         __syncwarp();
-        tile += 2 * it.tiles;
+        tile += T::KINDS * it.tiles;
         ++used;
         continue;
       }
@@ -934,8 +923,8 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       if (!ok) break;
       ++used;
       auto qk = [&](int j) {  // scores of token tile j
-        if (!wait_slot(tile + 2 * j)) return false;
-        const int slot = (tile + 2 * j) % SLOTS, sb = 2 * q + ((done + j) & 1);
+        if (!wait_slot(tile + T::KINDS * j)) return false;
+        const int slot = (tile + T::KINDS * j) % SLOTS, sb = 2 * q + ((done + j) & 1);
         if (elected) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
@@ -954,24 +943,29 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       for (int j = 0; j < 2 && j < it.tiles && ok; ++j) ok = qk(j);
 #pragma unroll 1
       for (int j = 0; j < it.tiles && ok; ++j) {
-        const int sb = 2 * q + ((done + j) & 1), slot = (tile + 2 * j + 1) % SLOTS;
-        ok = wait_slot(tile + 2 * j + 1) && wait_bounded(p_full(sb), ((done + j) >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+        const int sb = 2 * q + ((done + j) & 1);
+        for (int i = 1; i < T::KINDS && ok; ++i) ok = wait_slot(tile + T::KINDS * j + i);
+        ok = ok && wait_bounded(p_full(sb), ((done + j) >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         if (elected) {
 #pragma unroll
-          for (int kk = 0; kk < TN / 16; ++kk) {
-            const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
-            ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || kk > 0);
+          for (int i = 1; i < T::KINDS; ++i) {
+            const int slot = (tile + T::KINDS * j + i) % SLOTS;
+#pragma unroll
+            for (int kk = 0; kk < TN / 16; ++kk) {
+              const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
+              ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || i > 1 || kk > 0);
+            }
+            if (i == T::KINDS - 1) ptx::mma_commit<1>(o_done(q));
+            ptx::mma_commit<1>(slot_empty(slot));
           }
-          ptx::mma_commit<1>(o_done(q));
-          ptx::mma_commit<1>(slot_empty(slot));
         }
         __syncwarp();
         // (the scores go where the weights are: the MMAs of this thread run in order)
         if (j + 2 < it.tiles) ok = qk(j + 2);
       }
-      tile += 2 * it.tiles;
+      tile += T::KINDS * it.tiles;
       done += it.tiles;
     }
     if (!ok && elected) {
@@ -984,68 +978,94 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     __syncwarp();
   } else if (U4 && warp >= W_LOAD + 4) {
     // ------------------------------------------------------------------ K and V: 4-bit codes to binary16 tiles
-    // A group of TILE_WARPS warps has a place of the ring of codes for itself, of K or of V.
     constexpr int AT_ONCE = 32 * T::TILE_WARPS;     // threads of a tile
-    const int group = (warp - (W_LOAD + 4)) / T::TILE_WARPS, which = group & 1, stage = group >> 1;
-    const int ct = tid % AT_ONCE;
+    const int group = (warp - (W_LOAD + 4)) / T::TILE_WARPS, ct = tid % AT_ONCE;
     constexpr int PER_TOKEN = D / 32;               // 16-byte pieces of a token's codes: 32 d, 64 bytes of a row of a chunk
     constexpr int N = TN * PER_TOKEN / AT_ONCE;     // pieces per thread and tile
     constexpr int WARP_TOKENS = 32 / PER_TOKEN;     // tokens that a warp covers at a time (its lanes: neighbouring tokens, whose
                                                     // rows the swizzle keeps off one another's banks)
     const int piece = lane / WARP_TOKENS, t0 = ct / 32 * WARP_TOKENS + lane % WARP_TOKENS;
-    int nth = 0;  // token tile of the CTA
+    int tile = 0;  // of the ring
     bool ok = true;
 #pragma unroll 1
     for (int k = 0; ok; ++k) {
       AttnItem it;
       ok = next_item(k, it);
       if (!ok || it.tiles < 0) break;
+      const int tile0 = tile;
+      tile += T::KINDS * it.tiles;
 #pragma unroll 1
-      for (int j = 0; j < it.tiles; ++j, ++nth) {
-        if (nth % T::RAW_STAGES != stage) continue;
-        const int tile = 2 * nth + which, slot = tile % SLOTS;
+      for (int i = tile0 + (group + T::GROUPS * SLOTS - tile0 % T::GROUPS) % T::GROUPS; i < tile && group < T::GROUPS; i += T::GROUPS) {
+        const int nth = i / T::KINDS, kind = i - nth * T::KINDS, j = nth - tile0 / T::KINDS;  // token tile of the CTA, of the item
+        const int which = kind > 0, slot = i % SLOTS, stage = nth % T::RAW_STAGES;
         ok = wait_bounded(raw_full(which, stage), (nth / T::RAW_STAGES) & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
-             wait_bounded(slot_empty(slot), ((tile / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
+             wait_bounded(slot_empty(slot), ((i / SLOTS) & 1) ^ 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         const uint32_t codes = base + T::RAW_OFFSET + (2 * stage + which) * T::RAW_BYTES + static_cast<uint32_t>(piece * 16);
-        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + stage * 2 * T::SCALE_BYTES);
+        const uint32_t* const scales = reinterpret_cast<const uint32_t*>(base_ptr + T::SCALE_OFFSET + stage * 3 * T::SCALE_BYTES);
         const uint32_t to = base + T::SLOT_OFFSET + slot * T::TILE_BYTES + static_cast<uint32_t>((piece >> 1) * T::CHUNK);
         const int first = it.lo + j * TN;
-        if (which == 0) {  // the tokens' factors; a NaN for one whose key or value is not finite
+        // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
+        auto seen = [&](int tok) { return first + tok < it.hi && first + tok >= it.from; };
+        uint32_t of_token[TN / 32];  // V: factor and summand of tokens lane, lane + 32
+        if (kind == 0) {  // the scores' factors; a NaN for a token whose key or value is not finite
 #pragma unroll
           for (int tok = ct; tok < TN; tok += AT_ONCE) {
-            const uint32_t k_scale = scales[tok], v_scale = scales[TN + tok];
-            const float2 f = half2_of(k_scale), g = half2_of(v_scale);
-            const bool good = !not_finite2(k_scale) && !not_finite2(v_scale);
-            float* const table = reinterpret_cast<float*>(base_ptr + T::TABLE_OFFSET + (nth % T::TABLES) * T::TABLE_BYTES) + (tok >> 1) * 12 + (tok & 1);
-            const float sv = good ? kva_value_scale(g.x) : 1.0f;
-            const float inv = __fdividef(1.0f, sv);
-            // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
-            const bool seen = first + tok < it.hi && first + tok >= it.from;
-            table[0] = !seen ? 0.0f : good ? p.scale_log2 * f.x * 0x1p24f : __int_as_float(0x7fffffff);
-            table[2] = seen && good ? p.scale_log2 * f.y : 0.0f;
-            table[4] = seen ? __log2f(sv) : 0.0f;
-            table[8] = seen ? inv : 0.0f;
-            table[10] = seen && good ? fmaf(8.0f, g.x, g.y) * inv : 0.0f;
+            const uint32_t mine = scales[tok];
+            const float2 f = half2_of(mine);
+            const bool good = !not_finite2(mine) && !not_finite2(scales[TN + tok]);
+            float* const table = reinterpret_cast<float*>(base_ptr + T::TABLE_OFFSET + (nth % T::TABLES) * T::TABLE_BYTES) + (tok >> 1) * 4 + (tok & 1);
+            table[0] = !seen(tok) ? 0.0f : good ? p.scale_log2 * f.x * 0x1p24f : __int_as_float(0x7fffffff);
+            table[2] = seen(tok) && good ? p.scale_log2 * f.y : 0.0f;
+          }
+        } else {
+#pragma unroll
+          for (int u = 0; u < TN / 32; ++u) {
+            const int tok = lane + 32 * u;
+            const uint32_t mine = scales[2 * TN + tok];
+            // The scale's first seven bits and the rest; the middle (code 8) as a multiple of the unit that the former leaves, and the rest.
+            const uint32_t high = mine & 0xfff0u;
+            const float2 f = half2_of(mine);
+            const float scale_hi = __half2float(__ushort_as_half(static_cast<unsigned short>(high)));
+            const float middle = fmaf(8.0f, f.x, f.y);
+            // 1.5 2^23 units, a unit 2^-6 of the scale's power of two (of 2^-14 below the normal range)
+            const float round = __uint_as_float((__float_as_uint(fmaxf(scale_hi, 0x1p-14f)) & 0x7f800000u) + (17u << 23) + 0x400000u);
+            const float middle_hi = __half2float(__float2half_rn((middle + round) - round));
+            const uint32_t w = kind == 1 ? pack_halves(scale_hi, middle_hi) : pack_halves(f.x - scale_hi, middle - middle_hi);
+            of_token[u] = seen(tok) && !not_finite2(mine) ? w : 0u;
           }
         }
 #pragma unroll 4
-        for (int i = 0; i < N; ++i) {
-          const int tok = i * (AT_ONCE / PER_TOKEN) + t0;
+        for (int u = 0; u < N; ++u) {
+          const int tok = u * (AT_ONCE / PER_TOKEN) + t0;
           uint32_t w[4];
           ptx::ld_shared_v4(codes + tok * (D / 2), w[0], w[1], w[2], w[3]);
           const uint32_t at = to + static_cast<uint32_t>(tok * 128), sw = static_cast<uint32_t>(tok & 7);
+          if (kind == 0) {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const uint4 x = which ? value_codes(w[v]) : key_codes(w[v]);
-            ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), x.x, x.y, x.z, x.w);
+            for (int v = 0; v < 4; ++v) {
+              const uint4 x = key_codes(w[v]);
+              ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), x.x, x.y, x.z, x.w);
+            }
+          } else {
+            // (the tokens of a warp's lanes lie within 32 of one another's multiple)
+            uint32_t mine = __shfl_sync(0xffffffffu, of_token[0], tok & 31);
+            const uint32_t later = __shfl_sync(0xffffffffu, of_token[1], tok & 31);
+            if (tok >= 32) mine = later;
+            const uint32_t factor = __byte_perm(mine, 0, 0x1010), summand = __byte_perm(mine, 0, 0x3232);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const uint4 x = value_codes(w[v]);
+              ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), fma_h2(x.x, factor, summand),
+                                fma_h2(x.y, factor, summand), fma_h2(x.z, factor, summand), fma_h2(x.w, factor, summand));
+            }
           }
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          if (which == 0) ptx::mbar_arrive(table_full(nth % T::TABLES));
+          if (kind == 0) ptx::mbar_arrive(table_full(nth % T::TABLES));
           ptx::mbar_arrive(slot_full(slot));
           ptx::mbar_arrive(raw_empty(which, stage));
         }
