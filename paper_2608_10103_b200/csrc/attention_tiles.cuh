@@ -72,10 +72,10 @@ struct AttnTileShape {
   static constexpr int TN = 64;                  // tokens per tile
   static constexpr int ROWS = 128 * QT;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
-  static constexpr int CONVERT_WARPS = U4 ? 8 : 0;
+  static constexpr int CONVERT_WARPS = !U4 ? 0 : D == 256 ? 8 : 12;
   // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
   // at a time, as far as there is room for their codes: tile by tile by all warps took 1.4 times as long.
-  static constexpr int TILE_WARPS = D == 256 ? 8 : 1;
+  static constexpr int TILE_WARPS = D == 256 ? 8 : 2;
   static constexpr int GROUPS = D == 256 ? 1 : 6;
   static constexpr int KINDS = U4 ? 3 : 2;       // tiles of the ring for TN tokens: K, V, and what V's binary16 leaves of it
   static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
@@ -89,7 +89,7 @@ struct AttnTileShape {
   static constexpr int RAW_STAGES = D == 256 ? 1 : 4;  // rings of such tiles
   // A place of the ring of tiles, or of codes, belongs to one group of warps: it waits for every time that it is used, one by one, as a
   // barrier that tells a phase only from its neighbours needs it.
-  static_assert(!U4 || (SLOTS % GROUPS == 0 && (GROUPS == 1 || (GROUPS % KINDS == 0 && RAW_STAGES % (GROUPS / KINDS) == 0))), "places and groups");
+  static_assert(!U4 || (SLOTS % GROUPS == 0 && (GROUPS == 1 || (GROUPS % KINDS == 0 && RAW_STAGES * KINDS % GROUPS == 0))), "places and groups");
   static_assert(!U4 || GROUPS * TILE_WARPS <= CONVERT_WARPS, "warps of the groups");
   static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_STAGES * RAW_BYTES;
   static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // scales and offsets of a K or V tile
@@ -439,11 +439,11 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     return ok;
   };
 
-  if constexpr (U4 && QT == 2) {  // register shares: 256 x 128 + 384 x 72, of the 640 x 96 the block was launched with
+  if constexpr (U4 && QT == 2) {  // register shares: 256 x 128 + 512 x 56, of the 768 x 80 the block was launched with
     if (warp < T::SOFTMAX_WARPS)
       asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   }
   if (warp < T::SOFTMAX_WARPS) {
     // ------------------------------------------------------------------ softmax, one thread per row
