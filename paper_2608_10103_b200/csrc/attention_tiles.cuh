@@ -72,25 +72,24 @@ struct AttnTileShape {
   static constexpr int TN = 64;                  // tokens per tile
   static constexpr int ROWS = 128 * QT;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
-  static constexpr int CONVERT_WARPS = !U4 ? 0 : D == 256 ? 8 : 12;
+  static constexpr int CONVERT_WARPS = U4 ? 12 : 0;
   // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
   // at a time, as far as there is room for their codes: tile by tile by all warps took 1.4 times as long.
-  static constexpr int TILE_WARPS = D == 256 ? 8 : 2;
-  static constexpr int GROUPS = D == 256 ? 1 : 6;
+  static constexpr int TILE_WARPS = D == 256 ? 4 : 2;
+  static constexpr int GROUPS = CONVERT_WARPS / TILE_WARPS;
   static constexpr int KINDS = U4 ? 3 : 2;       // tiles of the ring for TN tokens: K, V, and what V's binary16 leaves of it
   static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
   static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
   static constexpr int TILE_BYTES = (D / 64) * CHUNK;
   static constexpr int Q_BYTES = QT * (D / 64) * 16384;
-  static constexpr int SLOTS = U4 ? (D == 64 ? 12 : D == 128 ? 6 : 4) : (D == 64 ? 12 : D == 128 ? 8 : 4);  // tiles in the ring
+  static constexpr int SLOTS = U4 ? (D == 64 ? 12 : D == 128 ? 6 : 3) : (D == 64 ? 12 : D == 128 ? 8 : 4);  // tiles in the ring
   static constexpr int SLOT_OFFSET = Q_BYTES;
   static constexpr int RAW_BYTES = U4 ? TN * D / 2 : 0;  // codes of a K or V tile
   static constexpr int RAW_OFFSET = SLOT_OFFSET + SLOTS * TILE_BYTES;
-  static constexpr int RAW_STAGES = D == 256 ? 1 : 4;  // rings of such tiles
+  static constexpr int RAW_STAGES = D == 256 ? 2 : 4;  // rings of such tiles
   // A place of the ring of tiles, or of codes, belongs to one group of warps: it waits for every time that it is used, one by one, as a
   // barrier that tells a phase only from its neighbours needs it.
-  static_assert(!U4 || (SLOTS % GROUPS == 0 && (GROUPS == 1 || (GROUPS % KINDS == 0 && RAW_STAGES * KINDS % GROUPS == 0))), "places and groups");
-  static_assert(!U4 || GROUPS * TILE_WARPS <= CONVERT_WARPS, "warps of the groups");
+  static_assert(!U4 || (SLOTS % GROUPS == 0 && GROUPS % KINDS == 0 && RAW_STAGES * KINDS % GROUPS == 0), "places and groups");
   static constexpr int SCALE_OFFSET = RAW_OFFSET + 2 * RAW_STAGES * RAW_BYTES;
   static constexpr int SCALE_BYTES = U4 ? TN * 4 : 0;    // scales and offsets of a K or V tile
   // Ring of the scores' factors, four floats for two tokens.  They are written with a tile of K, up to SLOTS / KINDS tiles ahead of
@@ -439,11 +438,18 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     return ok;
   };
 
-  if constexpr (U4 && QT == 2) {  // register shares: 256 x 128 + 512 x 56, of the 768 x 80 the block was launched with
-    if (warp < T::SOFTMAX_WARPS)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
-    else
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  if constexpr (U4) {  // register shares: 256 x 128 + 512 x 56 of the 768 x 80 that the block was launched with, or 128 x 168 + 512 x 72 of 640 x 96
+    if (warp < T::SOFTMAX_WARPS) {
+      if constexpr (QT == 2)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+      else
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    } else {
+      if constexpr (QT == 2)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+      else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    }
   }
   if (warp < T::SOFTMAX_WARPS) {
     // ------------------------------------------------------------------ softmax, one thread per row
@@ -995,7 +1001,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
       const int tile0 = tile;
       tile += T::KINDS * it.tiles;
 #pragma unroll 1
-      for (int i = tile0 + (group + T::GROUPS * SLOTS - tile0 % T::GROUPS) % T::GROUPS; i < tile && group < T::GROUPS; i += T::GROUPS) {
+      for (int i = tile0 + (group + T::GROUPS * SLOTS - tile0 % T::GROUPS) % T::GROUPS; i < tile; i += T::GROUPS) {
         const int nth = i / T::KINDS, kind = i - nth * T::KINDS, j = nth - tile0 / T::KINDS;  // token tile of the CTA, of the item
         const int which = kind > 0, slot = i % SLOTS, stage = nth % T::RAW_STAGES;
         ok = wait_bounded(raw_full(which, stage), (nth / T::RAW_STAGES) & 1, abort_flag, p.status, DEV_TIMEOUT_PRODUCER) &&
