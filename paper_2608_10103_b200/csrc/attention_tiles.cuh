@@ -9,9 +9,18 @@
 // registers. Scores, sums and statistics are FP32.
 //
 // Roles: a scheduler works out the next row tile while this one runs; a loader brings Q and, through a ring of tiles that runs
-// on from one row tile into the next, K and V; two issuers, one for each 128 rows, so that neither waits for the
-// other's softmax; the softmax warps hand their weights over in two halves, the first of which is multiplied while the second is
-// computed. One row tile at 256 d has two score buffers instead: the scores of the next tokens are computed meanwhile.
+// on from one row tile into the next, K and V; an issuer for each 128 rows, so that neither waits for the other's softmax. Every 128 rows
+// have two score buffers: the scores of the next tokens are computed while the softmax works on these.
+//
+// What bounds it, prompts at 128 d: 1550-1650 cycles per 64 tokens and pair of row tiles, where the products take the tensor pipe 1540 (scores
+// of 64 tokens as long as of 128: the pipe wants N = 128) and the exponentials 1024. With one buffer of 128 scores per row tile the products
+// would take 1024, but scores -> maximum -> weights -> products then is a chain of 3400-3600 per 128 tokens (8192 tokens: 472-495 us against
+// 455). Also tried there and slower: two threads per row (684 us), the first half of the weights multiplied early. An eighth to half of the
+// exponentials as polynomials, in either form: no faster.
+// A row tile's end, 6000 cycles of which 3600 are its results' way out, is a fifth of a prompt of 1000 tokens.
+// Measured: 8192 tokens, 32 heads on 8, 455-465 us (0.70 of the time that the operations take at the cuBLAS bf16 rate); 12 prompts of
+// up to 2048 tokens 169 us; 4096 tokens of 32 heads on 8 of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 291 us: some 2700 cycles
+// per 64 tokens, which the expansion of codes and the products each take by themselves, over memory that they share.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
 // other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies, and warps write the same tiles from them. Keys
@@ -20,7 +29,7 @@
 // exact in binary16; the second tile holds what is left. (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
 // results, only values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in
 // kv_attention_u4.cuh, need five factors a token for every row: what shared memory then hands to registers took longer, 340 us against
-// 250 for 2 x 1024 queries over up to 8192 tokens.)
+// 291.)
 //
 // What a masked place holds must not matter, but weight 0 times an infinity is NaN. A 4-bit token whose scale or
 // offset is not finite gets zeros for values and a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
@@ -76,7 +85,7 @@ struct AttnTileShape {
   // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
   // at a time, as far as there is room for their codes: tile by tile by all warps took 1.4 times as long.
   static constexpr int TILE_WARPS = D == 256 ? 4 : 2;
-  static constexpr int GROUPS = CONVERT_WARPS / TILE_WARPS;
+  static constexpr int GROUPS = 12 / TILE_WARPS;
   static constexpr int KINDS = U4 ? 3 : 2;       // tiles of the ring for TN tokens: K, V, and what V's binary16 leaves of it
   static constexpr int THREADS = 32 * (SOFTMAX_WARPS + 4 + CONVERT_WARPS);
   static constexpr int CHUNK = TN * 128;         // bytes of 64 d of a K or V tile
@@ -218,9 +227,6 @@ struct AttnOrder {
   }
 };
 
-#ifndef ATTN_TURN
-#define ATTN_TURN 1
-#endif
 namespace attn {
 
 // Pairs of FP32 values in one instruction.

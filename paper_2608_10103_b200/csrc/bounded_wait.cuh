@@ -21,11 +21,11 @@ enum DeviceStatus {
 
 // Bounded wait: polls the barrier; after the limit (or once another role has
 // given up) records `code` and returns false.  The caller then leaves its loop.
-template <bool BACKOFF = false, bool SPIN = false>
+template <bool BACKOFF = false>
 __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity,
                                              volatile uint32_t* abort_flag, int* status, int code,
                                              uint32_t backoff_ns = 0) {
-  auto done = [&]() { return SPIN ? ptx::mbar_test_wait(bar, parity) : ptx::mbar_try_wait(bar, parity); };
+  auto done = [&]() { return ptx::mbar_try_wait(bar, parity); };
   if (done()) return true;
   uint64_t t0 = 0;
   uint32_t spins = 0;

@@ -90,7 +90,8 @@ int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream
 template <int D, int NR>
 int launch_few_rows(const SharedDevice& dev, KvAttn4Params p, cudaStream_t stream) {
   static std::atomic<int> resident[MAX_DEV];
-  constexpr int room = 227 * 1024 / kva4_ctas(D, NR) - 2048 - kva4_q_bytes(D, NR);
+  // (1 KB of each CTA is the system's, a few bytes are static)
+  constexpr int room = 228 * 1024 / kva4_ctas(D, NR) - 1024 - 64 - kva4_q_bytes(D, NR);
   constexpr int slots = room / (KVA_WARPS * kva4_slot_bytes(D));
   constexpr int depth = slots < 8 ? slots : 8;
   static_assert(depth >= 2, "the ring holds two steps at least");

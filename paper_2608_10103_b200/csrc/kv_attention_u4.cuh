@@ -19,7 +19,15 @@
 // lanes exchange pieces within the warp, so that every copy is 16 bytes and rows lie such that no load has a bank conflict: the
 // row of a token and its 16-byte pieces are permuted by the token's low bits (`row_at`, `piece_at`).
 //
+// What a token's scale and offset come to (a logarithm, a reciprocal, four conversions) is worked out by one lane each and read
+// back by the others through shared memory: eight lanes share a token, and each of them doing it for itself took 5-8 % longer.
+//
 // Work split, hand-over and joins are those of kv_attention.cuh, with one row tile per sequence.
+//
+// Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 73.5 us, 3.9 TB/s of the cache; one of 1000 tokens 9.8 us.
+// 16 heads of 64 d, 131071 tokens, 4 queries: 53.8 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
+// codes meet as many scores, exponentials and factors, the instructions per byte are 1.5 times as many. Four CTAs per SM
+// with rings of three steps at 128 d: 2 % slower than three with four; steps of 64 tokens at 64 d: -2 to +3 %.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -58,11 +66,12 @@ struct KvAttn4Params {
 
 __host__ __device__ constexpr int kva4_step(int dim) { return dim == 256 ? 16 : 32; }  // tokens per step
 // What beginning a unit costs a CTA, in steps (see KVA_UNIT_COST).
-__host__ __device__ constexpr int kva4_unit_cost(int) { return 12; }
+__host__ __device__ constexpr int kva4_unit_cost(int) { return 8; }  // (6: 1-2 % slower on batches, 16: 2 %)
 // Bytes of one ring slot of a warp: a step's codes of K and V, and scales and offsets of both.
 __host__ __device__ constexpr int kva4_slot_bytes(int dim) { return kva4_step(dim) * (dim + 8); }
-__host__ __device__ constexpr int kva4_q_bytes(int dim, int nr) { return nr * (dim / 32) * 512; }
-__host__ __device__ constexpr int kva4_ctas(int dim, int nr) { return dim * nr <= 128 ? 4 : dim * nr <= 256 ? 3 : 2; }
+// q fragments, and for each warp five factors of every token of a step.
+__host__ __device__ constexpr int kva4_q_bytes(int dim, int nr) { return nr * (dim / 32) * 512 + KVA_WARPS * kva4_step(dim) * 20; }
+__host__ __device__ constexpr int kva4_ctas(int dim, int nr) { return dim * nr <= 64 ? 4 : dim * nr <= 256 ? 3 : 2; }
 __host__ __device__ constexpr int kva4_smem(int dim, int nr, int depth) {
   const int ring = KVA_WARPS * depth * kva4_slot_bytes(dim);
   const int merge = KVA_WARPS * 8 * nr * (dim + 4) * 4;
@@ -224,6 +233,8 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
   unsigned char* const rings = kva_smem_raw + kva4_q_bytes(D, NR);
   const uint32_t ring_at = ptx::smem_addr(rings) + static_cast<uint32_t>(warp * DEPTH) * SLOT;
   const uint32_t q_at = ptx::smem_addr(kva_smem_raw) + lane * 16;
+  // [two tokens][sk, sk, ok, ok], [two tokens][log2 sv, log2 sv, 1 / sv, 1 / sv], [token] ov + 8 sv
+  const uint32_t f_at_warp = ptx::smem_addr(kva_smem_raw) + NR * KW * 512 + static_cast<uint32_t>(warp * STEP * 20);
   float* const merge = reinterpret_cast<float*>(rings);
   // This lane's places in a slot: of its pieces as they arrive, and of what it reads.  All of them repeat every eight tokens.
   constexpr int PIECES = ROW / 16;              // 16-byte pieces of a token
@@ -427,6 +438,23 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
         c_slot = wrap ? 0 : c_slot;
         c_at += wrap ? static_cast<uint32_t>(-(DEPTH - 1) * SLOT) : SLOT;
         fetch();
+        // ---- the tokens' factors, a lane for each.  A token whose scale or offset is not finite: NaN for the rows that see it, nothing
+        // (-inf below, which such factors would turn into a NaN) for those that do not.
+        each<(STEP + 31) / 32>([&](auto part) {
+          if (STEP < 32 && lane >= STEP) return;
+          const uint32_t k_word = kva4::lds<S_AT + part * 128>(slot + lane * 4), v_word = kva4::lds<S_AT + STEP * 4 + part * 128>(slot + lane * 4);
+          auto finite = [](uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; };
+          const bool good = finite(k_word) && finite(v_word);
+          const float2 k = half2_of(k_word), x = half2_of(good ? v_word : 0x00003c00u);
+          const float sv = kva_value_scale(x.x);
+          const uint32_t to = f_at_warp + part * 256 + (lane >> 1) * 16 + (lane & 1) * 4;
+          auto put = [](uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); };
+          put(to, good ? k.x : __int_as_float(0x7fffffff));
+          put(to + 8, good ? k.y : 0.0f);
+          put(to + STEP * 8, __log2f(sv));
+          put(to + STEP * 8 + 8, __fdividef(1.0f, sv));
+          put(f_at_warp + STEP * 16 + part * 128 + lane * 4, fmaf(8.0f, x.x, x.y));
+        });
         // ---- scores: 8 NR rows x STEP tokens, two exact integer sums each; this lane: row g of each
         // group, tokens 8 j + 2t, + 1
         float sc[NR][NT][2];
@@ -459,47 +487,22 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
             for (int v = 0; v < 2; ++v)  // |254 q1 + q2| 15 D <= 32385 * 15 * 256 < 2^31
               sc[n][j][v] = static_cast<float>(sum[n][v] * 254 + sum[n][v + 2]);
         });
-        // ---- the tokens' factors
-        float lsv[NT][2], inv_sv[NT][2], mid[NT][2];
-        uint32_t ks[NT][2], vs[NT][2], check = 0;
-        each<NT>([&](auto j) {
-          const uint32_t from = slot + t * 8;
-          lds_v2<S_AT + j * 32>(from, ks[j][0], ks[j][1]);
-          lds_v2<S_AT + STEP * 4 + j * 32>(from, vs[j][0], vs[j][1]);
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(check) : "r"(ks[j][v]), "r"(0u));
-            asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(check) : "r"(vs[j][v]), "r"(0u));
-          }
-        });
-        // A token whose scale or offset is not finite (0 times it is NaN): NaN for the rows that see it, nothing (-inf below, which
-        // such factors would turn into a NaN) for those that do not.
-        if ((check & 0x7c007c00u) != 0) {
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-              auto bad = [](uint32_t w) { return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u; };
-              if (bad(ks[j][v]) || bad(vs[j][v])) {
-                ks[j][v] = 0x00007fffu;
-                vs[j][v] = 0x00003c00u;
-              }
-            }
-        }
+        __syncwarp();
         const int tok0 = lo + st * STEP;
+        const uint32_t factors = f_at_warp + t * 16;
+        float inv_sv[NT][2];
+        each<NT>([&](auto j) {
+          uint32_t k[4], v[4];
+          lds_v4<j * 64>(factors, k);
+          lds_v4<STEP * 8 + j * 64>(factors, v);
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const float2 k = half2_of(ks[j][v]), x = half2_of(vs[j][v]);
-            const float sv = kva_value_scale(x.x);
-            lsv[j][v] = __log2f(sv);
-            inv_sv[j][v] = __fdividef(1.0f, sv);
-            mid[j][v] = fmaf(8.0f, x.x, x.y);
+          for (int i = 0; i < 2; ++i) {
+            inv_sv[j][i] = __uint_as_float(v[2 + i]);
 #pragma unroll
             for (int n = 0; n < NR; ++n)
-              sc[n][j][v] = fmaf(fmaf(k.y, q_sum[n], k.x * sc[n][j][v]), krow[n], lsv[j][v]);
+              sc[n][j][i] = fmaf(fmaf(__uint_as_float(k[2 + i]), q_sum[n], __uint_as_float(k[i]) * sc[n][j][i]), krow[n], __uint_as_float(v[i]));
           }
+        });
         if (tok0 + STEP - 1 > all_hi || tok0 < all_lo) {
 #pragma unroll
           for (int n = 0; n < NR; ++n) {
@@ -515,6 +518,13 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
           }
         }
         uint32_t pw[NR][NT];
+        float mid[NT][2];
+        each<NT>([&](auto j) {
+          uint32_t a, b;
+          lds_v2<STEP * 16 + j * 32>(f_at_warp + t * 8, a, b);
+          mid[j][0] = __uint_as_float(a);
+          mid[j][1] = __uint_as_float(b);
+        });
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
           float top = fmaxf(sc[n][0][0], sc[n][0][1]);
