@@ -1,11 +1,12 @@
-"""One transformer decoder layer with INT8 weights, INT8 activations and an INT8 key/value cache, as a
+"""One transformer decoder layer with INT8 weights, INT8 activations and a quantised key/value cache, as a
 serving program runs it: a ragged batch of prompts first, then token after token.
 
     python examples/quantised_decoder_layer.py
 
 Per call: rows are normalised (plain torch), quantised, projected (INT8, bias) to queries, keys and values,
-the keys and values go to the cache, attention reads the cache, and the two projections back add onto the
-residual stream inside their epilogues.
+queries and keys are rotated by their positions if the layer has any, the keys and values go to the cache, attention
+reads the cache, and the two projections back add onto the residual stream inside their epilogues.  With the cache in 4 bits
+prompts attend over their own 16-bit keys and values, and what follows over the cache.
 """
 from __future__ import annotations
 
@@ -29,12 +30,18 @@ def normalise(x: torch.Tensor) -> torch.Tensor:
 
 
 class DecoderLayer:
-    """width = heads * dim; a two-matrix feed-forward block of `inner` columns with GELU."""
+    """width = heads * dim; a two-matrix feed-forward block of `inner` columns with GELU.  rotary_base: of the
+    frequencies of rotary positions (None: no positions); cache: "s8" or "u4"."""
 
-    def __init__(self, heads: int, kv_heads: int, dim: int, inner: int, seed: int = 0, device="cuda"):
+    def __init__(self, heads: int, kv_heads: int, dim: int, inner: int, seed: int = 0, device="cuda",
+                 rotary_base: float | None = None, cache: str = "s8"):
         g = torch.Generator(device=device)
         g.manual_seed(seed)
         self.heads, self.kv_heads, self.dim, self.width = heads, kv_heads, dim, heads * dim
+        self.bits = cache
+        self.inv_freq = None
+        if rotary_base is not None:
+            self.inv_freq = (rotary_base ** (-torch.arange(0, dim, 2, dtype=torch.float64) / dim)).float().to(device)
 
         def weight(rows, cols):
             return (torch.randn(rows, cols, generator=g, device=device) / cols ** 0.5).half()
@@ -49,12 +56,23 @@ class DecoderLayer:
         w, col_scale = self.weights[name]
         return binding.gemm_s8_linear(q, w, scale, col_scale, **kw)
 
-    def forward(self, x, cache, table, cu, past, kv_len, max_new):
-        """x: float16 (tokens, width), the new tokens of all sequences; updated in place."""
+    def forward(self, x, cache, table, cu, past, kv_len, max_new, positions=None, fresh=False):
+        """x: float16 (tokens, width), the new tokens of all sequences; updated in place.  positions: int32 (tokens,) for a
+        layer that has them; fresh: no sequence has tokens in the cache yet."""
         h, k, d = self.heads, self.kv_heads, self.dim
         qkv = self._linear("qkv", normalise(x), bias=self.qkv_bias).view(-1, h + 2 * k, d)
-        binding.kv_append_s8(cache, qkv[:, h:h + k], qkv[:, h + k:], cu, past, table, max_new)
-        a = binding.kv_attention_s8(qkv[:, :h], cache, cu, kv_len, table, max_new)
+        q, key, value = qkv[:, :h], qkv[:, h:h + k], qkv[:, h + k:]
+        if self.inv_freq is not None:
+            binding.rotary_fp16(q, key, positions, self.inv_freq, out=(q, key))
+        if self.bits == "s8":
+            binding.kv_append_s8(cache, key, value, cu, past, table, max_new)
+            a = binding.kv_attention_s8(q, cache, cu, kv_len, table, max_new)
+        else:
+            binding.kv_append_u4(cache, key, value, cu, past, table, max_new)
+            if fresh:
+                a = binding.attention_fp16(q, key, value, cu, max_new)
+            else:
+                a = binding.kv_attention_u4(q, cache, cu, kv_len, table, max_new)
         self._linear("out", a.view(-1, self.width), residual=x, C=x)
         f = self._linear("up", normalise(x), activation="gelu_tanh")
         return self._linear("down", f, residual=x, C=x)
@@ -65,7 +83,8 @@ class Batch:
 
     def __init__(self, layer: DecoderLayer, sequences: int, most: int, page: int = 64, device="cuda"):
         per = -(-most // page)
-        self.cache = binding.kv_cache_s8(sequences * per, layer.kv_heads, page, layer.dim, device)
+        make = binding.kv_cache_s8 if layer.bits == "s8" else binding.kv_cache_u4
+        self.cache = make(sequences * per, layer.kv_heads, page, layer.dim, device)
         self.table = torch.randperm(sequences * per, device=device).to(torch.int32).view(sequences, per)
         self.length = [0] * sequences
         self.device = device
@@ -80,18 +99,19 @@ class Batch:
         def ints(v):
             return torch.tensor(v, dtype=torch.int32, device=self.device)
 
-        y = layer.forward(x, self.cache, self.table, ints(starts), ints(self.length), ints(total), max(new))
+        positions = ints([p for a, n in zip(self.length, new) for p in range(a, a + n)])
+        y = layer.forward(x, self.cache, self.table, ints(starts), ints(self.length), ints(total), max(new), positions,
+                          fresh=not any(self.length))
         self.length = total
         return y
 
 
-def main():
-    torch.manual_seed(0)
-    layer = DecoderLayer(heads=16, kv_heads=4, dim=128, inner=8192)
+def run(layer: DecoderLayer):
     prompts = [300, 17, 1024, 1]
     batch = Batch(layer, len(prompts), most=2048)
     y = batch.step(layer, torch.randn(sum(prompts), layer.width, device="cuda").half(), prompts)
-    print("prompts of %s tokens: output %s, rms %.3f" % (prompts, tuple(y.shape), y.float().square().mean().sqrt()))
+    print("cache %s, prompts of %s tokens: output %s, rms %.3f"
+          % (layer.bits, prompts, tuple(y.shape), y.float().square().mean().sqrt()))
     for _ in range(3):      # the shapes of single tokens run for the first time
         batch.step(layer, torch.randn(len(prompts), layer.width, device="cuda").half(), [1] * len(prompts))
     a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -102,6 +122,12 @@ def main():
     b.record()
     torch.cuda.synchronize()
     print("one token of each: %.1f us a layer" % (a.elapsed_time(b) / 50 * 1e3))
+
+
+def main():
+    torch.manual_seed(0)
+    run(DecoderLayer(heads=16, kv_heads=4, dim=128, inner=8192))
+    run(DecoderLayer(heads=16, kv_heads=4, dim=128, inner=8192, rotary_base=10000.0, cache="u4"))
     if binding.gemm_last_device_status() != 0:
         raise SystemExit("a kernel reported an error")
 

@@ -647,61 +647,57 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
                                 : nullptr;
         if (U4 && part && live) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         __half* const dst = p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
-        uint32_t worst = 0;  // magnitude bits of the results
+        uint32_t finite[4] = {0, 0, 0, 0};  // sums of the results times 0
         const unsigned alive = __ballot_sync(0xffffffffu, live);
         const uint32_t stage = base + T::OUT_OFFSET + static_cast<uint32_t>(warp * 32 * T::OUT_PITCH);
         __half* run[4];  // of rows lane / 4 + 8 i
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           run[i] = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), lane / 4 + 8 * i)) + (lane & 3) * 8;
+        uint32_t x[32];
+#pragma unroll
+        for (int v = 0; v < 32; ++v) x[v] = 0;
+        if (it.tiles > 0) ptx::tmem_ld_32x32b_x32(o_at, x);
 #pragma unroll 1
         for (int d = 0; d < D; d += 32) {
-          uint32_t x[32];
-          if (it.tiles > 0) {
-            ptx::tmem_ld_32x32b_x32(o_at + d, x);
-            ptx::tmem_wait_ld();
-          } else {
+          ptx::tmem_wait_ld();
+          uint32_t z[32];
+          // (columns of 4-bit values lie in the order in which words of codes come apart: 0, 4, 1, 5, ...)
 #pragma unroll
-            for (int v = 0; v < 32; ++v) x[v] = 0;
-          }
-          if constexpr (U4) {
+          for (int v = 0; v < 32; ++v) z[v] = U4 ? x[(v & 24) + ((v & 7) < 4 ? 2 * (v & 7) : 2 * (v & 7) - 7)] : x[v];
+          uint32_t y[16];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {  // (columns of values lie in the order in which words of codes come apart: 0, 4, 1, 5, ...)
-              float y[8];
-#pragma unroll
-              for (int u = 0; u < 8; ++u) y[u] = __uint_as_float(x[8 * v + (u < 4 ? 2 * u : 2 * u - 7)]);
-#pragma unroll
-              for (int u = 0; u < 8; ++u) x[8 * v + u] = __float_as_uint(y[u]);
-            }
-          }
+          for (int v = 0; v < 16; ++v) y[v] = pack_halves(__uint_as_float(z[2 * v]) * inv, __uint_as_float(z[2 * v + 1]) * inv);
           if (U4 && part) {  // O as it stands, to be joined
 #pragma unroll
             for (int v = 0; v < 8; ++v)
-              if (live) *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(x[4 * v], x[4 * v + 1], x[4 * v + 2], x[4 * v + 3]);
-          } else {
+              if (live) *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]);
+            __syncwarp();
+          }
+          if (it.tiles > 0 && d + 32 < D) ptx::tmem_ld_32x32b_x32(o_at + d + 32, x);  // (on its way while these leave)
+          if (!(U4 && part)) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              uint32_t y[4];
+              if constexpr (!U4) {
 #pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                y[u] = pack_halves(__uint_as_float(x[8 * v + 2 * u]) * inv, __uint_as_float(x[8 * v + 2 * u + 1]) * inv);
-                if constexpr (!U4) worst = __vmaxu2(worst, y[u] & 0x7fff7fffu);
+                for (int u = 0; u < 4; ++u) finite[u] = fma_h2(y[4 * v + u], 0u, finite[u]);
               }
-              ptx::st_shared_v4(stage + lane * T::OUT_PITCH + v * 16, y[0], y[1], y[2], y[3]);
+              ptx::st_shared_v4(stage + lane * T::OUT_PITCH + v * 16, y[4 * v], y[4 * v + 1], y[4 * v + 2], y[4 * v + 3]);
             }
             __syncwarp();
+            uint4 w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t y[4];
-              ptx::ld_shared_v4(stage + (lane / 4 + 8 * i) * T::OUT_PITCH + (lane & 3) * 16, y[0], y[1], y[2], y[3]);
-              if (alive >> (lane / 4 + 8 * i) & 1u) *reinterpret_cast<uint4*>(run[i] + d) = make_uint4(y[0], y[1], y[2], y[3]);
-            }
+            for (int i = 0; i < 4; ++i)
+              ptx::ld_shared_v4(stage + (lane / 4 + 8 * i) * T::OUT_PITCH + (lane & 3) * 16, w[i].x, w[i].y, w[i].z, w[i].w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (alive >> (lane / 4 + 8 * i) & 1u) *reinterpret_cast<uint4*>(run[i] + d) = w[i];
+            __syncwarp();
           }
-          __syncwarp();
         }
         ptx::tc_fence_before_sync();
         if constexpr (!U4) {
-          if (live && max(worst & 0xffffu, worst >> 16) >= 0x7c00u) {
+          if (live && ((finite[0] | finite[1] | finite[2] | finite[3]) & 0x7c007c00u) != 0) {
             // Was it a value that this row does not see?  Tiles wholly visible to it hide none.
             const int end = it.lo + it.tiles * TN - 1;
             if (any_not_finite<D>(p, it.head, it.row0 + max(pos + 1, it.lo), it.row0 + end) ||
