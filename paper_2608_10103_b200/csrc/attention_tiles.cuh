@@ -12,15 +12,17 @@
 // on from one row tile into the next, K and V; an issuer for each 128 rows, so that neither waits for the other's softmax. Every 128 rows
 // have two score buffers: the scores of the next tokens are computed while the softmax works on these.
 //
-// What bounds it, prompts at 128 d: 1550-1650 cycles per 64 tokens and pair of row tiles, where the products take the tensor pipe 1540 (scores
-// of 64 tokens as long as of 128: the pipe wants N = 128) and the exponentials 1024. With one buffer of 128 scores per row tile the products
-// would take 1024, but scores -> maximum -> weights -> products then is a chain of 3400-3600 per 128 tokens (8192 tokens: 472-495 us against
-// 455). Also tried there and slower: two threads per row (684 us), the first half of the weights multiplied early. An eighth to half of the
-// exponentials as polynomials, in either form: no faster.
-// A row tile's end, 6000 cycles of which 3600 are its results' way out, is a fifth of a prompt of 1000 tokens.
-// Measured: 8192 tokens, 32 heads on 8, 455-465 us (0.70 of the time that the operations take at the cuBLAS bf16 rate); 12 prompts of
-// up to 2048 tokens 169 us; 4096 tokens of 32 heads on 8 of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 291 us: some 2700 cycles
-// per 64 tokens, which the expansion of codes and the products each take by themselves, over memory that they share.
+// What bounds it, prompts at 128 d: 1530-1580 cycles per 64 tokens and pair of row tiles, which the products take by themselves: an
+// instruction of Q K^T reads 128 rows of Q from shared memory, 64 cycles for 64 tokens as for 128, so that the two products come to 2 x (512 +
+// 256). One buffer of 128 scores per row tile would halve the first, but scores -> maximum -> weights -> products then is a chain of 3400-3600
+// cycles per 128 tokens (8192 tokens: 472-495 us against 453); tensor memory holds no more beside two results. The exponentials
+// take 1024 cycles of the 1530. Tried and slower: two threads per row (684 us), the first half of the weights multiplied
+// early; no faster: an eighth to half of the exponentials as polynomials, waits that spin. What would help is a pair of CTAs per pair of
+// row tiles (cta_group::2), which leaves each tensor memory for two buffers of 128 scores: not built.
+// A row tile's end, some 5000 cycles of which 2900 are its results' way out, is a sixth of a prompt of 1000 tokens.
+// Measured: 8192 tokens, 32 heads on 8, 453 us (0.72 of the time that the operations take at the cuBLAS bf16 rate); 12 prompts of
+// up to 2048 tokens 163 us; 4096 tokens of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 297 us: some 2700 cycles per 64
+// tokens. There the products are 2 x (512 + 512), the expansion of codes takes as long, and both want the same shared memory.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
 // other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies, and warps write the same tiles from them. Keys
@@ -29,7 +31,7 @@
 // exact in binary16; the second tile holds what is left. (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
 // results, only values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in
 // kv_attention_u4.cuh, need five factors a token for every row: what shared memory then hands to registers took longer, 340 us against
-// 291.)
+// 297.)
 //
 // What a masked place holds must not matter, but weight 0 times an infinity is NaN. A 4-bit token whose scale or
 // offset is not finite gets zeros for values and a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
@@ -896,85 +898,111 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     }
   } else if (warp < W_MMA + QT && warp >= W_MMA) {
     // ------------------------------------------------------------------ MMA issuer of tile q of the rows
-    const int q = warp - W_MMA;
+    // What addresses and control flow depend on is the same in all lanes; made from lane 0's, so that the compiler sees it and
+    // keeps descriptors in uniform registers.
+    const int q = __shfl_sync(0xffffffffu, warp, 0) - W_MMA;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const bool elected = ptx::elect_one();
     constexpr uint32_t idesc_qk = ptx::make_idesc<ptx::KIND_F16>(128, TN);
     constexpr uint32_t idesc_pv = ptx::make_idesc<ptx::KIND_F16>(128, D) | ptx::IDESC_B_MN_MAJOR;
-    int tile = 0;  // K and V tiles in the ring before this item
-    int done = 0;  // token tiles of these rows
+    const uint64_t q_desc = ptx::smem_desc_sw128(base + q * (D / 64) * 16384);
+    const uint64_t k_desc = ptx::smem_desc_sw128(base + T::SLOT_OFFSET);
+    const uint64_t v_desc = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET, T::CHUNK);
+    int slot = 0;          // of the next tile in the ring that has not been multiplied yet: V's, K's being up to two token tiles ahead
+    uint32_t phase = 0;    // of that place
+    int done = 0;          // token tiles of these rows
     bool ok = true;
-    auto wait_slot = [&](int i) {
-      const bool there = wait_bounded(slot_full(i % SLOTS), (i / SLOTS) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
-      if (there) ptx::tc_fence_after_sync();
-      return there;
+    // `ahead` tiles on from there
+    auto place = [&](int ahead, uint32_t& its_phase) {
+      const int s = slot + ahead;
+      its_phase = s >= SLOTS ? phase ^ 1u : phase;
+      return s >= SLOTS ? s - SLOTS : s;
+    };
+    auto wait_all = [&](uint32_t bar, uint32_t parity) {
+      const bool there = wait_bounded(bar, parity, abort_flag, p.status, DEV_TIMEOUT_MMA);
+      return __all_sync(0xffffffffu, there) != 0;
+    };
+    auto advance = [&](int by) {
+      slot += by;
+      if (slot >= SLOTS) {
+        slot -= SLOTS;
+        phase ^= 1u;
+      }
     };
 #pragma unroll 1
     for (int k = 0, used = 0; ok; ++k) {
       AttnItem it;
       ok = next_item(k, it);
-      if (!ok || it.tiles < 0) break;
-      if (it.tiles == 0) continue;
-      if (q >= it.active) {  // nothing to do but to let the ring go round
-        ok = wait_bounded(q_full, used & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
-        if (ok && elected) ptx::mbar_arrive(q_empty);
-#pragma unroll 1
-        for (int j = 0; j < T::KINDS * it.tiles && ok; ++j) {
-          ok = wait_slot(tile + j);
-          if (ok && elected) ptx::mbar_arrive(slot_empty((tile + j) % SLOTS));
-        }
-        __syncwarp();
-        tile += T::KINDS * it.tiles;
-        ++used;
-        continue;
-      }
-      ok = wait_bounded(q_full, used & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+      const int tiles = __shfl_sync(0xffffffffu, it.tiles, 0), active = __shfl_sync(0xffffffffu, it.active, 0);
+      if (!ok || tiles < 0) break;
+      if (tiles == 0) continue;
+      ok = wait_all(q_full, used & 1);
       if (!ok) break;
       ++used;
-      auto qk = [&](int j) {  // scores of token tile j
-        if (!wait_slot(tile + T::KINDS * j)) return false;
-        const int slot = (tile + T::KINDS * j) % SLOTS, sb = 2 * q + ((done + j) & 1);
+      if (q >= active) {  // nothing to do but to let the ring go round
+        if (elected) ptx::mbar_arrive(q_empty);
+#pragma unroll 1
+        for (int j = 0; j < T::KINDS * tiles && ok; ++j) {
+          ok = wait_all(slot_full(slot), phase);
+          if (ok && elected) ptx::mbar_arrive(slot_empty(slot));
+          __syncwarp();
+          advance(1);
+        }
+        continue;
+      }
+      // Scores of the token tile whose K lies `ahead` tiles on in the ring.
+      auto qk = [&](int j, int ahead) {
+        uint32_t its_phase;
+        int at = place(ahead % SLOTS, its_phase);
+        its_phase ^= static_cast<uint32_t>(ahead / SLOTS) & 1u;
+        if (!wait_all(slot_full(at), its_phase)) return false;
+        ptx::tc_fence_after_sync();
+        const int sb = 2 * q + ((done + j) & 1);
+        const uint64_t b = k_desc + static_cast<uint32_t>(at * (T::TILE_BYTES >> 4));
         if (elected) {
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t off = static_cast<uint32_t>((kk & 3) * 32);
-            const uint64_t a = ptx::smem_desc_sw128(base + (q * (D / 64) + (kk >> 2)) * 16384 + off);
-            const uint64_t b = ptx::smem_desc_sw128(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + (kk >> 2) * T::CHUNK + off);
-            ptx::mma_ss<ptx::KIND_F16, 1>(tmem + sb * TN, a, b, idesc_qk, kk > 0);
-          }
+          for (int kk = 0; kk < D / 16; ++kk)
+            ptx::mma_ss<ptx::KIND_F16, 1>(tm + sb * TN, q_desc + static_cast<uint32_t>((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                                          b + static_cast<uint32_t>((kk >> 2) * (T::CHUNK >> 4) + (kk & 3) * 2), idesc_qk, kk > 0);
           ptx::mma_commit<1>(s_full(sb));
-          ptx::mma_commit<1>(slot_empty(slot));
-          if (j == it.tiles - 1) ptx::mma_commit<1>(q_empty);
+          ptx::mma_commit<1>(slot_empty(at));
+          if (j == tiles - 1) ptx::mma_commit<1>(q_empty);
         }
         __syncwarp();
         return true;
       };
-      for (int j = 0; j < 2 && j < it.tiles && ok; ++j) ok = qk(j);
+      for (int j = 0; j < 2 && j < tiles && ok; ++j) ok = qk(j, T::KINDS * j);
 #pragma unroll 1
-      for (int j = 0; j < it.tiles && ok; ++j) {
+      for (int j = 0; j < tiles && ok; ++j) {
         const int sb = 2 * q + ((done + j) & 1);
-        for (int i = 1; i < T::KINDS && ok; ++i) ok = wait_slot(tile + T::KINDS * j + i);
-        ok = ok && wait_bounded(p_full(sb), ((done + j) >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_MMA);
+        int at[T::KINDS];
+#pragma unroll
+        for (int i = 1; i < T::KINDS; ++i) {
+          uint32_t its_phase;
+          at[i] = place(i, its_phase);
+          ok = ok && wait_all(slot_full(at[i]), its_phase);
+        }
+        ok = ok && wait_all(p_full(sb), ((done + j) >> 1) & 1);
         if (!ok) break;
         ptx::tc_fence_after_sync();
         if (elected) {
 #pragma unroll
           for (int i = 1; i < T::KINDS; ++i) {
-            const int slot = (tile + T::KINDS * j + i) % SLOTS;
+            const uint64_t v = v_desc + static_cast<uint32_t>(at[i] * (T::TILE_BYTES >> 4));
 #pragma unroll
-            for (int kk = 0; kk < TN / 16; ++kk) {
-              const uint64_t v = ptx::smem_desc_sw128_mn(base + T::SLOT_OFFSET + slot * T::TILE_BYTES + kk * 2048, T::CHUNK);
-              ptx::mma_f16_ts(tmem + T::O_COLUMN + q * D, tmem + sb * TN + kk * 8, v, idesc_pv, j > 0 || i > 1 || kk > 0);
-            }
+            for (int kk = 0; kk < TN / 16; ++kk)
+              ptx::mma_f16_ts(tm + T::O_COLUMN + q * D, tm + sb * TN + kk * 8, v + static_cast<uint32_t>(kk * (2048 >> 4)), idesc_pv,
+                              j > 0 || i > 1 || kk > 0);
             if (i == T::KINDS - 1) ptx::mma_commit<1>(o_done(q));
-            ptx::mma_commit<1>(slot_empty(slot));
+            ptx::mma_commit<1>(slot_empty(at[i]));
           }
         }
         __syncwarp();
         // (the scores go where the weights are: the MMAs of this thread run in order)
-        if (j + 2 < it.tiles) ok = qk(j + 2);
+        if (j + 2 < tiles) ok = qk(j + 2, 2 * T::KINDS);
+        advance(T::KINDS);
       }
-      tile += T::KINDS * it.tiles;
-      done += it.tiles;
+      done += tiles;
     }
     if (!ok && elected) {
       // Gave up: wait for the MMAs already issued before tensor memory is released.
