@@ -55,6 +55,7 @@ struct AttnTilesParams {
   const int* cu;
   const int* kv_len;  // null: each sequence's tokens are its rows
   int max_q, max_len, rows;
+  int units;          // row tiles x KV heads at most, which scratch is there for
   int group, heads;   // query heads per KV head, KV heads
   const __half* q;
   long long q_token_stride, q_head_stride;
@@ -764,7 +765,10 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
   } else if (warp == W_SCHEDULE) {
     // ------------------------------------------------------------------ scheduler
     const AttnOrder<TN> order(p, QT * per_tile, blockIdx.x == 0);
-    const int grid = static_cast<int>(gridDim.x), total = order.all * p.heads * p.splits;
+    // (sequences that overlap, or a count of row tiles that they make pass 32 bits: no row tile has a place behind the last)
+    const bool fits = order.all >= 0 && static_cast<long long>(order.all) * p.heads <= p.units;
+    if (!fits && blockIdx.x == 0 && lane == 0) kv_report(p.status);
+    const int grid = static_cast<int>(gridDim.x), total = (fits ? order.all * p.heads : order.all < 0 ? 0 : p.units) * p.splits;
     bool ok = true;
 #pragma unroll 1
     for (int k = 0, round = 0; ok; ++k, ++round) {
@@ -788,7 +792,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         const int queries = min(QT * per_tile, s.n - it.query);
         it.active = QT == 2 && queries > per_tile ? 2 : 1;
         it.hi = p.causal ? max(0, it.base + it.query + queries) : s.len;
-        it.from = p.window > 0 ? max(0, it.base + it.query - p.window + 1) : 0;
+        it.from = kv_first_seen(it.base + it.query, p.window);
         it.lo = it.from / TN * TN;
         it.tiles = max(0, (it.hi - it.lo + TN - 1) / TN);
         if (p.splits > 1) {  // this CTA's part of the tokens

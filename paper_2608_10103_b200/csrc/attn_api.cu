@@ -42,6 +42,7 @@ int launch_prompts(const SharedDevice& dev, AttnTilesParams& p, cudaStream_t str
   const long long by_longest = (static_cast<long long>(longest) + per_cta - 1) / per_cta * p.batch;
   const long long items = (by_rows < by_longest ? by_rows : by_longest) * p.heads;
   if (items > 0x3fffffffll) return GEMM_ERR_TOO_LARGE;
+  p.units = static_cast<int>(items);
   CUtensorMap q, k, v;
   int rc = shared_row_map(&q, p.q, D, p.heads * p.group, p.rows, p.q_token_stride, p.q_head_stride, p.group, per_tile);
   if (rc == GEMM_OK) rc = shared_row_map(&k, p.k, D, p.heads, p.rows, p.kv_token_stride, p.kv_head_stride, 1, T::TN);
@@ -86,7 +87,8 @@ int rotary_fp16(int tokens, int head_dim, int rotary_dim, int pairs, const rotar
                  r->y_token_stride, r->y_head_stride};
     heads += r->heads;
   }
-  if (heads * head_dim > (1ll << 26)) return GEMM_ERR_TOO_LARGE;  // (a CTA counts its pieces in 32 bits)
+  // (a CTA counts its pieces in 32 bits, and tokens a little beyond the last)
+  if (heads * head_dim > (1ll << 26) || tokens > 0x7fffffff - 1024) return GEMM_ERR_TOO_LARGE;
   SharedDevice dev;
   const int rc = shared_device(&dev);
   if (rc != GEMM_OK) return rc;

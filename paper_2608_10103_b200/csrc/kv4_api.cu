@@ -60,6 +60,7 @@ int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream
   const long long by_longest = (static_cast<long long>(longest) + per_cta - 1) / per_cta * p.batch;
   const long long units = (by_rows < by_longest ? by_rows : by_longest) * p.heads;
   if (units > 0x3fffffffll) return GEMM_ERR_TOO_LARGE;
+  p.units = static_cast<int>(units);
   CUtensorMap q;
   int rc = shared_row_map(&q, p.q, D, p.heads * p.group, p.rows, p.q_token_stride, p.q_head_stride, p.group, per_tile);
   if (rc != GEMM_OK) return rc;

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
   // Steps of a sequence, 0 = it has no row here; [lo, hi): the tokens that its queries see between them, lo rounded down.
   auto steps_of = [&](const KvSeq& s, int& lo, int& hi) {
     if (s.n == 0 || static_cast<long long>(s.n) * p.group > p.split_rows) return 0;
-    lo = p.window > 0 ? max(0, s.len - s.n - p.window + 1) / STEP * STEP : 0;
+    lo = kv_first_seen(s.len - s.n, p.window) / STEP * STEP;
     hi = max(s.len, lo);
     return max(1, (hi - lo + STEP - 1) / STEP);
   };
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
       // ids of 32 pages at a time, one per lane, the next 32 on their way
       const int* const table = p.table + static_cast<long long>(b) * p.table_stride;
       const int last_page = (hi - 1) >> p.c.page_shift;  // (nothing visible: below every page)
-      const int first_page = (p.window > 0 ? max(0, s.len - s.n - p.window + 1) : 0) >> p.c.page_shift;
+      const int first_page = kv_first_seen(s.len - s.n, p.window) >> p.c.page_shift;
       int id_first = (lo + w0 * STEP) >> p.c.page_shift;
       auto load_ids = [&](int first) {
         return first + lane <= last_page && first + lane >= first_page ? kv_ld(table + first + lane) : -1;

@@ -38,6 +38,9 @@ __device__ __forceinline__ int kv_ld(const int* p) {  // may have been written b
 }
 __device__ __forceinline__ void kv_report(int* status) { atomicCAS(status, 0, DEV_BAD_INDEX); }
 
+// First token that a query at position `pos` sees (0 where it sees none); window 0: all.
+__device__ __forceinline__ int kv_first_seen(int pos, int window) { return window > 0 && pos >= window ? pos - window + 1 : 0; }
+
 // Rows and positions of a sequence, cut to what the packed arrays, the table and the caller's bound allow.
 struct KvRange {
   int row0;   // first row in the packed arrays

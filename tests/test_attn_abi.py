@@ -46,6 +46,7 @@ def test_rotary_refusals(lib):
                dict(q=rows(x_token_stride=132)), dict(q=rows(y_head_stride=68))):
         assert call(**kw) == -2, kw
     assert call(q=rows(heads=1 << 21)) == -7
+    assert call(tokens=2 ** 31 - 1, axes=1, sections=None) == -7
 
 
 def test_prompt_attention_refusals(lib):

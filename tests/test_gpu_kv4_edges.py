@@ -107,3 +107,28 @@ def test_nothing_to_do():
     assert binding.rotary_fp16(e, None, dev([]), torch.ones(32, device="cuda")).shape == e.shape
     with pytest.raises(binding.GemmError):
         binding.attention_fp16(q, q[:, :2], q[:, :2], dev([0]), 1)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 4, 1000])
+@pytest.mark.parametrize("news", [[8, 5, 2], [100, 70, 9]])
+def test_wide_windows_over_short_sequences(news, window):
+    """More queries than tokens: the first stand at positions below 0, from which a window may reach further down than 32 bits do."""
+    lens = [4, 60, 1]
+    cache, table, q = setup(lens, news, 4, 2, 64, 16, seed=8)
+    got = binding.kv_attention_u4(q, cache, dev(starts(news)), dev(lens), dev(table), max(news), window=window)
+    ref, tol = reference(q, cache, table, lens, news, window, 64 ** -0.5)
+    assert ((got.double() - ref).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("batch", [9, 64])
+def test_sequences_that_overlap(batch):
+    """Row counts that fall and rise again name more rows than there are: reported, and nothing is written outside the result."""
+    rows = 1000
+    cu = dev([0 if i % 2 == 0 else rows for i in range(batch + 1)])
+    cache, table, q = setup([rows] * batch, [rows], 4, 2, 64, 16, seed=9)
+    guarded = torch.zeros(rows + 256, 4, 64, device="cuda").half()
+    binding.kv_attention_u4(q, cache, cu, dev([rows] * batch), dev(table), rows, out=guarded[128:128 + rows])
+    assert binding.gemm_last_device_status() == 6
+    binding.attention_fp16(q, q[:, :2], q[:, 2:], cu, rows, out=guarded[128:128 + rows])
+    assert binding.gemm_last_device_status() == 6
+    assert not guarded[:128].any() and not guarded[128 + rows:].any()
