@@ -120,8 +120,7 @@ __device__ __forceinline__ void kv_visible(const KvAttnParams& p, const KvSeq& s
                                            int& lo, int& hi) {
   const int base = s.len - s.n;  // position of query 0; may be negative
   hi = max(0, base + i1);
-  lo = p.window > 0 ? max(0, base + i0 - p.window + 1) : 0;
-  lo = lo / KVA_STEP * KVA_STEP;
+  lo = kv_first_seen(base + i0, p.window) / KVA_STEP * KVA_STEP;
   if (hi < lo) hi = lo;
 }
 __device__ __forceinline__ int kv_steps(int lo, int hi) {  // a unit has one step at least
