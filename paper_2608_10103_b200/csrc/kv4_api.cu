@@ -35,9 +35,9 @@ int check_cache(const kv_cache_u4_t* c, KvCacheU4View* v) {
   return GEMM_OK;
 }
 
-// Blocks of KV4_TOKENS tokens of every sequence; 0 = too many.
-int blocks_of(int max_rows, int batch, int* per_seq) {
-  *per_seq = static_cast<int>((static_cast<long long>(max_rows) + KV4_TOKENS - 1) / KV4_TOKENS);
+// Blocks of `tokens` tokens of every sequence; 0 = too many.
+int blocks_of(int max_rows, int tokens, int batch, int* per_seq) {
+  *per_seq = static_cast<int>((static_cast<long long>(max_rows) + tokens - 1) / tokens);
   const long long blocks = static_cast<long long>(*per_seq) * batch;
   return blocks > 0x7fffffffll ? 0 : static_cast<int>(blocks);
 }
@@ -175,7 +175,7 @@ int kv_append_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int
   if (!K || !V || token_stride < 0 || head_stride < p.c.dim) return GEMM_ERR_INVALID_ARG;
   if (misaligned(K, 16) || misaligned(V, 16) || token_stride % 8 || head_stride % 8)
     return GEMM_ERR_MISALIGNED;
-  const int blocks = blocks_of(max_new < rows ? max_new : rows, batch, &p.blocks_per_seq);
+  const int blocks = blocks_of(max_new < rows ? max_new : rows, kv4_tokens(p.c.dim), batch, &p.blocks_per_seq);
   if (!blocks) return GEMM_ERR_TOO_LARGE;
   SharedDevice dev;
   rc = shared_device(&dev);
@@ -203,7 +203,7 @@ int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* 
   if (rc != GEMM_OK) return rc;
   if (!K && !V) return GEMM_ERR_INVALID_ARG;
   if (misaligned(K, 16) || misaligned(V, 16)) return GEMM_ERR_MISALIGNED;
-  const int blocks = blocks_of(max_read < rows ? max_read : rows, batch, &p.blocks_per_seq);
+  const int blocks = blocks_of(max_read < rows ? max_read : rows, kv4_tokens(p.c.dim), batch, &p.blocks_per_seq);
   if (!blocks) return GEMM_ERR_TOO_LARGE;
   SharedDevice dev;
   rc = shared_device(&dev);
