@@ -7,7 +7,7 @@
 // Eight lanes share a row (a token's head), head_dim / 64 pieces of eight values each: 16 bytes of binary16 or 4 of codes, side by
 // side. The extrema of a row travel between them as one pair (max, -min), three shuffles. What a row costs besides its values
 // (where it lies, two divisions) is a third of the instructions so, instead of two thirds with one piece per lane
-// (4 x 8192 tokens of 8 heads of 128 written and 4 x 9192 read back: 104 -> 62 us; values by pairs, 62 -> 58: 0.75 of the copy rate, at
+// (4 x up to 8192 tokens of 8 heads of 128 written and 4 x up to 9192 read back: 104 -> 62 us; values by pairs, 62 -> 58: 0.75 of the copy rate, at
 // 256 d 0.88). Bound by 2 bytes read and 0.53 written per value (reading back: the reverse) and by issuing some 9 (5) instructions
 // for each, in single-token calls by a launch and two dependent loads.
 #pragma once
@@ -29,7 +29,7 @@ struct KvAppendU4Params {
 };
 
 constexpr int KV4_THREADS = 256;
-// Tokens per CTA: at 8 heads two turns through its rows (4 x 8192 tokens written and 4 x 9192 read at 64 d: 16 tokens, which one turn
+// Tokens per CTA: at 8 heads two turns through its rows (4 x up to 8192 tokens written and 9192 read at 64 d: 16 tokens, which one turn
 // takes, 47.4 us, 32 39.4, 64 41.0; at 128 d 8 tokens 69.7, 16 57.7, 32 57.9, 64 64.8).
 __host__ __device__ constexpr int kv4_tokens(int dim) { return dim == 64 ? 32 : 16; }
 constexpr int KV4_ROWS = KV4_THREADS / 8;  // rows a CTA works on at a time
