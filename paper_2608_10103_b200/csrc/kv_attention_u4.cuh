@@ -27,7 +27,8 @@
 // Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 73.5 us, 3.9 TB/s of the cache; one of 1000 tokens 9.8 us.
 // 16 heads of 64 d, 131071 tokens, 4 queries: 53.8 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
 // codes meet as many scores, exponentials and factors, the instructions per byte are 1.5 times as many. Four CTAs per SM
-// with rings of three steps at 128 d: 2 % slower than three with four; steps of 64 tokens at 64 d: -2 to +3 %.
+// with rings of three steps at 128 d: 2 % slower than three with four; steps of 64 tokens at 64 d: -2 to +3 %; the scores' arithmetic by pairs
+// of tokens, 7 % fewer instructions: 2 % faster at 64 d, level at 128 d, 9 % slower at 256 d (spills).
 #pragma once
 
 #include <cuda_fp16.h>
