@@ -21,7 +21,7 @@
 // row tiles (cta_group::2), which leaves each tensor memory for two buffers of 128 scores: not built.
 // A row tile's end, some 5000 cycles of which 2900 are its results' way out, is a sixth of a prompt of 1000 tokens.
 // Measured: 8192 tokens, 32 heads on 8, 453 us (0.72 of the time that the operations take at the cuBLAS bf16 rate); 12 prompts of
-// up to 2048 tokens 163 us; 4096 tokens of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 297 us: some 2700 cycles per 64
+// up to 2048 tokens 163 us; 4096 tokens of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 283 us: some 2700 cycles per 64
 // tokens. There the products are 2 x (512 + 512), the expansion of codes takes as long, and both want the same shared memory.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
@@ -117,8 +117,11 @@ struct AttnTileShape {
   // raw_full[2][4], raw_empty[2][4], table_full[8], turn_done[2][4], slot_full[], slot_empty[]
   static constexpr int BARS = 52 + 2 * SLOTS;
   static constexpr int MISC_OFFSET = BAR_OFFSET + BARS * 8;
-  // 32 rows of 32 results for each softmax warp, which leave as runs of 64 bytes: a row pitch of 80 keeps them off one another's banks
-  static constexpr int OUT_PITCH = 80;
+  // 32 rows of OUT_COLUMNS results for each softmax warp, which leave as runs of 64 or 32 bytes; the pitch keeps rows off one another's
+  // banks.  (Softmax warps of the 4-bit kernel have 128 registers up to 128 d: 16 columns at a time 292 -> 282 us there, at 256 d 619 -> 626,
+  // on prompts 160 -> 165.)
+  static constexpr int OUT_COLUMNS = U4 && D <= 128 ? 16 : 32;
+  static constexpr int OUT_PITCH = OUT_COLUMNS * 2 + 16;
   static constexpr int OUT_OFFSET = MISC_OFFSET + 16;
   static constexpr int DYN_BYTES = OUT_OFFSET + SOFTMAX_WARPS * 32 * OUT_PITCH + 1024;
   static constexpr uint32_t O_COLUMN = 256;      // score (and weight) buffer i at TN i, two for each tile of rows; O behind them
@@ -632,34 +635,42 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         uint32_t finite[4] = {0, 0, 0, 0};  // sums of the results times 0
         const unsigned alive = __ballot_sync(0xffffffffu, live);
         const uint32_t stage = base + T::OUT_OFFSET + static_cast<uint32_t>(warp * 32 * T::OUT_PITCH);
-        __half* run[4];  // of rows lane / 4 + 8 i
+        constexpr int COLUMNS = T::OUT_COLUMNS, PIECES = COLUMNS / 8, RUN_ROWS = 32 / PIECES;  // 16-byte pieces of a run, rows that a store covers
+        auto load_columns = [&](int d, uint32_t (&x)[COLUMNS]) {
+          if constexpr (COLUMNS == 32)
+            ptx::tmem_ld_32x32b_x32(o_at + d, x);
+          else
+            ptx::tmem_ld_32x32b_x16(o_at + d, x);
+        };
+        __half* run[PIECES];  // of rows lane / PIECES + RUN_ROWS i
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          run[i] = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), lane / 4 + 8 * i)) + (lane & 3) * 8;
-        uint32_t x[32];
+        for (int i = 0; i < PIECES; ++i)
+          run[i] = reinterpret_cast<__half*>(
+                       __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), lane / PIECES + RUN_ROWS * i)) + lane % PIECES * 8;
+        uint32_t x[COLUMNS];
 #pragma unroll
-        for (int v = 0; v < 32; ++v) x[v] = 0;
-        if (it.tiles > 0) ptx::tmem_ld_32x32b_x32(o_at, x);
+        for (int v = 0; v < COLUMNS; ++v) x[v] = 0;
+        if (it.tiles > 0) load_columns(0, x);
 #pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
+        for (int d = 0; d < D; d += COLUMNS) {
           ptx::tmem_wait_ld();
-          uint32_t z[32];
+          uint32_t z[COLUMNS];
           // (columns of 4-bit values lie in the order in which words of codes come apart: 0, 4, 1, 5, ...)
 #pragma unroll
-          for (int v = 0; v < 32; ++v) z[v] = U4 ? x[(v & 24) + ((v & 7) < 4 ? 2 * (v & 7) : 2 * (v & 7) - 7)] : x[v];
-          uint32_t y[16];
+          for (int v = 0; v < COLUMNS; ++v) z[v] = U4 ? x[(v & 24) + ((v & 7) < 4 ? 2 * (v & 7) : 2 * (v & 7) - 7)] : x[v];
+          uint32_t y[COLUMNS / 2];
 #pragma unroll
-          for (int v = 0; v < 16; ++v) y[v] = pack_halves(__uint_as_float(z[2 * v]) * inv, __uint_as_float(z[2 * v + 1]) * inv);
+          for (int v = 0; v < COLUMNS / 2; ++v) y[v] = pack_halves(__uint_as_float(z[2 * v]) * inv, __uint_as_float(z[2 * v + 1]) * inv);
           if (U4 && part) {  // O as it stands, to be joined
 #pragma unroll
-            for (int v = 0; v < 8; ++v)
+            for (int v = 0; v < COLUMNS / 4; ++v)
               if (live) *reinterpret_cast<uint4*>(part + d + 4 * v) = make_uint4(z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]);
             __syncwarp();
           }
-          if (it.tiles > 0 && d + 32 < D) ptx::tmem_ld_32x32b_x32(o_at + d + 32, x);  // (on its way while these leave)
+          if (it.tiles > 0 && d + COLUMNS < D) load_columns(d + COLUMNS, x);  // (on its way while these leave)
           if (!(U4 && part)) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
+            for (int v = 0; v < PIECES; ++v) {
               if constexpr (!U4) {
 #pragma unroll
                 for (int u = 0; u < 4; ++u) finite[u] = fma_h2(y[4 * v + u], 0u, finite[u]);
@@ -667,13 +678,13 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               ptx::st_shared_v4(stage + lane * T::OUT_PITCH + v * 16, y[4 * v], y[4 * v + 1], y[4 * v + 2], y[4 * v + 3]);
             }
             __syncwarp();
-            uint4 w[4];
+            uint4 w[PIECES];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              ptx::ld_shared_v4(stage + (lane / 4 + 8 * i) * T::OUT_PITCH + (lane & 3) * 16, w[i].x, w[i].y, w[i].z, w[i].w);
+            for (int i = 0; i < PIECES; ++i)
+              ptx::ld_shared_v4(stage + (lane / PIECES + RUN_ROWS * i) * T::OUT_PITCH + lane % PIECES * 16, w[i].x, w[i].y, w[i].z, w[i].w);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (alive >> (lane / 4 + 8 * i) & 1u) *reinterpret_cast<uint4*>(run[i] + d) = w[i];
+            for (int i = 0; i < PIECES; ++i)
+              if (alive >> (lane / PIECES + RUN_ROWS * i) & 1u) *reinterpret_cast<uint4*>(run[i] + d) = w[i];
             __syncwarp();
           }
         }
