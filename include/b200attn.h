@@ -58,8 +58,8 @@ int rotary_fp16(int tokens, int head_dim, int rotary_dim, int pairs, const rotar
  * Scores, softmax statistics and sums are FP32; the softmax weights are rounded to binary16 for the product with V,
  * by 2^-11 of themselves (2^-32 of the row's largest where they are below 2^-21 of it).  The tensor cores' sums cut off what
  * does not fit, up to 2e-9 of the result per token.
- * A token that a query does not see leaves it alone, whatever it holds; one that it sees counts as the formula has it, NaN and
- * infinities included.  (Rows next to hidden values that are not finite are computed one by one, slowly.)
+ * A token that a query does not see leaves it alone, whatever it holds, to the last bit; one that it sees counts as the formula
+ * has it, NaN and infinities included (but an infinite value with a weight below 2^-32 of the row's largest may give a NaN).
  */
 int attention_fp16(int batch, const int* cu, int max_len, int rows, int q_heads, int kv_heads,
                    int head_dim, const void* Q, long long q_token_stride, long long q_head_stride,
