@@ -132,7 +132,7 @@ int kv_attention_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, c
  * K and V are uint8 arrays [num_pages][kv_heads][page_size][head_dim / 2], code d of a token in bits
  * [4 (d & 1), 4 (d & 1) + 4) of byte d >> 1; k_scale and v_scale are pairs of binary16 (scale, offset),
  * [num_pages][kv_heads][page_size][2], 16-byte aligned like the codes.  The value of a code is
- * offset + code * scale; pages, tables, batches and what is done about bad ones are as above.
+ * offset + code * scale, within binary16's range; scales of either sign are read (none below 0 is written); pages, tables, batches and what is done about bad ones are as above.
  */
 typedef struct kv_cache_u4 {
   uint8_t* k;

@@ -1113,7 +1113,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             const float scale_hi = __half2float(__ushort_as_half(static_cast<unsigned short>(high)));
             const float middle = fmaf(8.0f, f.x, f.y);
             // 1.5 2^23 units, a unit 2^-6 of the scale's power of two (of 2^-14 below the normal range)
-            const float round = __uint_as_float((__float_as_uint(fmaxf(scale_hi, 0x1p-14f)) & 0x7f800000u) + (17u << 23) + 0x400000u);
+            const float round = __uint_as_float((__float_as_uint(fmaxf(fabsf(scale_hi), 0x1p-14f)) & 0x7f800000u) + (17u << 23) + 0x400000u);
             const float middle_hi = __half2float(__float2half_rn((middle + round) - round));
             const uint32_t w = kind == 1 ? pack_halves(scale_hi, middle_hi) : pack_halves(f.x - scale_hi, middle - middle_hi);
             of_token[u] = seen(tok) && !not_finite2(mine) ? w : 0u;

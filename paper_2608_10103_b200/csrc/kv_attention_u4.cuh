@@ -4,7 +4,7 @@
 // relative to a running reference m,
 //     t = c (sk (q . K) + ok sum(q)) + log2 sv,   w = 2^(t - m + 7),   u = w / sv,   l = sum u,
 //     O = sum w (V - 8) + sum u (ov + 8 sv),   out = O / l,
-// c = softmax_scale log2 e.  The value scale is folded into the exponent, as in kv_attention.cuh (see there for m, the 2^7 and
+// c = softmax_scale log2 e.  Where sv is negative, 15 - V, -sv and ov + 15 sv stand for V, sv and ov.  The value scale is folded into the exponent, as in kv_attention.cuh (see there for m, the 2^7 and
 // the bits of a weight), so that one accumulator serves tokens of any scale; the offsets are a single sum per row, in FP32.
 // w is rounded to binary16 for the product with V; counting codes from the middle of their range halves what that rounding does,
 // and keeps the sums small: a mean of many tokens is far below its terms, and the MMA's sums cut off what does not fit.
@@ -24,8 +24,8 @@
 //
 // Work split, hand-over and joins are those of kv_attention.cuh, with one row tile per sequence.
 //
-// Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 73.5 us, 3.9 TB/s of the cache; one of 1000 tokens 9.8 us.
-// 16 heads of 64 d, 131071 tokens, 4 queries: 53.8 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
+// Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 74.4 us, 3.9 TB/s of the cache; one of 1000 tokens 9.6 us.
+// 16 heads of 64 d, 131071 tokens, 4 queries: 54.0 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
 // codes meet as many scores, exponentials and factors, the instructions per byte are 1.5 times as many. Four CTAs per SM
 // with rings of three steps at 128 d: 2 % slower than three with four; steps of 64 tokens at 64 d: -2 to +3 %; the scores' arithmetic by pairs
 // of tokens, 7 % fewer instructions: 2 % faster at 64 d, level at 128 d, 9 % slower at 256 d (spills).
@@ -441,20 +441,22 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
         fetch();
         // ---- the tokens' factors, a lane for each.  A token whose scale or offset is not finite: NaN for the rows that see it, nothing
         // (-inf below, which such factors would turn into a NaN) for those that do not.
+        bool down = false;  // the lane's token counts from its maximum
         each<(STEP + 31) / 32>([&](auto part) {
           if (STEP < 32 && lane >= STEP) return;
           const uint32_t k_word = kva4::lds<S_AT + part * 128>(slot + lane * 4), v_word = kva4::lds<S_AT + STEP * 4 + part * 128>(slot + lane * 4);
           auto finite = [](uint32_t w) { return (w & 0x7c00u) != 0x7c00u && (w & 0x7c000000u) != 0x7c000000u; };
           const bool good = finite(k_word) && finite(v_word);
           const float2 k = half2_of(k_word), x = half2_of(good ? v_word : 0x00003c00u);
-          const float sv = kva_value_scale(x.x);
+          const float sv = kva_value_scale(fabsf(x.x));
+          down = x.x < 0.0f;
           const uint32_t to = f_at_warp + part * 256 + (lane >> 1) * 16 + (lane & 1) * 4;
           auto put = [](uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); };
           put(to, good ? k.x : __int_as_float(0x7fffffff));
           put(to + 8, good ? k.y : 0.0f);
           put(to + STEP * 8, __log2f(sv));
           put(to + STEP * 8 + 8, __fdividef(1.0f, sv));
-          put(f_at_warp + STEP * 16 + part * 128 + lane * 4, fmaf(8.0f, x.x, x.y));
+          put(f_at_warp + STEP * 16 + part * 128 + lane * 4, fmaf(x.x < 0.0f ? 7.0f : 8.0f, x.x, x.y));
         });
         // ---- scores: 8 NR rows x STEP tokens, two exact integer sums each; this lane: row g of each
         // group, tokens 8 j + 2t, + 1
@@ -488,6 +490,17 @@ __global__ void __launch_bounds__(KVA_THREADS, kva4_ctas(D, NR)) kv_attention_u4
             for (int v = 0; v < 2; ++v)  // |254 q1 + q2| 15 D <= 32385 * 15 * 256 < 2^31
               sc[n][j][v] = static_cast<float>(sum[n][v] * 254 + sum[n][v + 2]);
         });
+        if (__any_sync(0xffffffffu, down)) {  // (few caches have such tokens)
+          if (down) {
+            const uint32_t row = slot + V_AT + static_cast<uint32_t>((lane >> 3) * 8 * ROW + row_at<D>(lane & 7) * ROW);
+#pragma unroll 1
+            for (int i = 0; i < ROW; i += 16) {
+              uint32_t w[4];
+              ptx::ld_shared_v4(row + i, w[0], w[1], w[2], w[3]);
+              ptx::st_shared_v4(row + i, ~w[0], ~w[1], ~w[2], ~w[3]);
+            }
+          }
+        }
         __syncwarp();
         const int tok0 = lo + st * STEP;
         const uint32_t factors = f_at_warp + t * 16;
