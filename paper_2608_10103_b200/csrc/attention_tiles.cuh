@@ -28,7 +28,8 @@
 // other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies, and warps write the same tiles from them. Keys
 // are their codes, exact in binary16: a score is then scale (q . codes) + offset sum(q), by a table of two factors per token. Values are two
 // tiles, multiplied one after the other: with the scale's first seven bits, and the middle of the range rounded to units of that, a value is
-// exact in binary16; the second tile holds what is left. (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
+// exact in binary16 if the middle is no more than 16 of the scale's powers of two away from zero, as in every row with values of both signs; the second
+// tile holds what is left, and what the first had to round where values lie further away, itself rounded to binary16 (2^-22 of the value). (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
 // results, only values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in
 // kv_attention_u4.cuh, need five factors a token for every row: what shared memory then hands to registers took longer, 340 us against
 // 297.)
@@ -282,6 +283,11 @@ __device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
   return r;
 }
+__device__ __forceinline__ uint32_t add_h2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -302,6 +308,36 @@ __device__ __forceinline__ uint4 value_codes(uint32_t w) {
 // Two binary16 with 0 for what is not finite.
 __device__ __forceinline__ uint32_t finite_or_zero2(uint32_t w) {
   return ((w & 0x7c00u) == 0x7c00u ? 0u : w & 0xffffu) | ((w & 0x7c000000u) == 0x7c000000u ? 0u : w & 0xffff0000u);
+}
+
+// A 4-bit value as two binary16, code - 8 times a factor plus a summand each: the scale's first seven bits and the rest; the middle (code 8)
+// as a multiple of the unit that the former leaves, and the rest.
+struct Value4Parts {
+  float scale_hi, scale_lo, middle_hi, middle_lo;
+  float round;  // 1.5 2^23 units
+  __device__ uint32_t first() const { return kva::pack_halves(scale_hi, middle_hi); }
+  __device__ uint32_t rest() const { return kva::pack_halves(scale_lo, middle_lo); }
+  // Whether the first one may pass the 2^11 units that binary16 holds: 8 x 128 of the code's part and more than 1024 of the middle.
+  __device__ bool far() const { return scale_hi != 0.0f && fabsf(middle_hi) * 0x1.8p13f > round; }
+};
+__device__ __forceinline__ Value4Parts value4_parts(uint32_t scale_offset) {
+  Value4Parts x;
+  const float2 f = kva::half2_of(scale_offset);
+  x.scale_hi = __half2float(__ushort_as_half(static_cast<unsigned short>(scale_offset & 0xfff0u)));
+  x.scale_lo = f.x - x.scale_hi;
+  const float middle = fmaf(8.0f, f.x, f.y);
+  // (a unit is 2^-6 of the scale's power of two, of 2^-14 below the normal range)
+  x.round = __uint_as_float((__float_as_uint(fmaxf(fabsf(x.scale_hi), 0x1p-14f)) & 0x7f800000u) + (17u << 23) + 0x400000u);
+  x.middle_hi = __half2float(__float2half_rn((middle + x.round) - x.round));
+  x.middle_lo = middle - x.middle_hi;
+  return x;
+}
+// The second binary16 of two codes with what rounding took from the first. All of that is exact: the middle and the first one lie within a factor of
+// two of one another where the first was rounded, so that their difference is; with the code's part it is a rounding error, which has few bits.
+__device__ __forceinline__ uint32_t value4_rest(uint32_t codes, uint32_t first_of, uint32_t rest_of) {
+  const uint32_t factor = __byte_perm(first_of, 0, 0x1010), middle = __byte_perm(first_of, 0, 0x3232);
+  const uint32_t lost = fma_h2(codes, factor, sub_h2(middle, fma_h2(codes, factor, middle)));
+  return fma_h2(codes, __byte_perm(rest_of, 0, 0x1010), add_h2(__byte_perm(rest_of, 0, 0x3232), lost));
 }
 
 // Adds what is not finite in the values of tokens [first, last] of the packed arrays, 64 at most, to a row's results. An infinity has a
@@ -1092,6 +1128,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         // (what stands for tokens that no row sees was not loaded or may be anything: zeros)
         auto seen = [&](int tok) { return first + tok < it.hi && first + tok >= it.from; };
         uint32_t of_token[TN / 32];  // V: factor and summand of tokens lane, lane + 32
+        bool far = false;            // of these: the first tile may have had to round
         if (kind == 0) {  // the scores' factors; a NaN for a token whose key or value is not finite
 #pragma unroll
           for (int tok = ct; tok < TN; tok += AT_ONCE) {
@@ -1107,16 +1144,10 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           for (int u = 0; u < TN / 32; ++u) {
             const int tok = lane + 32 * u;
             const uint32_t mine = scales[2 * TN + tok];
-            // The scale's first seven bits and the rest; the middle (code 8) as a multiple of the unit that the former leaves, and the rest.
-            const uint32_t high = mine & 0xfff0u;
-            const float2 f = half2_of(mine);
-            const float scale_hi = __half2float(__ushort_as_half(static_cast<unsigned short>(high)));
-            const float middle = fmaf(8.0f, f.x, f.y);
-            // 1.5 2^23 units, a unit 2^-6 of the scale's power of two (of 2^-14 below the normal range)
-            const float round = __uint_as_float((__float_as_uint(fmaxf(fabsf(scale_hi), 0x1p-14f)) & 0x7f800000u) + (17u << 23) + 0x400000u);
-            const float middle_hi = __half2float(__float2half_rn((middle + round) - round));
-            const uint32_t w = kind == 1 ? pack_halves(scale_hi, middle_hi) : pack_halves(f.x - scale_hi, middle - middle_hi);
+            const Value4Parts x = value4_parts(mine);
+            const uint32_t w = kind == 1 ? x.first() : x.rest();
             of_token[u] = seen(tok) && !not_finite2(mine) ? w : 0u;
+            if (of_token[u] != 0 && x.far()) far = true;
           }
         }
 #pragma unroll 4
@@ -1142,6 +1173,25 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
               const uint4 x = value_codes(w[v]);
               ptx::st_shared_v4(at + (((static_cast<uint32_t>((piece & 1) * 4 + v)) ^ sw) << 4), fma_h2(x.x, factor, summand),
                                 fma_h2(x.y, factor, summand), fma_h2(x.z, factor, summand), fma_h2(x.w, factor, summand));
+            }
+          }
+        }
+        if (kind == 2 && __any_sync(0xffffffffu, far)) {  // values far from zero for their range: the same once more, with what was rounded
+#pragma unroll 1
+          for (int u = 0; u < N; ++u) {
+            const int tok = u * (AT_ONCE / PER_TOKEN) + t0;
+            const uint32_t mine = scales[2 * TN + tok];
+            const bool good = seen(tok) && !not_finite2(mine);
+            const Value4Parts x = value4_parts(mine);
+            const uint32_t first_of = good ? x.first() : 0u, rest_of = good ? x.rest() : 0u;
+#pragma unroll 1
+            for (int v = 0; v < 4; ++v) {
+              uint32_t w;
+              asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(codes + tok * (D / 2) + v * 4) : "memory");
+              const uint4 c = value_codes(w);
+              ptx::st_shared_v4(to + static_cast<uint32_t>(tok * 128) + ((static_cast<uint32_t>((piece & 1) * 4 + v) ^ static_cast<uint32_t>(tok & 7)) << 4),
+                                value4_rest(c.x, first_of, rest_of), value4_rest(c.y, first_of, rest_of),
+                                value4_rest(c.z, first_of, rest_of), value4_rest(c.w, first_of, rest_of));
             }
           }
         }
