@@ -83,6 +83,11 @@ int integer(PyObject* o, const char* what) {
   if (v == -1 && !overflow && PyErr_Occurred()) throw Raised{};
   return narrow(overflow ? INT64_MAX : v, what);
 }
+int truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw Raised{};
+  return v;
+}
 float number(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw Raised{};
@@ -422,7 +427,7 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k.tokens != q.tokens) throw Refused{PyExc_ValueError, "q, k and v must have the same tokens"};
     const int* const cu = static_cast<const int*>(dense(a[3], at::kInt, "cu"));
     const int batch = narrow(THPVariable_Unpack(a[3]).numel() - 1, "batch");
-    const int max_len = integer(a[4], "max_len"), causal = PyObject_IsTrue(a[6]), window = integer(a[7], "window");
+    const int max_len = integer(a[4], "max_len"), causal = truth(a[6]), window = integer(a[7], "window");
     const float scale = number(a[5]);
     const Launch s = stream_of(a[9]);
     at::Tensor out;
