@@ -67,6 +67,11 @@ constexpr float KVA_WEIGHT_BITS = 7.0f;
 // weight must stay in FP32.  127 * 2^-40 = 1.2e-10 is nothing to a binary16 result (multiples of 6e-8).
 __device__ __forceinline__ float kva_value_scale(float sv) { return sv < 0x1p-40f ? 0x1p-40f : sv; }
 
+// Whether a page's scale is not finite or below 0 (its sign would turn the -inf of hidden tokens round, and has no logarithm).
+__device__ __forceinline__ bool kva_no_scales(float sk, float sv) {
+  return !(sk >= 0.0f && sk < INFINITY && sv >= 0.0f && sv < INFINITY);
+}
+
 struct KvAttnParams {
   KvCacheView c;
   int batch;
@@ -595,9 +600,9 @@ __global__ void __launch_bounds__(KVA_THREADS, kva_ctas(D, NR)) kv_attention_ker
               kk[sub] = 0.0f;
               sv = 1.0f;
             }
-            // A page whose scale is not finite: NaN for the rows that see it, nothing (-inf below, which such factors
+            // A page whose scale is no scale: NaN for the rows that see it, nothing (-inf below, which such factors
             // would turn into a NaN) for those that do not.
-            if (!(fabsf(kk[sub]) < INFINITY && fabsf(sv) < INFINITY)) {
+            if (kva_no_scales(kk[sub], sv)) {
               kk[sub] = sv = 1.0f;
 #pragma unroll
               for (int n = 0; n < NR; ++n)

@@ -8,8 +8,8 @@
 // K and V arrive as int8, by bulk copies of whole pages of a head; four warps convert them
 // exactly to binary16 and write them as rows of 64 d in the 128-byte swizzle.  Such a tile is K-major for the
 // first product and, read the other way round, MN-major for the second: no transpose anywhere.
-// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own;
-// A page whose scale is not finite gets harmless factors and raises a flag: the rows then look through the pages
+// Page scales: a table of (c sk, log2 sv, 1 / sv) per 16 tokens, in a ring of its own.
+// A page whose scale is not finite or below 0 gets harmless factors and raises a flag: the rows then look through the pages
 // that they see themselves, at the end, and become NaN by their l (a test per tile of tokens costs 2 %).
 //
 // What bounds it: at 128 d, 1024 cycles of tensor pipe a tile pair of 128 x 128 against as many of exponentials
@@ -163,8 +163,6 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
   volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(base_ptr + T::MISC_OFFSET);
   volatile uint32_t* const abort_flag = tmem_holder + 1;
   volatile uint32_t* const poison_flag = tmem_holder + 2;  // a page of this CTA's tokens has a scale that is not finite
-  auto not_finite = [](float sk, float sv) { return !(fabsf(sk) < INFINITY && fabsf(sv) < INFINITY); };
-
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 31, warp = tid >> 5;
   if (tid == 0) ptx::grid_dep_launch_dependents();
 
@@ -410,7 +408,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           const int id = kv_ld(table + (t >> p.c.page_shift));
           if (id < 0 || id >= p.c.num_pages) continue;
           const long long ph = static_cast<long long>(id) * heads + head;
-          if (not_finite(ptx::ld_global_f32(p.c.scales[0] + ph), ptx::ld_global_f32(p.c.scales[1] + ph)))
+          if (kva_no_scales(ptx::ld_global_f32(p.c.scales[0] + ph), ptx::ld_global_f32(p.c.scales[1] + ph)))
             l = __int_as_float(0x7fffffff);
         }
       }
@@ -550,7 +548,7 @@ kv_attention_tiles_kernel(const __grid_constant__ KvAttnParams p) {
           // scales by groups of 16 tokens (a hidden token's -inf must stay one)
           const float v = kva_value_scale(sv), k = p.scale_log2 * sk;
           float4 c = make_float4(k == 0.0f ? 1e-30f : k, __log2f(v), __fdividef(1.0f, v), 0.0f);
-          if (not_finite(sk, sv)) {
+          if (kva_no_scales(sk, sv)) {
             c = make_float4(1e-30f, 0.0f, 1.0f, 0.0f);
             *poison_flag = 1;
           }
