@@ -57,7 +57,8 @@ int rotary_fp16(int tokens, int head_dim, int rotary_dim, int pairs, const rotar
  * sequence are left as they are.  K and V have one common pair of strides; heads of a row of out are dense.
  * Scores, softmax statistics and sums are FP32; the softmax weights are rounded to binary16 for the product with V,
  * by 2^-11 of themselves (2^-32 of the row's largest where they are below 2^-21 of it).  The tensor cores' sums cut off what
- * does not fit, up to 2e-9 of the result per token.
+ * does not fit, up to 2^-27 of the sum a token; a sum takes 16384 tokens at most (1.2e-4), and longer ones go on from its parts.
+ * out, which holds such parts while the call runs, overlaps no input.
  * A token that a query does not see leaves it alone, whatever it holds, to the last bit; one that it sees counts as the formula
  * has it, NaN and infinities included (but an infinite value with a weight below 2^-32 of the row's largest may give a NaN).
  */

@@ -99,7 +99,7 @@ int kv_read_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, const 
  * out, row * q_token_stride + head * q_head_stride + d for Q.  max_q: an upper bound of n
  * over the batch (rows beyond it are not computed, status 6).
  * Scores, softmax statistics and sums are FP32.  The tensor cores' sums of weighted values cut
- * off what does not fit, up to 2e-9 of the result per token of one sum: 16384 tokens at most, or for
+ * off what does not fit, up to 2^-27 of the sum a token: 16384 tokens at most (1.2e-4), or for
  * sequences of few rows (below) up to a quarter of the sequence.  Two operands have fewer bits:
  *   - the softmax weights (times their page's value scale) are rounded to binary16 for the
  *     product with the codes, which are exact there: by 2^-11 of themselves, or up to 2^-32 of
@@ -167,7 +167,8 @@ int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* 
  * or offset (of K or of V) is not finite gives NaN, as does one that holds a NaN or an infinity itself; tokens that it
  * does not see leave it alone.
  * Scores, softmax statistics and sums are FP32, and the softmax weights are rounded as for kv_attention_s8.
- * The tensor cores' sums cut off what does not fit, up to 2e-9 of the result per token of one sum.
+ * The tensor cores' sums cut off what does not fit, up to 2^-27 of the sum a token, and take 16384 tokens at most (1.2e-4), or for
+ * sequences of few rows up to a quarter of the sequence; longer ones go on from their parts, which out holds while the call runs.
  */
 int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,
                     const int* block_table, int table_stride, int max_q, int q_heads,

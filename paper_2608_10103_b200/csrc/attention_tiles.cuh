@@ -45,9 +45,12 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "bounded_wait.cuh"
 #include "kv_attention.cuh"
 #include "kv_common.cuh"
+#include "kv_host.cuh"
 #include "ptx.cuh"
 
 namespace b200gemm {
@@ -85,6 +88,9 @@ struct AttnTileShape {
   static constexpr int QT = D <= 128 ? 2 : 1;    // row tiles of 128 per CTA
   static constexpr int TN = 64;                  // tokens per tile
   static constexpr int ROWS = 128 * QT;
+  // Tiles of tokens that O takes up before it is split, see split_sums: 16384 tokens, in which 1e-4 of a result can be lost (8192 tokens: 5e-5, and
+  // 1024 queries over 65536 tokens in 4 bits 1740 us instead of 1710; without it 1690).
+  static constexpr int SUM_TILES = 16384 / TN;
   static constexpr int SOFTMAX_WARPS = 4 * QT;
   static constexpr int CONVERT_WARPS = U4 ? 12 : 0;
   // Warps that expand one tile of K or V together.  What a tile costs a warp is mostly waiting, so that several tiles are worked on
@@ -340,6 +346,35 @@ __device__ __forceinline__ uint32_t value4_rest(uint32_t codes, uint32_t first_o
   return fma_h2(codes, __byte_perm(rest_of, 0, 0x1010), add_h2(__byte_perm(rest_of, 0, 0x3232), lost));
 }
 
+// Long sums. An instruction of 16 tokens cuts off up to two units of 2^-24 of what an accumulator holds, always towards zero: 131072 tokens of one
+// sign in one sum lose 8.3e-4 of the result, more than its rounding to binary16. So a row's sums are split every 16384 tokens: their first eleven bits
+// are put by as binary16, where the row's results will be (no scratch, and nothing shared), the rest stays and the sum goes on from there. The parts are
+// exact. At the end they come together again.
+// o: eight columns; held: what was put by, `factor` a unit of it; unit: of what is put by now, a power of two above the row's sum of weights; 0: the end.
+__device__ __forceinline__ void split_sums(uint32_t* o, uint4* held, float factor, float unit) {
+  uint32_t w[4] = {0, 0, 0, 0};
+  if (factor != 0.0f) {
+    const uint4 old = *held;
+    w[0] = old.x; w[1] = old.y; w[2] = old.z; w[3] = old.w;
+  }
+  const float per = unit == 0.0f ? 0.0f : __uint_as_float(0x7f000000u - __float_as_uint(unit));
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float2 old = kva::half2_of(w[u]);
+    const float a = fmaf(old.x, factor, __uint_as_float(o[2 * u])), b = fmaf(old.y, factor, __uint_as_float(o[2 * u + 1]));
+    o[2 * u] = __float_as_uint(a);
+    o[2 * u + 1] = __float_as_uint(b);
+    if (unit != 0.0f) {
+      w[u] = kva::pack_halves(a * per, b * per);
+      const float2 now = kva::half2_of(w[u]);
+      // (an infinity is put by as a whole)
+      o[2 * u] = fabsf(now.x) < INFINITY ? __float_as_uint(fmaf(-now.x, unit, a)) : 0u;
+      o[2 * u + 1] = fabsf(now.y) < INFINITY ? __float_as_uint(fmaf(-now.y, unit, b)) : 0u;
+    }
+  }
+  if (unit != 0.0f) *held = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Adds what is not finite in the values of tokens [first, last] of the packed arrays, 64 at most, to a row's results. An infinity has a
 // weight above 0, however small, unless the row's score of it is -inf, which makes the product a NaN.
 template <int D>
@@ -401,7 +436,9 @@ __device__ __noinline__ void add_not_finite(const AttnTilesParams& p, int row, i
 
 }  // namespace attn
 
-template <int D, bool U4>
+// LONG: rows may see more than SUM_TILES tiles. (Calls whose bounds exclude it go without: over 4-bit pages the code for it takes
+// 3 % by itself, 1640 -> 1690 us.)
+template <int D, bool U4, bool LONG>
 __global__ void __launch_bounds__(AttnTileShape<D, U4>::THREADS, 1)
 attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                        const __grid_constant__ CUtensorMap v_map, const __grid_constant__ AttnTilesParams p) {
@@ -493,6 +530,11 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
                      p.causal ? it.base + it.query : it.base + it.n - 1);
   };
 
+  // A row's part of its results, where its tokens are divided: [D] sums, maximum, sum of weights.
+  [[maybe_unused]] auto part_of = [&](const AttnItem& it, int row) {
+    return p.partial + ((static_cast<long long>(it.unit) * p.splits + it.split) * T::ROWS + row) * (D + 4);
+  };
+
   if constexpr (U4) {  // register shares: 256 x 128 + 512 x 56 of the 768 x 80 that the block was launched with, or 128 x 168 + 512 x 72 of 640 x 96
     if (warp < T::SOFTMAX_WARPS) {
       if constexpr (QT == 2)
@@ -557,7 +599,10 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           q_sum2 = pair(sum, sum);
         }
 #pragma unroll 1
-        for (int j = 0; j < it.tiles; ++j, ++done) {
+        for (int j = 0; ok && j < it.tiles;) {
+        const int end = LONG ? min(it.tiles, j + T::SUM_TILES) : it.tiles;
+#pragma unroll 1
+        for (; j < end; ++j, ++done) {
           const int sb = 2 * q + (done & 1);  // score buffer
           const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(sb * TN);
           ok = wait_bounded(s_full(sb), (done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
@@ -666,7 +711,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
             }
           }
           ptx::tmem_wait_st();
-          if (j > 0 && j == it.tiles - 1) {
+          if (j > 0 && j == end - 1) {
             // A barrier tells a phase from the one before or behind it only.  That S was there says that the products of the tile before
             // the last are done (they were issued earlier, by the same thread); the last one's are seen to here, in front of this one's,
             // so that the wait for these, below, is not taken in by them.
@@ -680,6 +725,41 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
           const float2 total = unpair(add2(sum[0], sum[1]));
           l += total.x + total.y;
         }
+        if (!LONG || !ok || it.tiles <= T::SUM_TILES) break;
+        // ---- long sums
+        ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        ptx::tc_fence_after_sync();
+        const bool parts = U4 && it.split >= 0;
+        __half* const mine = parts ? reinterpret_cast<__half*>(part_of(it, q * 128 + r)) + D
+                                   : p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
+        // (all rows have a place: eight columns of 32 rows side by side, or every access is to 32 lines)
+        const bool dense = __all_sync(0xffffffffu, parts || live);
+        // log2 of the unit of what was put by, with the reference of that time: in the row's place for results on their way out, which is free here
+        const uint32_t held_at = base + T::OUT_OFFSET + static_cast<uint32_t>((warp * 32 + lane) * T::OUT_PITCH);
+        float held = -INFINITY;
+        if (j > T::SUM_TILES) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(held) : "r"(held_at) : "memory");
+        const float factor = held == -INFINITY ? 0.0f : exp2_approx(held - m);
+        const float unit = j == it.tiles ? 0.0f : l > 0.0f && l < 0x1p100f ? __uint_as_float((__float_as_uint(l) & 0x7f800000u) + 0x1000000u) : 1.0f;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t y[16];
+          ptx::tmem_ld_32x32b_x16(o_at + d, y);
+          ptx::tmem_wait_ld();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int piece = (d / 8 + h) * 32 + lane;
+            __half* const there = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), piece / (D / 8))) + piece % (D / 8) * 8;
+            if (dense || live) split_sums(y + 8 * h, reinterpret_cast<uint4*>(dense ? there : mine + d + 8 * h), factor, unit);
+          }
+          __syncwarp();
+          ptx::tmem_st_32x32b_x16(o_at + d, y);
+        }
+        ptx::tmem_wait_st();
+        held = m + (static_cast<float>(__float_as_uint(unit) >> 23) - 127.0f);
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(held_at), "f"(held) : "memory");
+        }
         if (!ok) break;
         // ---- the rows' results
         if (it.tiles > 0) {
@@ -691,9 +771,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         // (a row that sees a token has l > 0, or NaN; or all its scores are -inf, which makes it NaN)
         if (l == 0.0f && pos >= max(from, 0) && it.split < 0) l = __int_as_float(0x7fffffff);
         const float inv = l == 0.0f ? 0.0f : __fdividef(1.0f, l);
-        float* const part = U4 && it.split >= 0
-                                ? p.partial + ((static_cast<long long>(it.unit) * p.splits + it.split) * T::ROWS + q * 128 + r) * (D + 4)
-                                : nullptr;
+        float* const part = U4 && it.split >= 0 ? part_of(it, q * 128 + r) : nullptr;
         if (U4 && part && live) *reinterpret_cast<float2*>(part + D) = make_float2(m, l);
         __half* const dst = p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
         const unsigned alive = __ballot_sync(0xffffffffu, live);
@@ -1213,6 +1291,19 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     ptx::tc_fence_after_sync();
     ptx::tmem_dealloc<1>(tmem, 512);
   }
+}
+
+// longest: what a row may see at most.
+template <int D, bool U4>
+int launch_attention_tiles(const SharedDevice& dev, int longest, int grid, cudaStream_t stream, const CUtensorMap& q, const CUtensorMap& k,
+                           const CUtensorMap& v, const AttnTilesParams& p) {
+  using T = AttnTileShape<D, U4>;
+  auto with = [&](auto is_long) {
+    constexpr auto kernel = attention_tiles_kernel<D, U4, decltype(is_long)::value>;
+    const int rc = allow_smem<kernel>(dev, T::DYN_BYTES);
+    return rc != GEMM_OK ? rc : launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, k, v, p);
+  };
+  return longest > T::SUM_TILES * T::TN ? with(std::true_type{}) : with(std::false_type{});
 }
 
 }  // namespace b200gemm

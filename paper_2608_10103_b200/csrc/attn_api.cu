@@ -27,14 +27,7 @@ int check_rotary_rows(const rotary_rows_t& r, int least) {
 
 template <int D>
 int launch_prompts(const SharedDevice& dev, AttnTilesParams& p, cudaStream_t stream) {
-  static std::atomic<bool> ready[MAX_DEV];
   using T = AttnTileShape<D, false>;
-  auto kernel = attention_tiles_kernel<D, false>;
-  if (!ready[dev.device].load()) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::DYN_BYTES);
-    if (e != cudaSuccess) return shared_cuda_fail(e);
-    ready[dev.device].store(true);
-  }
   const int per_tile = 128 / p.group, per_cta = T::QT * per_tile;
   const int longest = p.max_q < p.rows ? p.max_q : p.rows;
   // row tiles: one more a sequence than its rows would fill, and no more than the longest allows
@@ -49,7 +42,7 @@ int launch_prompts(const SharedDevice& dev, AttnTilesParams& p, cudaStream_t str
   if (rc == GEMM_OK) rc = shared_row_map(&v, p.v, D, p.heads, p.rows, p.kv_token_stride, p.kv_head_stride, 1, T::TN);
   if (rc != GEMM_OK) return rc;
   const int grid = items < dev.num_sms ? static_cast<int>(items) : dev.num_sms;
-  return launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, k, v, p);
+  return launch_attention_tiles<D, false>(dev, longest, grid, stream, q, k, v, p);
 }
 
 }  // namespace

@@ -45,14 +45,7 @@ int blocks_of(int max_rows, int tokens, int batch, int* per_seq) {
 // Sequences with more than p.split_rows rows, on the tensor cores.
 template <int D>
 int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream) {
-  static std::atomic<bool> ready[MAX_DEV];
   using T = AttnTileShape<D, true>;
-  auto kernel = attention_tiles_kernel<D, true>;
-  if (!ready[dev.device].load()) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::DYN_BYTES);
-    if (e != cudaSuccess) return shared_cuda_fail(e);
-    ready[dev.device].store(true);
-  }
   const int per_tile = 128 / p.group, per_cta = T::QT * per_tile;
   const int longest = p.max_q < p.rows ? p.max_q : p.rows;
   // row tiles: one more a sequence than its rows would fill, and no more than the longest allows
@@ -75,14 +68,14 @@ int launch_tiles(const SharedDevice& dev, AttnTilesParams p, cudaStream_t stream
   }
   const long long items = units * p.splits;
   const int grid = items < dev.num_sms ? static_cast<int>(items) : dev.num_sms;
-  if (p.splits == 1) return launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, q, q, p);
+  if (p.splits == 1) return launch_attention_tiles<D, true>(dev, p.max_len, grid, stream, q, q, q, p);
   SharedLease lease;
   rc = shared_scratch(dev.device, stream, static_cast<size_t>(items) * T::ROWS * (D + 4) * 4,
                       (static_cast<size_t>(units) * 4 + 255) / 256 * 256, &lease);
   if (rc != GEMM_OK) return rc;
   p.arrived = static_cast<unsigned*>(lease.head);
   p.partial = static_cast<float*>(lease.data);
-  rc = launch(dev, kernel, dim3(grid), T::THREADS, T::DYN_BYTES, stream, q, q, q, p);
+  rc = launch_attention_tiles<D, true>(dev, p.max_len, grid, stream, q, q, q, p);
   const int done = shared_scratch_done(dev.device, stream, lease);
   return rc != GEMM_OK ? rc : done;
 }

@@ -62,7 +62,7 @@ struct KvTileShape {
   static constexpr int DYN_BYTES = MISC_OFFSET + 16 + 1024;
   static constexpr uint32_t O_COLUMN = 256;        // S (and P) of tile q at 128 q, O behind both
   // O is summed in tensor memory over this many tiles of tokens at most, 16384 tokens: the accumulator cuts off what does
-  // not fit, 1e-9 to 2e-9 of the result a token, all with one sign (131072 tokens in one sum: 1.3e-4 to 2.8e-4, as much
+  // not fit, 1e-9 to 2e-9 of the result a token (6.4e-9 with values of one sign), always towards zero (131072 tokens in one sum: 1.3e-4 to 2.8e-4, as much
   // as the rounding to binary16).  Then the rows' threads add it to a sum in scratch.
   static constexpr int SUM_TILES = 16384 / TN;
   static_assert(DYN_BYTES <= 232448, "exceeds the 227 KB shared-memory limit per CTA");

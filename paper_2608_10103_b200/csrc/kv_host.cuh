@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "../../include/b200gemm.h"
 #include "kv_common.cuh"
 #include "shared_state.h"
@@ -45,6 +47,17 @@ int launch(const SharedDevice& dev, Kernel kernel, dim3 grid, int threads, size_
   cfg.numAttrs = dev.plain_order ? 0 : 1;
   const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p...);
   return e == cudaSuccess ? GEMM_OK : shared_cuda_fail(e);
+}
+
+// Dynamic shared memory beyond 48 KB, once per kernel and device.
+template <auto Kernel>
+int allow_smem(const SharedDevice& dev, int bytes) {
+  static std::atomic<bool> ready[MAX_DEV];
+  if (ready[dev.device].load()) return GEMM_OK;
+  const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return shared_cuda_fail(e);
+  ready[dev.device].store(true);
+  return GEMM_OK;
 }
 
 }  // namespace
