@@ -132,7 +132,8 @@ int kv_attention_s8_rows(const kv_cache_s8_t* cache, int batch, const int* cu, c
  * K and V are uint8 arrays [num_pages][kv_heads][page_size][head_dim / 2], code d of a token in bits
  * [4 (d & 1), 4 (d & 1) + 4) of byte d >> 1; k_scale and v_scale are pairs of binary16 (scale, offset),
  * [num_pages][kv_heads][page_size][2], 16-byte aligned like the codes.  The value of a code is
- * offset + code * scale, within binary16's range; scales of either sign are read (none below 0 is written); pages, tables, batches and what is done about bad ones are as above.
+ * offset + code * scale, within binary16's range; scales of either sign are read (none below 0 is
+ * written).  Pages, tables, batches and what is done about bad ones are as above.
  */
 typedef struct kv_cache_u4 {
   uint8_t* k;
@@ -166,9 +167,17 @@ int kv_read_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* 
  * Attention over it, as kv_attention_s8_rows; q_heads / kv_heads: up to 128.  A query that sees a token whose scale
  * or offset (of K or of V) is not finite gives NaN, as does one that holds a NaN or an infinity itself; tokens that it
  * does not see leave it alone.
- * Scores, softmax statistics and sums are FP32, and the softmax weights are rounded as for kv_attention_s8.
- * The tensor cores' sums cut off what does not fit, up to 2^-27 of the sum a token, and take 16384 tokens at most (1.2e-4), or for
- * sequences of few rows up to a quarter of the sequence; longer ones go on from their parts, which out holds while the call runs.
+ * Scores, softmax statistics and sums are FP32.  The tensor cores' sums cut off what does not fit, up to 2^-27 of the
+ * sum a token, and take 16384 tokens at most (1.2e-4), or for sequences of few rows up to a quarter of the sequence; longer
+ * ones go on from their parts, which out holds while the call runs: it overlaps no input.  Operands with fewer bits:
+ *   - the softmax weights, as for kv_attention_s8 (in sequences of few rows times their token's value scale);
+ *   - sequences of up to 16 rows (n * q_heads / kv_heads) are scored on the integer codes, with Q in fixed point of 16 bits as
+ *     there: a value is off by up to max|q| / 64516 of its row.  Longer ones take Q as it is;
+ *   - values are exact in sequences of few rows (codes, and a sum of offsets in FP32), and within 2^-22 of themselves in
+ *     longer ones, as two binary16.
+ * So what a token gets depends, within these bounds, on how many come with it.
+ * GEMM_ERR_TOO_LARGE: batch * kv_heads * (tokens a row of the table can name / 32 + 9) of 2^30 or more (/ 16 for head_dim 256),
+ * or max_q * q_heads / kv_heads near 2^31.
  */
 int kv_attention_u4(const kv_cache_u4_t* cache, int batch, const int* cu, const int* kv_len,
                     const int* block_table, int table_stride, int max_q, int q_heads,

@@ -20,19 +20,21 @@
 // early; no faster: an eighth to half of the exponentials as polynomials, waits that spin. What would help is a pair of CTAs per pair of
 // row tiles (cta_group::2), which leaves each tensor memory for two buffers of 128 scores: not built.
 // A row tile's end, some 5000 cycles of which 2900 are its results' way out, is a sixth of a prompt of 1000 tokens.
-// Measured: 8192 tokens, 32 heads on 8, 453 us (0.72 of the time that the operations take at the cuBLAS bf16 rate); 12 prompts of
-// up to 2048 tokens 163 us; 4096 tokens of 256 d 262 us. 2 x 1024 queries over up to 8192 tokens in 4 bits 283 us: some 2700 cycles per 64
-// tokens. There the products are 2 x (512 + 512), the expansion of codes takes as long, and both want the same shared memory.
+// Measured, a few launches back to back: 8192 tokens, 32 heads on 8, 455 us (0.71 of the cuBLAS bf16 rate); 12 prompts of up to 2048 tokens
+// 165 us; 4096 tokens of 256 d 265 us. In longer runs, and call by call with everything out of L2, the first two take 521 us (0.62) and 192: the
+// clocks go down under the power limit, and 12 prompts' operands come from memory. 2 x 1024 queries over up to 8192 tokens in 4 bits 277-281 us, call
+// by call 286: some 2700 cycles per 64 tokens. There the products are 2 x (512 + 512), the expansion of codes takes as long, and both want the
+// same shared memory.
 //
 // Keys and values in binary16 come by tensor maps straight into the 128-byte swizzle: K-major for the first product and, read the
 // other way round, MN-major for the second. Pages of 4-bit codes come by bulk copies, and warps write the same tiles from them. Keys
 // are their codes, exact in binary16: a score is then scale (q . codes) + offset sum(q), by a table of two factors per token. Values are two
 // tiles, multiplied one after the other: with the scale's first seven bits, and the middle of the range rounded to units of that, a value is
 // exact in binary16 if the middle is no more than 16 of the scale's powers of two away from zero, as in every row with values of both signs; the second
-// tile holds what is left, and what the first had to round where values lie further away, itself rounded to binary16 (2^-22 of the value). (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact
-// results, only values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in
-// kv_attention_u4.cuh, need five factors a token for every row: what shared memory then hands to registers took longer, 340 us against
-// 297.)
+// tile holds what is left, and what the first had to round where values lie further away, itself rounded to binary16 (2^-22 of the value; a tile is
+// written twice then: 273 -> 373 us if all are such). (Keys and values rounded to binary16 once are 6e-4 of their norm away from the exact results, only
+// values so 3.5e-4, this 2.5e-4; the rounded exact ones are 2e-4. Value scales folded into the weights, as in kv_attention_u4.cuh, need five
+// factors a token for every row: what shared memory then hands to registers took longer, 340 us against 297.)
 //
 // What a masked place holds must not matter, but weight 0 times an infinity is NaN. A 4-bit token whose scale or
 // offset is not finite gets zeros for values and a NaN for the scores' factor: NaN for the rows that see it, nothing for those that mask it.
@@ -174,7 +176,8 @@ struct AttnOrder {
   __device__ int tiles_of(const KvSeq& s) const {
     return static_cast<long long>(s.n) * p.group <= p.split_rows ? 0 : (s.n + queries - 1) / queries;
   }
-  // row tiles of a sequence that are at least x token tiles long: their last query sees beyond (x - 1) TN
+  // Row tiles of a sequence that are at least x token tiles long: their last query sees beyond (x - 1) TN. A window is left out of
+  // account: with one, the order is by position, and lengths are much alike but for a sequence's first tiles.
   __device__ int long_tiles(const KvSeq& s, int x) const {
     const int count = tiles_of(s);
     if (x <= 0) return count;

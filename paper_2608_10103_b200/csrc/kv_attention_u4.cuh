@@ -4,8 +4,9 @@
 // relative to a running reference m,
 //     t = c (sk (q . K) + ok sum(q)) + log2 sv,   w = 2^(t - m + 7),   u = w / sv,   l = sum u,
 //     O = sum w (V - 8) + sum u (ov + 8 sv),   out = O / l,
-// c = softmax_scale log2 e.  Where sv is negative, 15 - V, -sv and ov + 15 sv stand for V, sv and ov.  The value scale is folded into the exponent, as in kv_attention.cuh (see there for m, the 2^7 and
-// the bits of a weight), so that one accumulator serves tokens of any scale; the offsets are a single sum per row, in FP32.
+// c = softmax_scale log2 e.  Where sv is negative, 15 - V, -sv and ov + 15 sv stand for V, sv and ov.  The value scale is folded into
+// the exponent, as in kv_attention.cuh (see there for m, the 2^7 and the bits of a weight), so that one accumulator serves tokens of any
+// scale; the offsets are a single sum per row, in FP32.
 // w is rounded to binary16 for the product with V; counting codes from the middle of their range halves what that rounding does,
 // and keeps the sums small: a mean of many tokens is far below its terms, and the MMA's sums cut off what does not fit.
 //
@@ -24,8 +25,8 @@
 //
 // Work split, hand-over and joins are those of kv_attention.cuh, with one row tile per sequence.
 //
-// Measured (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 74.4 us, 3.9 TB/s of the cache; one of 1000 tokens 9.6 us.
-// 16 heads of 64 d, 131071 tokens, 4 queries: 54.0 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
+// Measured, back to back (32 heads on 8 KV heads, 128 d): 64 sequences of up to 8192 tokens 74.4 us, 3.9 TB/s of the cache (call by
+// call with everything out of L2 77 us); one of 1000 tokens 9.6 us. 16 heads of 64 d, 131071 tokens, 4 queries: 54.0 us, 2.8 TB/s. 0.6 of the issue slots are busy at 128 d; at 64 d, where half the
 // codes meet as many scores, exponentials and factors, the instructions per byte are 1.5 times as many. Four CTAs per SM
 // with rings of three steps at 128 d: 2 % slower than three with four; steps of 64 tokens at 64 d: -2 to +3 %; the scores' arithmetic by pairs
 // of tokens, 7 % fewer instructions: 2 % faster at 64 d, level at 128 d, 9 % slower at 256 d (spills).
