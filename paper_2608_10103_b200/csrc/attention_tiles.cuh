@@ -200,30 +200,41 @@ struct AttnOrder {
     longest = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(longest)));
     all = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(all)));
   }
-  // (sequence, row tile) of a rank below `all`
-  __device__ int2 at(int rank) const {
+  // Where the last rank was: row tiles of x_lo token tiles (between x_lo and x_hi there are none), `beyond` of all sequences are longer, `upto`
+  // that long or longer, `passed` of that length belong to sequences in front of `block`.
+  int x_lo = 0, x_hi = 0, beyond = 0, upto = 0, block = 0, passed = 0;
+  // (sequence, row tile) of a rank below `all`, none of them below the one before: looks on from there, as a search over all sequences for every rank
+  // would take the square of their number (16384 sequences of 3 tokens: 84 ms).
+  __device__ int2 at(int rank) {
     const int lane = static_cast<int>(threadIdx.x) & 31;
     if (p.batch == 1) return make_int2(0, all - 1 - rank);
-    int x_lo = 0, x_hi = longest + 1, beyond = 0;  // more than rank tiles are x_lo long, `beyond` <= rank are x_hi long
+    if (rank >= upto) {
+      x_hi = upto == 0 ? longest + 1 : x_lo;
+      beyond = upto;
+      x_lo = 0;
+      upto = all;
 #pragma unroll 1
-    while (x_hi - x_lo > 1) {
-      const int mid = (x_lo + x_hi) / 2;
-      int c = 0;
-      for (int i = lane; i < p.batch; i += 32) c += long_tiles(seq(i), mid);
-      c = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
-      if (c > rank) {
-        x_lo = mid;
-      } else {
-        x_hi = mid;
-        beyond = c;
+      while (x_hi - x_lo > 1) {  // more than rank tiles are x_lo long, `beyond` <= rank are x_hi long
+        const int mid = (x_lo + x_hi) / 2;
+        int c = 0;
+        for (int i = lane; i < p.batch; i += 32) c += long_tiles(seq(i), mid);
+        c = static_cast<int>(__reduce_add_sync(0xffffffffu, static_cast<unsigned>(c)));
+        if (c > rank) {
+          x_lo = mid;
+          upto = c;
+        } else {
+          x_hi = mid;
+          beyond = c;
+        }
       }
+      block = passed = 0;
     }
-    int left = rank - beyond;  // among the tiles of exactly that length, by sequence
+    int left = rank - beyond - passed;  // among the tiles of exactly that length, by sequence
 #pragma unroll 1
-    for (int i0 = 0; i0 < p.batch; i0 += 32) {
+    for (; block < p.batch; block += 32) {
       int same = 0, qt = 0;
-      if (i0 + lane < p.batch) {
-        const KvSeq s = seq(i0 + lane);
+      if (block + lane < p.batch) {
+        const KvSeq s = seq(block + lane);
         const int longer = long_tiles(s, x_hi);
         same = long_tiles(s, x_lo) - longer;
         qt = tiles_of(s) - 1 - longer;  // its longest tile of that length
@@ -236,9 +247,11 @@ struct AttnOrder {
       const unsigned holds = __ballot_sync(0xffffffffu, left < incl);
       if (holds) {
         const int from = __ffs(holds) - 1;
-        return make_int2(i0 + from, __shfl_sync(0xffffffffu, qt - (left - (incl - same)), from));
+        return make_int2(block + from, __shfl_sync(0xffffffffu, qt - (left - (incl - same)), from));
       }
-      left -= __shfl_sync(0xffffffffu, incl, 31);
+      const int here = __shfl_sync(0xffffffffu, incl, 31);
+      left -= here;
+      passed += here;
     }
     return make_int2(0, 0);  // (not reached: there are `rank - beyond` and more tiles of that length)
   }
@@ -895,7 +908,7 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
     }
   } else if (warp == W_SCHEDULE) {
     // ------------------------------------------------------------------ scheduler
-    const AttnOrder<TN> order(p, QT * per_tile, blockIdx.x == 0);
+    AttnOrder<TN> order(p, QT * per_tile, blockIdx.x == 0);
     // (sequences that overlap, or a count of row tiles that they make pass 32 bits: no row tile has a place behind the last)
     const bool fits = order.all >= 0 && static_cast<long long>(order.all) * p.heads <= p.units;
     if (!fits && blockIdx.x == 0 && lane == 0) kv_report(p.status);
