@@ -616,165 +616,165 @@ attention_tiles_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_c
         }
 #pragma unroll 1
         for (int j = 0; ok && j < it.tiles;) {
-        const int end = LONG ? min(it.tiles, j + T::SUM_TILES) : it.tiles;
+          const int end = LONG ? min(it.tiles, j + T::SUM_TILES) : it.tiles;
 #pragma unroll 1
-        for (; j < end; ++j, ++done) {
-          const int sb = 2 * q + (done & 1);  // score buffer
-          const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(sb * TN);
-          ok = wait_bounded(s_full(sb), (done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          ptx::tc_fence_after_sync();
-          uint32_t x[TN / 32][32];
-#pragma unroll
-          for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
-          ptx::tmem_wait_ld();
-          if constexpr (U4) {  // scores in the units of the exponent: scale (q . codes) + offset sum(q)
-            ok = wait_bounded(table_full((ring0 + j) % T::TABLES), ((ring0 + j) / T::TABLES) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          for (; j < end; ++j, ++done) {
+            const int sb = 2 * q + (done & 1);  // score buffer
+            const uint32_t s_at = tmem + lane_base + static_cast<uint32_t>(sb * TN);
+            ok = wait_bounded(s_full(sb), (done >> 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
+            ptx::tc_fence_after_sync();
+            uint32_t x[TN / 32][32];
 #pragma unroll
-            for (int h = 0; h < TN / 32; ++h)
+            for (int h = 0; h < TN / 32; ++h) ptx::tmem_ld_32x32b_x32(s_at + h * 32, x[h]);
+            ptx::tmem_wait_ld();
+            if constexpr (U4) {  // scores in the units of the exponent: scale (q . codes) + offset sum(q)
+              ok = wait_bounded(table_full((ring0 + j) % T::TABLES), ((ring0 + j) / T::TABLES) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              const uint32_t table = base + T::TABLE_OFFSET + static_cast<uint32_t>(((ring0 + j) % T::TABLES) * T::TABLE_BYTES);
 #pragma unroll
-              for (int v = 0; v < 32; v += 2) {
-                uint64_t a, b;
-                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(table + (h * 32 + v) * 8) : "memory");
-                const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), a, mul2(b, q_sum2)));
-                x[h][v] = __float_as_uint(t.x);
-                x[h][v + 1] = __float_as_uint(t.y);
+              for (int h = 0; h < TN / 32; ++h)
+#pragma unroll
+                for (int v = 0; v < 32; v += 2) {
+                  uint64_t a, b;
+                  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(table + (h * 32 + v) * 8) : "memory");
+                  const float2 t = unpair(fma2(pair(__uint_as_float(x[h][v]), __uint_as_float(x[h][v + 1])), a, mul2(b, q_sum2)));
+                  x[h][v] = __float_as_uint(t.x);
+                  x[h][v + 1] = __float_as_uint(t.y);
+                }
+            }
+            const int tok0 = it.lo + j * TN;
+            if (tok0 + TN - 1 > all_hi || tok0 < all_lo) {
+              const int last = pos - tok0, first = from - tok0;
+#pragma unroll
+              for (int h = 0; h < TN / 32; ++h)
+#pragma unroll
+                for (int v = 0; v < 32; ++v)
+                  if (h * 32 + v > last || h * 32 + v < first) x[h][v] = 0xff800000u;  // -inf
+            }
+            float mx[8];  // (chains of their own)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) mx[u] = fmaxf(__uint_as_float(x[0][u]), __uint_as_float(x[0][u + 8]));
+#pragma unroll
+            for (int i = 16; i < TN; i += 16)
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+                mx[u] = max3(mx[u], __uint_as_float(x[(i + u) / 32][(i + u) % 32]), __uint_as_float(x[(i + u + 8) / 32][(i + u + 8) % 32]));
+            float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+            if constexpr (!U4) top *= c;
+            const bool grow = top > m + 8.0f;
+            if (__any_sync(0xffffffffu, grow)) {
+              const float now = grow ? top : m;
+              const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
+              m = now;
+              l *= f;
+              if (j > 0) {  // O of the tiles before, once their products are done
+                ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
+#pragma unroll 1
+                for (int d = 0; d < D; d += 16) {
+                  uint32_t y[16];  // (few registers: the scores are in the others)
+                  ptx::tmem_ld_32x32b_x16(o_at + d, y);
+                  ptx::tmem_wait_ld();
+#pragma unroll
+                  for (int v = 0; v < 16; ++v) y[v] = __float_as_uint(__uint_as_float(y[v]) * f);
+                  ptx::tmem_st_32x32b_x16(o_at + d, y);
+                }
+                ptx::tmem_wait_st();
               }
-          }
-          const int tok0 = it.lo + j * TN;
-          if (tok0 + TN - 1 > all_hi || tok0 < all_lo) {
-            const int last = pos - tok0, first = from - tok0;
+            }
+            // The warps of an SM quarter that have a row tile each take turns at the exponentials, which one warp keeps busy.
+            // (Left alone they fall into step: both at the exponentials, then both at everything else.)
+            if (it.active == 2) {
+              if (q == 1 || turns > 0)
+                ok = wait_bounded(turn_done(q ^ 1, warp & 3), (q == 1 ? turns : turns - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              ++turns;
+            }
+            // weights, two per column, over the scores: 32 tokens take 16 columns
+            const float at_ref = KVA_WEIGHT_BITS - (m == -INFINITY ? 0.0f : m);
+            const uint64_t at2 = pair(at_ref, at_ref);
+            uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+            {
+              // Pair i is summed up and packed LAG pairs after its exponentials were asked for.
+              constexpr int PAIRS = TN / 2, LAG = 4;
+              auto exponent = [&](int i) {
+                const uint64_t x2 = pair(__uint_as_float(x[i / 16][i % 16 * 2]), __uint_as_float(x[i / 16][i % 16 * 2 + 1]));
+                return unpair(U4 ? add2_here(x2, at2) : fma2_here(x2, c2, at2));
+              };
+              float2 e[LAG + 1], t = exponent(0);
+              uint32_t w[16];
 #pragma unroll
-            for (int h = 0; h < TN / 32; ++h)
-#pragma unroll
-              for (int v = 0; v < 32; ++v)
-                if (h * 32 + v > last || h * 32 + v < first) x[h][v] = 0xff800000u;  // -inf
-          }
-          float mx[8];  // (chains of their own)
-#pragma unroll
-          for (int u = 0; u < 8; ++u) mx[u] = fmaxf(__uint_as_float(x[0][u]), __uint_as_float(x[0][u + 8]));
-#pragma unroll
-          for (int i = 16; i < TN; i += 16)
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-              mx[u] = max3(mx[u], __uint_as_float(x[(i + u) / 32][(i + u) % 32]), __uint_as_float(x[(i + u + 8) / 32][(i + u + 8) % 32]));
-          float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
-          if constexpr (!U4) top *= c;
-          const bool grow = top > m + 8.0f;
-          if (__any_sync(0xffffffffu, grow)) {
-            const float now = grow ? top : m;
-            const float f = now == -INFINITY ? 1.0f : exp2_approx(m - now);
-            m = now;
-            l *= f;
-            if (j > 0) {  // O of the tiles before, once their products are done
+              for (int i = 0; i < PAIRS + LAG; ++i) {
+                if (i < PAIRS) {
+                  e[i % (LAG + 1)].x = exp2_here(t.x);
+                  e[i % (LAG + 1)].y = exp2_here(t.y);
+                  if (i + 1 < PAIRS) t = exponent(i + 1);
+                }
+                if (i == PAIRS - 1 && it.active == 2 && lane == 0) ptx::mbar_arrive(turn_done(q, warp & 3));
+                if (i >= LAG) {
+                  const int o = i - LAG;
+                  const float2 v = e[o % (LAG + 1)];
+                  sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
+                  w[o % 16] = pack_here(v.x, v.y);
+                  if (o % 16 == 15) ptx::tmem_st_32x32b_x16(s_at + (o / 16) * 16, w);
+                }
+              }
+            }
+            ptx::tmem_wait_st();
+            if (j > 0 && j == end - 1) {
+              // A barrier tells a phase from the one before or behind it only.  That S was there says that the products of the tile before
+              // the last are done (they were issued earlier, by the same thread); the last one's are seen to here, in front of this one's,
+              // so that the wait for these, below, is not taken in by them.
               ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
-              ptx::tc_fence_after_sync();
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(p_full(sb));
+            const float2 total = unpair(add2(sum[0], sum[1]));
+            l += total.x + total.y;
+          }
+          if (!LONG || !ok || it.tiles <= T::SUM_TILES) break;
+          // ---- long sums
+          ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          ptx::tc_fence_after_sync();
+          const bool parts = U4 && it.split >= 0;
+          __half* const mine = parts ? reinterpret_cast<__half*>(part_of(it, q * 128 + r)) + D
+                                     : p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
+          // (all rows have a place: eight columns of 32 rows side by side, or every access is to 32 lines)
+          const bool dense = __all_sync(0xffffffffu, parts || live);
+          // log2 of the unit of what was put by, with the reference of that time: in the row's place for results on their way out, which is free here
+          const uint32_t held_at = base + T::OUT_OFFSET + static_cast<uint32_t>((warp * 32 + lane) * T::OUT_PITCH);
+          float held = -INFINITY;
+          if (j > T::SUM_TILES) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(held) : "r"(held_at) : "memory");
+          const float factor = held == -INFINITY ? 0.0f : exp2_approx(held - m);
+          const float unit = j == it.tiles ? 0.0f : l > 0.0f && l < 0x1p100f ? __uint_as_float((__float_as_uint(l) & 0x7f800000u) + 0x1000000u) : 1.0f;
 #pragma unroll 1
-              for (int d = 0; d < D; d += 16) {
-                uint32_t y[16];  // (few registers: the scores are in the others)
-                ptx::tmem_ld_32x32b_x16(o_at + d, y);
-                ptx::tmem_wait_ld();
+          for (int d = 0; d < D; d += 16) {
+            uint32_t y[16];
+            ptx::tmem_ld_32x32b_x16(o_at + d, y);
+            ptx::tmem_wait_ld();
 #pragma unroll
-                for (int v = 0; v < 16; ++v) y[v] = __float_as_uint(__uint_as_float(y[v]) * f);
-                ptx::tmem_st_32x32b_x16(o_at + d, y);
-              }
-              ptx::tmem_wait_st();
+            for (int h = 0; h < 2; ++h) {
+              const int piece = (d / 8 + h) * 32 + lane;
+              __half* const there = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), piece / (D / 8))) + piece % (D / 8) * 8;
+              if (dense || live) split_sums(y + 8 * h, reinterpret_cast<uint4*>(dense ? there : mine + d + 8 * h), factor, unit);
             }
-          }
-          // The warps of an SM quarter that have a row tile each take turns at the exponentials, which one warp keeps busy.
-          // (Left alone they fall into step: both at the exponentials, then both at everything else.)
-          if (it.active == 2) {
-            if (q == 1 || turns > 0)
-              ok = wait_bounded(turn_done(q ^ 1, warp & 3), (q == 1 ? turns : turns - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            ++turns;
-          }
-          // weights, two per column, over the scores: 32 tokens take 16 columns
-          const float at_ref = KVA_WEIGHT_BITS - (m == -INFINITY ? 0.0f : m);
-          const uint64_t at2 = pair(at_ref, at_ref);
-          uint64_t sum[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
-          {
-            // Pair i is summed up and packed LAG pairs after its exponentials were asked for.
-            constexpr int PAIRS = TN / 2, LAG = 4;
-            auto exponent = [&](int i) {
-              const uint64_t x2 = pair(__uint_as_float(x[i / 16][i % 16 * 2]), __uint_as_float(x[i / 16][i % 16 * 2 + 1]));
-              return unpair(U4 ? add2_here(x2, at2) : fma2_here(x2, c2, at2));
-            };
-            float2 e[LAG + 1], t = exponent(0);
-            uint32_t w[16];
-#pragma unroll
-            for (int i = 0; i < PAIRS + LAG; ++i) {
-              if (i < PAIRS) {
-                e[i % (LAG + 1)].x = exp2_here(t.x);
-                e[i % (LAG + 1)].y = exp2_here(t.y);
-                if (i + 1 < PAIRS) t = exponent(i + 1);
-              }
-              if (i == PAIRS - 1 && it.active == 2 && lane == 0) ptx::mbar_arrive(turn_done(q, warp & 3));
-              if (i >= LAG) {
-                const int o = i - LAG;
-                const float2 v = e[o % (LAG + 1)];
-                sum[o & 1] = add2_here(sum[o & 1], pair(v.x, v.y));
-                w[o % 16] = pack_here(v.x, v.y);
-                if (o % 16 == 15) ptx::tmem_st_32x32b_x16(s_at + (o / 16) * 16, w);
-              }
-            }
+            __syncwarp();
+            ptx::tmem_st_32x32b_x16(o_at + d, y);
           }
           ptx::tmem_wait_st();
-          if (j > 0 && j == end - 1) {
-            // A barrier tells a phase from the one before or behind it only.  That S was there says that the products of the tile before
-            // the last are done (they were issued earlier, by the same thread); the last one's are seen to here, in front of this one's,
-            // so that the wait for these, below, is not taken in by them.
-            ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-          }
-          ptx::tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(p_full(sb));
-          const float2 total = unpair(add2(sum[0], sum[1]));
-          l += total.x + total.y;
-        }
-        if (!LONG || !ok || it.tiles <= T::SUM_TILES) break;
-        // ---- long sums
-        ok = wait_bounded(o_done(q), (done - 1) & 1, abort_flag, p.status, DEV_TIMEOUT_EPILOGUE);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        ptx::tc_fence_after_sync();
-        const bool parts = U4 && it.split >= 0;
-        __half* const mine = parts ? reinterpret_cast<__half*>(part_of(it, q * 128 + r)) + D
-                                   : p.out + (static_cast<long long>(it.row0) + qi) * p.out_token_stride + static_cast<long long>(hq) * D;
-        // (all rows have a place: eight columns of 32 rows side by side, or every access is to 32 lines)
-        const bool dense = __all_sync(0xffffffffu, parts || live);
-        // log2 of the unit of what was put by, with the reference of that time: in the row's place for results on their way out, which is free here
-        const uint32_t held_at = base + T::OUT_OFFSET + static_cast<uint32_t>((warp * 32 + lane) * T::OUT_PITCH);
-        float held = -INFINITY;
-        if (j > T::SUM_TILES) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(held) : "r"(held_at) : "memory");
-        const float factor = held == -INFINITY ? 0.0f : exp2_approx(held - m);
-        const float unit = j == it.tiles ? 0.0f : l > 0.0f && l < 0x1p100f ? __uint_as_float((__float_as_uint(l) & 0x7f800000u) + 0x1000000u) : 1.0f;
-#pragma unroll 1
-        for (int d = 0; d < D; d += 16) {
-          uint32_t y[16];
-          ptx::tmem_ld_32x32b_x16(o_at + d, y);
-          ptx::tmem_wait_ld();
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int piece = (d / 8 + h) * 32 + lane;
-            __half* const there = reinterpret_cast<__half*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), piece / (D / 8))) + piece % (D / 8) * 8;
-            if (dense || live) split_sums(y + 8 * h, reinterpret_cast<uint4*>(dense ? there : mine + d + 8 * h), factor, unit);
-          }
-          __syncwarp();
-          ptx::tmem_st_32x32b_x16(o_at + d, y);
-        }
-        ptx::tmem_wait_st();
-        held = m + (static_cast<float>(__float_as_uint(unit) >> 23) - 127.0f);
-        asm volatile("st.shared.f32 [%0], %1;" ::"r"(held_at), "f"(held) : "memory");
+          held = m + (static_cast<float>(__float_as_uint(unit) >> 23) - 127.0f);
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(held_at), "f"(held) : "memory");
         }
         if (!ok) break;
         // ---- the rows' results
